@@ -502,6 +502,134 @@ int soma_get_phase_times(soma_ctx* ctx, soma_phase_times* out);
  * test has to ask).  Errors: SOMA_EINVAL for a NULL argument. */
 int soma_get_narrow_projections(const soma_ctx* ctx, int32_t* launches);
 
+/* ---------------------------------------------------------------------------
+ * Operators of first-order training, next to the zero-order step: a gated
+ * linear recurrence, the softmax cross entropy of a large vocabulary with its
+ * gradients, and an AdamW step over many tensors.  They follow the conventions
+ * at the top; beyond those:
+ *   - the current device must be the one that `stream` belongs to and that
+ *     holds the arrays;
+ *   - two calls that overlap (two streams, two threads, two replayed graphs)
+ *     need workspaces of their own;
+ *   - arrays of one call do not overlap unless its description says that they
+ *     may;
+ *   - every sum is formed in a fixed order in 32 bits or more: repeated calls
+ *     give the same bits;
+ *   - every call can be captured into a HIP graph (soma_adamw_create cannot:
+ *     it waits for its copy to the device).
+ * ------------------------------------------------------------------------- */
+
+/* Types of the operators' arrays. */
+enum soma_type {
+  SOMA_FLOAT = 0,  /* fp32 */
+  SOMA_BFLOAT = 1  /* bfloat16 */
+};
+
+/* Gated linear recurrence: the LSTM's cell with gates that read the input
+ * alone, so that time needs no matrix product and can run side by side,
+ *   c_t = sigma(f_t) c_{t-1} + sigma(i_t) tanh(g_t),  h_t = sigma(o_t) tanh(c_t),
+ * over sequences that lie behind one another in one array of rows.
+ *   gates   [rows][4 width], consecutive rows gate_stride elements apart: the
+ *           pre-activations in blocks i, f, g, o of `width` channels (the row
+ *           order of the LSTM's weights above).
+ *   offsets [sequences + 1] int32 (device): sequence s has the rows
+ *           offsets[s] .. offsets[s + 1] - 1.  offsets[0] = 0, ascending; a
+ *           sequence may be empty.  Rows behind the last sequence are neither
+ *           read nor written.  Offsets that break these rules give unspecified
+ *           results, but are never followed outside [0, rows).  NULL: every
+ *           sequence has rows / sequences rows (rows must be a multiple).
+ *   c0, cT  [sequences][width] fp32, the states in front of the first row and
+ *           behind the last.  c0 NULL: zeros; cT NULL: not wanted.  They may
+ *           be the same array.  An empty sequence keeps its state.
+ *   h       [rows][width], rows contiguous.
+ *   states  [ceil(rows / SOMA_SCAN_BLOCK)][width] fp32: what the backward pass
+ *           needs, the state in front of every SOMA_SCAN_BLOCK-th row.  NULL:
+ *           not wanted.
+ * gates and h have `type`; states and arithmetic are fp32.  Constraints: rows
+ * in [0, 2^30], width in [1, 2^20], sequences in [1, 65535]. */
+#define SOMA_SCAN_BLOCK 64
+
+typedef struct soma_scan_config {
+  int32_t rows;
+  int32_t width;
+  int32_t sequences;
+  int32_t type;         /* enum soma_type */
+  int64_t gate_stride;  /* elements between rows of gates, >= 4 width */
+} soma_scan_config;
+
+/* Bytes of device workspace of soma_scan_forward and soma_scan_backward; it
+ * grows with width and sequences only.  Pure. */
+int soma_scan_workspace_size(const soma_scan_config* cfg, size_t* bytes);
+
+int soma_scan_forward(const soma_scan_config* cfg, const void* gates_dev, const int32_t* offsets_dev,
+                      const float* c0_dev, void* h_dev, float* cT_dev, float* states_dev, void* workspace_dev,
+                      size_t workspace_bytes, void* stream);
+
+/* The gradients of soma_scan_forward's inputs from those of its outputs, with
+ * the gates, offsets and c0 of that call and the states it gave.
+ *   dh      [rows][width] of `type`; dcT [sequences][width] fp32, NULL: zeros.
+ *   dgates  [rows][4 width] of `type`, rows contiguous; an array of its own.
+ *   dc0     [sequences][width] fp32, NULL: not wanted; may be dcT. */
+int soma_scan_backward(const soma_scan_config* cfg, const void* gates_dev, const int32_t* offsets_dev,
+                       const float* c0_dev, const float* states_dev, const void* dh_dev, const float* dcT_dev,
+                       void* dgates_dev, float* dc0_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* One row for every sequence (rows = sequences), as when text is generated:
+ * cT from c0 (which may be the same array; NULL: zeros) and h. */
+int soma_scan_step(const soma_scan_config* cfg, const void* gates_dev, const float* c0_dev, float* cT_dev, void* h_dev,
+                   void* stream);
+
+/* One AdamW step (decoupled weight decay) over many tensors in one launch:
+ *   g = s grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
+ *   param <- (1 - lr weight_decay) param
+ *            - lr / (1 - beta1^t) m / (sqrt(v) / sqrt(1 - beta2^t) + delta)
+ * in fp32, param rounded once to its type.  The moments are held in fp32
+ * [count], or in 8 bits: uint8 codes [count] and one fp32 scale for every
+ * SOMA_ADAMW_BLOCK elements, [ceil(count / SOMA_ADAMW_BLOCK)] each,
+ *   m = e4m3(code) m_scale;  v = (r(code) v_scale)^2,
+ *   r(0) = 0, r(k) = (16 + k % 16) 2^(k / 16 - 19),
+ * rounded to nearest even, with the block's largest magnitude at the largest
+ * code (448; 1.9375).  A v that is not 0 keeps at least code 1.  All zeros is
+ * the state before the first update.  A gradient that is not finite makes its
+ * own element's param and moments so, and no other's. */
+#define SOMA_ADAMW_BLOCK 256
+
+typedef struct soma_adamw_tensor {
+  void* param;          /* [count] of param_type, updated in place */
+  const void* grad;     /* [count] of grad_type */
+  void* m;              /* moments, updated in place */
+  void* v;
+  float* m_scale;       /* 8 bits only */
+  float* v_scale;
+  void* copy;           /* [count] bf16 out: the new param; NULL: not wanted */
+  int64_t count;        /* elements; 0 is allowed */
+  double weight_decay;  /* finite */
+  int32_t param_type;   /* enum soma_type */
+  int32_t grad_type;
+  int32_t state_bits;   /* 32 or 8 */
+  int32_t reserved;     /* 0 */
+} soma_adamw_tensor;
+
+typedef struct soma_adamw soma_adamw;
+
+/* A plan holds the tensors' addresses: they must stay valid while it is used.
+ * soma_adamw_create copies the table to the device and waits for the copy.
+ * `tensors` is a host array.  Pointers need only their elements' alignment; 16
+ * bytes (fp32), 8 (bf16) and 4 (codes) are faster. */
+int soma_adamw_workspace_size(const soma_adamw_tensor* tensors, int32_t n, size_t* bytes);
+int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspace_dev, size_t workspace_bytes,
+                      void* stream, soma_adamw** out);
+void soma_adamw_destroy(soma_adamw* plan);
+
+/* Update number t >= 1 of every tensor.  grad_scale_dev: s, one fp32 value on
+ * the device (loss scaling, clipping); NULL: 1. */
+int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double beta2, double delta,
+                    const float* grad_scale_dev, void* stream);
+
+/* The values of the moments in fp32, e.g. for a checkpoint: m_out[i] and
+ * v_out[i] (host arrays of device pointers) receive tensor i's [count]. */
+int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_out, void* stream);
+
 /* Thread-local description of the last error ("" if none). */
 const char* soma_last_error(void);
 

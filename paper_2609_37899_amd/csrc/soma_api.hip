@@ -53,6 +53,7 @@
 #include "soma_narrow.hpp"
 #include "soma_wide.hpp"
 #include "soma_rec.hpp"
+#include "soma_host.hpp"
 
 namespace {
 
@@ -73,6 +74,25 @@ int ok() {
   g_last_error.clear();
   return SOMA_OK;
 }
+
+}  // namespace
+
+namespace soma {
+
+int set_error(int code, const char* fmt, ...) {
+  char buf[512];
+  va_list ap;
+  va_start(ap, fmt);
+  vsnprintf(buf, sizeof buf, fmt, ap);
+  va_end(ap);
+  return fail(code, "%s", buf);
+}
+
+int set_ok() { return ok(); }
+
+}  // namespace soma
+
+namespace {
 
 constexpr size_t kAlign = 256;
 constexpr int kMaxGroups = 1024;              // persistent-recurrence groups (counters in the workspace)

@@ -1,0 +1,41 @@
+// soma_host.hpp -- what the translation units of the C ABI share on the host:
+// the thread's last error and the checks in front of a launch.
+#pragma once
+
+#include <hip/hip_runtime.h>
+#include <stddef.h>
+#include <stdint.h>
+
+#include "soma.h"
+
+namespace soma {
+
+// Record a description of the error `code` for soma_last_error(); returns code.
+int set_error(int code, const char* fmt, ...) __attribute__((format(printf, 2, 3)));
+// Clear it; returns SOMA_OK.
+int set_ok();
+
+inline hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s); }
+
+inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
+
+inline int launched(const char* what) {
+  const hipError_t e = hipGetLastError();
+  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+  return SOMA_OK;
+}
+
+inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+inline bool is_type(int32_t t) { return t == SOMA_FLOAT || t == SOMA_BFLOAT; }
+inline size_t type_size(int32_t t) { return t == SOMA_BFLOAT ? 2 : 4; }
+
+inline int check_workspace(const void* ws, size_t have, size_t need) {
+  if (need == 0) return SOMA_OK;
+  if (!ws) return set_error(SOMA_EWORKSPACE, "workspace is NULL");
+  if (!is_aligned(ws, 256)) return set_error(SOMA_EWORKSPACE, "workspace must be 256-byte aligned");
+  if (have < need) return set_error(SOMA_EWORKSPACE, "workspace too small: %zu < %zu bytes", have, need);
+  return SOMA_OK;
+}
+
+}  // namespace soma

@@ -29,7 +29,9 @@ EXPORTS = ("soma_param_count", "soma_workspace_size", "soma_create", "soma_destr
            "soma_schedule_observe", "soma_estimator_moments", "soma_set_tied_head", "soma_head_delta",
            "soma_gaussian", "soma_probe", "soma_philox", "soma_box_muller", "soma_set_phase_timing",
            "soma_get_phase_times", "soma_get_narrow_projections", "soma_set_spin_limit", "soma_spsa_step_noalloc",
-           "soma_last_error")
+           "soma_scan_workspace_size", "soma_scan_forward", "soma_scan_backward", "soma_scan_step",
+           "soma_adamw_workspace_size", "soma_adamw_create", "soma_adamw_destroy", "soma_adamw_step",
+           "soma_adamw_moments", "soma_last_error")
 
 
 class SomaError(RuntimeError):
@@ -76,6 +78,22 @@ class Config(ctypes.Structure):
         "pair_chunk", "flags", "probe", "accum", "arch")] + [("perturb_mask", ctypes.c_uint32)]
 
 
+TYPE_FLOAT, TYPE_BFLOAT = 0, 1
+SCAN_BLOCK = 64             # rows between the states that a backward scan starts from
+ADAMW_BLOCK = 256           # elements that share the scales of 8-bit moments
+
+
+class ScanConfig(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("sequences", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("gate_stride", ctypes.c_int64)]
+
+
+class AdamWTensor(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
+        ("count", ctypes.c_int64), ("weight_decay", ctypes.c_double)] + [
+        (n, ctypes.c_int32) for n in ("param_type", "grad_type", "state_bits", "reserved")]
+
+
 _lib = None
 
 
@@ -119,6 +137,17 @@ def load():
             "soma_set_spin_limit": (ctypes.c_int, [vp, ctypes.c_uint32]),
             "soma_get_phase_times": (ctypes.c_int, [vp, ctypes.POINTER(PhaseTimes)]),
             "soma_get_narrow_projections": (ctypes.c_int, [vp, ctypes.POINTER(ctypes.c_int32)]),
+            "soma_scan_workspace_size": (ctypes.c_int, [ctypes.POINTER(ScanConfig), ctypes.POINTER(ctypes.c_size_t)]),
+            "soma_scan_forward": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 7 + [ctypes.c_size_t, vp]),
+            "soma_scan_backward": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
+            "soma_scan_step": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 5),
+            "soma_adamw_workspace_size": (ctypes.c_int, [ctypes.POINTER(AdamWTensor), ctypes.c_int32,
+                                                         ctypes.POINTER(ctypes.c_size_t)]),
+            "soma_adamw_create": (ctypes.c_int, [ctypes.POINTER(AdamWTensor), ctypes.c_int32, vp, ctypes.c_size_t, vp,
+                                                 ctypes.POINTER(vp)]),
+            "soma_adamw_destroy": (None, [vp]),
+            "soma_adamw_step": (ctypes.c_int, [vp, ctypes.c_int64] + [ctypes.c_double] * 4 + [vp, vp]),
+            "soma_adamw_moments": (ctypes.c_int, [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]),
             "soma_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -389,3 +418,249 @@ def seeds_tensor(seeds, device="cuda"):
     import torch
     a = np.ascontiguousarray(seeds, dtype=np.uint64).view(np.int64)
     return torch.from_numpy(a.copy()).to(device)
+
+
+# ---------------------------------------------------------------------------
+# Operators of first-order training
+
+def _type_of(dtype) -> int:
+    import torch
+    if dtype == torch.float32:
+        return TYPE_FLOAT
+    if dtype == torch.bfloat16:
+        return TYPE_BFLOAT
+    raise TypeError(f"dtype must be torch.float32 or torch.bfloat16, got {dtype}")
+
+
+class _Plan:
+    """What the operators' classes share: one device, a workspace on it, and
+    the checks of their arguments.  A plan must not be used by two streams at
+    once, nor by two captured graphs that may run at once: its workspace is
+    shared."""
+
+    def _start(self, nbytes: int, device):
+        import torch
+        self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise TypeError("device must be a GPU")
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self.workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
+        self._stream0 = torch.cuda.current_stream(self.device).cuda_stream
+        self._ws = ctypes.c_void_p(self.workspace.data_ptr())
+
+    def _call(self, stream, fn, *args):
+        """fn(*args, stream) with the plan's device current."""
+        import torch
+        with torch.cuda.device(self.device):
+            st = stream if stream is not None else torch.cuda.current_stream(self.device)
+            if st.device != self.device:
+                raise ValueError(f"stream belongs to {st.device}, the plan to {self.device}")
+            if st.cuda_stream != self._stream0:
+                self.workspace.record_stream(st)      # not handed out again before this stream is done with it
+            _check(fn(*args, ctypes.c_void_p(st.cuda_stream)))
+
+    def _ptr(self, t, name, dtype, shape, optional=False, strided=False):
+        """The address of a tensor of this type and shape on the plan's device
+        (strided: rows may lie further apart than their length)."""
+        import torch
+        if t is None and optional:
+            return None
+        if not isinstance(t, torch.Tensor) or t.device != self.device:
+            raise TypeError(f"{name} must be a tensor on {self.device}")
+        if t.dtype != dtype:
+            raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
+        if tuple(t.shape) != tuple(shape):
+            raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+        if strided and t.dim() == 2:
+            if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
+                raise ValueError(f"{name} must have contiguous rows that do not overlap")
+        elif not t.is_contiguous():
+            raise ValueError(f"{name} must be contiguous")
+        return ctypes.c_void_p(t.data_ptr())
+
+
+def _row_stride(t) -> int:
+    """Elements between rows (of one row, its length)."""
+    return t.stride(0) if t.shape[0] > 1 else t.shape[1]
+
+
+class GatedScan(_Plan):
+    """The gated linear recurrence: the LSTM's cell with gates that read the
+    input alone, c_t = s(f_t) c_{t-1} + s(i_t) tanh(g_t), h_t = s(o_t) tanh(c_t),
+    over ``sequences`` sequences that lie behind one another in at most ``rows``
+    rows of ``width`` channels.  ``dtype`` (float32 or bfloat16) is the type of
+    gates, h and their gradients; states are float32.
+
+    gates [n][4 width] hold the pre-activations in blocks i, f, g, o; rows may be
+    strided.  offsets [sequences + 1] (int32, on the device) gives each
+    sequence's first row; None: all sequences have n / sequences rows.  Rows
+    behind the last sequence are neither read nor written."""
+
+    def __init__(self, rows: int, sequences: int, width: int, dtype, device="cuda"):
+        self.rows, self.sequences, self.width, self.dtype = int(rows), int(sequences), int(width), dtype
+        self._type = _type_of(dtype)
+        for name in ("rows", "sequences", "width"):
+            if not 0 <= getattr(self, name) < 2**31:
+                raise ValueError(f"{name} must fit 31 bits")
+        out = ctypes.c_size_t()
+        _check(load().soma_scan_workspace_size(ctypes.byref(self._cfg(self.rows, 4 * self.width)), ctypes.byref(out)))
+        self._bytes = out.value
+        self._start(out.value, device)
+
+    def _cfg(self, rows, stride):
+        return ScanConfig(rows, self.width, self.sequences, self._type, stride)
+
+    def new_states(self):
+        """An array for forward's states (what backward starts from)."""
+        import torch
+        return torch.empty((-(-self.rows // SCAN_BLOCK), self.width), dtype=torch.float32, device=self.device)
+
+    def _gates(self, gates, offsets):
+        import torch
+        if not isinstance(gates, torch.Tensor) or gates.dim() != 2:
+            raise TypeError("gates must be a tensor [rows][4 width]")
+        n = gates.shape[0]
+        if n > self.rows:
+            raise ValueError(f"{n} rows, but the plan was made for {self.rows}")
+        return (n, self._cfg(n, _row_stride(gates)), self._ptr(gates, "gates", self.dtype, (n, 4 * self.width), strided=True),
+                self._ptr(offsets, "offsets", torch.int32, (self.sequences + 1,), optional=True))
+
+    def _states(self, states, n, optional):
+        import torch
+        if states is None and optional:
+            return None
+        if not isinstance(states, torch.Tensor) or states.dim() != 2 or states.shape[0] < -(-n // SCAN_BLOCK):
+            raise ValueError(f"states must be a tensor of {-(-n // SCAN_BLOCK)} rows or more (new_states())")
+        return self._ptr(states, "states", torch.float32, (states.shape[0], self.width))
+
+    def forward(self, gates, h, c0=None, cT=None, states=None, offsets=None, stream=None):
+        """h [n][width] from gates; cT [sequences][width] receives the states
+        behind the last rows (it may be c0), states what backward needs."""
+        import torch
+        n, cfg, pg, po = self._gates(gates, offsets)
+        end = (self.sequences, self.width)
+        self._call(stream, load().soma_scan_forward, ctypes.byref(cfg), pg, po,
+                   self._ptr(c0, "c0", torch.float32, end, optional=True), self._ptr(h, "h", self.dtype, (n, self.width)),
+                   self._ptr(cT, "cT", torch.float32, end, optional=True), self._states(states, n, True), self._ws,
+                   self._bytes)
+
+    def backward(self, gates, states, dh, dgates, c0=None, dcT=None, dc0=None, offsets=None, stream=None):
+        """dgates [n][4 width] and dc0 from dh [n][width] and dcT, with the
+        gates, offsets and c0 that forward had and the states it gave."""
+        import torch
+        n, cfg, pg, po = self._gates(gates, offsets)
+        end = (self.sequences, self.width)
+        self._call(stream, load().soma_scan_backward, ctypes.byref(cfg), pg, po,
+                   self._ptr(c0, "c0", torch.float32, end, optional=True), self._states(states, n, False),
+                   self._ptr(dh, "dh", self.dtype, (n, self.width)),
+                   self._ptr(dcT, "dcT", torch.float32, end, optional=True),
+                   self._ptr(dgates, "dgates", self.dtype, (n, 4 * self.width)),
+                   self._ptr(dc0, "dc0", torch.float32, end, optional=True), self._ws, self._bytes)
+
+    def step(self, gates, c0, cT, h, stream=None):
+        """One row for every sequence: cT (it may be c0) and h [sequences][width]."""
+        import torch
+        n, cfg, pg, _ = self._gates(gates, None)
+        end = (self.sequences, self.width)
+        self._call(stream, load().soma_scan_step, ctypes.byref(cfg), pg,
+                   self._ptr(c0, "c0", torch.float32, end, optional=True), self._ptr(cT, "cT", torch.float32, end),
+                   self._ptr(h, "h", self.dtype, end))
+
+
+class AdamW(_Plan):
+    """AdamW over many tensors in one launch.  params and grads are lists of
+    contiguous tensors (float32 or bfloat16, a pair may differ), whose memory the
+    plan uses at every step: keep them in place.  bits: moments in 32 or in 8.
+    weight_decay: one value, or one for each tensor.  moments: a list of (m, v),
+    or for 8 bits (m, v, m_scale, v_scale), to go on from; None: zeros.  copies:
+    bfloat16 tensors (or None) that receive the new parameters too."""
+
+    def __init__(self, params, grads, bits: int = 32, weight_decay=0.01, betas=(0.9, 0.999), delta: float = 1e-8,
+                 moments=None, copies=None, stream=None):
+        import torch
+        self._h = ctypes.c_void_p()
+        params, grads = list(params), list(grads)
+        n = len(params)
+        copies = list(copies) if copies is not None else [None] * n
+        decay = list(weight_decay) if isinstance(weight_decay, (list, tuple)) else [weight_decay] * n
+        if n == 0 or len(grads) != n or len(copies) != n or len(decay) != n:
+            raise ValueError("params must not be empty; grads, copies and weight_decay must be as many")
+        if bits not in (8, 32):
+            raise ValueError("bits must be 8 or 32")
+        if not isinstance(params[0], torch.Tensor) or params[0].device.type != "cuda":
+            raise TypeError("params must be device tensors")
+        self.device, self.bits, self.betas, self.delta = params[0].device, bits, tuple(betas), float(delta)
+        state = torch.float32 if bits == 32 else torch.uint8
+        if moments is None:
+            moments = []
+            for p in params:
+                blocks = -(-p.numel() // ADAMW_BLOCK)
+                x = [torch.zeros(p.numel(), dtype=state, device=self.device) for _ in range(2)]
+                if bits == 8:
+                    x += [torch.zeros(blocks, dtype=torch.float32, device=self.device) for _ in range(2)]
+                moments.append(tuple(x))
+        self.state = [tuple(x) for x in moments]
+        if len(self.state) != n or any(len(x) != (2 if bits == 32 else 4) for x in self.state):
+            raise ValueError("moments must hold (m, v) for each tensor, or (m, v, m_scale, v_scale) for 8 bits")
+        table = (AdamWTensor * n)()
+        for i, (p, g, x, c, w) in enumerate(zip(params, grads, self.state, copies, decay)):
+            at = f"params[{i}]"
+            pp = self._ptr(p, at, p.dtype if isinstance(p, torch.Tensor) else None, p.shape)
+            pg = self._ptr(g, f"grads[{i}]", g.dtype if isinstance(g, torch.Tensor) else None, p.shape)
+            px = [self._ptr(t.view(-1) if t.is_contiguous() else t, f"moments[{i}]", d, (k,))
+                  for t, d, k in zip(x, (state, state, torch.float32, torch.float32),
+                                     (p.numel(), p.numel()) + (-(-p.numel() // ADAMW_BLOCK),) * 2)]
+            px += [None] * (4 - len(px))
+            table[i] = AdamWTensor(pp, pg, *px, self._ptr(c, f"copies[{i}]", torch.bfloat16, p.shape, optional=True),
+                                   p.numel(), float(w), _type_of(p.dtype), _type_of(g.dtype), bits, 0)
+        self.params, self.grads, self.copies = params, grads, copies
+        out = ctypes.c_size_t()
+        _check(load().soma_adamw_workspace_size(table, n, ctypes.byref(out)))
+        self._start(out.value, self.device)
+        plan = ctypes.c_void_p()
+        with torch.cuda.device(self.device):
+            st = stream if stream is not None else torch.cuda.current_stream(self.device)
+            _check(load().soma_adamw_create(table, n, self._ws, out.value, ctypes.c_void_p(st.cuda_stream),
+                                            ctypes.byref(plan)))
+        self._h = plan
+
+    def close(self):
+        if self._h.value:
+            load().soma_adamw_destroy(self._h)
+            self._h = ctypes.c_void_p()
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+    def step(self, t: int, lr: float, grad_scale=None, stream=None):
+        """Update number t >= 1.  grad_scale: one float32 value on the device
+        that every gradient is multiplied with (None: 1)."""
+        import torch
+        if not self._h.value:
+            raise RuntimeError("the plan is closed")
+        if grad_scale is not None:
+            grad_scale = self._ptr(grad_scale.view(-1) if isinstance(grad_scale, torch.Tensor) else grad_scale,
+                                   "grad_scale", torch.float32, (1,))
+        self._call(stream, load().soma_adamw_step, self._h, int(t), float(lr), float(self.betas[0]),
+                   float(self.betas[1]), self.delta, grad_scale)
+
+    def moments(self, m_out, v_out, stream=None):
+        """The values of the moments, in float32: lists of tensors as large as
+        the parameters."""
+        import torch
+        if not self._h.value:
+            raise RuntimeError("the plan is closed")
+        n = len(self.params)
+        if len(m_out) != n or len(v_out) != n:
+            raise ValueError(f"m_out and v_out must hold {n} tensors")
+        arrays = []
+        for name, x in (("m_out", m_out), ("v_out", v_out)):
+            a = (ctypes.c_void_p * n)()
+            for i, (t, p) in enumerate(zip(x, self.params)):
+                a[i] = self._ptr(t, f"{name}[{i}]", torch.float32, p.shape)
+            arrays.append(a)
+        self._call(stream, load().soma_adamw_moments, self._h, *arrays)
