@@ -579,6 +579,47 @@ int soma_scan_backward(const soma_scan_config* cfg, const void* gates_dev, const
 int soma_scan_step(const soma_scan_config* cfg, const void* gates_dev, const float* c0_dev, float* cT_dev, void* h_dev,
                    void* stream);
 
+/* Softmax cross entropy of a linear head over a vocabulary of any size, and
+ * its gradients, without the logits in memory:
+ *   l_rv = f_r . E_v,  lse_r = log sum_v exp(l_rv),  loss_r = lse_r - l_{r,t_r}.
+ *   f       [rows][width], decoder inputs, rows f_stride elements apart.
+ *   E       [vocab][width], the head, rows e_stride elements apart.
+ *   targets [rows] int32.  A negative one: the row has no target; its loss and
+ *           lse are 0, its gradient is zeros, and nothing that its f holds
+ *           (infinities, NaN) reaches any result.  One >= vocab: the row's loss
+ *           is NaN, and so are the gradients that it enters.
+ * f, E and their gradients have `type`.  Products accumulate in fp32; fp32
+ * operands enter as two fp16 parts with a power of two as scale for each array:
+ * 2^-22 of a value, or 2^-38 of the array's largest finite magnitude where that
+ * is more; bf16 operands enter as they are, and the softmax's part of a gradient
+ * is rounded to bf16 (2^-8) before its products.
+ * Constraints: rows in [0, 2^20], vocab in [1, 2^24], width in [1, 2^16]. */
+typedef struct soma_ce_config {
+  int32_t rows;
+  int32_t vocab;
+  int32_t width;
+  int32_t type;      /* enum soma_type */
+  int64_t f_stride;  /* elements, >= width */
+  int64_t e_stride;
+} soma_ce_config;
+
+/* Bytes of device workspace of soma_ce_loss, or (grad != 0) of both calls.  It
+ * does not shrink with more rows, so a workspace serves calls of fewer.  Pure. */
+int soma_ce_workspace_size(const soma_ce_config* cfg, int grad, size_t* bytes);
+
+/* loss [rows] and lse [rows] (fp32); either may be NULL. */
+int soma_ce_loss(const soma_ce_config* cfg, const void* f_dev, const void* E_dev, const int32_t* targets_dev,
+                 float* loss_dev, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The gradients of sum_r w_r loss_r (w = grad_loss [rows] fp32, of any sign),
+ * with the lse that soma_ce_loss gave:
+ *   df_r = w_r (sum_v p_rv E_v - E_{t_r}),  dE_v = sum_r w_r (p_rv - [v = t_r]) f_r.
+ *   df [rows][width], dE [vocab][width], contiguous, 16-byte aligned; either
+ *   may be NULL: not wanted. */
+int soma_ce_grad(const soma_ce_config* cfg, const void* f_dev, const void* E_dev, const int32_t* targets_dev,
+                 const float* lse_dev, const float* grad_loss_dev, void* df_dev, void* dE_dev, void* workspace_dev,
+                 size_t workspace_bytes, void* stream);
+
 /* One AdamW step (decoupled weight decay) over many tensors in one launch:
  *   g = s grad;  m <- beta1 m + (1 - beta1) g;  v <- beta2 v + (1 - beta2) g^2;
  *   param <- (1 - lr weight_decay) param

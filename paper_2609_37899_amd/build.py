@@ -12,7 +12,8 @@ import sys
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
-SRCS = [os.path.join(PKG, "csrc", f) for f in ("soma_api.hip", "soma_rec.hip", "soma_scan.hip", "soma_adamw.hip")]
+SRCS = [os.path.join(PKG, "csrc", f) for f in ("soma_api.hip", "soma_rec.hip", "soma_scan.hip", "soma_ce.hip",
+                                               "soma_adamw.hip")]
 LIB = os.path.join(PKG, "libsoma.so")
 ARCH = os.environ.get("SOMA_OFFLOAD_ARCH", "gfx950")
 

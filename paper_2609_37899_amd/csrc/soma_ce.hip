@@ -1,0 +1,1019 @@
+// soma_ce.hip -- softmax cross entropy of a linear head over a large vocabulary
+// and its gradients, without the logits in memory.
+//
+//   l_rv = f_r . E_v,   lse_r = log sum_v e^l_rv,   loss_r = lse_r - l_{r,t_r};
+//   G_rv = w_r (e^(l_rv - lse_r) - [v = t_r]),   df = G E,   dE = G^T f.
+//
+// All four products run on the matrix cores (k_ce_mm) over operands in MFMA
+// fragment order (below).  The loss keeps, of every row, the maximum and the
+// sum of exponentials of each 64 or 128 logits, and joins them at the end; the
+// gradient forms the logits again, a piece of kPiece vocabulary rows at a time,
+// stores the piece of G only (in 16 bits, in the order that either product
+// reads), and multiplies it by the piece of E (added to df) and by f (the piece
+// of dE).  So the work is 8 R V K operations instead of 6, for R kPiece values
+// in memory instead of R V.
+//
+// Types.  bf16: E and f as they are, G rounded to bf16 (half a step, 2^-8, of
+// every value; as much as the result's own rounding), sums in fp32.  fp32: every
+// operand as two fp16 parts, x s = hi + lo to nearest with a power of two s that
+// brings its array's largest magnitude to 2^13 .. 2^14, and a b as lo hi + hi lo
+// + hi hi: 2^-22 of a value, or 2^-38 of its array's largest.  The weight w_r
+// enters as c (w_r / c) with c = max |w|, whose c is multiplied in fp32: under a
+// mean, the common case, the factor inside is exactly 1.
+//
+// Fragment order: a matrix [rows][K] is blocks of 1 KiB, [row / 16][part][k / 32],
+// of 64 words of 8 halves, word 16 lg + lr holding row lr, k 8 lg .. + 7: what lane
+// (lr, lg) feeds an MFMA.  A block moves to LDS by one DMA.  The packing kernels
+// write it (rows and their transpose), zeros beyond the matrix; so sizes, strides
+// and rows without a target are theirs alone to deal with.
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "soma.h"
+#include "soma_host.hpp"
+#include "soma_kernels.hpp"
+#include "soma_types.hpp"
+
+namespace soma {
+namespace {
+
+constexpr int kPiece = 8192;          // vocabulary rows of a piece
+constexpr int kMaxima = 256;          // partial maxima of an array
+constexpr float kLog2 = 0.6931471805599453f;
+constexpr int kBlk = 512;             // halves of a fragment block
+constexpr int kXcd = 8;
+
+// One row's part of the problem.  A row without a target has rho = 0, lse = 0.
+struct RowMeta {
+  float lse, rho;
+  int target, pad;
+};
+
+// Scales of the fp32 path (1 for bf16) and the largest weight.
+struct Scales {
+  float f, e, c, pad;
+};
+constexpr float kScaleG = 8192.0f;    // |G / c| <= 1
+
+// 2^n with n chosen so that top 2^n lies in [2^13, 2^14).
+__device__ __forceinline__ float power_scale(float top) {
+  if (!(top > 0.0f)) return 1.0f;
+  int n = 13 - (static_cast<int>((__float_as_uint(top) >> 23) & 255u) - 127);
+  n = n > 120 ? 120 : n;              // tiny arrays: the scale stays finite
+  return __uint_as_float(static_cast<uint32_t>(n + 127) << 23);
+}
+
+__device__ __forceinline__ float finite_abs(float x) {
+  const float a = __builtin_fabsf(x);
+  return a <= 3.402823466e38f ? a : 0.0f;
+}
+
+// Maximum over a block of 256 threads.
+__device__ __forceinline__ float block_max(float v, float* lds) {
+  v = wave_max(v);
+  if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = v;
+  __syncthreads();
+  v = fmaxf(fmaxf(lds[0], lds[1]), fmaxf(lds[2], lds[3]));
+  __syncthreads();
+  return v;
+}
+
+// ---------------------------------------------------------------------------
+// Largest finite magnitudes: f (rows with a target), E, and the weights.
+// Block x of array y writes maxima[y][x].
+// ---------------------------------------------------------------------------
+struct MaxArgs {
+  const void *f, *E;
+  const float* w;
+  const int32_t* targets;
+  int64_t f_stride, e_stride;
+  int R, V, K;
+  float* maxima;        // [3][kMaxima]
+};
+
+template <class T>
+__global__ __launch_bounds__(256) void k_ce_max(MaxArgs a, int first) {
+  __shared__ float lds[4];
+  const int which = first + blockIdx.y;
+  float top = 0.0f;
+  if (which < 2) {
+    const T* x = static_cast<const T*>(which ? a.E : a.f);
+    const int64_t stride = which ? a.e_stride : a.f_stride;
+    const int rows = which ? a.V : a.R;
+    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    for (int r = blockIdx.x * 4 + wave; r < rows; r += gridDim.x * 4) {
+      if (!which && a.targets[r] < 0) continue;
+      const T* p = x + r * stride;
+#pragma unroll 4
+      for (int k = lane; k < a.K; k += 64) top = fmaxf(top, finite_abs(load_value(p + k)));
+    }
+  } else if (a.w) {
+    // not finite: the largest is not either, and every gradient says so
+    for (int r = blockIdx.x * 256 + threadIdx.x; r < a.R; r += gridDim.x * 256)
+      if (a.targets[r] >= 0) {
+        const float w = __builtin_fabsf(a.w[r]);
+        top = w <= 3.402823466e38f ? fmaxf(top, w) : __builtin_inff();
+      }
+  }
+  top = block_max(top, lds);
+  if (threadIdx.x == 0) a.maxima[which * kMaxima + blockIdx.x] = top;
+}
+
+// ---------------------------------------------------------------------------
+// Packing: rows [row0, row0 + n) of a matrix into fragment order, and its
+// transpose.  A block takes 64 rows x 64 columns through LDS; out-of-range ones
+// and rows without a target are zeros.
+// ---------------------------------------------------------------------------
+struct PackArgs {
+  const void* x;
+  int64_t stride;
+  int n, K;                  // rows, columns
+  int np, Kp;                // padded to 64
+  const int32_t* targets;    // f only: rows with a negative target are zeros
+  uint16_t *frag, *fragT;    // [np / 16][parts][Kp / 32], [Kp / 16][parts][np / 32] blocks; or NULL
+  const float* maxima;       // [3][kMaxima] or NULL: scale 1, c 1
+  int which;                 // the scale to use: 0 f, 1 E
+  int nmax;                  // partial maxima in use
+  Scales* scales;            // f: written by block (0, 0)
+  RowMeta* meta;             // f: rows' constants, or NULL
+  const float *lse, *w;
+  int V;
+};
+
+__device__ __forceinline__ void split_rn(float x, uint16_t& hi, uint16_t& lo) {
+  const _Float16 h = static_cast<_Float16>(x);
+  hi = __builtin_bit_cast(uint16_t, h);
+  lo = __builtin_bit_cast(uint16_t, static_cast<_Float16>(x - static_cast<float>(h)));
+}
+
+__device__ __forceinline__ uint4 pack8(const uint16_t (&h)[8]) {
+  return make_uint4(h[0] | uint32_t(h[1]) << 16, h[2] | uint32_t(h[3]) << 16, h[4] | uint32_t(h[5]) << 16,
+                    h[6] | uint32_t(h[7]) << 16);
+}
+
+template <class T, int PARTS>
+__device__ __forceinline__ void store_fragment(uint16_t* dst, int64_t part_step, const float (&v)[8], float scale) {
+  if constexpr (PARTS == 1) {
+    *reinterpret_cast<uint4*>(dst) =
+        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+  } else {
+    uint16_t hi[8], lo[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) split_rn(v[i] * scale, hi[i], lo[i]);
+    *reinterpret_cast<uint4*>(dst) = pack8(hi);
+    *reinterpret_cast<uint4*>(dst + part_step) = pack8(lo);
+  }
+}
+
+template <class T, int PARTS>
+__global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
+  __shared__ float tile[64][65];
+  __shared__ float red[4];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+  float scale = 1.0f, c = 1.0f;
+  if (a.maxima) {
+    float t = 0.0f;
+    if constexpr (PARTS == 2) {
+      t = int(threadIdx.x) < a.nmax ? a.maxima[a.which * kMaxima + threadIdx.x] : 0.0f;
+      scale = power_scale(block_max(t, red));
+    }
+    if (a.scales && blockIdx.y == 0) {       // f, its first columns: the rows' constants too
+      t = int(threadIdx.x) < a.nmax ? a.maxima[2 * kMaxima + threadIdx.x] : 0.0f;
+      c = block_max(t, red);
+      float e = 1.0f;
+      if constexpr (PARTS == 2) {
+        t = int(threadIdx.x) < a.nmax ? a.maxima[kMaxima + threadIdx.x] : 0.0f;
+        e = power_scale(block_max(t, red));
+      }
+      if (blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{scale, e, c, 0.0f};
+    }
+  }
+  if (a.meta && blockIdx.y == 0 && threadIdx.x < 64) {
+    const int r = r0 + threadIdx.x;          // < np
+    RowMeta m{0.0f, 0.0f, -1, 0};
+    if (r < a.n) {
+      const int t = a.targets[r];
+      if (t >= 0) {
+        m.lse = a.lse[r];
+        m.rho = c > 0.0f ? a.w[r] / c : 0.0f;
+        m.target = t;
+        if (t >= a.V) m.rho = __builtin_nanf("");
+      }
+    }
+    a.meta[r] = m;
+  }
+  const T* x = static_cast<const T*>(a.x);
+#pragma unroll 4
+  for (int i = 0; i < 16; ++i) {
+    const int r = r0 + wave * 16 + i, k = k0 + lane;
+    float v = 0.0f;
+    if (r < a.n && k < a.K && (!a.targets || a.targets[r] >= 0)) v = load_value(x + r * a.stride + k);
+    tile[wave * 16 + i][lane] = v;
+  }
+  __syncthreads();
+  const int lr = lane & 15, lg = lane >> 4;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    const int b = wave * 2 + i, rt = b >> 1, kc = b & 1;      // 4 row tiles x 2 chunks
+    float v[8];
+    if (a.frag) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[rt * 16 + lr][kc * 32 + 8 * lg + j];
+      const int64_t KC = a.Kp / 32;
+      store_fragment<T, PARTS>(a.frag + ((int64_t(r0 / 16 + rt) * PARTS) * KC + (k0 / 32 + kc)) * kBlk + lane * 8,
+                               KC * kBlk, v, scale);
+    }
+    if (a.fragT) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = tile[kc * 32 + 8 * lg + j][rt * 16 + lr];
+      const int64_t RC = a.np / 32;
+      store_fragment<T, PARTS>(a.fragT + ((int64_t(k0 / 16 + rt) * PARTS) * RC + (r0 / 32 + kc)) * kBlk + lane * 8,
+                               RC * kBlk, v, scale);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Products: C[m][n] = sum_k A[m][k] W[n][k], both in fragment order.
+//
+// 16 TM x 16 TN per block; a stage brings two blocks of every row tile to LDS
+// (two chunks of 32 columns, or hi and lo of one), the next stage's are in
+// flight under its products.  256 x 256 with 8 waves: 64 KiB of DMA for 1,024
+// (bf16) or 1,536 (split) clocks of MFMA on each SIMD, one block per compute unit that
+// works through its items one after another.  128 x 128 with 4 waves, two
+// blocks a compute unit, where 256 x 256 leaves compute units idle.  An item is
+// a tile, or one of `splits` shares of a tile's stages.  Each XCD (blocks go
+// round-robin) works through a contiguous range of items, 8 n tiles wide at a
+// time, so that the tiles in flight share operands in its L2.
+// ---------------------------------------------------------------------------
+enum CeEpi { kStats = 0, kGrad = 1, kOut = 2, kPart = 3 };
+
+struct CeMmArgs {
+  const uint16_t *A, *W;
+  int ta, tw;                // row tiles of 16 in A and W
+  int KC;                    // chunks of 32 columns
+  int ntm, ntn, splits;
+  int64_t items;
+  const Scales* scales;      // NULL: all 1
+  // kStats
+  float2* part;              // [sub][part_stride]
+  int part_stride, sub0;
+  float* hit;                // [rows]: the target's logit
+  const int32_t* targets;
+  int R, V, v0;              // rows; vocabulary rows of the piece; its first
+  // kGrad
+  const RowMeta* meta;
+  uint16_t *G, *GT;          // [ta][parts][tw / 2], [tw][parts][ta / 2] blocks
+  // kOut: C to out; kPart: fp32 accumulators, added to if `add`
+  void* out;
+  int M, N;                  // of out
+  int is_de;                 // the scale to undo: 0 df (E), 1 dE (f)
+  float4* acc;
+  int add;
+};
+
+typedef __bf16 b8 __attribute__((ext_vector_type(8)));
+
+template <int PARTS>
+__device__ __forceinline__ f32x4 mma(const uint4& a, const uint4& b, f32x4 c) {
+  if constexpr (PARTS == 1)
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(b8, a), __builtin_bit_cast(b8, b), c, 0, 0, 0);
+  else
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(h8, a), __builtin_bit_cast(h8, b), c, 0, 0, 0);
+}
+
+// What multiplies an accumulator of a product with G.
+__device__ __forceinline__ float out_scale(const CeMmArgs& p, int parts) {
+  const float c = p.scales->c;
+  return parts == 1 ? c : c * (1.0f / kScaleG) * (1.0f / (p.is_de ? p.scales->f : p.scales->e));
+}
+
+template <class T>
+__device__ __forceinline__ void store_out(const CeMmArgs& p, int m, int n, const f32x4& v, float s) {
+  T* o = static_cast<T*>(p.out) + int64_t(m) * p.N + n;
+  const float x[4] = {v[0] * s, v[1] * s, v[2] * s, v[3] * s};
+  if (n + 4 <= p.N && p.N % 4 == 0) {
+    store_four(o, make_float4(x[0], x[1], x[2], x[3]));
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < p.N) store_value(o + i, x[i]);
+  }
+}
+
+// A 4 x 4 transpose of 16-bit values within quads of lanes: lane q (of 4) holds
+// x[i] for i = 0 .. 3 (pairs p01, p23) and receives element q of lanes 0 .. 3.
+__device__ __forceinline__ uint2 transpose4(uint32_t p01, uint32_t p23, int lane) {
+  const uint32_t q01 = __builtin_amdgcn_mov_dpp(p01, 0xB1, 0xF, 0xF, true);   // the neighbour's
+  const uint32_t q23 = __builtin_amdgcn_mov_dpp(p23, 0xB1, 0xF, 0xF, true);
+  // even lanes: (own even, neighbour's even); odd: (neighbour's odd, own odd).
+  // v_perm: bytes 0 - 3 come from the second operand, 4 - 7 from the first.
+  const uint32_t sel = lane & 1 ? 0x03020706u : 0x05040100u;
+  const uint32_t r0 = __builtin_amdgcn_perm(q01, p01, sel);
+  const uint32_t r1 = __builtin_amdgcn_perm(q23, p23, sel);
+  const uint32_t s = lane & 2 ? r0 : r1;
+  const uint32_t t = __builtin_amdgcn_mov_dpp(s, 0x4E, 0xF, 0xF, true);       // lane ^ 2's
+  return lane & 2 ? make_uint2(t, r1) : make_uint2(r0, t);
+}
+
+template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_ce_mm(CeMmArgs p) {
+  constexpr int NW = WN * WM, tn = TN / WN, tm = TM / WM;
+  constexpr int BUF = 2 * (TN + TM) * kBlk;             // one stage, in halves
+  constexpr int DPW = 2 * (TN + TM) / NW;               // blocks a wave moves per stage
+  constexpr int WWAVES = TN * NW / (TN + TM);           // waves that move W
+  static_assert(DPW * NW == 2 * (TN + TM) && WWAVES * DPW == 2 * TN && DPW % 2 == 0, "whole row tiles per wave");
+  constexpr bool kLoop = NW == 8;
+  constexpr int kStep = PARTS == 1 ? 2 : 1;             // chunks of a stage
+  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
+  uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
+  const int64_t per_xcd = (p.items + kXcd - 1) / kXcd;
+  const int64_t first = (blockIdx.x % kXcd) * per_xcd;
+  const int64_t last = first + per_xcd < p.items ? first + per_xcd : p.items;
+  const int64_t stride = gridDim.x / kXcd;
+  int64_t item = first + blockIdx.x / kXcd;
+  if (item >= last) return;                             // block-uniform
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int wn = wave % WN, wm = wave / WN;
+  const int stages = p.KC / kStep;
+
+  struct Where {
+    int nt, mt, split, s0, s1;
+  };
+  auto where = [&](int64_t t) {
+    Where w;
+    w.split = static_cast<int>(t / (int64_t(p.ntm) * p.ntn));
+    int i = static_cast<int>(t - int64_t(w.split) * p.ntm * p.ntn);
+    const int band = i / (8 * p.ntm);                   // 8 n tiles
+    const int width = min(8, p.ntn - 8 * band);
+    i -= band * 8 * p.ntm;
+    w.mt = i / width;
+    w.nt = 8 * band + i - w.mt * width;
+    w.s0 = static_cast<int>(int64_t(stages) * w.split / p.splits);
+    w.s1 = static_cast<int>(int64_t(stages) * (w.split + 1) / p.splits);
+    return w;
+  };
+  const bool weights = wave < WWAVES;
+  i32x4 rs;
+  uint32_t voff[DPW];
+  auto aim = [&](const Where& w) {
+    // The tile's own rows, as many as the matrix has: beyond them zeros.
+    const int t0 = weights ? w.nt * TN : w.mt * TM;
+    const int have = min(weights ? TN : TM, (weights ? p.tw : p.ta) - t0);
+    const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * PARTS * p.KC * kBlk;
+    rs = buffer_words(base, static_cast<uint32_t>(have) * PARTS * p.KC * (kBlk * 2));
+    const int mine = weights ? wave * (DPW / 2) : (wave - WWAVES) * (DPW / 2);
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) {
+      const int block = PARTS == 1 ? (mine + (i >> 1)) * p.KC + w.s0 * 2 + (i & 1)
+                                   : ((mine + (i >> 1)) * 2 + (i & 1)) * p.KC + w.s0;
+      voff[i] = static_cast<uint32_t>(block) * (kBlk * 2) + lane * 16;
+    }
+  };
+  const uint32_t dst0 = lds_address(lds + wave * DPW * kBlk);
+  auto issue = [&](int buf) {
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) {
+      dma16(rs, voff[i], 0u, dst0 + static_cast<uint32_t>((buf * BUF + i * kBlk) * 2));
+      voff[i] += kStep * kBlk * 2;
+    }
+  };
+  const uint16_t* const wl0 = lds + wn * tn * 2 * kBlk + lane * 8;
+  const uint16_t* const al0 = lds + (TN + wm * tm) * 2 * kBlk + lane * 8;
+
+  Where w = where(item);
+  aim(w);
+  issue(0);
+  int buf = 0;
+  for (;;) {
+    f32x4 acc[tn][tm];
+#pragma unroll
+    for (int i = 0; i < tn; ++i)
+#pragma unroll
+      for (int j = 0; j < tm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    const int64_t next = item + stride;
+    const bool more = kLoop && next < last;             // block-uniform
+    const Where wnext = more ? where(next) : w;
+    for (int c = w.s0; c < w.s1; ++c) {
+      wait_vmem();                                      // the stage has landed
+      __syncthreads();                                  // and every wave is done with the other buffer
+      if (c + 1 < w.s1) {
+        issue(buf ^ 1);
+      } else if (more) {
+        aim(wnext);
+        issue(buf ^ 1);
+      }
+      uint4 b0[tm], b1[tm];
+#pragma unroll
+      for (int j = 0; j < tm; ++j) {
+        b0[j] = *reinterpret_cast<const uint4*>(al0 + buf * BUF + 2 * j * kBlk);
+        b1[j] = *reinterpret_cast<const uint4*>(al0 + buf * BUF + (2 * j + 1) * kBlk);
+      }
+#pragma unroll
+      for (int i = 0; i < tn; ++i) {
+        const uint4 w0 = *reinterpret_cast<const uint4*>(wl0 + buf * BUF + 2 * i * kBlk);
+        const uint4 w1 = *reinterpret_cast<const uint4*>(wl0 + buf * BUF + (2 * i + 1) * kBlk);
+        if constexpr (PARTS == 1) {
+#pragma unroll
+          for (int j = 0; j < tm; ++j) acc[i][j] = mma<1>(w0, b0[j], acc[i][j]);
+#pragma unroll
+          for (int j = 0; j < tm; ++j) acc[i][j] = mma<1>(w1, b1[j], acc[i][j]);
+        } else {                                        // hi in 0, lo in 1
+#pragma unroll
+          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w1, b0[j], acc[i][j]);
+#pragma unroll
+          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w0, b1[j], acc[i][j]);
+#pragma unroll
+          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w0, b0[j], acc[i][j]);
+        }
+      }
+      buf ^= 1;
+    }
+
+    // acc[i][j][q] = C[16 (TM mt + tm wm + j) + lr][16 (TN nt + tn wn + i) + 4 lg + q]
+    const int mt0 = w.mt * TM + wm * tm, nt0 = w.nt * TN + wn * tn;
+    if constexpr (kEpi == kStats) {
+      const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
+      const int sub = p.sub0 + w.nt * WN + wn;
+#pragma unroll
+      for (int j = 0; j < tm; ++j) {
+        const int m = (mt0 + j) * 16 + lr;
+        const bool live = m < p.R;
+        const int target = live ? p.targets[m] - p.v0 : -1;
+        float top = -3.402823466e38f;
+#pragma unroll
+        for (int i = 0; i < tn; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int v = (nt0 + i) * 16 + 4 * lg + q;
+            acc[i][j][q] = v < p.V ? acc[i][j][q] * undo : -__builtin_inff();
+            top = fmaxf(top, acc[i][j][q]);
+            if (v == target && v < p.V) p.hit[m] = acc[i][j][q];
+          }
+        top = group4_max(top);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < tn; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (acc[i][j][q] - top));
+        sum = group4_sum(sum);
+        if (live && lg == 0) p.part[int64_t(sub) * p.part_stride + m] = make_float2(top, sum);
+      }
+    } else if constexpr (kEpi == kGrad) {
+      const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
+      const int GC = p.tw / 2, TC = p.ta / 2;           // chunks of 32 in G's and GT's rows
+#pragma unroll
+      for (int j = 0; j < tm; ++j) {
+        const int rt = mt0 + j;
+        if (rt >= p.ta) continue;                       // wave-uniform
+        const RowMeta m = p.meta[rt * 16 + lr];
+        const int target = m.target - p.v0;
+#pragma unroll
+        for (int i = 0; i < tn; ++i) {
+          const int nt = nt0 + i;
+          if (nt >= p.tw) continue;
+          float g[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            const int v = nt * 16 + 4 * lg + q;
+            const float e = exp2_f(kLog2e * (acc[i][j][q] * undo - m.lse));
+            g[q] = v < p.V ? m.rho * (v == target ? e - 1.0f : e) : 0.0f;
+          }
+          // G: row lr of its tile, columns 4 lg .. of 16.  GT: row 4 lg + (lr & 3), columns 4 (lr / 4) .. .
+          uint16_t* G = p.G + (int64_t(rt) * PARTS * GC + nt / 2) * kBlk +
+                        (16 * (2 * (nt & 1) + (lg >> 1)) + lr) * 8 + 4 * (lg & 1);
+          uint16_t* GT = p.GT + (int64_t(nt) * PARTS * TC + rt / 2) * kBlk +
+                         (16 * (2 * (rt & 1) + (lr >> 3)) + 4 * lg + (lr & 3)) * 8 + 4 * ((lr >> 2) & 1);
+          if constexpr (PARTS == 1) {
+            const uint32_t x = bf16_pair(g[0], g[1]), y = bf16_pair(g[2], g[3]);
+            *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
+            *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
+          } else {
+            uint16_t hi[4], lo[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) split_rn(g[q] * kScaleG, hi[q], lo[q]);
+            const uint32_t x = hi[0] | uint32_t(hi[1]) << 16, y = hi[2] | uint32_t(hi[3]) << 16;
+            const uint32_t z = lo[0] | uint32_t(lo[1]) << 16, u = lo[2] | uint32_t(lo[3]) << 16;
+            *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
+            *reinterpret_cast<uint2*>(G + int64_t(GC) * kBlk) = make_uint2(z, u);
+            *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
+            *reinterpret_cast<uint2*>(GT + int64_t(TC) * kBlk) = transpose4(z, u, lane);
+          }
+        }
+      }
+    } else if constexpr (kEpi == kOut) {
+      const float s = out_scale(p, PARTS);
+#pragma unroll
+      for (int i = 0; i < tn; ++i)
+#pragma unroll
+        for (int j = 0; j < tm; ++j) {
+          const int m = (mt0 + j) * 16 + lr, n = (nt0 + i) * 16 + 4 * lg;
+          if (m < p.M && n < p.N) store_out<T>(p, m, n, acc[i][j], s);
+        }
+    } else {
+      float4* a = p.acc + ((int64_t(w.split) * p.ntm + w.mt) * p.ntn + w.nt) * (TN * TM * 64) +
+                  wave * (tn * tm * 64) + lane;
+#pragma unroll
+      for (int i = 0; i < tn; ++i)
+#pragma unroll
+        for (int j = 0; j < tm; ++j) {
+          float4 v = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
+          if (p.add) {
+            const float4 o = a[(i * tm + j) * 64];
+            v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
+          }
+          a[(i * tm + j) * 64] = v;
+        }
+    }
+    if (!more) break;
+    item = next;
+    w = wnext;
+  }
+}
+
+// The shares of kPart's accumulators summed in order, to the result.
+template <class T, int PARTS, int TN, int TM, int WN, int WM>
+__global__ __launch_bounds__(64 * WN * WM) void k_ce_sum(CeMmArgs p) {
+  constexpr int tn = TN / WN, tm = TM / WM;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int wn = wave % WN, wm = wave / WN;
+  const int tile = blockIdx.x, mt = tile / p.ntn, nt = tile % p.ntn;
+  const int i = blockIdx.y / tm, j = blockIdx.y % tm;
+  const int m = (mt * TM + wm * tm + j) * 16 + lr, n = (nt * TN + wn * tn + i) * 16 + 4 * lg;
+  if (m >= p.M || n >= p.N) return;
+  const float4* a = p.acc + int64_t(tile) * (TN * TM * 64) + wave * (tn * tm * 64) + (i * tm + j) * 64 + lane;
+  const int64_t step = int64_t(p.ntm) * p.ntn * (TN * TM * 64);
+  f32x4 v{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < p.splits; ++s) {
+    const float4 x = a[s * step];
+    v[0] += x.x, v[1] += x.y, v[2] += x.z, v[3] += x.w;
+  }
+  store_out<T>(p, m, n, v, out_scale(p, PARTS));
+}
+
+// ---------------------------------------------------------------------------
+// The loss of a few rows (up to 16): E is read once and is all there is to
+// read.  A wave takes 16 vocabulary rows at a time straight from E into MFMA
+// operands (lane (lr, lg): row lr, 8 or 4 consecutive columns), the rows of f
+// wait in LDS; a lane keeps the running maximum and sum of its logits.  fp32
+// uses the fp32 matrix instruction.
+// ---------------------------------------------------------------------------
+struct RowsArgs {
+  const void *f, *E;
+  int64_t f_stride, e_stride;
+  const int32_t* targets;
+  int R, V, K;
+  float2* part;             // [gridDim.x][16]
+  float* hit;
+};
+
+constexpr int kRowsWaves = 8;
+
+template <class T>
+__global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
+  constexpr bool kB = sizeof(T) == 2;
+  constexpr int kW = 16 / sizeof(T);                    // columns of a lane's 16 bytes
+  constexpr int kChunk = 4 * kW;                        // columns of one step
+  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
+  T* const fl = reinterpret_cast<T*>(ce_lds);           // [chunk][lane][kW]
+  __shared__ float2 red[kRowsWaves][16];
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
+  const int chunks = (a.K + kChunk - 1) / kChunk;
+  const T* f = static_cast<const T*>(a.f);
+  for (int c = wave; c < chunks; c += kRowsWaves)
+#pragma unroll
+    for (int j = 0; j < kW; ++j) {
+      const int k = c * kChunk + lg * kW + j;
+      const bool on = lr < a.R && k < a.K && a.targets[lr] >= 0;
+      T z{};
+      fl[(c * 64 + lane) * kW + j] = on ? f[lr * a.f_stride + k] : z;
+    }
+  __syncthreads();
+  const int target = lr < a.R ? a.targets[lr] : -1;
+  float top = -3.402823466e38f, sum = 0.0f;
+  const int tiles = (a.V + 15) / 16;
+  const int full = a.K / kChunk;                        // chunks without a tail
+  const T* E = static_cast<const T*>(a.E);
+  for (int t = blockIdx.x * kRowsWaves + wave; t < tiles; t += gridDim.x * kRowsWaves) {
+    const int row = min(t * 16 + lr, a.V - 1);          // rows past the end repeat the last and are masked below
+    const T* e = E + row * a.e_stride + lg * kW;
+    f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
+    auto step = [&](const uint4& x, int c) {
+      const uint4 y = *reinterpret_cast<const uint4*>(fl + (c * 64 + lane) * kW);
+      if constexpr (kB) {
+        if (c & 1)
+          acc2 = mma<1>(x, y, acc2);
+        else
+          acc = mma<1>(x, y, acc);
+      } else {
+        const float4 xf = __builtin_bit_cast(float4, x), yf = __builtin_bit_cast(float4, y);
+        if (c & 1)
+          acc2 = mfma_k16(xf, yf, acc2);
+        else
+          acc = mfma_k16(xf, yf, acc);
+      }
+    };
+    int c = 0;
+    for (; c + 8 <= full; c += 8) {
+      uint4 x[8];
+#pragma unroll
+      for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const uint4*>(e + (c + u) * kChunk);
+#pragma unroll
+      for (int u = 0; u < 8; ++u) step(x[u], c + u);
+    }
+    for (; c < full; ++c) step(*reinterpret_cast<const uint4*>(e + c * kChunk), c);
+    if (c < chunks) {                                   // the tail, column by column
+      T tail[kW];
+#pragma unroll
+      for (int j = 0; j < kW; ++j) {
+        T z{};
+        tail[j] = c * kChunk + lg * kW + j < a.K ? e[c * kChunk + j] : z;
+      }
+      uint4 x;
+      __builtin_memcpy(&x, tail, 16);
+      step(x, c);
+    }
+    // acc[q] = logit of row lr, vocabulary row 16 t + 4 lg + q
+    float l[4], most = top;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int v = t * 16 + 4 * lg + q;
+      l[q] = v < a.V ? acc[q] + acc2[q] : -__builtin_inff();
+      most = fmaxf(most, l[q]);
+      if (v == target && v < a.V) a.hit[lr] = l[q];
+    }
+    sum *= exp2_f(kLog2e * (top - most));
+#pragma unroll
+    for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (l[q] - most));
+    top = most;
+  }
+  const float all = group4_max(top);
+  sum = group4_sum(sum * exp2_f(kLog2e * (top - all)));
+  if (lg == 0) red[wave][lr] = make_float2(all, sum);
+  __syncthreads();
+  if (threadIdx.x < 16) {
+    float m = -3.402823466e38f, s = 0.0f;
+    for (int w = 0; w < kRowsWaves; ++w) m = fmaxf(m, red[w][threadIdx.x].x);
+    for (int w = 0; w < kRowsWaves; ++w) s += red[w][threadIdx.x].y * exp2_f(kLog2e * (red[w][threadIdx.x].x - m));
+    a.part[blockIdx.x * 16 + threadIdx.x] = make_float2(m, s);
+  }
+}
+
+// ---------------------------------------------------------------------------
+// The parts of every row joined, 16 rows a block: lse and loss.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void k_ce_join(const float2* part, int subs, int stride, const int32_t* targets,
+                                                 const float* hit, int R, int V, float* loss, float* lse) {
+  __shared__ float2 red[16][16];
+  const int lr = threadIdx.x & 15, w = threadIdx.x >> 4, r = blockIdx.x * 16 + lr;
+  float top = -3.402823466e38f, sum = 0.0f;
+  if (r < R)
+    for (int s = w; s < subs; s += 16) {
+      const float2 x = part[int64_t(s) * stride + r];
+      const float m = fmaxf(top, x.x);
+      sum = sum * exp2_f(kLog2e * (top - m)) + x.y * exp2_f(kLog2e * (x.x - m));
+      top = m;
+    }
+  red[w][lr] = make_float2(top, sum);
+  __syncthreads();
+  if (w != 0 || r >= R) return;
+  float m = -3.402823466e38f, s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = fmaxf(m, red[i][lr].x);
+#pragma unroll
+  for (int i = 0; i < 16; ++i) s += red[i][lr].y * exp2_f(kLog2e * (red[i][lr].x - m));
+  const int t = targets[r];
+  float l = 0.0f, out = 0.0f;
+  if (t >= 0) {
+    l = m + kLog2 * __builtin_amdgcn_logf(s);
+    out = t < V ? (m - hit[r]) + kLog2 * __builtin_amdgcn_logf(s) : __builtin_nanf("");
+  }
+  if (lse) lse[r] = l;
+  if (loss) loss[r] = out;
+}
+
+__global__ __launch_bounds__(256) void k_ce_zero(uint16_t* x, int64_t halves) {
+  for (int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x; i < halves; i += int64_t(gridDim.x) * 256) x[i] = 0;
+}
+
+// ---------------------------------------------------------------------------
+// Host
+// ---------------------------------------------------------------------------
+constexpr int64_t kFill = 256;            // tiles that fill the card
+constexpr int kRowsBlocks = 512;          // blocks of k_ce_rows
+constexpr size_t kRowsLds = 65536;        // f's rows in LDS
+
+int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
+
+struct Sizes {
+  int64_t Rp, Kp, Vp;                     // padded to 64; Vp of the largest piece
+  int parts;
+  size_t part, hit, maxima, scales, meta, f, fT, e, eT, G, GT, accf, acce, total;
+};
+
+// Accumulators of a product of m x n outputs over k columns whose stages are
+// shared out: at most max(tiles, 2 kFill) tiles (choose_splits), for either
+// size of tile.
+size_t acc_bytes(int64_t m, int64_t n, int64_t stages) {
+  int64_t most = 0;
+  for (int64_t side : {128, 256}) {
+    const int64_t tiles = up(m, side) / side * (up(n, side) / side);
+    most = std::max(most, std::max(tiles, std::min(tiles * stages, 2 * kFill)) * side * side);
+  }
+  return size_t(most) * 4;
+}
+
+Sizes sizes_of(const soma_ce_config& c, bool grad) {
+  Sizes s{};
+  s.Rp = up(c.rows, 64);
+  s.Kp = up(c.width, 64);
+  s.Vp = up(std::min<int64_t>(c.vocab, kPiece), 64);
+  s.parts = c.type == SOMA_FLOAT ? 2 : 1;
+  size_t at = 0;
+  auto take = [&](size_t bytes) {
+    const size_t o = at;
+    at += up256(bytes);
+    return o;
+  };
+  const size_t half = size_t(s.parts) * 2;
+  if (!grad) {
+    s.part = take(std::max(size_t(up(c.vocab, 64) / 64 + 4 * (c.vocab / kPiece + 1)) * s.Rp, size_t(kRowsBlocks) * 16) * 8);
+    s.hit = take(size_t(s.Rp) * 4);
+  } else {
+    s.meta = take(size_t(s.Rp) * sizeof(RowMeta));
+  }
+  s.maxima = take(3 * kMaxima * 4);
+  s.scales = take(sizeof(Scales));
+  s.f = take(size_t(s.Rp) * s.Kp * half);
+  s.e = take(size_t(s.Vp) * s.Kp * half);
+  if (grad) {
+    s.fT = take(size_t(s.Rp) * s.Kp * half);
+    s.eT = take(size_t(s.Vp) * s.Kp * half);
+    s.G = take(size_t(s.Rp) * s.Vp * half);
+    s.GT = take(size_t(s.Rp) * s.Vp * half);
+    s.accf = take(acc_bytes(s.Rp, s.Kp, s.Vp / 32));
+    s.acce = take(acc_bytes(s.Vp, s.Kp, s.Rp / 32));
+  }
+  s.total = at;
+  return s;
+}
+
+int check_ce(const soma_ce_config* c) {
+  if (!c) return set_error(SOMA_EINVAL, "cfg is NULL");
+  if (!is_type(c->type)) return set_error(SOMA_EINVAL, "unknown type %d", c->type);
+  // a row tile of G^T is addressed in 32 bits
+  if (c->rows < 0 || c->rows > (1 << 20)) return set_error(SOMA_ESHAPE, "rows must be in [0, 2^20]");
+  if (c->vocab < 1 || c->vocab > (1 << 24)) return set_error(SOMA_ESHAPE, "vocab must be in [1, 2^24]");
+  if (c->width < 1 || c->width > (1 << 16)) return set_error(SOMA_ESHAPE, "width must be in [1, 2^16]");
+  if (c->f_stride < c->width || c->e_stride < c->width || c->f_stride > (int64_t(1) << 32) ||
+      c->e_stride > (int64_t(1) << 32))
+    return set_error(SOMA_ESHAPE, "f_stride and e_stride must be at least width");
+  return SOMA_OK;
+}
+
+// Shares of every tile's stages: as many as bring the items to kFill, at
+// least four stages each.
+int choose_splits(int64_t tiles, int64_t stages) {
+  return int(std::max<int64_t>(1, std::min(kFill / std::max<int64_t>(tiles, 1), stages / 4)));
+}
+
+template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM>
+int launch_mm_tile(CeMmArgs& p, hipStream_t st) {
+  p.items = int64_t(p.ntm) * p.ntn * p.splits;
+  int64_t blocks = up(p.items, kXcd);
+  if (WN * WM == 8) blocks = std::min<int64_t>(blocks, kFill);
+  if (blocks >= (int64_t(1) << 31)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
+  constexpr unsigned lds = 2u * 2u * unsigned(TN + TM) * 1024u;
+  const void* kern = reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, TN, TM, WN, WM>);
+  const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
+  hipLaunchKernelGGL((k_ce_mm<T, PARTS, kEpi, TN, TM, WN, WM>), dim3(unsigned(blocks)), dim3(64 * WN * WM), lds, st, p);
+  return launched("k_ce_mm");
+}
+
+// 256 x 256 where those tiles (or their shares) fill the card, else 128 x 128.
+bool large_tiles(int64_t m, int64_t n, int64_t stages, bool shares) {
+  const int64_t tiles = up(m, 256) / 256 * (up(n, 256) / 256);
+  if (up(m, 256) - m >= 128 || up(n, 256) - n >= 128) return tiles >= 2 * kFill;
+  return tiles * (shares ? choose_splits(tiles, stages) : 1) >= kFill * 3 / 4;
+}
+
+void tiles_of(CeMmArgs& p, int side) {
+  p.ntm = (p.ta + side / 16 - 1) / (side / 16);
+  p.ntn = (p.tw + side / 16 - 1) / (side / 16);
+}
+
+template <class T, int PARTS, int kEpi>
+int launch_logits(CeMmArgs& p, bool large, hipStream_t st) {
+  p.splits = 1;
+  tiles_of(p, large ? 256 : 128);
+  return large ? launch_mm_tile<T, PARTS, kEpi, 16, 16, 2, 4>(p, st) : launch_mm_tile<T, PARTS, kEpi, 8, 8, 2, 2>(p, st);
+}
+
+// How the products of all pieces are shared out, by the first and largest.
+struct Shares {
+  bool large;
+  int splits;
+};
+Shares shares_of(int64_t m, int64_t n, int64_t stages) {
+  const bool large = large_tiles(m, n, stages, true);
+  const int64_t side = large ? 256 : 128;
+  return {large, choose_splits(up(m, side) / side * (up(n, side) / side), stages)};
+}
+
+// One product with G.  `single`: it alone gives the result; else the result
+// is the sum of several calls (`add` from the second on), which the one with
+// `finish` brings to the output.
+template <class T, int PARTS>
+int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipStream_t st) {
+  tiles_of(p, sh.large ? 256 : 128);
+  p.splits = sh.splits;
+  if (single && p.splits == 1)
+    return sh.large ? launch_mm_tile<T, PARTS, kOut, 16, 16, 2, 4>(p, st)
+                    : launch_mm_tile<T, PARTS, kOut, 8, 8, 2, 2>(p, st);
+  // A last piece of fewer stages than shares adds to the first ones only.
+  p.splits = std::min(sh.splits, p.KC / (PARTS == 1 ? 2 : 1));
+  if (int rc = sh.large ? launch_mm_tile<T, PARTS, kPart, 16, 16, 2, 4>(p, st)
+                        : launch_mm_tile<T, PARTS, kPart, 8, 8, 2, 2>(p, st))
+    return rc;
+  if (!finish) return SOMA_OK;
+  p.splits = sh.splits;
+  if (sh.large)
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 4>), dim3(unsigned(p.ntm * p.ntn), 8 * 4), dim3(512), 0, st, p);
+  else
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8, 2, 2>), dim3(unsigned(p.ntm * p.ntn), 4 * 4), dim3(256), 0, st, p);
+  return launched("k_ce_sum");
+}
+
+template <class T, int PARTS>
+int launch_pack(const PackArgs& a, hipStream_t st) {
+  hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(unsigned(a.np / 64), unsigned(a.Kp / 64)), dim3(256), 0, st, a);
+  return launched("k_ce_pack");
+}
+
+template <class T, int PARTS>
+int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int32_t* targets, float* loss, float* lse,
+               char* ws, hipStream_t st) {
+  const Sizes s = sizes_of(c, false);
+  float2* part = reinterpret_cast<float2*>(ws + s.part);
+  float* hit = reinterpret_cast<float*>(ws + s.hit);
+  int subs = 0, stride = 0;
+  // A few rows: E straight from memory, where its rows allow 16-byte loads.
+  const size_t rows_lds = size_t(up(c.width, 64)) * 16 * sizeof(T);
+  if (c.rows <= 16 && rows_lds <= kRowsLds && is_aligned(E, 16) && c.e_stride * sizeof(T) % 16 == 0) {
+    const RowsArgs a{f, E, c.f_stride, c.e_stride, targets, c.rows, c.vocab, c.width, part, hit};
+    subs = int(std::min<int64_t>(kRowsBlocks, (up(c.vocab, 16) / 16 + kRowsWaves - 1) / kRowsWaves));
+    stride = 16;
+    const hipError_t he = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ce_rows<T>),
+                                              hipFuncAttributeMaxDynamicSharedMemorySize, int(kRowsLds));
+    if (he != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(he));
+    hipLaunchKernelGGL(k_ce_rows<T>, dim3(subs), dim3(64 * kRowsWaves), unsigned(rows_lds), st, a);
+    if (int rc = launched("k_ce_rows")) return rc;
+  } else {
+    float* maxima = reinterpret_cast<float*>(ws + s.maxima);
+    Scales* scales = reinterpret_cast<Scales*>(ws + s.scales);
+    uint16_t* fp = reinterpret_cast<uint16_t*>(ws + s.f);
+    uint16_t* ep = reinterpret_cast<uint16_t*>(ws + s.e);
+    if (PARTS == 2) {
+      const MaxArgs m{f, E, nullptr, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
+      hipLaunchKernelGGL(k_ce_max<T>, dim3(kMaxima, 3), dim3(256), 0, st, m, 0);
+      if (int rc = launched("k_ce_max")) return rc;
+    }
+    PackArgs a{};
+    a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
+    a.targets = targets, a.frag = fp, a.maxima = PARTS == 2 ? maxima : nullptr, a.nmax = kMaxima, a.scales = scales;
+    a.V = c.vocab;
+    if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
+    stride = int(s.Rp);
+    for (int v0 = 0; v0 < c.vocab; v0 += kPiece) {
+      const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
+      PackArgs b{};
+      b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
+      b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.which = 1, b.nmax = kMaxima;
+      if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
+      CeMmArgs p{};
+      p.A = fp, p.W = ep, p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
+      p.part = part, p.part_stride = stride, p.sub0 = subs, p.hit = hit, p.targets = targets, p.R = c.rows, p.V = n, p.v0 = v0;
+      const bool large = large_tiles(s.Rp, np, 0, false);
+      if (int rc = launch_logits<T, PARTS, kStats>(p, large, st)) return rc;
+      subs += p.ntn * 2;
+    }
+  }
+  hipLaunchKernelGGL(k_ce_join, dim3((c.rows + 15) / 16), dim3(256), 0, st, part, subs, stride, targets, hit, c.rows,
+                     c.vocab, loss, lse);
+  return launched("k_ce_join");
+}
+
+template <class T, int PARTS>
+int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int32_t* targets, const float* lse,
+               const float* w, void* df, void* dE, char* ws, hipStream_t st) {
+  const Sizes s = sizes_of(c, true);
+  float* maxima = reinterpret_cast<float*>(ws + s.maxima);
+  Scales* scales = reinterpret_cast<Scales*>(ws + s.scales);
+  RowMeta* meta = reinterpret_cast<RowMeta*>(ws + s.meta);
+  auto at = [&](size_t o) { return reinterpret_cast<uint16_t*>(ws + o); };
+  const MaxArgs m{f, E, w, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
+  hipLaunchKernelGGL(k_ce_max<T>, dim3(kMaxima, PARTS == 2 ? 3 : 1), dim3(256), 0, st, m, PARTS == 2 ? 0 : 2);
+  if (int rc = launched("k_ce_max")) return rc;
+  PackArgs a{};
+  a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
+  a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = kMaxima;
+  a.scales = scales, a.meta = meta, a.lse = lse, a.w = w, a.V = c.vocab;
+  if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
+  constexpr int kStageCols = PARTS == 1 ? 64 : 32;
+  const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp / kStageCols);
+  for (int v0 = 0; v0 < c.vocab; v0 += kPiece) {
+    const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
+    PackArgs b{};
+    b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
+    b.np = np, b.Kp = int(s.Kp), b.frag = at(s.e), b.fragT = df ? at(s.eT) : nullptr;
+    b.maxima = PARTS == 2 ? maxima : nullptr, b.which = 1, b.nmax = kMaxima;
+    if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
+    CeMmArgs p{};
+    p.A = at(s.f), p.W = at(s.e), p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
+    p.meta = meta, p.G = at(s.G), p.GT = at(s.GT), p.V = n, p.v0 = v0;
+    if (int rc = launch_logits<T, PARTS, kGrad>(p, large_tiles(s.Rp, np, 0, false), st)) return rc;
+    if (df) {
+      CeMmArgs q{};
+      q.A = at(s.G), q.W = at(s.eT), q.ta = int(s.Rp / 16), q.tw = int(s.Kp / 16), q.KC = np / 32, q.scales = scales;
+      q.out = df, q.M = c.rows, q.N = c.width, q.acc = reinterpret_cast<float4*>(ws + s.accf), q.add = v0 > 0;
+      if (int rc = launch_product<T, PARTS>(q, of_df, c.vocab <= kPiece, v0 + kPiece >= c.vocab, st)) return rc;
+    }
+    if (dE) {
+      CeMmArgs q{};
+      q.A = at(s.GT), q.W = at(s.fT), q.ta = np / 16, q.tw = int(s.Kp / 16), q.KC = int(s.Rp / 32), q.scales = scales;
+      q.out = static_cast<T*>(dE) + int64_t(v0) * c.width, q.M = n, q.N = c.width, q.is_de = 1;
+      q.acc = reinterpret_cast<float4*>(ws + s.acce);
+      if (int rc = launch_product<T, PARTS>(q, shares_of(np, s.Kp, s.Rp / kStageCols), true, true, st)) return rc;
+    }
+  }
+  return SOMA_OK;
+}
+
+}  // namespace
+}  // namespace soma
+
+using namespace soma;
+
+extern "C" {
+
+int soma_ce_workspace_size(const soma_ce_config* cfg, int grad, size_t* bytes) {
+  if (int rc = check_ce(cfg)) return rc;
+  if (!bytes) return set_error(SOMA_EINVAL, "bytes is NULL");
+  *bytes = sizes_of(*cfg, false).total;
+  if (grad) *bytes = std::max(*bytes, sizes_of(*cfg, true).total);
+  return set_ok();
+}
+
+int soma_ce_loss(const soma_ce_config* cfg, const void* f, const void* E, const int32_t* targets, float* loss, float* lse,
+                 void* workspace, size_t ws_bytes, void* stream) {
+  if (int rc = check_ce(cfg)) return rc;
+  const soma_ce_config& c = *cfg;
+  if (c.rows == 0) return set_ok();
+  if (!f || !E || !targets || (!loss && !lse)) return set_error(SOMA_EINVAL, "NULL device pointer");
+  const size_t e = type_size(c.type);
+  if (!is_aligned(f, e) || !is_aligned(E, e) || !is_aligned(targets, 4) || !is_aligned(loss, 4) || !is_aligned(lse, 4))
+    return set_error(SOMA_EINVAL, "a pointer is not aligned to its elements");
+  if (int rc = check_workspace(workspace, ws_bytes, sizes_of(c, false).total)) return rc;
+  char* ws = static_cast<char*>(workspace);
+  const hipStream_t st = stream_of(stream);
+  if (int rc = c.type == SOMA_FLOAT ? loss_typed<float, 2>(c, f, E, targets, loss, lse, ws, st)
+                                    : loss_typed<bf16, 1>(c, f, E, targets, loss, lse, ws, st))
+    return rc;
+  return set_ok();
+}
+
+int soma_ce_grad(const soma_ce_config* cfg, const void* f, const void* E, const int32_t* targets, const float* lse,
+                 const float* grad_loss, void* df, void* dE, void* workspace, size_t ws_bytes, void* stream) {
+  if (int rc = check_ce(cfg)) return rc;
+  const soma_ce_config& c = *cfg;
+  const size_t e = type_size(c.type);
+  if (!df && !dE) return set_error(SOMA_EINVAL, "neither df nor dE is wanted");
+  if (c.rows > 0 && (!f || !E || !targets || !lse || !grad_loss)) return set_error(SOMA_EINVAL, "NULL device pointer");
+  if (!is_aligned(f, e) || !is_aligned(E, e) || !is_aligned(targets, 4) || !is_aligned(lse, 4) ||
+      !is_aligned(grad_loss, 4))
+    return set_error(SOMA_EINVAL, "a pointer is not aligned to its elements");
+  if (!is_aligned(df, 16) || !is_aligned(dE, 16)) return set_error(SOMA_EINVAL, "df and dE must be 16-byte aligned");
+  if (int rc = check_workspace(workspace, ws_bytes, sizes_of(c, true).total)) return rc;
+  const hipStream_t st = stream_of(stream);
+  if (c.rows == 0) {                      // no row: dE is a sum of nothing
+    if (dE) {
+      const int64_t halves = int64_t(c.vocab) * c.width * int64_t(e) / 2;
+      hipLaunchKernelGGL(k_ce_zero, dim3(1024), dim3(256), 0, st, static_cast<uint16_t*>(dE), halves);
+      if (int rc = launched("k_ce_zero")) return rc;
+    }
+    return set_ok();
+  }
+  char* ws = static_cast<char*>(workspace);
+  if (int rc = c.type == SOMA_FLOAT ? grad_typed<float, 2>(c, f, E, targets, lse, grad_loss, df, dE, ws, st)
+                                    : grad_typed<bf16, 1>(c, f, E, targets, lse, grad_loss, df, dE, ws, st))
+    return rc;
+  return set_ok();
+}
+
+}  // extern "C"

@@ -30,8 +30,8 @@ EXPORTS = ("soma_param_count", "soma_workspace_size", "soma_create", "soma_destr
            "soma_gaussian", "soma_probe", "soma_philox", "soma_box_muller", "soma_set_phase_timing",
            "soma_get_phase_times", "soma_get_narrow_projections", "soma_set_spin_limit", "soma_spsa_step_noalloc",
            "soma_scan_workspace_size", "soma_scan_forward", "soma_scan_backward", "soma_scan_step",
-           "soma_adamw_workspace_size", "soma_adamw_create", "soma_adamw_destroy", "soma_adamw_step",
-           "soma_adamw_moments", "soma_last_error")
+           "soma_ce_workspace_size", "soma_ce_loss", "soma_ce_grad", "soma_adamw_workspace_size", "soma_adamw_create",
+           "soma_adamw_destroy", "soma_adamw_step", "soma_adamw_moments", "soma_last_error")
 
 
 class SomaError(RuntimeError):
@@ -88,6 +88,11 @@ class ScanConfig(ctypes.Structure):
                 ("type", ctypes.c_int32), ("gate_stride", ctypes.c_int64)]
 
 
+class CrossEntropyConfig(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("vocab", ctypes.c_int32), ("width", ctypes.c_int32),
+                ("type", ctypes.c_int32), ("f_stride", ctypes.c_int64), ("e_stride", ctypes.c_int64)]
+
+
 class AdamWTensor(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("param", "grad", "m", "v", "m_scale", "v_scale", "copy")] + [
         ("count", ctypes.c_int64), ("weight_decay", ctypes.c_double)] + [
@@ -141,6 +146,10 @@ def load():
             "soma_scan_forward": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 7 + [ctypes.c_size_t, vp]),
             "soma_scan_backward": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
             "soma_scan_step": (ctypes.c_int, [ctypes.POINTER(ScanConfig)] + [vp] * 5),
+            "soma_ce_workspace_size": (ctypes.c_int, [ctypes.POINTER(CrossEntropyConfig), ctypes.c_int,
+                                                      ctypes.POINTER(ctypes.c_size_t)]),
+            "soma_ce_loss": (ctypes.c_int, [ctypes.POINTER(CrossEntropyConfig)] + [vp] * 6 + [ctypes.c_size_t, vp]),
+            "soma_ce_grad": (ctypes.c_int, [ctypes.POINTER(CrossEntropyConfig)] + [vp] * 8 + [ctypes.c_size_t, vp]),
             "soma_adamw_workspace_size": (ctypes.c_int, [ctypes.POINTER(AdamWTensor), ctypes.c_int32,
                                                          ctypes.POINTER(ctypes.c_size_t)]),
             "soma_adamw_create": (ctypes.c_int, [ctypes.POINTER(AdamWTensor), ctypes.c_int32, vp, ctypes.c_size_t, vp,
@@ -485,6 +494,12 @@ def _row_stride(t) -> int:
     return t.stride(0) if t.shape[0] > 1 else t.shape[1]
 
 
+def _check_sizes(**sizes):
+    for name, n in sizes.items():
+        if not 0 <= n < 2**31:
+            raise ValueError(f"{name} must be in [0, 2^31)")
+
+
 class GatedScan(_Plan):
     """The gated linear recurrence: the LSTM's cell with gates that read the
     input alone, c_t = s(f_t) c_{t-1} + s(i_t) tanh(g_t), h_t = s(o_t) tanh(c_t),
@@ -500,9 +515,7 @@ class GatedScan(_Plan):
     def __init__(self, rows: int, sequences: int, width: int, dtype, device="cuda"):
         self.rows, self.sequences, self.width, self.dtype = int(rows), int(sequences), int(width), dtype
         self._type = _type_of(dtype)
-        for name in ("rows", "sequences", "width"):
-            if not 0 <= getattr(self, name) < 2**31:
-                raise ValueError(f"{name} must fit 31 bits")
+        _check_sizes(rows=self.rows, sequences=self.sequences, width=self.width)
         out = ctypes.c_size_t()
         _check(load().soma_scan_workspace_size(ctypes.byref(self._cfg(self.rows, 4 * self.width)), ctypes.byref(out)))
         self._bytes = out.value
@@ -566,6 +579,57 @@ class GatedScan(_Plan):
         self._call(stream, load().soma_scan_step, ctypes.byref(cfg), pg,
                    self._ptr(c0, "c0", torch.float32, end, optional=True), self._ptr(cT, "cT", torch.float32, end),
                    self._ptr(h, "h", self.dtype, end))
+
+
+class CrossEntropy(_Plan):
+    """Softmax cross entropy of a linear head, logits f E^T, for at most ``rows``
+    rows f [n][width] and a head E [vocab][width] of ``dtype`` (float32 or
+    bfloat16; rows may be strided), without the logits in memory.  targets [n]
+    int32; a row with a negative one counts for nothing.  grad: gradients are
+    wanted too (a larger workspace)."""
+
+    def __init__(self, rows: int, vocab: int, width: int, dtype, grad: bool = True, device="cuda"):
+        self.rows, self.vocab, self.width, self.dtype, self.with_grad = int(rows), int(vocab), int(width), dtype, bool(grad)
+        self._type = _type_of(dtype)
+        _check_sizes(rows=self.rows, vocab=self.vocab, width=self.width)
+        out = ctypes.c_size_t()
+        cfg = CrossEntropyConfig(self.rows, self.vocab, self.width, self._type, self.width, self.width)
+        _check(load().soma_ce_workspace_size(ctypes.byref(cfg), int(self.with_grad), ctypes.byref(out)))
+        self._bytes = out.value
+        self._start(out.value, device)
+
+    def _inputs(self, f, E, targets):
+        import torch
+        if not isinstance(f, torch.Tensor) or f.dim() != 2:
+            raise TypeError("f must be a tensor [rows][width]")
+        n = f.shape[0]
+        if n > self.rows:
+            raise ValueError(f"{n} rows, but the plan was made for {self.rows}")
+        pf = self._ptr(f, "f", self.dtype, (n, self.width), strided=True)
+        pe = self._ptr(E, "E", self.dtype, (self.vocab, self.width), strided=True)
+        cfg = CrossEntropyConfig(n, self.vocab, self.width, self._type, _row_stride(f), _row_stride(E))
+        return n, cfg, pf, pe, self._ptr(targets, "targets", torch.int32, (n,))
+
+    def loss(self, f, E, targets, loss, lse=None, stream=None):
+        """loss [n] and lse [n] (float32): the rows' cross entropies in nats and
+        log-sum-exps."""
+        import torch
+        n, cfg, pf, pe, pt = self._inputs(f, E, targets)
+        self._call(stream, load().soma_ce_loss, ctypes.byref(cfg), pf, pe, pt,
+                   self._ptr(loss, "loss", torch.float32, (n,), optional=True),
+                   self._ptr(lse, "lse", torch.float32, (n,), optional=True), self._ws, self._bytes)
+
+    def grad(self, f, E, targets, lse, grad_loss, df=None, dE=None, stream=None):
+        """df [n][width] and dE [vocab][width] (either may be None) of
+        sum(grad_loss * loss), with the lse that loss() gave."""
+        import torch
+        if not self.with_grad:
+            raise ValueError("the plan was made without gradients")
+        n, cfg, pf, pe, pt = self._inputs(f, E, targets)
+        self._call(stream, load().soma_ce_grad, ctypes.byref(cfg), pf, pe, pt,
+                   self._ptr(lse, "lse", torch.float32, (n,)), self._ptr(grad_loss, "grad_loss", torch.float32, (n,)),
+                   self._ptr(df, "df", self.dtype, (n, self.width), optional=True),
+                   self._ptr(dE, "dE", self.dtype, (self.vocab, self.width), optional=True), self._ws, self._bytes)
 
 
 class AdamW(_Plan):

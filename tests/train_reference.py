@@ -98,3 +98,45 @@ def adamw(p, g, m, v, t, lr, b1, b2, delta, decay, scale=1.0):
     m = b1 * m + (1 - b1) * g
     v = b2 * v + (1 - b2) * g * g
     return (1 - lr * decay) * p - lr * (m / (1 - b1 ** t)) / (np.sqrt(v / (1 - b2 ** t)) + delta), m, v
+
+
+def cross_entropy(f, E, targets, w=None):
+    """f [R][K], E [V][K] (float64), targets; rows with a negative target are left out.  Returns a dict of loss, lse
+    (and df, dE) with bounds under the name + "_err" in units that the caller scales: "<name>_fp32", sums of absolute
+    products (times 2^-24 and a small count), and "<name>_g16", what rounding the softmax's part to bf16 may add;
+    "<name>_tiny" is the bound of what parts of fp32 operands in fp16's subnormals may add."""
+    has = targets >= 0
+    f = np.where(has[:, None], f, 0.0)
+    at = np.where(has, targets, 0)
+    l = f @ E.T
+    mag = np.abs(f) @ np.abs(E).T                      # sums of absolute products
+    top = l.max(1, keepdims=True)
+    lse = (top + np.log(np.exp(l - top).sum(1, keepdims=True)))[:, 0]
+    rows = np.arange(len(at))
+    p = np.exp(l - lse[:, None])
+    out = {"lse": np.where(has, lse, 0.0), "loss": np.where(has, lse - l[rows, at], 0.0)}
+    # an error of every logit of e_l = d mag_rv moves lse by at most its average over p
+    out["lse_fp32"] = np.where(has, (p * mag).sum(1) + np.abs(lse), 0.0)
+    out["loss_fp32"] = np.where(has, (p * mag).sum(1) + mag[rows, at] + np.abs(out["loss"]) + np.abs(lse), 0.0)
+    if w is None:
+        return out
+    w = np.where(has, w, 0.0)
+    g = p.copy()
+    g[rows, at] -= 1.0
+    g *= w[:, None]
+    out["df"], out["dE"] = g @ E, g.T @ f
+    # a logit's error e_l changes p by p (e_l + its row's lse error); then the product's own sums
+    gl = np.abs(w)[:, None] * p * (mag + (p * mag).sum(1, keepdims=True) + 2 * np.abs(l - lse[:, None]) + 1.0)
+    out["df_fp32"] = gl @ np.abs(E) + np.abs(g) @ np.abs(E)
+    out["dE_fp32"] = gl.T @ np.abs(f) + np.abs(g).T @ np.abs(f)
+    # fp32 operands are two fp16 parts of x s, s a power of two that brings the array's largest to 2^13 or more: where
+    # the second part is subnormal its rounding is 2^-25, so x is off by up to 2^-25 / s <= 2^-38 of the largest.
+    # (G's largest counts as max |w|.)
+    tiny = 2.0 ** -38
+    c, mf, mE = np.abs(w).max(), np.abs(f).max(), np.abs(E).max()
+    el = tiny * (mf * np.abs(E).sum(1)[None, :] + mE * np.abs(f).sum(1)[:, None])
+    gt = np.abs(w)[:, None] * p * (el + (p * el).sum(1, keepdims=True)) + c * tiny
+    out["df_tiny"] = gt @ np.abs(E) + tiny * mE * np.abs(g).sum(1, keepdims=True)
+    out["dE_tiny"] = gt.T @ np.abs(f) + tiny * mf * np.abs(g).sum(0)[:, None]
+    out["df_g16"], out["dE_g16"] = np.abs(g) @ np.abs(E), np.abs(g).T @ np.abs(f)
+    return out
