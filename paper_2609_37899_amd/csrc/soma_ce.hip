@@ -30,6 +30,7 @@
 
 #include <algorithm>
 #include <cmath>
+#include <type_traits>
 
 #include "soma.h"
 #include "soma_host.hpp"
@@ -40,7 +41,7 @@ namespace soma {
 namespace {
 
 constexpr int kPiece = 8192;          // vocabulary rows of a piece
-constexpr int kMaxima = 256;          // partial maxima of an array
+constexpr int kMaxima = 1024;         // partial maxima of an array
 constexpr float kLog2 = 0.6931471805599453f;
 constexpr int kBlk = 512;             // halves of a fragment block
 constexpr int kXcd = 8;
@@ -80,6 +81,13 @@ __device__ __forceinline__ float block_max(float v, float* lds) {
   return v;
 }
 
+// The largest of an array's partial maxima.
+__device__ __forceinline__ float maximum_of(const float* m, int n, float* lds) {
+  static_assert(kMaxima == 4 * 256, "four a thread");
+  const float4 v = int(threadIdx.x) * 4 < n ? reinterpret_cast<const float4*>(m)[threadIdx.x] : make_float4(0.f, 0.f, 0.f, 0.f);
+  return block_max(fmaxf(fmaxf(v.x, v.y), fmaxf(v.z, v.w)), lds);
+}
+
 // ---------------------------------------------------------------------------
 // Largest finite magnitudes: f (rows with a target), E, and the weights.
 // Block x of array y writes maxima[y][x].
@@ -103,11 +111,21 @@ __global__ __launch_bounds__(256) void k_ce_max(MaxArgs a, int first) {
     const int64_t stride = which ? a.e_stride : a.f_stride;
     const int rows = which ? a.V : a.R;
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    const bool four = reinterpret_cast<uintptr_t>(x) % (4 * sizeof(T)) == 0 && stride % 4 == 0;
     for (int r = blockIdx.x * 4 + wave; r < rows; r += gridDim.x * 4) {
       if (!which && a.targets[r] < 0) continue;
       const T* p = x + r * stride;
+      int k = lane * 4;
+      if (four) {
 #pragma unroll 4
-      for (int k = lane; k < a.K; k += 64) top = fmaxf(top, finite_abs(load_value(p + k)));
+        for (; k + 4 <= a.K; k += 256) {
+          const float4 v = load_four(p + k);
+          top = fmaxf(fmaxf(fmaxf(top, finite_abs(v.x)), fmaxf(finite_abs(v.y), finite_abs(v.z))), finite_abs(v.w));
+        }
+        for (int i = 0; i < 4 && k + i < a.K; ++i) top = fmaxf(top, finite_abs(load_value(p + k + i)));
+      } else {
+        for (k = lane; k < a.K; k += 64) top = fmaxf(top, finite_abs(load_value(p + k)));
+      }
     }
   } else if (a.w) {
     // not finite: the largest is not either, and every gradient says so
@@ -135,7 +153,7 @@ struct PackArgs {
   uint16_t *frag, *fragT;    // [np / 16][parts][Kp / 32], [Kp / 16][parts][np / 32] blocks; or NULL
   const float* maxima;       // [3][kMaxima] or NULL: scale 1, c 1
   int which;                 // the scale to use: 0 f, 1 E
-  int nmax;                  // partial maxima in use
+  int nmax;                  // partial maxima in use, a multiple of 4
   Scales* scales;            // f: written by block (0, 0)
   RowMeta* meta;             // f: rows' constants, or NULL
   const float *lse, *w;
@@ -175,18 +193,14 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
   const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
   float scale = 1.0f, c = 1.0f;
   if (a.maxima) {
-    float t = 0.0f;
     if constexpr (PARTS == 2) {
-      t = int(threadIdx.x) < a.nmax ? a.maxima[a.which * kMaxima + threadIdx.x] : 0.0f;
-      scale = power_scale(block_max(t, red));
+      scale = power_scale(maximum_of(a.maxima + a.which * kMaxima, a.nmax, red));
     }
     if (a.scales && blockIdx.y == 0) {       // f, its first columns: the rows' constants too
-      t = int(threadIdx.x) < a.nmax ? a.maxima[2 * kMaxima + threadIdx.x] : 0.0f;
-      c = block_max(t, red);
+      c = maximum_of(a.maxima + 2 * kMaxima, a.nmax, red);
       float e = 1.0f;
       if constexpr (PARTS == 2) {
-        t = int(threadIdx.x) < a.nmax ? a.maxima[kMaxima + threadIdx.x] : 0.0f;
-        e = power_scale(block_max(t, red));
+        e = power_scale(maximum_of(a.maxima + kMaxima, a.nmax, red));
       }
       if (blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{scale, e, c, 0.0f};
     }
@@ -249,6 +263,16 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
 // round-robin) works through a contiguous range of items, 8 n tiles wide at a
 // time, so that the tiles in flight share operands in its L2.
 // ---------------------------------------------------------------------------
+// Division by a number that is known on the host: n / d = (mulhi(m, n) + n) >> l
+// with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1, for 0 <= n < 2^31.
+struct Divider {
+  uint32_t m, l;
+  int d;
+  __device__ __forceinline__ int of(int n) const {
+    return static_cast<int>((__umulhi(m, static_cast<uint32_t>(n)) + static_cast<uint32_t>(n)) >> l);
+  }
+};
+
 enum CeEpi { kStats = 0, kGrad = 1, kOut = 2, kPart = 3 };
 
 struct CeMmArgs {
@@ -256,7 +280,9 @@ struct CeMmArgs {
   int ta, tw;                // row tiles of 16 in A and W
   int KC;                    // chunks of 32 columns
   int ntm, ntn, splits;
-  int64_t items;
+  int stages;                // of a row tile: 64 columns (bf16), 32 (split)
+  int items;
+  Divider by_tiles, by_band, by_rest, by_splits;   // ntm ntn, 8 ntm, ntn % 8, splits
   const Scales* scales;      // NULL: all 1
   // kStats
   float2* part;              // [sub][part_stride]
@@ -319,94 +345,253 @@ __device__ __forceinline__ uint2 transpose4(uint32_t p01, uint32_t p23, int lane
   return lane & 2 ? make_uint2(t, r1) : make_uint2(r0, t);
 }
 
-template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_ce_mm(CeMmArgs p) {
-  constexpr int NW = WN * WM, tn = TN / WN, tm = TM / WM;
-  constexpr int BUF = 2 * (TN + TM) * kBlk;             // one stage, in halves
-  constexpr int DPW = 2 * (TN + TM) / NW;               // blocks a wave moves per stage
-  constexpr int WWAVES = TN * NW / (TN + TM);           // waves that move W
-  static_assert(DPW * NW == 2 * (TN + TM) && WWAVES * DPW == 2 * TN && DPW % 2 == 0, "whole row tiles per wave");
-  constexpr bool kLoop = NW == 8;
-  constexpr int kStep = PARTS == 1 ? 2 : 1;             // chunks of a stage
-  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
-  uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
-  const int64_t per_xcd = (p.items + kXcd - 1) / kXcd;
-  const int64_t first = (blockIdx.x % kXcd) * per_xcd;
-  const int64_t last = first + per_xcd < p.items ? first + per_xcd : p.items;
-  const int64_t stride = gridDim.x / kXcd;
-  int64_t item = first + blockIdx.x / kXcd;
-  if (item >= last) return;                             // block-uniform
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int wn = wave % WN, wm = wave / WN;
-  const int stages = p.KC / kStep;
+// Item t: its tile, and the stages [s0, s1) of its share.
+struct CeItem {
+  int nt, mt, split, s0, s1;
+};
+__device__ __forceinline__ CeItem item_at(const CeMmArgs& p, int t) {
+  CeItem w;
+  w.split = p.by_tiles.of(t);
+  int i = t - w.split * p.by_tiles.d;
+  const int band = p.by_band.of(i);                     // 8 n tiles
+  i -= band * p.by_band.d;
+  const bool full = 8 * band + 8 <= p.ntn;
+  w.mt = full ? i >> 3 : p.by_rest.of(i);
+  w.nt = 8 * band + i - w.mt * (full ? 8 : p.by_rest.d);
+  w.s0 = p.by_splits.of(p.stages * w.split);
+  w.s1 = p.by_splits.of(p.stages * (w.split + 1));
+  return w;
+}
 
-  struct Where {
-    int nt, mt, split, s0, s1;
-  };
-  auto where = [&](int64_t t) {
-    Where w;
-    w.split = static_cast<int>(t / (int64_t(p.ntm) * p.ntn));
-    int i = static_cast<int>(t - int64_t(w.split) * p.ntm * p.ntn);
-    const int band = i / (8 * p.ntm);                   // 8 n tiles
-    const int width = min(8, p.ntn - 8 * band);
-    i -= band * 8 * p.ntm;
-    w.mt = i / width;
-    w.nt = 8 * band + i - w.mt * width;
-    w.s0 = static_cast<int>(int64_t(stages) * w.split / p.splits);
-    w.s1 = static_cast<int>(int64_t(stages) * (w.split + 1) / p.splits);
-    return w;
-  };
-  const bool weights = wave < WWAVES;
+// What becomes of a wave's accumulators:
+// acc[i][j][q] = C[16 (mt0 + j) + lr][16 (nt0 + i) + 4 lg + q].
+// It reads the kernel's arguments again from where they were passed, and hides
+// the lane from the compiler: what it would compute from them ahead of the main
+// loop takes the loop's registers, whose spills wait for the DMAs in flight.
+template <class T, int PARTS, int kEpi, int TN, int TM, int tn, int tm>
+__device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int nt0, int split, int wave, int lane) {
+#ifdef __HIP_DEVICE_COMPILE__
+  typedef const __attribute__((address_space(4))) CeMmArgs* ArgsPtr;
+  uint64_t at = reinterpret_cast<uint64_t>(__builtin_amdgcn_kernarg_segment_ptr());
+  asm volatile("" : "+s"(at), "+v"(lane));
+  const CeMmArgs p = *reinterpret_cast<ArgsPtr>(at);
+#else
+  const CeMmArgs p{};
+#endif
+  const int lr = lane & 15, lg = lane >> 4;
+  if constexpr (kEpi == kStats) {
+    const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
+    const int sub = p.sub0 + nt0 / tn;
+    const int left = p.V - nt0 * 16 - 4 * lg;             // this lane's columns 16 i + q below it are in the vocabulary
+    // No branch inside: results wait in registers until the end, and the tile
+    // that the vocabulary ends in has code of its own.
+    float tops[tm], sums[tm], hits[tm];
+    int targets[tm];
+#pragma unroll
+    for (int j = 0; j < tm; ++j) targets[j] = p.targets[min((mt0 + j) * 16 + lr, p.R - 1)] - p.v0 - nt0 * 16 - 4 * lg;
+    auto rows = [&](auto whole) {
+#pragma unroll
+      for (int j = 0; j < tm; ++j) {
+        __builtin_amdgcn_sched_barrier(0);  // one column of tiles at a time: the accumulators fill half of the registers
+        int l = left;
+        if constexpr (!decltype(whole)::value) asm volatile("" : "+v"(l));   // the comparisons are not kept from j to j
+        float top = -3.402823466e38f, hit = 0.0f, x[tn][4];
+#pragma unroll
+        for (int i = 0; i < tn; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            x[i][q] = acc[i][j][q] * undo;
+            if constexpr (!decltype(whole)::value) x[i][q] = 16 * i + q < l ? x[i][q] : -__builtin_inff();
+            hit = targets[j] == 16 * i + q ? x[i][q] : hit;
+            top = fmaxf(top, x[i][q]);
+          }
+        top = group4_max(top);
+        float sum = 0.0f;
+#pragma unroll
+        for (int i = 0; i < tn; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (x[i][q] - top));
+        tops[j] = top, sums[j] = group4_sum(sum), hits[j] = hit;
+      }
+    };
+    if (p.V - nt0 * 16 >= 16 * tn)                        // wave-uniform
+      rows(std::true_type{});
+    else
+      rows(std::false_type{});
+#pragma unroll
+    for (int j = 0; j < tm; ++j) {
+      const int m = (mt0 + j) * 16 + lr, t = targets[j];
+      if (m < p.R) {
+        if (t >= 0 && t < 16 * tn && t < left && (t & 15) < 4) p.hit[m] = hits[j];
+        if (lg == 0) p.part[int64_t(sub) * p.part_stride + m] = make_float2(tops[j], sums[j]);
+      }
+    }
+  } else if constexpr (kEpi == kGrad) {
+    const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
+    const int GC = p.tw / 2, TC = p.ta / 2;           // chunks of 32 in G's and GT's rows
+#pragma unroll
+    for (int j = 0; j < tm; ++j) {
+      const int rt = mt0 + j;
+      if (rt >= p.ta) continue;                       // wave-uniform
+      const RowMeta m = p.meta[rt * 16 + lr];
+      const int target = m.target - p.v0;
+#pragma unroll
+      for (int i = 0; i < tn; ++i) {
+        const int nt = nt0 + i;
+        if (nt >= p.tw) continue;
+        float g[4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int v = nt * 16 + 4 * lg + q;
+          const float e = exp2_f(kLog2e * (acc[i][j][q] * undo - m.lse));
+          g[q] = v < p.V ? m.rho * (v == target ? e - 1.0f : e) : 0.0f;
+        }
+        // G: row lr of its tile, columns 4 lg .. of 16.  GT: row 4 lg + (lr & 3), columns 4 (lr / 4) .. .
+        uint16_t* G = p.G + (int64_t(rt) * PARTS * GC + nt / 2) * kBlk +
+                      (16 * (2 * (nt & 1) + (lg >> 1)) + lr) * 8 + 4 * (lg & 1);
+        uint16_t* GT = p.GT + (int64_t(nt) * PARTS * TC + rt / 2) * kBlk +
+                       (16 * (2 * (rt & 1) + (lr >> 3)) + 4 * lg + (lr & 3)) * 8 + 4 * ((lr >> 2) & 1);
+        if constexpr (PARTS == 1) {
+          const uint32_t x = bf16_pair(g[0], g[1]), y = bf16_pair(g[2], g[3]);
+          *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
+          *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
+        } else {
+          uint16_t hi[4], lo[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) split_rn(g[q] * kScaleG, hi[q], lo[q]);
+          const uint32_t x = hi[0] | uint32_t(hi[1]) << 16, y = hi[2] | uint32_t(hi[3]) << 16;
+          const uint32_t z = lo[0] | uint32_t(lo[1]) << 16, u = lo[2] | uint32_t(lo[3]) << 16;
+          *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
+          *reinterpret_cast<uint2*>(G + int64_t(GC) * kBlk) = make_uint2(z, u);
+          *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
+          *reinterpret_cast<uint2*>(GT + int64_t(TC) * kBlk) = transpose4(z, u, lane);
+        }
+      }
+    }
+  } else if constexpr (kEpi == kOut) {
+    const float s = out_scale(p, PARTS);
+#pragma unroll
+    for (int i = 0; i < tn; ++i)
+#pragma unroll
+      for (int j = 0; j < tm; ++j) {
+        __builtin_amdgcn_sched_barrier(0);
+        const int m = (mt0 + j) * 16 + lr, n = (nt0 + i) * 16 + 4 * lg;
+        if (m < p.M && n < p.N) store_out<T>(p, m, n, acc[i][j], s);
+      }
+  } else {
+    float4* a = p.acc + ((int64_t(split) * p.ntm + mt0 / TM) * p.ntn + nt0 / TN) * (TN * TM * 64) +
+                wave * (tn * tm * 64) + lane;
+#pragma unroll
+    for (int i = 0; i < tn; ++i) {
+      __builtin_amdgcn_sched_barrier(0);    // a row's loads at a time
+      float4 o[tm];
+#pragma unroll
+      for (int j = 0; j < tm; ++j) o[j] = p.add ? a[(i * tm + j) * 64] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int j = 0; j < tm; ++j)
+        a[(i * tm + j) * 64] = make_float4(o[j].x + acc[i][j][0], o[j].y + acc[i][j][1], o[j].z + acc[i][j][2],
+                                           o[j].w + acc[i][j][3]);
+    }
+  }
+}
+
+// Fetching stages of row tiles into LDS, in the order in which the block's items
+// use them and across their borders.  A wave moves DPW blocks of every stage:
+// halves (two chunks, or hi and lo) of DPW / 2 row tiles of W or of A, or one
+// chunk of DPW row tiles (kWide).
+template <int PARTS, int TN, int TM, int NW, int DPW, bool kWide>
+struct CeFetch {
+  static constexpr int kBuf = (kWide ? 1 : 2) * (TN + TM) * kBlk;      // one stage, in halves
+  static constexpr int kStep = PARTS == 1 && !kWide ? 2 : 1;           // chunks of a stage
+  const CeMmArgs& p;
   i32x4 rs;
-  uint32_t voff[DPW];
-  auto aim = [&](const Where& w) {
-    // The tile's own rows, as many as the matrix has: beyond them zeros.
+  uint32_t soff[DPW];                                   // scalars: vector registers are dear
+  uint32_t voff, dst;
+  int wave, item, stride, last, c, end;
+  bool more = true;
+
+  __device__ __forceinline__ CeFetch(const CeMmArgs& p_, const uint16_t* lds, int wave_, int lane, int item_, int stride_,
+                                     int last_)
+      : p(p_), voff(lane * 16), dst(lds_address(lds + wave_ * DPW * kBlk)), wave(wave_), item(item_), stride(stride_),
+        last(last_) {
+    aim();
+  }
+  __device__ __forceinline__ void aim() {
+    // Row tiles past the matrix repeat its last: nothing of theirs is used.
+    constexpr int per = kWide ? DPW : DPW / 2;          // row tiles of a wave
+    const CeItem w = item_at(p, item);
+    const bool weights = wave * per < TN;
     const int t0 = weights ? w.nt * TN : w.mt * TM;
     const int have = min(weights ? TN : TM, (weights ? p.tw : p.ta) - t0);
     const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * PARTS * p.KC * kBlk;
     rs = buffer_words(base, static_cast<uint32_t>(have) * PARTS * p.KC * (kBlk * 2));
-    const int mine = weights ? wave * (DPW / 2) : (wave - WWAVES) * (DPW / 2);
+    const int mine = wave * per - (weights ? 0 : TN);
+    const int scale = kWide ? 2 : 1;                    // item_at counts pairs of wide stages
+    c = scale * w.s0, end = scale * w.s1;
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      const int block = PARTS == 1 ? (mine + (i >> 1)) * p.KC + w.s0 * 2 + (i & 1)
-                                   : ((mine + (i >> 1)) * 2 + (i & 1)) * p.KC + w.s0;
-      voff[i] = static_cast<uint32_t>(block) * (kBlk * 2) + lane * 16;
+      const int tile = min(mine + (kWide ? i : i >> 1), have - 1);
+      const int block = PARTS == 1 ? tile * p.KC + c * kStep + (kWide ? 0 : i & 1) : (tile * 2 + (i & 1)) * p.KC + c;
+      soff[i] = static_cast<uint32_t>(block) * (kBlk * 2);
     }
-  };
-  const uint32_t dst0 = lds_address(lds + wave * DPW * kBlk);
-  auto issue = [&](int buf) {
+  }
+  // The next stage, if there is one, into LDS buffer `buf`.
+  __device__ __forceinline__ void issue(int buf) {
+    if (!more) return;
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      dma16(rs, voff[i], 0u, dst0 + static_cast<uint32_t>((buf * BUF + i * kBlk) * 2));
-      voff[i] += kStep * kBlk * 2;
+      dma16(rs, voff, soff[i], dst + static_cast<uint32_t>((buf * kBuf + i * kBlk) * 2));
+      soff[i] += kStep * kBlk * 2;
     }
-  };
+    if (++c == end) {
+      item += stride;
+      more = item < last;
+      if (more) aim();
+    }
+  }
+};
+
+// kBufs LDS buffers: kBufs - 1 stages are on their way or landed ahead.
+template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM, int kBufs>
+__global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_ce_mm(CeMmArgs p) {
+  constexpr int NW = WN * WM, tn = TN / WN, tm = TM / WM;
+  constexpr int DPW = 2 * (TN + TM) / NW;               // blocks a wave moves per stage
+  static_assert(DPW * NW == 2 * (TN + TM) && DPW % 2 == 0 && TN % (DPW / 2) == 0, "whole row tiles per wave");
+  typedef CeFetch<PARTS, TN, TM, NW, DPW, false> Fetch;
+  constexpr int BUF = Fetch::kBuf;
+  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
+  uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
+  const int per_xcd = (p.items + kXcd - 1) / kXcd;
+  const int first = (blockIdx.x % kXcd) * per_xcd;
+  const int last = min(first + per_xcd, p.items);
+  const int stride = gridDim.x / kXcd;
+  int item = first + blockIdx.x / kXcd;
+  if (item >= last) return;                             // block-uniform
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int wn = wave % WN, wm = wave / WN;
+  Fetch fetch(p, lds, wave, lane, item, stride, last);
   const uint16_t* const wl0 = lds + wn * tn * 2 * kBlk + lane * 8;
   const uint16_t* const al0 = lds + (TN + wm * tm) * 2 * kBlk + lane * 8;
-
-  Where w = where(item);
-  aim(w);
-  issue(0);
+#pragma unroll
+  for (int i = 0; i < kBufs - 1; ++i) fetch.issue(i);
   int buf = 0;
   for (;;) {
+    const CeItem w = item_at(p, item);
     f32x4 acc[tn][tm];
 #pragma unroll
     for (int i = 0; i < tn; ++i)
 #pragma unroll
       for (int j = 0; j < tm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    const int64_t next = item + stride;
-    const bool more = kLoop && next < last;             // block-uniform
-    const Where wnext = more ? where(next) : w;
     for (int c = w.s0; c < w.s1; ++c) {
-      wait_vmem();                                      // the stage has landed
-      __syncthreads();                                  // and every wave is done with the other buffer
-      if (c + 1 < w.s1) {
-        issue(buf ^ 1);
-      } else if (more) {
-        aim(wnext);
-        issue(buf ^ 1);
-      }
+      // The stage has landed (while there is one to fetch, kBufs - 2 later ones
+      // may be out), and every wave is done with the buffer of the one before.
+      if (fetch.more)
+        wait_vmem_but<(kBufs - 2) * DPW>();
+      else
+        wait_vmem();
+      __syncthreads();
+      fetch.issue(buf == 0 ? kBufs - 1 : buf - 1);
       uint4 b0[tm], b1[tm];
 #pragma unroll
       for (int j = 0; j < tm; ++j) {
@@ -431,107 +616,90 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2,
           for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w0, b0[j], acc[i][j]);
         }
       }
-      buf ^= 1;
+      buf = buf == kBufs - 1 ? 0 : buf + 1;
     }
+    ce_epilogue<T, PARTS, kEpi, TN, TM, tn, tm>(acc, w.mt * TM + wm * tm, w.nt * TN + wn * tn, w.split, wave, lane);
+    item += stride;
+    if (item >= last) break;
+  }
+}
 
-    // acc[i][j][q] = C[16 (TM mt + tm wm + j) + lr][16 (TN nt + tn wn + i) + 4 lg + q]
-    const int mt0 = w.mt * TM + wm * tm, nt0 = w.nt * TN + wn * tn;
-    if constexpr (kEpi == kStats) {
-      const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
-      const int sub = p.sub0 + w.nt * WN + wn;
+// bf16, 256 x 256 with 4 waves of 128 x 128: one wave on each SIMD.  With 8 waves
+// of 128 x 64 the LDS moves 256 KiB for 64 columns (192 read, 64 written by DMA),
+// 2,048 clocks, as long as their MFMAs take; with 128 x 128 per wave 192 KiB.  One
+// wave has nobody to hide behind, so everything is ahead of time: a stage is one
+// chunk of 32 columns (64 MFMAs, 1,024 clocks), its DMA is issued four stages before
+// (four LDS buffers of 32 KiB), and its fragments are read into registers under the
+// MFMAs of the stage before (the second of two register sets; stages come in pairs).
+template <class T, int kEpi>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_ce_mm_wide(CeMmArgs p) {
+  constexpr int T16 = 16, t8 = 8, DPW = 8;
+  typedef CeFetch<1, T16, T16, 4, DPW, true> Fetch;
+  constexpr int BUF = Fetch::kBuf;
+  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
+  uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
+  const int per_xcd = (p.items + kXcd - 1) / kXcd;
+  const int first = (blockIdx.x % kXcd) * per_xcd;
+  const int last = min(first + per_xcd, p.items);
+  const int stride = gridDim.x / kXcd;
+  int item = first + blockIdx.x / kXcd;
+  if (item >= last) return;                             // block-uniform
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int lane = threadIdx.x & 63;
+  const int wn = wave & 1, wm = wave >> 1;
+  Fetch fetch(p, lds, wave, lane, item, stride, last);
+  const uint16_t* const wl = lds + wn * t8 * kBlk + lane * 8;
+  const uint16_t* const al = lds + (T16 + wm * t8) * kBlk + lane * 8;
+  uint4 fw[2][t8], fa[2][t8];
+  auto read = [&](int set, int buf) {
 #pragma unroll
-      for (int j = 0; j < tm; ++j) {
-        const int m = (mt0 + j) * 16 + lr;
-        const bool live = m < p.R;
-        const int target = live ? p.targets[m] - p.v0 : -1;
-        float top = -3.402823466e38f;
-#pragma unroll
-        for (int i = 0; i < tn; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int v = (nt0 + i) * 16 + 4 * lg + q;
-            acc[i][j][q] = v < p.V ? acc[i][j][q] * undo : -__builtin_inff();
-            top = fmaxf(top, acc[i][j][q]);
-            if (v == target && v < p.V) p.hit[m] = acc[i][j][q];
-          }
-        top = group4_max(top);
-        float sum = 0.0f;
-#pragma unroll
-        for (int i = 0; i < tn; ++i)
-#pragma unroll
-          for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (acc[i][j][q] - top));
-        sum = group4_sum(sum);
-        if (live && lg == 0) p.part[int64_t(sub) * p.part_stride + m] = make_float2(top, sum);
-      }
-    } else if constexpr (kEpi == kGrad) {
-      const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
-      const int GC = p.tw / 2, TC = p.ta / 2;           // chunks of 32 in G's and GT's rows
-#pragma unroll
-      for (int j = 0; j < tm; ++j) {
-        const int rt = mt0 + j;
-        if (rt >= p.ta) continue;                       // wave-uniform
-        const RowMeta m = p.meta[rt * 16 + lr];
-        const int target = m.target - p.v0;
-#pragma unroll
-        for (int i = 0; i < tn; ++i) {
-          const int nt = nt0 + i;
-          if (nt >= p.tw) continue;
-          float g[4];
-#pragma unroll
-          for (int q = 0; q < 4; ++q) {
-            const int v = nt * 16 + 4 * lg + q;
-            const float e = exp2_f(kLog2e * (acc[i][j][q] * undo - m.lse));
-            g[q] = v < p.V ? m.rho * (v == target ? e - 1.0f : e) : 0.0f;
-          }
-          // G: row lr of its tile, columns 4 lg .. of 16.  GT: row 4 lg + (lr & 3), columns 4 (lr / 4) .. .
-          uint16_t* G = p.G + (int64_t(rt) * PARTS * GC + nt / 2) * kBlk +
-                        (16 * (2 * (nt & 1) + (lg >> 1)) + lr) * 8 + 4 * (lg & 1);
-          uint16_t* GT = p.GT + (int64_t(nt) * PARTS * TC + rt / 2) * kBlk +
-                         (16 * (2 * (rt & 1) + (lr >> 3)) + 4 * lg + (lr & 3)) * 8 + 4 * ((lr >> 2) & 1);
-          if constexpr (PARTS == 1) {
-            const uint32_t x = bf16_pair(g[0], g[1]), y = bf16_pair(g[2], g[3]);
-            *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
-            *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
-          } else {
-            uint16_t hi[4], lo[4];
-#pragma unroll
-            for (int q = 0; q < 4; ++q) split_rn(g[q] * kScaleG, hi[q], lo[q]);
-            const uint32_t x = hi[0] | uint32_t(hi[1]) << 16, y = hi[2] | uint32_t(hi[3]) << 16;
-            const uint32_t z = lo[0] | uint32_t(lo[1]) << 16, u = lo[2] | uint32_t(lo[3]) << 16;
-            *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
-            *reinterpret_cast<uint2*>(G + int64_t(GC) * kBlk) = make_uint2(z, u);
-            *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
-            *reinterpret_cast<uint2*>(GT + int64_t(TC) * kBlk) = transpose4(z, u, lane);
-          }
-        }
-      }
-    } else if constexpr (kEpi == kOut) {
-      const float s = out_scale(p, PARTS);
-#pragma unroll
-      for (int i = 0; i < tn; ++i)
-#pragma unroll
-        for (int j = 0; j < tm; ++j) {
-          const int m = (mt0 + j) * 16 + lr, n = (nt0 + i) * 16 + 4 * lg;
-          if (m < p.M && n < p.N) store_out<T>(p, m, n, acc[i][j], s);
-        }
-    } else {
-      float4* a = p.acc + ((int64_t(w.split) * p.ntm + w.mt) * p.ntn + w.nt) * (TN * TM * 64) +
-                  wave * (tn * tm * 64) + lane;
-#pragma unroll
-      for (int i = 0; i < tn; ++i)
-#pragma unroll
-        for (int j = 0; j < tm; ++j) {
-          float4 v = make_float4(acc[i][j][0], acc[i][j][1], acc[i][j][2], acc[i][j][3]);
-          if (p.add) {
-            const float4 o = a[(i * tm + j) * 64];
-            v = make_float4(o.x + v.x, o.y + v.y, o.z + v.z, o.w + v.w);
-          }
-          a[(i * tm + j) * 64] = v;
-        }
+    for (int i = 0; i < t8; ++i) {
+      fw[set][i] = *reinterpret_cast<const uint4*>(wl + buf * BUF + i * kBlk);
+      fa[set][i] = *reinterpret_cast<const uint4*>(al + buf * BUF + i * kBlk);
     }
-    if (!more) break;
-    item = next;
-    w = wnext;
+  };
+  // Four stages on their way; then the first one's fragments.
+#pragma unroll
+  for (int i = 0; i < 4; ++i) fetch.issue(i);
+  wait_vmem();
+  __syncthreads();
+  read(0, 0);
+  int buf = 0;
+  for (;;) {
+    const CeItem w = item_at(p, item);
+    f32x4 acc[t8][t8];
+#pragma unroll
+    for (int i = 0; i < t8; ++i)
+#pragma unroll
+      for (int j = 0; j < t8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int c = w.s0; c < w.s1; ++c) {
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        // The next stage has landed (while there is one to fetch, two later
+        // ones may be out), and every wave holds this one's fragments, so its
+        // buffer is free.
+        if (fetch.more)
+          wait_vmem_but<2 * DPW>();
+        else
+          wait_vmem();
+        __syncthreads();
+        fetch.issue(buf);
+        buf = (buf + 1) & 3;
+        read(half ^ 1, buf);
+#pragma unroll
+        for (int i = 0; i < t8; ++i)
+#pragma unroll
+          for (int j = 0; j < t8; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+#pragma unroll
+        for (int i = 0; i < 2 * t8; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // one LDS read,
+          __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);   // four MFMAs
+        }
+      }
+    }
+    ce_epilogue<T, 1, kEpi, T16, T16, t8, t8>(acc, w.mt * T16 + wm * t8, w.nt * T16 + wn * t8, w.split, wave, lane);
+    item += stride;
+    if (item >= last) break;
   }
 }
 
@@ -667,13 +835,15 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
 // ---------------------------------------------------------------------------
 // The parts of every row joined, 16 rows a block: lse and loss.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void k_ce_join(const float2* part, int subs, int stride, const int32_t* targets,
+template <int kParts>
+__global__ __launch_bounds__(16 * kParts) void k_ce_join(const float2* part, int subs, int stride, const int32_t* targets,
                                                  const float* hit, int R, int V, float* loss, float* lse) {
-  __shared__ float2 red[16][16];
+  __shared__ float2 red[kParts][17];
   const int lr = threadIdx.x & 15, w = threadIdx.x >> 4, r = blockIdx.x * 16 + lr;
   float top = -3.402823466e38f, sum = 0.0f;
   if (r < R)
-    for (int s = w; s < subs; s += 16) {
+#pragma unroll 4
+    for (int s = w; s < subs; s += kParts) {
       const float2 x = part[int64_t(s) * stride + r];
       const float m = fmaxf(top, x.x);
       sum = sum * exp2_f(kLog2e * (top - m)) + x.y * exp2_f(kLog2e * (x.x - m));
@@ -681,12 +851,21 @@ __global__ __launch_bounds__(256) void k_ce_join(const float2* part, int subs, i
     }
   red[w][lr] = make_float2(top, sum);
   __syncthreads();
+  // The first half of the parts takes the other's in, and so on.
+  for (int h = kParts / 2; h >= 8; h /= 2) {
+    if (w < h) {
+      const float2 x = red[w][lr], y = red[w + h][lr];
+      const float m = fmaxf(x.x, y.x);
+      red[w][lr] = make_float2(m, x.y * exp2_f(kLog2e * (x.x - m)) + y.y * exp2_f(kLog2e * (y.x - m)));
+    }
+    __syncthreads();
+  }
   if (w != 0 || r >= R) return;
   float m = -3.402823466e38f, s = 0.0f;
 #pragma unroll
-  for (int i = 0; i < 16; ++i) m = fmaxf(m, red[i][lr].x);
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, red[i][lr].x);
 #pragma unroll
-  for (int i = 0; i < 16; ++i) s += red[i][lr].y * exp2_f(kLog2e * (red[i][lr].x - m));
+  for (int i = 0; i < 8; ++i) s += red[i][lr].y * exp2_f(kLog2e * (red[i][lr].x - m));
   const int t = targets[r];
   float l = 0.0f, out = 0.0f;
   if (t >= 0) {
@@ -776,54 +955,76 @@ int check_ce(const soma_ce_config* c) {
   return SOMA_OK;
 }
 
-// Shares of every tile's stages: as many as bring the items to kFill, at
+// Shares of every tile's stages: as many as bring the items to `fill`, at
 // least four stages each.
-int choose_splits(int64_t tiles, int64_t stages) {
-  return int(std::max<int64_t>(1, std::min(kFill / std::max<int64_t>(tiles, 1), stages / 4)));
+int choose_splits(int64_t tiles, int64_t stages, int64_t fill) {
+  return int(std::max<int64_t>(1, std::min(fill / std::max<int64_t>(tiles, 1), stages / 4)));
 }
 
-template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM>
-int launch_mm_tile(CeMmArgs& p, hipStream_t st) {
-  p.items = int64_t(p.ntm) * p.ntn * p.splits;
-  int64_t blocks = up(p.items, kXcd);
-  if (WN * WM == 8) blocks = std::min<int64_t>(blocks, kFill);
-  if (blocks >= (int64_t(1) << 31)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
-  constexpr unsigned lds = 2u * 2u * unsigned(TN + TM) * 1024u;
-  const void* kern = reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, TN, TM, WN, WM>);
-  const hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+Divider divider(int d) {
+  uint32_t l = 0;
+  while ((int64_t(1) << l) < d) ++l;
+  return {uint32_t((uint64_t(1) << 32) * ((uint64_t(1) << l) - uint64_t(d)) / uint64_t(d)) + 1u, l, d};
+}
+
+int launch_items(const void* kern, CeMmArgs& p, int threads, bool loop, unsigned lds, hipStream_t st) {
+  const int64_t items = int64_t(p.ntm) * p.ntn * p.splits;
+  if (items >= (int64_t(1) << 30)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
+  p.items = int(items);
+  p.by_tiles = divider(p.ntm * p.ntn), p.by_band = divider(8 * p.ntm), p.by_rest = divider(std::max(p.ntn % 8, 1));
+  p.by_splits = divider(p.splits);
+  int64_t blocks = up(items, kXcd);
+  if (loop) blocks = std::min<int64_t>(blocks, kFill);
+  hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-  hipLaunchKernelGGL((k_ce_mm<T, PARTS, kEpi, TN, TM, WN, WM>), dim3(unsigned(blocks)), dim3(64 * WN * WM), lds, st, p);
-  return launched("k_ce_mm");
+  void* args[] = {&p};
+  e = hipLaunchKernel(kern, dim3(unsigned(blocks)), dim3(threads), args, lds, st);
+  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "k_ce_mm: %s", hipGetErrorString(e));
+  return SOMA_OK;
 }
 
-// 256 x 256 where those tiles (or their shares) fill the card, else 128 x 128.
-bool large_tiles(int64_t m, int64_t n, int64_t stages, bool shares) {
-  const int64_t tiles = up(m, 256) / 256 * (up(n, 256) / 256);
-  if (up(m, 256) - m >= 128 || up(n, 256) - n >= 128) return tiles >= 2 * kFill;
-  return tiles * (shares ? choose_splits(tiles, stages) : 1) >= kFill * 3 / 4;
-}
-
-void tiles_of(CeMmArgs& p, int side) {
-  p.ntm = (p.ta + side / 16 - 1) / (side / 16);
-  p.ntn = (p.tw + side / 16 - 1) / (side / 16);
-}
-
+// A product on 256 x 256 tiles (one block per compute unit works through
+// them) or on 128 x 128.
 template <class T, int PARTS, int kEpi>
-int launch_logits(CeMmArgs& p, bool large, hipStream_t st) {
-  p.splits = 1;
-  tiles_of(p, large ? 256 : 128);
-  return large ? launch_mm_tile<T, PARTS, kEpi, 16, 16, 2, 4>(p, st) : launch_mm_tile<T, PARTS, kEpi, 8, 8, 2, 2>(p, st);
+int launch_mm(CeMmArgs& p, bool large, hipStream_t st) {
+  const int side = large ? 16 : 8;
+  p.ntm = (p.ta + side - 1) / side;
+  p.ntn = (p.tw + side - 1) / side;
+  p.stages = p.KC / (PARTS == 1 ? 2 : 1);
+  if constexpr (PARTS == 1) {
+    if (large) return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi>), p, 256, true, 131072, st);
+  } else {
+    if (large)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, true, 131072, st);
+  }
+  // One block a compute unit: its four buffers hide what a second block would.
+  if (int64_t(p.ntm) * p.ntn * p.splits <= kFill)
+    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 4>), p, 256, false, 131072, st);
+  return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 2>), p, 256, false, 65536, st);
 }
 
-// How the products of all pieces are shared out, by the first and largest.
+int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return up(m, side) / side * (up(n, side) / side); }
+
+// Logits on 256 x 256 tiles where they come to three quarters of the compute
+// units and their padding is no larger than a quarter.
+bool large_logits(int64_t m, int64_t n) {
+  return tiles_of(m, n, 256) >= kFill * 3 / 4 && up(m, 256) * up(n, 256) <= m * n * 5 / 4;
+}
+
+// How the products with G are shared out, by the first and largest piece.
 struct Shares {
   bool large;
   int splits;
 };
-Shares shares_of(int64_t m, int64_t n, int64_t stages) {
-  const bool large = large_tiles(m, n, stages, true);
-  const int64_t side = large ? 256 : 128;
-  return {large, choose_splits(up(m, side) / side * (up(n, side) / side), stages)};
+Shares shares_of(int64_t m, int64_t n, int64_t columns, int parts) {
+  const int64_t stages = columns / (parts == 1 ? 64 : 32);
+  const int64_t large = tiles_of(m, n, 256), small = tiles_of(m, n, 128);
+  // Shares write and read their sums, 8 bytes an output each: with few columns
+  // that is longer than the product, and whole small tiles are better.
+  if (large < kFill && small >= kFill && columns <= 1024) return {false, 1};
+  const int s = choose_splits(large, stages, kFill);
+  if (large * s >= kFill * 3 / 4 && up(m, 256) * up(n, 256) <= m * n * 5 / 4) return {true, s};
+  return {false, choose_splits(small, stages, 2 * kFill)};
 }
 
 // One product with G.  `single`: it alone gives the result; else the result
@@ -831,22 +1032,20 @@ Shares shares_of(int64_t m, int64_t n, int64_t stages) {
 // `finish` brings to the output.
 template <class T, int PARTS>
 int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipStream_t st) {
-  tiles_of(p, sh.large ? 256 : 128);
   p.splits = sh.splits;
-  if (single && p.splits == 1)
-    return sh.large ? launch_mm_tile<T, PARTS, kOut, 16, 16, 2, 4>(p, st)
-                    : launch_mm_tile<T, PARTS, kOut, 8, 8, 2, 2>(p, st);
+  if (single && p.splits == 1) return launch_mm<T, PARTS, kOut>(p, sh.large, st);
   // A last piece of fewer stages than shares adds to the first ones only.
   p.splits = std::min(sh.splits, p.KC / (PARTS == 1 ? 2 : 1));
-  if (int rc = sh.large ? launch_mm_tile<T, PARTS, kPart, 16, 16, 2, 4>(p, st)
-                        : launch_mm_tile<T, PARTS, kPart, 8, 8, 2, 2>(p, st))
-    return rc;
+  if (int rc = launch_mm<T, PARTS, kPart>(p, sh.large, st)) return rc;
   if (!finish) return SOMA_OK;
   p.splits = sh.splits;
-  if (sh.large)
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 4>), dim3(unsigned(p.ntm * p.ntn), 8 * 4), dim3(512), 0, st, p);
+  const unsigned tiles = unsigned(p.ntm * p.ntn);
+  if (!sh.large)
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8, 2, 2>), dim3(tiles, 4 * 4), dim3(256), 0, st, p);
+  else if constexpr (PARTS == 1)
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 2>), dim3(tiles, 8 * 8), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8, 2, 2>), dim3(unsigned(p.ntm * p.ntn), 4 * 4), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 4>), dim3(tiles, 8 * 4), dim3(512), 0, st, p);
   return launched("k_ce_sum");
 }
 
@@ -854,6 +1053,11 @@ template <class T, int PARTS>
 int launch_pack(const PackArgs& a, hipStream_t st) {
   hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(unsigned(a.np / 64), unsigned(a.Kp / 64)), dim3(256), 0, st, a);
   return launched("k_ce_pack");
+}
+
+// Partial maxima of each array: a block for every four rows of the larger one.
+int maxima_of(const soma_ce_config& c) {
+  return int(std::min<int64_t>(kMaxima, up((std::max(c.rows, c.vocab) + 3) / 4, 4)));
 }
 
 template <class T, int PARTS>
@@ -879,14 +1083,15 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     Scales* scales = reinterpret_cast<Scales*>(ws + s.scales);
     uint16_t* fp = reinterpret_cast<uint16_t*>(ws + s.f);
     uint16_t* ep = reinterpret_cast<uint16_t*>(ws + s.e);
+    const int nmax = maxima_of(c);
     if (PARTS == 2) {
       const MaxArgs m{f, E, nullptr, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
-      hipLaunchKernelGGL(k_ce_max<T>, dim3(kMaxima, 3), dim3(256), 0, st, m, 0);
+      hipLaunchKernelGGL(k_ce_max<T>, dim3(nmax, 3), dim3(256), 0, st, m, 0);
       if (int rc = launched("k_ce_max")) return rc;
     }
     PackArgs a{};
     a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
-    a.targets = targets, a.frag = fp, a.maxima = PARTS == 2 ? maxima : nullptr, a.nmax = kMaxima, a.scales = scales;
+    a.targets = targets, a.frag = fp, a.maxima = PARTS == 2 ? maxima : nullptr, a.nmax = nmax, a.scales = scales;
     a.V = c.vocab;
     if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
     stride = int(s.Rp);
@@ -894,18 +1099,23 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
       PackArgs b{};
       b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
-      b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.which = 1, b.nmax = kMaxima;
+      b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.nmax = nmax, b.which = 1;
       if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
       CeMmArgs p{};
       p.A = fp, p.W = ep, p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
       p.part = part, p.part_stride = stride, p.sub0 = subs, p.hit = hit, p.targets = targets, p.R = c.rows, p.V = n, p.v0 = v0;
-      const bool large = large_tiles(s.Rp, np, 0, false);
-      if (int rc = launch_logits<T, PARTS, kStats>(p, large, st)) return rc;
+      const bool large = large_logits(s.Rp, np);
+      p.splits = 1;
+      if (int rc = launch_mm<T, PARTS, kStats>(p, large, st)) return rc;
       subs += p.ntn * 2;
     }
   }
-  hipLaunchKernelGGL(k_ce_join, dim3((c.rows + 15) / 16), dim3(256), 0, st, part, subs, stride, targets, hit, c.rows,
-                     c.vocab, loss, lse);
+  const dim3 jgrid((c.rows + 15) / 16);
+  if (subs <= 32)
+    hipLaunchKernelGGL(k_ce_join<8>, jgrid, dim3(128), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss, lse);
+  else
+    hipLaunchKernelGGL(k_ce_join<64>, jgrid, dim3(1024), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss,
+                       lse);
   return launched("k_ce_join");
 }
 
@@ -918,26 +1128,27 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   RowMeta* meta = reinterpret_cast<RowMeta*>(ws + s.meta);
   auto at = [&](size_t o) { return reinterpret_cast<uint16_t*>(ws + o); };
   const MaxArgs m{f, E, w, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
-  hipLaunchKernelGGL(k_ce_max<T>, dim3(kMaxima, PARTS == 2 ? 3 : 1), dim3(256), 0, st, m, PARTS == 2 ? 0 : 2);
+  const int nmax = PARTS == 2 ? maxima_of(c) : 64;
+  hipLaunchKernelGGL(k_ce_max<T>, dim3(nmax, PARTS == 2 ? 3 : 1), dim3(256), 0, st, m, PARTS == 2 ? 0 : 2);
   if (int rc = launched("k_ce_max")) return rc;
   PackArgs a{};
   a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
-  a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = kMaxima;
+  a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = nmax;
   a.scales = scales, a.meta = meta, a.lse = lse, a.w = w, a.V = c.vocab;
   if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
-  constexpr int kStageCols = PARTS == 1 ? 64 : 32;
-  const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp / kStageCols);
+  const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp, PARTS);
   for (int v0 = 0; v0 < c.vocab; v0 += kPiece) {
     const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
     PackArgs b{};
     b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
     b.np = np, b.Kp = int(s.Kp), b.frag = at(s.e), b.fragT = df ? at(s.eT) : nullptr;
-    b.maxima = PARTS == 2 ? maxima : nullptr, b.which = 1, b.nmax = kMaxima;
+    b.maxima = PARTS == 2 ? maxima : nullptr, b.nmax = nmax, b.which = 1;
     if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
     CeMmArgs p{};
     p.A = at(s.f), p.W = at(s.e), p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
     p.meta = meta, p.G = at(s.G), p.GT = at(s.GT), p.V = n, p.v0 = v0;
-    if (int rc = launch_logits<T, PARTS, kGrad>(p, large_tiles(s.Rp, np, 0, false), st)) return rc;
+    p.splits = 1;
+    if (int rc = launch_mm<T, PARTS, kGrad>(p, large_logits(s.Rp, np), st)) return rc;
     if (df) {
       CeMmArgs q{};
       q.A = at(s.G), q.W = at(s.eT), q.ta = int(s.Rp / 16), q.tw = int(s.Kp / 16), q.KC = np / 32, q.scales = scales;
@@ -949,7 +1160,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       q.A = at(s.GT), q.W = at(s.fT), q.ta = np / 16, q.tw = int(s.Kp / 16), q.KC = int(s.Rp / 32), q.scales = scales;
       q.out = static_cast<T*>(dE) + int64_t(v0) * c.width, q.M = n, q.N = c.width, q.is_de = 1;
       q.acc = reinterpret_cast<float4*>(ws + s.acce);
-      if (int rc = launch_product<T, PARTS>(q, shares_of(np, s.Kp, s.Rp / kStageCols), true, true, st)) return rc;
+      if (int rc = launch_product<T, PARTS>(q, shares_of(np, s.Kp, s.Rp, PARTS), true, true, st)) return rc;
     }
   }
   return SOMA_OK;
