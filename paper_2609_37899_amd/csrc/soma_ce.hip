@@ -479,17 +479,18 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
         if (m < p.M && n < p.N) store_out<T>(p, m, n, acc[i][j], s);
       }
   } else {
+    // [split][m tile][n tile][TN][TM][lane], however many waves share it
     float4* a = p.acc + ((int64_t(split) * p.ntm + mt0 / TM) * p.ntn + nt0 / TN) * (TN * TM * 64) +
-                wave * (tn * tm * 64) + lane;
+                ((nt0 % TN) * TM + mt0 % TM) * 64 + lane;
 #pragma unroll
     for (int i = 0; i < tn; ++i) {
       __builtin_amdgcn_sched_barrier(0);    // a row's loads at a time
       float4 o[tm];
 #pragma unroll
-      for (int j = 0; j < tm; ++j) o[j] = p.add ? a[(i * tm + j) * 64] : make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int j = 0; j < tm; ++j) o[j] = p.add ? a[(i * TM + j) * 64] : make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int j = 0; j < tm; ++j)
-        a[(i * tm + j) * 64] = make_float4(o[j].x + acc[i][j][0], o[j].y + acc[i][j][1], o[j].z + acc[i][j][2],
+        a[(i * TM + j) * 64] = make_float4(o[j].x + acc[i][j][0], o[j].y + acc[i][j][1], o[j].z + acc[i][j][2],
                                            o[j].w + acc[i][j][3]);
     }
   }
@@ -497,12 +498,11 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
 
 // Fetching stages of row tiles into LDS, in the order in which the block's items
 // use them and across their borders.  A wave moves DPW blocks of every stage:
-// halves (two chunks, or hi and lo) of DPW / 2 row tiles of W or of A, or one
-// chunk of DPW row tiles (kWide).
-template <int PARTS, int TN, int TM, int NW, int DPW, bool kWide>
+// halves (two chunks, or hi and lo) of DPW / 2 row tiles of W or of A.
+template <int PARTS, int TN, int TM, int DPW>
 struct CeFetch {
-  static constexpr int kBuf = (kWide ? 1 : 2) * (TN + TM) * kBlk;      // one stage, in halves
-  static constexpr int kStep = PARTS == 1 && !kWide ? 2 : 1;           // chunks of a stage
+  static constexpr int kBuf = 2 * (TN + TM) * kBlk;     // one stage, in halves
+  static constexpr int kStep = PARTS == 1 ? 2 : 1;      // chunks of a stage
   const CeMmArgs& p;
   i32x4 rs;
   uint32_t soff[DPW];                                   // scalars: vector registers are dear
@@ -518,7 +518,7 @@ struct CeFetch {
   }
   __device__ __forceinline__ void aim() {
     // Row tiles past the matrix repeat its last: nothing of theirs is used.
-    constexpr int per = kWide ? DPW : DPW / 2;          // row tiles of a wave
+    constexpr int per = DPW / 2;                        // row tiles of a wave
     const CeItem w = item_at(p, item);
     const bool weights = wave * per < TN;
     const int t0 = weights ? w.nt * TN : w.mt * TM;
@@ -526,12 +526,11 @@ struct CeFetch {
     const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * PARTS * p.KC * kBlk;
     rs = buffer_words(base, static_cast<uint32_t>(have) * PARTS * p.KC * (kBlk * 2));
     const int mine = wave * per - (weights ? 0 : TN);
-    const int scale = kWide ? 2 : 1;                    // item_at counts pairs of wide stages
-    c = scale * w.s0, end = scale * w.s1;
+    c = w.s0, end = w.s1;
 #pragma unroll
     for (int i = 0; i < DPW; ++i) {
-      const int tile = min(mine + (kWide ? i : i >> 1), have - 1);
-      const int block = PARTS == 1 ? tile * p.KC + c * kStep + (kWide ? 0 : i & 1) : (tile * 2 + (i & 1)) * p.KC + c;
+      const int tile = min(mine + (i >> 1), have - 1);
+      const int block = PARTS == 1 ? tile * p.KC + c * kStep + (i & 1) : (tile * 2 + (i & 1)) * p.KC + c;
       soff[i] = static_cast<uint32_t>(block) * (kBlk * 2);
     }
   }
@@ -557,7 +556,7 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2,
   constexpr int NW = WN * WM, tn = TN / WN, tm = TM / WM;
   constexpr int DPW = 2 * (TN + TM) / NW;               // blocks a wave moves per stage
   static_assert(DPW * NW == 2 * (TN + TM) && DPW % 2 == 0 && TN % (DPW / 2) == 0, "whole row tiles per wave");
-  typedef CeFetch<PARTS, TN, TM, NW, DPW, false> Fetch;
+  typedef CeFetch<PARTS, TN, TM, DPW> Fetch;
   constexpr int BUF = Fetch::kBuf;
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
   uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
@@ -629,13 +628,15 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2,
 // 2,048 clocks, as long as their MFMAs take; with 128 x 128 per wave 192 KiB.  One
 // wave has nobody to hide behind, so everything is ahead of time: a stage is one
 // chunk of 32 columns (64 MFMAs, 1,024 clocks), its DMA is issued four stages before
-// (four LDS buffers of 32 KiB), and its fragments are read into registers under the
-// MFMAs of the stage before (the second of two register sets; stages come in pairs).
+// (four LDS buffers of 32 KiB), its fragments are read into registers under the
+// MFMAs of the stage before (the second of two register sets; stages come in pairs),
+// and both are dealt out between the MFMAs.  A stage has no branch: while an item's
+// last four run, the next item's first four are fetched (behind the last item its
+// own first again, which nobody reads).  An item has four stages at least.
 template <class T, int kEpi>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_ce_mm_wide(CeMmArgs p) {
   constexpr int T16 = 16, t8 = 8, DPW = 8;
-  typedef CeFetch<1, T16, T16, 4, DPW, true> Fetch;
-  constexpr int BUF = Fetch::kBuf;
+  constexpr int BUF = 2 * T16 * kBlk;                   // one stage, in halves
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
   uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
   const int per_xcd = (p.items + kXcd - 1) / kXcd;
@@ -647,73 +648,114 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
   const int wn = wave & 1, wm = wave >> 1;
-  Fetch fetch(p, lds, wave, lane, item, stride, last);
+  const bool weights = wave < 2;
+  i32x4 rs;
+  uint32_t soff[DPW];                                   // scalars: no vector registers are to spare
+  const uint32_t voff = lane * 16;
+  const uint32_t dst = lds_address(lds + wave * DPW * kBlk);
+  auto aim = [&](const CeItem& w) {
+    // Row tiles past the matrix repeat its last: nothing of theirs is used.
+    const int t0 = (weights ? w.nt : w.mt) * T16;
+    const int have = min(T16, (weights ? p.tw : p.ta) - t0);
+    const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * p.KC * kBlk;
+    rs = buffer_words(base, static_cast<uint32_t>(have) * p.KC * (kBlk * 2));
+    const int mine = (wave & 1) * DPW;
+#pragma unroll
+    for (int i = 0; i < DPW; ++i)
+      soff[i] = static_cast<uint32_t>(min(mine + i, have - 1) * p.KC + 2 * w.s0) * (kBlk * 2);
+  };
+  auto fetch = [&](int i, int buf) {
+    dma16(rs, voff, soff[i], dst + static_cast<uint32_t>((buf * BUF + i * kBlk) * 2));
+    soff[i] += kBlk * 2;
+  };
   const uint16_t* const wl = lds + wn * t8 * kBlk + lane * 8;
   const uint16_t* const al = lds + (T16 + wm * t8) * kBlk + lane * 8;
   uint4 fw[2][t8], fa[2][t8];
-  auto read = [&](int set, int buf) {
-#pragma unroll
-    for (int i = 0; i < t8; ++i) {
-      fw[set][i] = *reinterpret_cast<const uint4*>(wl + buf * BUF + i * kBlk);
-      fa[set][i] = *reinterpret_cast<const uint4*>(al + buf * BUF + i * kBlk);
-    }
+  auto read = [&](int set, int buf, int k) {            // fragment k of 16
+    if (k & 1)
+      fa[set][k >> 1] = *reinterpret_cast<const uint4*>(al + buf * BUF + (k >> 1) * kBlk);
+    else
+      fw[set][k >> 1] = *reinterpret_cast<const uint4*>(wl + buf * BUF + (k >> 1) * kBlk);
   };
-  // Four stages on their way; then the first one's fragments.
+  CeItem w = item_at(p, item);
+  aim(w);
 #pragma unroll
-  for (int i = 0; i < 4; ++i) fetch.issue(i);
+  for (int s = 0; s < 4; ++s)
+#pragma unroll
+    for (int i = 0; i < DPW; ++i) fetch(i, s);
   wait_vmem();
   __syncthreads();
-  read(0, 0);
+#pragma unroll
+  for (int k = 0; k < 2 * t8; ++k) read(0, 0, k);
   int buf = 0;
   for (;;) {
-    const CeItem w = item_at(p, item);
     f32x4 acc[t8][t8];
 #pragma unroll
     for (int i = 0; i < t8; ++i)
 #pragma unroll
       for (int j = 0; j < t8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int c = w.s0; c < w.s1; ++c) {
+    auto pair = [&]() {
 #pragma unroll
       for (int half = 0; half < 2; ++half) {
-        // The next stage has landed (while there is one to fetch, two later
-        // ones may be out), and every wave holds this one's fragments, so its
-        // buffer is free.
-        if (fetch.more)
-          wait_vmem_but<2 * DPW>();
-        else
-          wait_vmem();
+        // The next stage has landed (the two behind it may be out), and every
+        // wave holds this one's fragments, so its buffer is free.
+        wait_vmem_but<2 * DPW>();
         __syncthreads();
-        fetch.issue(buf);
-        buf = (buf + 1) & 3;
-        read(half ^ 1, buf);
+        const int here = buf, next = (buf + 1) & 3;
 #pragma unroll
-        for (int i = 0; i < t8; ++i)
+        for (int i = 0; i < t8; ++i) {
+          // eight MFMAs, a DMA and the next stage's fragments (all by the sixth)
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-          for (int j = 0; j < t8; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+          for (int j = 0; j < 2; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+          __builtin_amdgcn_sched_barrier(0);
+          fetch(i, here);
+          __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-        for (int i = 0; i < 2 * t8; ++i) {
-          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);   // one LDS read,
-          __builtin_amdgcn_sched_group_barrier(0x008, 4, 0);   // four MFMAs
+          for (int j = 2; j < t8; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+          if (i < 4) {
+            read(half ^ 1, next, 3 * i), read(half ^ 1, next, 3 * i + 1), read(half ^ 1, next, 3 * i + 2);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
+          } else if (i < 6) {
+            read(half ^ 1, next, 2 * i + 4), read(half ^ 1, next, 2 * i + 5);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
+          }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        buf = next;
       }
-    }
-    ce_epilogue<T, 1, kEpi, T16, T16, t8, t8>(acc, w.mt * T16 + wm * t8, w.nt * T16 + wn * t8, w.split, wave, lane);
+    };
+    for (int c = w.s0; c < w.s1 - 2; ++c) pair();
+    const int mt0 = w.mt * T16 + wm * t8, nt0 = w.nt * T16 + wn * t8, split = w.split;
     item += stride;
-    if (item >= last) break;
+    const bool more = item < last;                      // block-uniform
+    if (more) w = item_at(p, item);
+    aim(w);
+    pair();
+    pair();
+    ce_epilogue<T, 1, kEpi, T16, T16, t8, t8>(acc, mt0, nt0, split, wave, lane);
+    if (!more) break;
   }
+  wait_vmem();                                          // the last fetches, before the LDS is another block's
 }
 
 // The shares of kPart's accumulators summed in order, to the result.
-template <class T, int PARTS, int TN, int TM, int WN, int WM>
-__global__ __launch_bounds__(64 * WN * WM) void k_ce_sum(CeMmArgs p) {
-  constexpr int tn = TN / WN, tm = TM / WM;
+template <class T, int PARTS, int TN, int TM>
+__global__ __launch_bounds__(256) void k_ce_sum(CeMmArgs p) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int wn = wave % WN, wm = wave / WN;
   const int tile = blockIdx.x, mt = tile / p.ntn, nt = tile % p.ntn;
-  const int i = blockIdx.y / tm, j = blockIdx.y % tm;
-  const int m = (mt * TM + wm * tm + j) * 16 + lr, n = (nt * TN + wn * tn + i) * 16 + 4 * lg;
+  const int part = blockIdx.y * 4 + wave, i = part / TM, j = part % TM;
+  const int m = (mt * TM + j) * 16 + lr, n = (nt * TN + i) * 16 + 4 * lg;
   if (m >= p.M || n >= p.N) return;
-  const float4* a = p.acc + int64_t(tile) * (TN * TM * 64) + wave * (tn * tm * 64) + (i * tm + j) * 64 + lane;
+  const float4* a = p.acc + int64_t(tile) * (TN * TM * 64) + part * 64 + lane;
   const int64_t step = int64_t(p.ntm) * p.ntn * (TN * TM * 64);
   f32x4 v{0.f, 0.f, 0.f, 0.f};
 #pragma unroll 8
@@ -992,11 +1034,11 @@ int launch_mm(CeMmArgs& p, bool large, hipStream_t st) {
   p.ntn = (p.tw + side - 1) / side;
   p.stages = p.KC / (PARTS == 1 ? 2 : 1);
   if constexpr (PARTS == 1) {
-    if (large) return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi>), p, 256, true, 131072, st);
-  } else {
-    if (large)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, true, 131072, st);
+    if (large && p.stages / p.splits >= 2)              // four stages of its own an item
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi>), p, 256, true, 131072, st);
   }
+  if (large)
+    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, true, 131072, st);
   // One block a compute unit: its four buffers hide what a second block would.
   if (int64_t(p.ntm) * p.ntn * p.splits <= kFill)
     return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 4>), p, 256, false, 131072, st);
@@ -1040,12 +1082,10 @@ int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipSt
   if (!finish) return SOMA_OK;
   p.splits = sh.splits;
   const unsigned tiles = unsigned(p.ntm * p.ntn);
-  if (!sh.large)
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8, 2, 2>), dim3(tiles, 4 * 4), dim3(256), 0, st, p);
-  else if constexpr (PARTS == 1)
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 2>), dim3(tiles, 8 * 8), dim3(256), 0, st, p);
+  if (sh.large)
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16>), dim3(tiles, 64), dim3(256), 0, st, p);
   else
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16, 2, 4>), dim3(tiles, 8 * 4), dim3(512), 0, st, p);
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8>), dim3(tiles, 16), dim3(256), 0, st, p);
   return launched("k_ce_sum");
 }
 
