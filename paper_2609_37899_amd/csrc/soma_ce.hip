@@ -7,11 +7,11 @@
 // All four products run on the matrix cores (k_ce_mm) over operands in MFMA
 // fragment order (below).  The loss keeps, of every row, the maximum and the
 // sum of exponentials of each 64 or 128 logits, and joins them at the end; the
-// gradient forms the logits again, a piece of kPiece vocabulary rows at a time,
+// gradient forms the logits again, a piece of the vocabulary at a time,
 // stores the piece of G only (in 16 bits, in the order that either product
 // reads), and multiplies it by the piece of E (added to df) and by f (the piece
-// of dE).  So the work is 8 R V K operations instead of 6, for R kPiece values
-// in memory instead of R V.
+// of dE).  So the work is 8 R V K operations instead of 6, for a piece's
+// values in memory instead of R V.
 //
 // Types.  bf16: E and f as they are, G rounded to bf16 (half a step, 2^-8, of
 // every value; as much as the result's own rounding), sums in fp32.  fp32: every
@@ -40,9 +40,14 @@
 namespace soma {
 namespace {
 
-constexpr int kPiece = 8192;          // vocabulary rows of a piece
+// Vocabulary rows of a piece.  Each adds its part of df to the sums of the ones
+// before (8 bytes of each output moved), and at 16,384 the products of a training
+// batch of 8,192 rows fill the card without shares; at more rows 8,192, which
+// halves what a piece of G takes.
+constexpr int kPiece = 8192, kLongPiece = 16384, kLongRows = 8192;
 constexpr int kMaxima = 1024;         // partial maxima of an array
 constexpr float kLog2 = 0.6931471805599453f;
+constexpr float kLowest = -2.3e38f;   // below every logit that counts; log2 e times it is finite
 constexpr int kBlk = 512;             // halves of a fragment block
 constexpr int kXcd = 8;
 
@@ -287,6 +292,7 @@ struct CeMmArgs {
   // kStats
   float2* part;              // [sub][part_stride]
   int part_stride, sub0;
+  int tile_subs;             // parts of a row in one tile (the host's)
   float* hit;                // [rows]: the target's logit
   const int32_t* targets;
   int R, V, v0;              // rows; vocabulary rows of the piece; its first
@@ -363,6 +369,13 @@ __device__ __forceinline__ CeItem item_at(const CeMmArgs& p, int t) {
   return w;
 }
 
+// e^(x - top).  bf16: one rounding of x log2 e - top log2 e, 2^-24 |top| beside
+// bf16's own; fp32 operands: the difference first, exact for x near top.
+template <int PARTS>
+__device__ __forceinline__ float shifted_exp(float x, float top) {
+  return exp2_f(PARTS == 1 ? __builtin_fmaf(x, kLog2e, -kLog2e * top) : kLog2e * (x - top));
+}
+
 // What becomes of a wave's accumulators:
 // acc[i][j][q] = C[16 (mt0 + j) + lr][16 (nt0 + i) + 4 lg + q].
 // It reads the kernel's arguments again from where they were passed, and hides
@@ -381,11 +394,11 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
   const int lr = lane & 15, lg = lane >> 4;
   if constexpr (kEpi == kStats) {
     const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
-    const int sub = p.sub0 + nt0 / tn;
+    const int sub = p.sub0 + nt0 / tn;                    // tn: a wave's share of the columns
     const int left = p.V - nt0 * 16 - 4 * lg;             // this lane's columns 16 i + q below it are in the vocabulary
     // No branch inside: results wait in registers until the end, and the tile
     // that the vocabulary ends in has code of its own.
-    float tops[tm], sums[tm], hits[tm];
+    float tops[tm], sums[tm];
     int targets[tm];
 #pragma unroll
     for (int j = 0; j < tm; ++j) targets[j] = p.targets[min((mt0 + j) * 16 + lr, p.R - 1)] - p.v0 - nt0 * 16 - 4 * lg;
@@ -395,14 +408,13 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
         __builtin_amdgcn_sched_barrier(0);  // one column of tiles at a time: the accumulators fill half of the registers
         int l = left;
         if constexpr (!decltype(whole)::value) asm volatile("" : "+v"(l));   // the comparisons are not kept from j to j
-        float top = -3.402823466e38f, hit = 0.0f, x[tn][4];
+        float top = kLowest, x[tn][4];
 #pragma unroll
         for (int i = 0; i < tn; ++i)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
             x[i][q] = acc[i][j][q] * undo;
             if constexpr (!decltype(whole)::value) x[i][q] = 16 * i + q < l ? x[i][q] : -__builtin_inff();
-            hit = targets[j] == 16 * i + q ? x[i][q] : hit;
             top = fmaxf(top, x[i][q]);
           }
         top = group4_max(top);
@@ -410,8 +422,8 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
 #pragma unroll
         for (int i = 0; i < tn; ++i)
 #pragma unroll
-          for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (x[i][q] - top));
-        tops[j] = top, sums[j] = group4_sum(sum), hits[j] = hit;
+          for (int q = 0; q < 4; ++q) sum += shifted_exp<PARTS>(x[i][q], top);
+        tops[j] = top, sums[j] = group4_sum(sum);
       }
     };
     if (p.V - nt0 * 16 >= 16 * tn)                        // wave-uniform
@@ -421,20 +433,31 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
 #pragma unroll
     for (int j = 0; j < tm; ++j) {
       const int m = (mt0 + j) * 16 + lr, t = targets[j];
-      if (m < p.R) {
-        if (t >= 0 && t < 16 * tn && t < left && (t & 15) < 4) p.hit[m] = hits[j];
-        if (lg == 0) p.part[int64_t(sub) * p.part_stride + m] = make_float2(tops[j], sums[j]);
+      const bool in = m < p.R && t >= 0 && t < 16 * tn && t < left && (t & 15) < 4;
+      if (__any(in)) {                                    // few tiles of a large vocabulary hold a row's target
+        float hit = 0.0f;
+#pragma unroll
+        for (int i = 0; i < tn; ++i)
+#pragma unroll
+          for (int q = 0; q < 4; ++q) hit = t == 16 * i + q ? acc[i][j][q] : hit;
+        if (in) p.hit[m] = hit * undo;
       }
+      if (m < p.R && lg == 0) p.part[int64_t(sub) * p.part_stride + m] = make_float2(tops[j], sums[j]);
     }
   } else if constexpr (kEpi == kGrad) {
     const float undo = PARTS == 1 ? 1.0f : (1.0f / p.scales->f) * (1.0f / p.scales->e);
-    const int GC = p.tw / 2, TC = p.ta / 2;           // chunks of 32 in G's and GT's rows
+    const int GC = p.tw / 2, TC = p.ta / 2;               // chunks of 32 in G's and GT's rows
+    const int left = p.V - nt0 * 16 - 4 * lg;             // this lane's columns 16 i + q below it are in the vocabulary
+    const bool whole = p.V - nt0 * 16 >= 16 * tn;         // wave-uniform
+    RowMeta meta[tm];
+#pragma unroll
+    for (int j = 0; j < tm; ++j) meta[j] = p.meta[min((mt0 + j) * 16, (p.ta - 1) * 16) + lr];
 #pragma unroll
     for (int j = 0; j < tm; ++j) {
       const int rt = mt0 + j;
-      if (rt >= p.ta) continue;                       // wave-uniform
-      const RowMeta m = p.meta[rt * 16 + lr];
-      const int target = m.target - p.v0;
+      if (rt >= p.ta) continue;                           // wave-uniform
+      const float lse = meta[j].lse, rho = meta[j].rho;
+      const int target = meta[j].target - p.v0 - nt0 * 16 - 4 * lg;
 #pragma unroll
       for (int i = 0; i < tn; ++i) {
         const int nt = nt0 + i;
@@ -442,9 +465,12 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
         float g[4];
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int v = nt * 16 + 4 * lg + q;
-          const float e = exp2_f(kLog2e * (acc[i][j][q] * undo - m.lse));
-          g[q] = v < p.V ? m.rho * (v == target ? e - 1.0f : e) : 0.0f;
+          const float e = shifted_exp<PARTS>(acc[i][j][q] * undo, lse);
+          g[q] = rho * (target == 16 * i + q ? e - 1.0f : e);
+        }
+        if (!whole) {
+#pragma unroll
+          for (int q = 0; q < 4; ++q) g[q] = 16 * i + q < left ? g[q] : 0.0f;
         }
         // G: row lr of its tile, columns 4 lg .. of 16.  GT: row 4 lg + (lr & 3), columns 4 (lr / 4) .. .
         uint16_t* G = p.G + (int64_t(rt) * PARTS * GC + nt / 2) * kBlk +
@@ -623,20 +649,27 @@ __global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2,
   }
 }
 
-// bf16, 256 x 256 with 4 waves of 128 x 128: one wave on each SIMD.  With 8 waves
-// of 128 x 64 the LDS moves 256 KiB for 64 columns (192 read, 64 written by DMA),
-// 2,048 clocks, as long as their MFMAs take; with 128 x 128 per wave 192 KiB.  One
-// wave has nobody to hide behind, so everything is ahead of time: a stage is one
-// chunk of 32 columns (64 MFMAs, 1,024 clocks), its DMA is issued four stages before
-// (four LDS buffers of 32 KiB), its fragments are read into registers under the
-// MFMAs of the stage before (the second of two register sets; stages come in pairs),
-// and both are dealt out between the MFMAs.  A stage has no branch: while an item's
-// last four run, the next item's first four are fetched (behind the last item its
-// own first again, which nobody reads).  An item has four stages at least.
-template <class T, int kEpi>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) void k_ce_mm_wide(CeMmArgs p) {
-  constexpr int T16 = 16, t8 = 8, DPW = 8;
-  constexpr int BUF = 2 * T16 * kBlk;                   // one stage, in halves
+// bf16 with 4 waves a block.
+//  * 256 x 256, 128 x 128 a wave, one wave on each SIMD (the products with G).
+//    With 8 waves of 128 x 64 the LDS moves 256 KiB for 64 columns (192 read, 64
+//    written by DMA), 2,048 clocks, as long as their MFMAs take; with 128 x 128
+//    per wave 192 KiB.  Four LDS buffers.
+//  * 256 rows x 128 vocabulary rows, 64 x 128 a wave, two blocks a compute unit
+//    (the logits): what becomes of a tile, exponentials and stores, takes half as
+//    long as its MFMAs, and runs beside the other block's.  Three buffers.
+// A stage is one chunk of 32 columns.  Everything is ahead of time: its DMA is
+// issued as many stages before as there are buffers, its fragments are read into
+// registers under the MFMAs of the stage before (the second of two register sets;
+// stages come in pairs), and both are dealt out between the MFMAs.  A stage has no
+// branch: while an item's last stages run, the next item's first are fetched
+// (behind the last item its own first again, which nobody reads).  An item has
+// four stages at least.
+template <class T, int kEpi, int TN, int WN, int kBufs, int kPerEu>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPerEu))) void k_ce_mm_wide(CeMmArgs p) {
+  constexpr int TM = 16, WM = 4 / WN, tn = TN / WN, tm = TM / WM;
+  constexpr int FW = TN / 4, FA = TM / 4, DPW = FW + FA;   // blocks of W and of A that a wave fetches
+  constexpr int BUF = (TN + TM) * kBlk;                 // one stage, in halves
+  constexpr int kFrags = tn + tm;
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
   uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
   const int per_xcd = (p.items + kXcd - 1) / kXcd;
@@ -647,101 +680,98 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(1, 1))) voi
   if (item >= last) return;                             // block-uniform
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
-  const int wn = wave & 1, wm = wave >> 1;
-  const bool weights = wave < 2;
-  i32x4 rs;
+  const int wn = wave % WN, wm = wave / WN;
+  i32x4 rw, ra;
   uint32_t soff[DPW];                                   // scalars: no vector registers are to spare
   const uint32_t voff = lane * 16;
-  const uint32_t dst = lds_address(lds + wave * DPW * kBlk);
+  const uint32_t dw = lds_address(lds + wave * FW * kBlk), da = lds_address(lds + (TN + wave * FA) * kBlk);
   auto aim = [&](const CeItem& w) {
     // Row tiles past the matrix repeat its last: nothing of theirs is used.
-    const int t0 = (weights ? w.nt : w.mt) * T16;
-    const int have = min(T16, (weights ? p.tw : p.ta) - t0);
-    const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * p.KC * kBlk;
-    rs = buffer_words(base, static_cast<uint32_t>(have) * p.KC * (kBlk * 2));
-    const int mine = (wave & 1) * DPW;
+    const int hw = min(TN, p.tw - w.nt * TN), ha = min(TM, p.ta - w.mt * TM);
+    rw = buffer_words(p.W + int64_t(w.nt) * TN * p.KC * kBlk, static_cast<uint32_t>(hw) * p.KC * (kBlk * 2));
+    ra = buffer_words(p.A + int64_t(w.mt) * TM * p.KC * kBlk, static_cast<uint32_t>(ha) * p.KC * (kBlk * 2));
 #pragma unroll
     for (int i = 0; i < DPW; ++i)
-      soff[i] = static_cast<uint32_t>(min(mine + i, have - 1) * p.KC + 2 * w.s0) * (kBlk * 2);
+      soff[i] = static_cast<uint32_t>((i < FW ? min(wave * FW + i, hw - 1) : min(wave * FA + i - FW, ha - 1)) * p.KC +
+                                      2 * w.s0) * (kBlk * 2);
   };
   auto fetch = [&](int i, int buf) {
-    dma16(rs, voff, soff[i], dst + static_cast<uint32_t>((buf * BUF + i * kBlk) * 2));
+    if (i < FW)
+      dma16(rw, voff, soff[i], dw + static_cast<uint32_t>((buf * BUF + i * kBlk) * 2));
+    else
+      dma16(ra, voff, soff[i], da + static_cast<uint32_t>((buf * BUF + (i - FW) * kBlk) * 2));
     soff[i] += kBlk * 2;
   };
-  const uint16_t* const wl = lds + wn * t8 * kBlk + lane * 8;
-  const uint16_t* const al = lds + (T16 + wm * t8) * kBlk + lane * 8;
-  uint4 fw[2][t8], fa[2][t8];
-  auto read = [&](int set, int buf, int k) {            // fragment k of 16
-    if (k & 1)
-      fa[set][k >> 1] = *reinterpret_cast<const uint4*>(al + buf * BUF + (k >> 1) * kBlk);
+  const uint16_t* const wl = lds + wn * tn * kBlk + lane * 8;
+  const uint16_t* const al = lds + (TN + wm * tm) * kBlk + lane * 8;
+  uint4 fw[2][tn], fa[2][tm];
+  auto read = [&](int set, int buf, int k) {            // fragment k: A's first, all of which the first MFMAs need
+    if (k < tm)
+      fa[set][k] = *reinterpret_cast<const uint4*>(al + buf * BUF + k * kBlk);
     else
-      fw[set][k >> 1] = *reinterpret_cast<const uint4*>(wl + buf * BUF + (k >> 1) * kBlk);
+      fw[set][k - tm] = *reinterpret_cast<const uint4*>(wl + buf * BUF + (k - tm) * kBlk);
   };
   CeItem w = item_at(p, item);
   aim(w);
 #pragma unroll
-  for (int s = 0; s < 4; ++s)
+  for (int s = 0; s < kBufs; ++s)
 #pragma unroll
     for (int i = 0; i < DPW; ++i) fetch(i, s);
   wait_vmem();
   __syncthreads();
 #pragma unroll
-  for (int k = 0; k < 2 * t8; ++k) read(0, 0, k);
+  for (int k = 0; k < kFrags; ++k) read(0, 0, k);
   int buf = 0;
   for (;;) {
-    f32x4 acc[t8][t8];
+    f32x4 acc[tn][tm];
 #pragma unroll
-    for (int i = 0; i < t8; ++i)
+    for (int i = 0; i < tn; ++i)
 #pragma unroll
-      for (int j = 0; j < t8; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto pair = [&]() {
+      for (int j = 0; j < tm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
+    auto stage = [&](auto set) {
+      constexpr int half = decltype(set)::value;
+      // The next stage has landed (those behind it may be out), and every wave
+      // holds this one's fragments, so its buffer is free.
+      wait_vmem_but<(kBufs - 2) * DPW>();
+      __syncthreads();
+      const int here = buf, next = buf == kBufs - 1 ? 0 : buf + 1;
+      // Groups of four MFMAs, all but the last ones (LDS reads take time) with
+      // their share of the DMAs and of the next stage's fragments.
+      constexpr int kGroups = tn * tm / 4, kLoaded = kGroups - kGroups / 4;
 #pragma unroll
-      for (int half = 0; half < 2; ++half) {
-        // The next stage has landed (the two behind it may be out), and every
-        // wave holds this one's fragments, so its buffer is free.
-        wait_vmem_but<2 * DPW>();
-        __syncthreads();
-        const int here = buf, next = (buf + 1) & 3;
-#pragma unroll
-        for (int i = 0; i < t8; ++i) {
-          // eight MFMAs, a DMA and the next stage's fragments (all by the sixth)
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 0; j < 2; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
-          __builtin_amdgcn_sched_barrier(0);
-          fetch(i, here);
-          __builtin_amdgcn_sched_barrier(0);
-#pragma unroll
-          for (int j = 2; j < t8; ++j) acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
-          if (i < 4) {
-            read(half ^ 1, next, 3 * i), read(half ^ 1, next, 3 * i + 1), read(half ^ 1, next, 3 * i + 2);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 2, 0);
-          } else if (i < 6) {
-            read(half ^ 1, next, 2 * i + 4), read(half ^ 1, next, 2 * i + 5);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
-            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
-            __builtin_amdgcn_sched_group_barrier(0x008, 3, 0);
-          }
-        }
+      for (int g = 0; g < kGroups; ++g) {
         __builtin_amdgcn_sched_barrier(0);
-        buf = next;
+#pragma unroll
+        for (int d = DPW * g / kLoaded; d < DPW * (g + 1) / kLoaded && d < DPW; ++d) fetch(d, here);
+#pragma unroll
+        for (int k = kFrags * g / kLoaded; k < kFrags * (g + 1) / kLoaded && k < kFrags; ++k) read(half ^ 1, next, k);
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int i = (g * 4 + q) / tm, j = (g * 4 + q) % tm;
+          acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+        }
       }
+      __builtin_amdgcn_sched_barrier(0);
+      buf = next;
     };
-    for (int c = w.s0; c < w.s1 - 2; ++c) pair();
-    const int mt0 = w.mt * T16 + wm * t8, nt0 = w.nt * T16 + wn * t8, split = w.split;
+    constexpr std::integral_constant<int, 0> even;
+    constexpr std::integral_constant<int, 1> odd;
+    for (int c = w.s0; c < w.s1 - 2; ++c) {
+      stage(even);
+      stage(odd);
+    }
+    const int mt0 = w.mt * TM + wm * tm, nt0 = w.nt * TN + wn * tn, split = w.split;
     item += stride;
     const bool more = item < last;                      // block-uniform
     if (more) w = item_at(p, item);
-    aim(w);
-    pair();
-    pair();
-    ce_epilogue<T, 1, kEpi, T16, T16, t8, t8>(acc, mt0, nt0, split, wave, lane);
+    static_assert(kBufs == 3 || kBufs == 4, "the last kBufs stages fetch from the next item");
+    if constexpr (kBufs == 4) aim(w);
+    stage(even);
+    if constexpr (kBufs == 3) aim(w);
+    stage(odd);
+    stage(even);
+    stage(odd);
+    ce_epilogue<T, 1, kEpi, TN, TM, tn, tm>(acc, mt0, nt0, split, wave, lane);
     if (!more) break;
   }
   wait_vmem();                                          // the last fetches, before the LDS is another block's
@@ -805,7 +835,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
     }
   __syncthreads();
   const int target = lr < a.R ? a.targets[lr] : -1;
-  float top = -3.402823466e38f, sum = 0.0f;
+  float top = kLowest, sum = 0.0f;
   const int tiles = (a.V + 15) / 16;
   const int full = a.K / kChunk;                        // chunks without a tail
   const T* E = static_cast<const T*>(a.E);
@@ -867,7 +897,7 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
   if (lg == 0) red[wave][lr] = make_float2(all, sum);
   __syncthreads();
   if (threadIdx.x < 16) {
-    float m = -3.402823466e38f, s = 0.0f;
+    float m = kLowest, s = 0.0f;
     for (int w = 0; w < kRowsWaves; ++w) m = fmaxf(m, red[w][threadIdx.x].x);
     for (int w = 0; w < kRowsWaves; ++w) s += red[w][threadIdx.x].y * exp2_f(kLog2e * (red[w][threadIdx.x].x - m));
     a.part[blockIdx.x * 16 + threadIdx.x] = make_float2(m, s);
@@ -882,7 +912,7 @@ __global__ __launch_bounds__(16 * kParts) void k_ce_join(const float2* part, int
                                                  const float* hit, int R, int V, float* loss, float* lse) {
   __shared__ float2 red[kParts][17];
   const int lr = threadIdx.x & 15, w = threadIdx.x >> 4, r = blockIdx.x * 16 + lr;
-  float top = -3.402823466e38f, sum = 0.0f;
+  float top = kLowest, sum = 0.0f;
   if (r < R)
 #pragma unroll 4
     for (int s = w; s < subs; s += kParts) {
@@ -903,7 +933,7 @@ __global__ __launch_bounds__(16 * kParts) void k_ce_join(const float2* part, int
     __syncthreads();
   }
   if (w != 0 || r >= R) return;
-  float m = -3.402823466e38f, s = 0.0f;
+  float m = kLowest, s = 0.0f;
 #pragma unroll
   for (int i = 0; i < 8; ++i) m = fmaxf(m, red[i][lr].x);
 #pragma unroll
@@ -949,12 +979,18 @@ size_t acc_bytes(int64_t m, int64_t n, int64_t stages) {
   return size_t(most) * 4;
 }
 
+int piece_of(const soma_ce_config& c) { return c.rows <= kLongRows ? kLongPiece : kPiece; }
+
+// Every part grows with the rows, also where the piece gets shorter, so that a
+// workspace for many rows holds a call of fewer.
 Sizes sizes_of(const soma_ce_config& c, bool grad) {
   Sizes s{};
   s.Rp = up(c.rows, 64);
   s.Kp = up(c.width, 64);
-  s.Vp = up(std::min<int64_t>(c.vocab, kPiece), 64);
+  s.Vp = up(std::min<int64_t>(c.vocab, piece_of(c)), 64);
   s.parts = c.type == SOMA_FLOAT ? 2 : 1;
+  const int64_t longest = up(std::min<int64_t>(c.vocab, kLongPiece), 64);
+  const int64_t area = std::max(s.Rp * s.Vp, std::min<int64_t>(s.Rp, kLongRows) * longest);
   size_t at = 0;
   auto take = [&](size_t bytes) {
     const size_t o = at;
@@ -971,14 +1007,14 @@ Sizes sizes_of(const soma_ce_config& c, bool grad) {
   s.maxima = take(3 * kMaxima * 4);
   s.scales = take(sizeof(Scales));
   s.f = take(size_t(s.Rp) * s.Kp * half);
-  s.e = take(size_t(s.Vp) * s.Kp * half);
+  s.e = take(size_t(longest) * s.Kp * half);
   if (grad) {
     s.fT = take(size_t(s.Rp) * s.Kp * half);
-    s.eT = take(size_t(s.Vp) * s.Kp * half);
-    s.G = take(size_t(s.Rp) * s.Vp * half);
-    s.GT = take(size_t(s.Rp) * s.Vp * half);
-    s.accf = take(acc_bytes(s.Rp, s.Kp, s.Vp / 32));
-    s.acce = take(acc_bytes(s.Vp, s.Kp, s.Rp / 32));
+    s.eT = take(size_t(longest) * s.Kp * half);
+    s.G = take(size_t(area) * half);
+    s.GT = take(size_t(area) * half);
+    s.accf = take(acc_bytes(s.Rp, s.Kp, longest / 32));
+    s.acce = take(acc_bytes(longest, s.Kp, s.Rp / 32));
   }
   s.total = at;
   return s;
@@ -1009,14 +1045,15 @@ Divider divider(int d) {
   return {uint32_t((uint64_t(1) << 32) * ((uint64_t(1) << l) - uint64_t(d)) / uint64_t(d)) + 1u, l, d};
 }
 
-int launch_items(const void* kern, CeMmArgs& p, int threads, bool loop, unsigned lds, hipStream_t st) {
+// most: blocks that work through the items one after another; 0: a block each.
+int launch_items(const void* kern, CeMmArgs& p, int threads, int64_t most, unsigned lds, hipStream_t st) {
   const int64_t items = int64_t(p.ntm) * p.ntn * p.splits;
   if (items >= (int64_t(1) << 30)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
   p.items = int(items);
   p.by_tiles = divider(p.ntm * p.ntn), p.by_band = divider(8 * p.ntm), p.by_rest = divider(std::max(p.ntn % 8, 1));
   p.by_splits = divider(p.splits);
   int64_t blocks = up(items, kXcd);
-  if (loop) blocks = std::min<int64_t>(blocks, kFill);
+  if (most) blocks = std::min(blocks, most);
   hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
   void* args[] = {&p};
@@ -1025,24 +1062,30 @@ int launch_items(const void* kern, CeMmArgs& p, int threads, bool loop, unsigned
   return SOMA_OK;
 }
 
-// A product on 256 x 256 tiles (one block per compute unit works through
-// them) or on 128 x 128.
+// A product on tiles of 16 side x 16 side, side = 16 or 8; bf16 logits on large
+// tiles take 8 x 16.
 template <class T, int PARTS, int kEpi>
 int launch_mm(CeMmArgs& p, bool large, hipStream_t st) {
-  const int side = large ? 16 : 8;
-  p.ntm = (p.ta + side - 1) / side;
-  p.ntn = (p.tw + side - 1) / side;
+  constexpr bool kLogits = kEpi == kStats || kEpi == kGrad;
   p.stages = p.KC / (PARTS == 1 ? 2 : 1);
-  if constexpr (PARTS == 1) {
-    if (large && p.stages / p.splits >= 2)              // four stages of its own an item
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi>), p, 256, true, 131072, st);
+  const bool wide = PARTS == 1 && large && p.stages / p.splits >= 2;     // four stages of its own an item
+  const int tm = large ? 16 : 8, tn = wide && kLogits ? 8 : tm;
+  p.ntm = (p.ta + tm - 1) / tm;
+  p.ntn = (p.tw + tn - 1) / tn;
+  p.tile_subs = wide ? 1 : 2;
+  if constexpr (PARTS == 1 && kLogits) {
+    if (wide)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi, 8, 1, 3, 2>), p, 256, 2 * kFill, 73728, st);
+  } else if constexpr (PARTS == 1) {
+    if (wide)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi, 16, 2, 4, 1>), p, 256, kFill, 131072, st);
   }
   if (large)
-    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, true, 131072, st);
+    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, kFill, 131072, st);
   // One block a compute unit: its four buffers hide what a second block would.
   if (int64_t(p.ntm) * p.ntn * p.splits <= kFill)
-    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 4>), p, 256, false, 131072, st);
-  return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 2>), p, 256, false, 65536, st);
+    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 4>), p, 256, 0, 131072, st);
+  return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 2>), p, 256, 0, 65536, st);
 }
 
 int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return up(m, side) / side * (up(n, side) / side); }
@@ -1135,8 +1178,9 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     a.V = c.vocab;
     if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
     stride = int(s.Rp);
-    for (int v0 = 0; v0 < c.vocab; v0 += kPiece) {
-      const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
+    const int piece = piece_of(c);
+    for (int v0 = 0; v0 < c.vocab; v0 += piece) {
+      const int n = std::min(piece, c.vocab - v0), np = int(up(n, 64));
       PackArgs b{};
       b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
       b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.nmax = nmax, b.which = 1;
@@ -1147,7 +1191,7 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       const bool large = large_logits(s.Rp, np);
       p.splits = 1;
       if (int rc = launch_mm<T, PARTS, kStats>(p, large, st)) return rc;
-      subs += p.ntn * 2;
+      subs += p.tile_subs * p.ntn;
     }
   }
   const dim3 jgrid((c.rows + 15) / 16);
@@ -1177,8 +1221,9 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   a.scales = scales, a.meta = meta, a.lse = lse, a.w = w, a.V = c.vocab;
   if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
   const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp, PARTS);
-  for (int v0 = 0; v0 < c.vocab; v0 += kPiece) {
-    const int n = std::min(kPiece, c.vocab - v0), np = int(up(n, 64));
+  const int piece = piece_of(c);
+  for (int v0 = 0; v0 < c.vocab; v0 += piece) {
+    const int n = std::min(piece, c.vocab - v0), np = int(up(n, 64));
     PackArgs b{};
     b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
     b.np = np, b.Kp = int(s.Kp), b.frag = at(s.e), b.fragT = df ? at(s.eT) : nullptr;
@@ -1193,7 +1238,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       CeMmArgs q{};
       q.A = at(s.G), q.W = at(s.eT), q.ta = int(s.Rp / 16), q.tw = int(s.Kp / 16), q.KC = np / 32, q.scales = scales;
       q.out = df, q.M = c.rows, q.N = c.width, q.acc = reinterpret_cast<float4*>(ws + s.accf), q.add = v0 > 0;
-      if (int rc = launch_product<T, PARTS>(q, of_df, c.vocab <= kPiece, v0 + kPiece >= c.vocab, st)) return rc;
+      if (int rc = launch_product<T, PARTS>(q, of_df, c.vocab <= piece, v0 + piece >= c.vocab, st)) return rc;
     }
     if (dE) {
       CeMmArgs q{};

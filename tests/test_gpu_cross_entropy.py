@@ -58,7 +58,7 @@ def check(x, y, dtype, names=("loss", "lse", "df", "dE")):
             else:
                 tol = tol + want[name + "_tiny"]
             tol = tol * (1 + 2.0 ** -8) + ref.half_step(dtype) * np.abs(exact)
-        bad = np.abs(got - exact) > tol
+        bad = ~(np.abs(got - exact) <= tol)            # NaN counts as wrong
         assert not bad.any(), (f"{name}: {bad.sum()} of {bad.size}, worst {np.nanmax(np.abs(got - exact) / tol):.3g} of "
                                f"the bound, not finite {np.sum(~np.isfinite(got))}")
         if name in ("df", "dE") and exact.size:

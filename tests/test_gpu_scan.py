@@ -54,7 +54,7 @@ def check(y, want, dtype):
         assert np.all(got[outside] == 7.0), f"{name}: rows behind the last sequence were written"
         # the type's smallest steps as well
         tol = want[name + "_err"] * (1 + step) + step * np.abs(np.nan_to_num(exact)) + 1e-37
-        bad = np.abs(got - exact) > tol
+        bad = ~(np.abs(got - exact) <= tol)            # NaN counts as wrong
         bad[outside] = False
         assert not bad.any(), (f"{name}: {bad.sum()} of {bad.size}, worst {np.nanmax(np.abs(got - exact) / tol):.2f} "
                                f"of the bound")
