@@ -268,6 +268,18 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
 // round-robin) works through a contiguous range of items, 8 n tiles wide at a
 // time, so that the tiles in flight share operands in its L2.
 // ---------------------------------------------------------------------------
+// Rows of eight from fours: lanes lr of which (lr & 4) == 0 receive their own a and
+// lane lr ^ 4's, the others lane lr ^ 4's b and their own.
+__device__ __forceinline__ uint4 join_eight(const uint2& a, const uint2& b, int lane) {
+  // from lane + 4 (a rotation by 12 of 16) in the even groups of four, from lane
+  // - 4 (by 4) in the odd ones
+  uint32_t x = __builtin_amdgcn_update_dpp(0u, a.x, 0x12C, 0xF, 0x5, false);
+  uint32_t y = __builtin_amdgcn_update_dpp(0u, a.y, 0x12C, 0xF, 0x5, false);
+  x = __builtin_amdgcn_update_dpp(x, b.x, 0x124, 0xF, 0xA, false);
+  y = __builtin_amdgcn_update_dpp(y, b.y, 0x124, 0xF, 0xA, false);
+  return lane & 4 ? make_uint4(x, y, b.x, b.y) : make_uint4(a.x, a.y, x, y);
+}
+
 // Division by a number that is known on the host: n / d = (mulhi(m, n) + n) >> l
 // with l = ceil(log2 d), m = floor(2^32 (2^l - d) / d) + 1, for 0 <= n < 2^31.
 struct Divider {
@@ -449,53 +461,92 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
     const int GC = p.tw / 2, TC = p.ta / 2;               // chunks of 32 in G's and GT's rows
     const int left = p.V - nt0 * 16 - 4 * lg;             // this lane's columns 16 i + q below it are in the vocabulary
     const bool whole = p.V - nt0 * 16 >= 16 * tn;         // wave-uniform
+    static_assert(tm % 2 == 0 && tn % 2 == 0, "tiles are stored in pairs, a block of 32 columns each way");
     RowMeta meta[tm];
 #pragma unroll
     for (int j = 0; j < tm; ++j) meta[j] = p.meta[min((mt0 + j) * 16, (p.ta - 1) * 16) + lr];
+    // They arrive here: a load that is still out on some path makes the
+    // compiler wait for everything, DMAs too, where its register is used next.
 #pragma unroll
-    for (int j = 0; j < tm; ++j) {
-      const int rt = mt0 + j;
-      if (rt >= p.ta) continue;                           // wave-uniform
-      const float lse = meta[j].lse, rho = meta[j].rho;
-      const int target = meta[j].target - p.v0 - nt0 * 16 - 4 * lg;
+    for (int j = 0; j < tm; ++j) asm volatile("" : "+v"(meta[j].lse), "+v"(meta[j].rho), "+v"(meta[j].target));
+    // Column tiles i, i + 1 of row tiles j, j + 1 (an even number of either):
+    // g of all four, then two blocks of G and two of G^T.
+    auto quad = [&](auto has_target, int j, int i) {
+      uint32_t x[2][2][PARTS][2];                         // [row tile][column tile][part][pairs of columns]
 #pragma unroll
-      for (int i = 0; i < tn; ++i) {
-        const int nt = nt0 + i;
-        if (nt >= p.tw) continue;
-        float g[4];
+      for (int jj = 0; jj < 2; ++jj)
 #pragma unroll
-        for (int q = 0; q < 4; ++q) {
-          const float e = shifted_exp<PARTS>(acc[i][j][q] * undo, lse);
-          g[q] = rho * (target == 16 * i + q ? e - 1.0f : e);
+        for (int ii = 0; ii < 2; ++ii) {
+          const float lse = meta[j + jj].lse, rho = meta[j + jj].rho;
+          const int target = meta[j + jj].target - p.v0 - nt0 * 16 - 4 * lg;
+          float g[4];
+#pragma unroll
+          for (int q = 0; q < 4; ++q) {
+            float e = shifted_exp<PARTS>(acc[i + ii][j + jj][q] * undo, lse);
+            if constexpr (decltype(has_target)::value) e = target == 16 * (i + ii) + q ? e - 1.0f : e;
+            g[q] = rho * e;
+          }
+          if (!whole) {
+#pragma unroll
+            for (int q = 0; q < 4; ++q) g[q] = 16 * (i + ii) + q < left ? g[q] : 0.0f;
+          }
+          if constexpr (PARTS == 1) {
+            x[jj][ii][0][0] = bf16_pair(g[0], g[1]), x[jj][ii][0][1] = bf16_pair(g[2], g[3]);
+          } else {
+            uint16_t hi[4], lo[4];
+#pragma unroll
+            for (int q = 0; q < 4; ++q) split_rn(g[q] * kScaleG, hi[q], lo[q]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+              x[jj][ii][0][h] = hi[2 * h] | uint32_t(hi[2 * h + 1]) << 16;
+              x[jj][ii][PARTS - 1][h] = lo[2 * h] | uint32_t(lo[2 * h + 1]) << 16;
+            }
+          }
         }
-        if (!whole) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) g[q] = 16 * i + q < left ? g[q] : 0.0f;
-        }
-        // G: row lr of its tile, columns 4 lg .. of 16.  GT: row 4 lg + (lr & 3), columns 4 (lr / 4) .. .
-        uint16_t* G = p.G + (int64_t(rt) * PARTS * GC + nt / 2) * kBlk +
-                      (16 * (2 * (nt & 1) + (lg >> 1)) + lr) * 8 + 4 * (lg & 1);
-        uint16_t* GT = p.GT + (int64_t(nt) * PARTS * TC + rt / 2) * kBlk +
-                       (16 * (2 * (rt & 1) + (lr >> 3)) + 4 * lg + (lr & 3)) * 8 + 4 * ((lr >> 2) & 1);
-        if constexpr (PARTS == 1) {
-          const uint32_t x = bf16_pair(g[0], g[1]), y = bf16_pair(g[2], g[3]);
-          *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
-          *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
-        } else {
-          uint16_t hi[4], lo[4];
+      for (int part = 0; part < PARTS; ++part) {
 #pragma unroll
-          for (int q = 0; q < 4; ++q) split_rn(g[q] * kScaleG, hi[q], lo[q]);
-          const uint32_t x = hi[0] | uint32_t(hi[1]) << 16, y = hi[2] | uint32_t(hi[3]) << 16;
-          const uint32_t z = lo[0] | uint32_t(lo[1]) << 16, u = lo[2] | uint32_t(lo[3]) << 16;
-          *reinterpret_cast<uint2*>(G) = make_uint2(x, y);
-          *reinterpret_cast<uint2*>(G + int64_t(GC) * kBlk) = make_uint2(z, u);
-          *reinterpret_cast<uint2*>(GT) = transpose4(x, y, lane);
-          *reinterpret_cast<uint2*>(GT + int64_t(TC) * kBlk) = transpose4(z, u, lane);
+        for (int jj = 0; jj < 2; ++jj) {
+          // G: a lane has columns 4 lg .. + 3 of two tiles; with the neighbouring
+          // group's (rows of 16 lanes trade places) it has 8 of one: the block's
+          // word of lane (lr, 2 (lg & 1) + lg / 2).
+          const auto s0 = __builtin_amdgcn_permlane16_swap(x[jj][0][part][0], x[jj][1][part][0], false, false);
+          const auto s1 = __builtin_amdgcn_permlane16_swap(x[jj][0][part][1], x[jj][1][part][1], false, false);
+          uint16_t* G = p.G + ((int64_t(mt0 + j + jj) * PARTS + part) * GC + (nt0 + i) / 2) * kBlk +
+                        (16 * (2 * (lg & 1) + (lg >> 1)) + lr) * 8;
+          *reinterpret_cast<uint4*>(G) = make_uint4(s0[0], s1[0], s0[1], s1[1]);
         }
+#pragma unroll
+        for (int ii = 0; ii < 2; ++ii) {
+          // G^T: transposed, a lane has rows 4 (lr / 4) .. + 3 of column 4 lg +
+          // lr % 4 of two row tiles; with those of lane lr ^ 4 it has 8 of one.
+          const uint2 t0 = transpose4(x[0][ii][part][0], x[0][ii][part][1], lane);
+          const uint2 t1 = transpose4(x[1][ii][part][0], x[1][ii][part][1], lane);
+          const uint4 t = join_eight(t0, t1, lane);
+          uint16_t* GT = p.GT + ((int64_t(nt0 + i + ii) * PARTS + part) * TC + (mt0 + j) / 2) * kBlk +
+                         (16 * (2 * ((lr >> 2) & 1) + (lr >> 3)) + 4 * lg + (lr & 3)) * 8;
+          *reinterpret_cast<uint4*>(GT) = t;
+        }
+      }
+    };
+#pragma unroll
+    for (int j = 0; j < tm; j += 2) {
+      if (mt0 + j >= p.ta) continue;                      // wave-uniform; the tiles come in fours
+      const int t0 = meta[j].target - p.v0 - nt0 * 16, t1 = meta[j + 1].target - p.v0 - nt0 * 16;
+      const bool hit = (t0 >= 0 && t0 < 16 * tn) || (t1 >= 0 && t1 < 16 * tn);
+      if (__any(hit)) {                                   // few tiles of a large vocabulary
+#pragma unroll
+        for (int i = 0; i < tn; i += 2)
+          if (nt0 + i < p.tw) quad(std::true_type{}, j, i);
+      } else {
+#pragma unroll
+        for (int i = 0; i < tn; i += 2)
+          if (nt0 + i < p.tw) quad(std::false_type{}, j, i);
       }
     }
   } else if constexpr (kEpi == kOut) {
-    const float s = out_scale(p, PARTS);
+    float s = out_scale(p, PARTS);
+    asm volatile("" : "+v"(s));                           // arrived, as above
 #pragma unroll
     for (int i = 0; i < tn; ++i)
 #pragma unroll
@@ -670,6 +721,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
   constexpr int FW = TN / 4, FA = TM / 4, DPW = FW + FA;   // blocks of W and of A that a wave fetches
   constexpr int BUF = (TN + TM) * kBlk;                 // one stage, in halves
   constexpr int kFrags = tn + tm;
+  // Stores of a whole tile's epilogue that the first two stages of the next item
+  // need not wait for (with three buffers they are younger than what those need).
+  constexpr int kStores = kEpi == kGrad && kBufs == 3 ? tn * tm : 0;
+  static_assert((kBufs - 2) * DPW + kStores < 64, "the counter has six bits");
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
   uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
   const int per_xcd = (p.items + kXcd - 1) / kXcd;
@@ -722,17 +777,22 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
 #pragma unroll
   for (int k = 0; k < kFrags; ++k) read(0, 0, k);
   int buf = 0;
+  bool stored = false;
   for (;;) {
     f32x4 acc[tn][tm];
 #pragma unroll
     for (int i = 0; i < tn; ++i)
 #pragma unroll
       for (int j = 0; j < tm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    auto stage = [&](auto set) {
+    auto stage = [&](auto set, bool after_stores) {
       constexpr int half = decltype(set)::value;
-      // The next stage has landed (those behind it may be out), and every wave
-      // holds this one's fragments, so its buffer is free.
-      wait_vmem_but<(kBufs - 2) * DPW>();
+      // The next stage has landed (those behind it may be out, and at the start
+      // of an item the stores of the one before), and every wave holds this
+      // one's fragments, so its buffer is free.
+      if (kStores > 0 && after_stores)
+        wait_vmem_but<(kBufs - 2) * DPW + kStores>();
+      else
+        wait_vmem_but<(kBufs - 2) * DPW>();
       __syncthreads();
       const int here = buf, next = buf == kBufs - 1 ? 0 : buf + 1;
       // Groups of four MFMAs, all but the last ones (LDS reads take time) with
@@ -757,8 +817,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
     constexpr std::integral_constant<int, 0> even;
     constexpr std::integral_constant<int, 1> odd;
     for (int c = w.s0; c < w.s1 - 2; ++c) {
-      stage(even);
-      stage(odd);
+      stage(even, stored);
+      stage(odd, stored);
+      stored = false;
     }
     const int mt0 = w.mt * TM + wm * tm, nt0 = w.nt * TN + wn * tn, split = w.split;
     item += stride;
@@ -766,12 +827,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
     if (more) w = item_at(p, item);
     static_assert(kBufs == 3 || kBufs == 4, "the last kBufs stages fetch from the next item");
     if constexpr (kBufs == 4) aim(w);
-    stage(even);
+    stage(even, false);
     if constexpr (kBufs == 3) aim(w);
-    stage(odd);
-    stage(even);
-    stage(odd);
+    stage(odd, false);
+    stage(even, false);
+    stage(odd, false);
     ce_epilogue<T, 1, kEpi, TN, TM, tn, tm>(acc, mt0, nt0, split, wave, lane);
+    stored = mt0 + tm <= p.ta && nt0 + tn <= p.tw;      // every store was issued
     if (!more) break;
   }
   wait_vmem();                                          // the last fetches, before the LDS is another block's
