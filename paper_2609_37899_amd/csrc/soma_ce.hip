@@ -159,6 +159,7 @@ struct PackArgs {
   const float* maxima;       // [3][kMaxima] or NULL: scale 1, c 1
   int which;                 // the scale to use: 0 f, 1 E
   int nmax;                  // partial maxima in use, a multiple of 4
+  int eight;                 // x allows loads of four values at any multiple of four
   Scales* scales;            // f: written by block (0, 0)
   RowMeta* meta;             // f: rows' constants, or NULL
   const float *lse, *w;
@@ -176,26 +177,49 @@ __device__ __forceinline__ uint4 pack8(const uint16_t (&h)[8]) {
                     h[6] | uint32_t(h[7]) << 16);
 }
 
-template <class T, int PARTS>
-__device__ __forceinline__ void store_fragment(uint16_t* dst, int64_t part_step, const float (&v)[8], float scale) {
+// Eight values as a word of 8 halves of each part.
+template <int PARTS>
+__device__ __forceinline__ void fragment_words(const float (&v)[8], float scale, uint4 (&w)[PARTS]) {
   if constexpr (PARTS == 1) {
-    *reinterpret_cast<uint4*>(dst) =
-        make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
+    w[0] = make_uint4(bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7]));
   } else {
     uint16_t hi[8], lo[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) split_rn(v[i] * scale, hi[i], lo[i]);
-    *reinterpret_cast<uint4*>(dst) = pack8(hi);
-    *reinterpret_cast<uint4*>(dst + part_step) = pack8(lo);
+    w[0] = pack8(hi);
+    w[PARTS - 1] = pack8(lo);
   }
 }
 
+// A wave takes a row tile (16 rows) of the block's 64 columns: a lane's eight
+// values are a word of the fragment as they come from memory.  For the transpose
+// the words go through LDS, where a lane picks eight rows of its column.
 template <class T, int PARTS>
 __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
-  __shared__ float tile[64][65];
+  constexpr int kRow = 64 + 8;               // halves: 16-byte rows, columns of 8 rows on different banks
+  __shared__ __attribute__((aligned(16))) uint16_t tile[PARTS][64][kRow];
   __shared__ float red[4];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+  const T* x = static_cast<const T*>(a.x);
+  const int row = r0 + wave * 16 + lr;
+  float v[2][8] = {};
+  if (row < a.n && (!a.targets || a.targets[row] >= 0)) {
+    const T* p = x + row * a.stride + k0 + 8 * lg;
+#pragma unroll
+    for (int kc = 0; kc < 2; ++kc) {
+      const int left = a.K - (k0 + 32 * kc + 8 * lg);
+      if (a.eight && left >= 8) {
+        const float4 lo = load_four(p + 32 * kc), hi = load_four(p + 32 * kc + 4);
+        v[kc][0] = lo.x, v[kc][1] = lo.y, v[kc][2] = lo.z, v[kc][3] = lo.w;
+        v[kc][4] = hi.x, v[kc][5] = hi.y, v[kc][6] = hi.z, v[kc][7] = hi.w;
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (j < left) v[kc][j] = load_value(p + 32 * kc + j);
+      }
+    }
+  }
   float scale = 1.0f, c = 1.0f;
   if (a.maxima) {
     if constexpr (PARTS == 2) {
@@ -224,35 +248,30 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
     }
     a.meta[r] = m;
   }
-  const T* x = static_cast<const T*>(a.x);
-#pragma unroll 4
-  for (int i = 0; i < 16; ++i) {
-    const int r = r0 + wave * 16 + i, k = k0 + lane;
-    float v = 0.0f;
-    if (r < a.n && k < a.K && (!a.targets || a.targets[r] >= 0)) v = load_value(x + r * a.stride + k);
-    tile[wave * 16 + i][lane] = v;
+#pragma unroll
+  for (int kc = 0; kc < 2; ++kc) {
+    uint4 w[PARTS];
+    fragment_words<PARTS>(v[kc], scale, w);
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+      if (a.frag)
+        *reinterpret_cast<uint4*>(a.frag + ((int64_t(r0 / 16 + wave) * PARTS + part) * (a.Kp / 32) + k0 / 32 + kc) * kBlk +
+                                  lane * 8) = w[part];
+      if (a.fragT) *reinterpret_cast<uint4*>(&tile[part][wave * 16 + lr][kc * 32 + 8 * lg]) = w[part];
+    }
   }
+  if (!a.fragT) return;                      // block-uniform
   __syncthreads();
-  const int lr = lane & 15, lg = lane >> 4;
 #pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int b = wave * 2 + i, rt = b >> 1, kc = b & 1;      // 4 row tiles x 2 chunks
-    float v[8];
-    if (a.frag) {
+  for (int rc = 0; rc < 2; ++rc)
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = tile[rt * 16 + lr][kc * 32 + 8 * lg + j];
-      const int64_t KC = a.Kp / 32;
-      store_fragment<T, PARTS>(a.frag + ((int64_t(r0 / 16 + rt) * PARTS) * KC + (k0 / 32 + kc)) * kBlk + lane * 8,
-                               KC * kBlk, v, scale);
+    for (int part = 0; part < PARTS; ++part) {
+      uint16_t h[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) h[j] = tile[part][rc * 32 + 8 * lg + j][wave * 16 + lr];
+      *reinterpret_cast<uint4*>(a.fragT + ((int64_t(k0 / 16 + wave) * PARTS + part) * (a.np / 32) + r0 / 32 + rc) * kBlk +
+                                lane * 8) = pack8(h);
     }
-    if (a.fragT) {
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] = tile[kc * 32 + 8 * lg + j][rt * 16 + lr];
-      const int64_t RC = a.np / 32;
-      store_fragment<T, PARTS>(a.fragT + ((int64_t(k0 / 16 + rt) * PARTS) * RC + (r0 / 32 + kc)) * kBlk + lane * 8,
-                               RC * kBlk, v, scale);
-    }
-  }
 }
 
 // ---------------------------------------------------------------------------
@@ -874,7 +893,7 @@ struct RowsArgs {
   float* hit;
 };
 
-constexpr int kRowsWaves = 8;
+constexpr int kRowsWaves = 16;
 
 template <class T>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
@@ -887,6 +906,26 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int chunks = (a.K + kChunk - 1) / kChunk;
   const T* f = static_cast<const T*>(a.f);
+  const int full = a.K / kChunk;                        // chunks without a tail
+  const T* E = static_cast<const T*>(a.E);
+  // The block's tiles: a contiguous share, so that every compute unit gets the
+  // same number but for one.
+  const int tiles = (a.V + 15) / 16;
+  const int last = static_cast<int>(int64_t(tiles) * (blockIdx.x + 1) / gridDim.x);
+  int t = static_cast<int>(int64_t(tiles) * blockIdx.x / gridDim.x) + wave;
+  // rows past the end repeat the last and are masked below
+  auto row_of = [&](int tile) { return E + min(tile * 16 + lr, a.V - 1) * a.e_stride + lg * kW; };
+  // Two batches of eight loads: one is multiplied while the other is on its way,
+  // the next tile's first behind the last of this one, the first of all before f
+  // is brought to LDS.
+  auto load = [&](uint4 (&x)[8], const T* e, int c) {
+#pragma unroll
+    for (int u = 0; u < 8; ++u)
+      if (c + u < full) x[u] = *reinterpret_cast<const uint4*>(e + (c + u) * kChunk);
+  };
+  uint4 x0[8], x1[8];
+  const T* e = row_of(t);
+  if (t < last) load(x0, e, 0);
   for (int c = wave; c < chunks; c += kRowsWaves)
 #pragma unroll
     for (int j = 0; j < kW; ++j) {
@@ -898,37 +937,31 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
   __syncthreads();
   const int target = lr < a.R ? a.targets[lr] : -1;
   float top = kLowest, sum = 0.0f;
-  const int tiles = (a.V + 15) / 16;
-  const int full = a.K / kChunk;                        // chunks without a tail
-  const T* E = static_cast<const T*>(a.E);
-  for (int t = blockIdx.x * kRowsWaves + wave; t < tiles; t += gridDim.x * kRowsWaves) {
-    const int row = min(t * 16 + lr, a.V - 1);          // rows past the end repeat the last and are masked below
-    const T* e = E + row * a.e_stride + lg * kW;
+  for (; t < last; t += kRowsWaves) {
     f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
-    auto step = [&](const uint4& x, int c) {
+    auto step = [&](const uint4& x, int c, bool odd) {
       const uint4 y = *reinterpret_cast<const uint4*>(fl + (c * 64 + lane) * kW);
-      if constexpr (kB) {
-        if (c & 1)
-          acc2 = mma<1>(x, y, acc2);
-        else
-          acc = mma<1>(x, y, acc);
-      } else {
-        const float4 xf = __builtin_bit_cast(float4, x), yf = __builtin_bit_cast(float4, y);
-        if (c & 1)
-          acc2 = mfma_k16(xf, yf, acc2);
-        else
-          acc = mfma_k16(xf, yf, acc);
-      }
+      f32x4& to = odd ? acc2 : acc;
+      if constexpr (kB)
+        to = mma<1>(x, y, to);
+      else
+        to = mfma_k16(__builtin_bit_cast(float4, x), __builtin_bit_cast(float4, y), to);
     };
-    int c = 0;
-    for (; c + 8 <= full; c += 8) {
-      uint4 x[8];
+    const T* ahead = row_of(t + kRowsWaves);
+    for (int c = 0; c < full; c += 16) {
+      load(x1, e, c + 8);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) x[u] = *reinterpret_cast<const uint4*>(e + (c + u) * kChunk);
+      for (int u = 0; u < 8; ++u)
+        if (c + u < full) step(x0[u], c + u, u & 1);
+      if (c + 16 < full)
+        load(x0, e, c + 16);
+      else if (t + kRowsWaves < last)
+        load(x0, ahead, 0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u) step(x[u], c + u);
+      for (int u = 0; u < 8; ++u)
+        if (c + 8 + u < full) step(x1[u], c + 8 + u, u & 1);
     }
-    for (; c < full; ++c) step(*reinterpret_cast<const uint4*>(e + c * kChunk), c);
+    int c = full;
     if (c < chunks) {                                   // the tail, column by column
       T tail[kW];
 #pragma unroll
@@ -938,8 +971,9 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
       }
       uint4 x;
       __builtin_memcpy(&x, tail, 16);
-      step(x, c);
+      step(x, c, false);
     }
+    e = ahead;
     // acc[q] = logit of row lr, vocabulary row 16 t + 4 lg + q
     float l[4], most = top;
 #pragma unroll
@@ -1018,7 +1052,7 @@ __global__ __launch_bounds__(256) void k_ce_zero(uint16_t* x, int64_t halves) {
 // Host
 // ---------------------------------------------------------------------------
 constexpr int64_t kFill = 256;            // tiles that fill the card
-constexpr int kRowsBlocks = 512;          // blocks of k_ce_rows
+constexpr int kRowsBlocks = 256;          // blocks of k_ce_rows
 constexpr size_t kRowsLds = 65536;        // f's rows in LDS
 
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
@@ -1195,7 +1229,8 @@ int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipSt
 }
 
 template <class T, int PARTS>
-int launch_pack(const PackArgs& a, hipStream_t st) {
+int launch_pack(PackArgs& a, hipStream_t st) {
+  a.eight = is_aligned(a.x, 4 * sizeof(T)) && a.stride % 4 == 0;
   hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(unsigned(a.np / 64), unsigned(a.Kp / 64)), dim3(256), 0, st, a);
   return launched("k_ce_pack");
 }
