@@ -153,7 +153,7 @@ struct PackArgs {
   const void* x;
   int64_t stride;
   int n, K;                  // rows, columns
-  int np, Kp;                // padded to 64
+  int np, Kp;                // padded to 128
   const int32_t* targets;    // f only: rows with a negative target are zeros
   uint16_t *frag, *fragT;    // [np / 16][parts][Kp / 32], [Kp / 16][parts][np / 32] blocks; or NULL
   const float* maxima;       // [3][kMaxima] or NULL: scale 1, c 1
@@ -276,17 +276,8 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
 
 // ---------------------------------------------------------------------------
 // Products: C[m][n] = sum_k A[m][k] W[n][k], both in fragment order.
-//
-// 16 TM x 16 TN per block; a stage brings two blocks of every row tile to LDS
-// (two chunks of 32 columns, or hi and lo of one), the next stage's are in
-// flight under its products.  256 x 256 with 8 waves: 64 KiB of DMA for 1,024
-// (bf16) or 1,536 (split) clocks of MFMA on each SIMD, one block per compute unit that
-// works through its items one after another.  128 x 128 with 4 waves, two
-// blocks a compute unit, where 256 x 256 leaves compute units idle.  An item is
-// a tile, or one of `splits` shares of a tile's stages.  Each XCD (blocks go
-// round-robin) works through a contiguous range of items, 8 n tiles wide at a
-// time, so that the tiles in flight share operands in its L2.
 // ---------------------------------------------------------------------------
+
 // Rows of eight from fours: lanes lr of which (lr & 4) == 0 receive their own a and
 // lane lr ^ 4's, the others lane lr ^ 4's b and their own.
 __device__ __forceinline__ uint4 join_eight(const uint2& a, const uint2& b, int lane) {
@@ -316,7 +307,7 @@ struct CeMmArgs {
   int ta, tw;                // row tiles of 16 in A and W
   int KC;                    // chunks of 32 columns
   int ntm, ntn, splits;
-  int stages;                // of a row tile: 64 columns (bf16), 32 (split)
+  int stages;                // pairs of a row tile's: 64 columns each
   int items;
   Divider by_tiles, by_band, by_rest, by_splits;   // ntm ntn, 8 ntm, ntn % 8, splits
   const Scales* scales;      // NULL: all 1
@@ -592,158 +583,40 @@ __device__ __forceinline__ void ce_epilogue(f32x4 (&acc)[tn][tm], int mt0, int n
   }
 }
 
-// Fetching stages of row tiles into LDS, in the order in which the block's items
-// use them and across their borders.  A wave moves DPW blocks of every stage:
-// halves (two chunks, or hi and lo) of DPW / 2 row tiles of W or of A.
-template <int PARTS, int TN, int TM, int DPW>
-struct CeFetch {
-  static constexpr int kBuf = 2 * (TN + TM) * kBlk;     // one stage, in halves
-  static constexpr int kStep = PARTS == 1 ? 2 : 1;      // chunks of a stage
-  const CeMmArgs& p;
-  i32x4 rs;
-  uint32_t soff[DPW];                                   // scalars: vector registers are dear
-  uint32_t voff, dst;
-  int wave, item, stride, last, c, end;
-  bool more = true;
-
-  __device__ __forceinline__ CeFetch(const CeMmArgs& p_, const uint16_t* lds, int wave_, int lane, int item_, int stride_,
-                                     int last_)
-      : p(p_), voff(lane * 16), dst(lds_address(lds + wave_ * DPW * kBlk)), wave(wave_), item(item_), stride(stride_),
-        last(last_) {
-    aim();
-  }
-  __device__ __forceinline__ void aim() {
-    // Row tiles past the matrix repeat its last: nothing of theirs is used.
-    constexpr int per = DPW / 2;                        // row tiles of a wave
-    const CeItem w = item_at(p, item);
-    const bool weights = wave * per < TN;
-    const int t0 = weights ? w.nt * TN : w.mt * TM;
-    const int have = min(weights ? TN : TM, (weights ? p.tw : p.ta) - t0);
-    const uint16_t* base = (weights ? p.W : p.A) + int64_t(t0) * PARTS * p.KC * kBlk;
-    rs = buffer_words(base, static_cast<uint32_t>(have) * PARTS * p.KC * (kBlk * 2));
-    const int mine = wave * per - (weights ? 0 : TN);
-    c = w.s0, end = w.s1;
-#pragma unroll
-    for (int i = 0; i < DPW; ++i) {
-      const int tile = min(mine + (i >> 1), have - 1);
-      const int block = PARTS == 1 ? tile * p.KC + c * kStep + (i & 1) : (tile * 2 + (i & 1)) * p.KC + c;
-      soff[i] = static_cast<uint32_t>(block) * (kBlk * 2);
-    }
-  }
-  // The next stage, if there is one, into LDS buffer `buf`.
-  __device__ __forceinline__ void issue(int buf) {
-    if (!more) return;
-#pragma unroll
-    for (int i = 0; i < DPW; ++i) {
-      dma16(rs, voff, soff[i], dst + static_cast<uint32_t>((buf * kBuf + i * kBlk) * 2));
-      soff[i] += kStep * kBlk * 2;
-    }
-    if (++c == end) {
-      item += stride;
-      more = item < last;
-      if (more) aim();
-    }
-  }
-};
-
-// kBufs LDS buffers: kBufs - 1 stages are on their way or landed ahead.
-template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int WM, int kBufs>
-__global__ __launch_bounds__(64 * WN * WM) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_ce_mm(CeMmArgs p) {
-  constexpr int NW = WN * WM, tn = TN / WN, tm = TM / WM;
-  constexpr int DPW = 2 * (TN + TM) / NW;               // blocks a wave moves per stage
-  static_assert(DPW * NW == 2 * (TN + TM) && DPW % 2 == 0 && TN % (DPW / 2) == 0, "whole row tiles per wave");
-  typedef CeFetch<PARTS, TN, TM, DPW> Fetch;
-  constexpr int BUF = Fetch::kBuf;
-  extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
-  uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
-  const int per_xcd = (p.items + kXcd - 1) / kXcd;
-  const int first = (blockIdx.x % kXcd) * per_xcd;
-  const int last = min(first + per_xcd, p.items);
-  const int stride = gridDim.x / kXcd;
-  int item = first + blockIdx.x / kXcd;
-  if (item >= last) return;                             // block-uniform
-  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int lane = threadIdx.x & 63;
-  const int wn = wave % WN, wm = wave / WN;
-  Fetch fetch(p, lds, wave, lane, item, stride, last);
-  const uint16_t* const wl0 = lds + wn * tn * 2 * kBlk + lane * 8;
-  const uint16_t* const al0 = lds + (TN + wm * tm) * 2 * kBlk + lane * 8;
-#pragma unroll
-  for (int i = 0; i < kBufs - 1; ++i) fetch.issue(i);
-  int buf = 0;
-  for (;;) {
-    const CeItem w = item_at(p, item);
-    f32x4 acc[tn][tm];
-#pragma unroll
-    for (int i = 0; i < tn; ++i)
-#pragma unroll
-      for (int j = 0; j < tm; ++j) acc[i][j] = f32x4{0.f, 0.f, 0.f, 0.f};
-    for (int c = w.s0; c < w.s1; ++c) {
-      // The stage has landed (while there is one to fetch, kBufs - 2 later ones
-      // may be out), and every wave is done with the buffer of the one before.
-      if (fetch.more)
-        wait_vmem_but<(kBufs - 2) * DPW>();
-      else
-        wait_vmem();
-      __syncthreads();
-      fetch.issue(buf == 0 ? kBufs - 1 : buf - 1);
-      uint4 b0[tm], b1[tm];
-#pragma unroll
-      for (int j = 0; j < tm; ++j) {
-        b0[j] = *reinterpret_cast<const uint4*>(al0 + buf * BUF + 2 * j * kBlk);
-        b1[j] = *reinterpret_cast<const uint4*>(al0 + buf * BUF + (2 * j + 1) * kBlk);
-      }
-#pragma unroll
-      for (int i = 0; i < tn; ++i) {
-        const uint4 w0 = *reinterpret_cast<const uint4*>(wl0 + buf * BUF + 2 * i * kBlk);
-        const uint4 w1 = *reinterpret_cast<const uint4*>(wl0 + buf * BUF + (2 * i + 1) * kBlk);
-        if constexpr (PARTS == 1) {
-#pragma unroll
-          for (int j = 0; j < tm; ++j) acc[i][j] = mma<1>(w0, b0[j], acc[i][j]);
-#pragma unroll
-          for (int j = 0; j < tm; ++j) acc[i][j] = mma<1>(w1, b1[j], acc[i][j]);
-        } else {                                        // hi in 0, lo in 1
-#pragma unroll
-          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w1, b0[j], acc[i][j]);
-#pragma unroll
-          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w0, b1[j], acc[i][j]);
-#pragma unroll
-          for (int j = 0; j < tm; ++j) acc[i][j] = mma<2>(w0, b0[j], acc[i][j]);
-        }
-      }
-      buf = buf == kBufs - 1 ? 0 : buf + 1;
-    }
-    ce_epilogue<T, PARTS, kEpi, TN, TM, tn, tm>(acc, w.mt * TM + wm * tm, w.nt * TN + wn * tn, w.split, wave, lane);
-    item += stride;
-    if (item >= last) break;
-  }
-}
-
-// bf16 with 4 waves a block.
-//  * 256 x 256, 128 x 128 a wave, one wave on each SIMD (the products with G).
-//    With 8 waves of 128 x 64 the LDS moves 256 KiB for 64 columns (192 read, 64
-//    written by DMA), 2,048 clocks, as long as their MFMAs take; with 128 x 128
-//    per wave 192 KiB.  Four LDS buffers.
-//  * 256 rows x 128 vocabulary rows, 64 x 128 a wave, two blocks a compute unit
-//    (the logits): what becomes of a tile, exponentials and stores, takes half as
-//    long as its MFMAs, and runs beside the other block's.  Three buffers.
-// A stage is one chunk of 32 columns.  Everything is ahead of time: its DMA is
-// issued as many stages before as there are buffers, its fragments are read into
-// registers under the MFMAs of the stage before (the second of two register sets;
-// stages come in pairs), and both are dealt out between the MFMAs.  A stage has no
-// branch: while an item's last stages run, the next item's first are fetched
+// Blocks of 4 waves work through items: a tile, or one of `splits` shares of a
+// tile's columns.  Each XCD (blocks go round-robin) works through a contiguous
+// range of items, 8 n tiles wide at a time, so that the tiles in flight share
+// operands in its L2.  Tiles (rows of A x rows of W; 4 waves share it WN ways over
+// the rows of W):
+//   bf16, products with G   256 x 256, 128 x 128 a wave, one wave on each SIMD.
+//     8 waves of 128 x 64 would move 256 KiB through the LDS for 64 columns (192
+//     read, 64 written by DMA), 2,048 clocks, as long as their MFMAs take;
+//     128 x 128 a wave moves 192 KiB.
+//   bf16, logits            256 x 128, 64 x 128 a wave, two blocks a compute unit:
+//     what becomes of a tile (exponentials, stores) runs beside the other block's
+//     MFMAs.
+//   split                   256 x 128, one block a compute unit (three products
+//     for twice the bytes).
+//   few tiles               128 x 128.
+// A stage is one chunk of 32 columns (of both parts).  One or two waves a SIMD
+// have little to hide behind, so everything is ahead of time: a stage's DMA is
+// issued as many stages before as there are LDS buffers, its fragments are read
+// into registers under the MFMAs of the stage before (the second of two register
+// sets; stages come in pairs), and both are dealt out between the MFMAs.  A stage
+// has no branch: while an item's last stages run, the next item's first are fetched
 // (behind the last item its own first again, which nobody reads).  An item has
-// four stages at least.
-template <class T, int kEpi, int TN, int WN, int kBufs, int kPerEu>
-__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPerEu))) void k_ce_mm_wide(CeMmArgs p) {
-  constexpr int TM = 16, WM = 4 / WN, tn = TN / WN, tm = TM / WM;
-  constexpr int FW = TN / 4, FA = TM / 4, DPW = FW + FA;   // blocks of W and of A that a wave fetches
-  constexpr int BUF = (TN + TM) * kBlk;                 // one stage, in halves
-  constexpr int kFrags = tn + tm;
+// four stages at least: every matrix is padded to 128 columns.
+template <class T, int PARTS, int kEpi, int TN, int TM, int WN, int kBufs, int kPerEu>
+__global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPerEu))) void k_ce_mm(CeMmArgs p) {
+  constexpr int WM = 4 / WN, tn = TN / WN, tm = TM / WM;
+  constexpr int FW = PARTS * TN / 4, FA = PARTS * TM / 4, DPW = FW + FA;   // blocks of W and of A that a wave fetches
+  constexpr int BUF = PARTS * (TN + TM) * kBlk;         // one stage, in halves
+  constexpr int kFrags = PARTS * (tn + tm);
+  constexpr int kPasses = PARTS == 1 ? 1 : 3;           // products of parts
   // Stores of a whole tile's epilogue that the first two stages of the next item
-  // need not wait for (with three buffers they are younger than what those need).
-  constexpr int kStores = kEpi == kGrad && kBufs == 3 ? tn * tm : 0;
-  static_assert((kBufs - 2) * DPW + kStores < 64, "the counter has six bits");
+  // need not wait for: they are younger than what those need.
+  constexpr int kAll = kEpi == kGrad ? PARTS * tn * tm : 0;
+  constexpr int kStores = (kBufs - 2) * DPW + kAll < 64 ? kAll : 0;        // the counter has six bits
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
   uint16_t* const lds = reinterpret_cast<uint16_t*>(ce_lds);
   const int per_xcd = (p.items + kXcd - 1) / kXcd;
@@ -758,16 +631,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
   i32x4 rw, ra;
   uint32_t soff[DPW];                                   // scalars: no vector registers are to spare
   const uint32_t voff = lane * 16;
-  const uint32_t dw = lds_address(lds + wave * FW * kBlk), da = lds_address(lds + (TN + wave * FA) * kBlk);
+  const uint32_t dw = lds_address(lds + wave * FW * kBlk), da = lds_address(lds + (PARTS * TN + wave * FA) * kBlk);
   auto aim = [&](const CeItem& w) {
     // Row tiles past the matrix repeat its last: nothing of theirs is used.
     const int hw = min(TN, p.tw - w.nt * TN), ha = min(TM, p.ta - w.mt * TM);
-    rw = buffer_words(p.W + int64_t(w.nt) * TN * p.KC * kBlk, static_cast<uint32_t>(hw) * p.KC * (kBlk * 2));
-    ra = buffer_words(p.A + int64_t(w.mt) * TM * p.KC * kBlk, static_cast<uint32_t>(ha) * p.KC * (kBlk * 2));
+    const int row = PARTS * p.KC;                       // blocks of a row tile
+    rw = buffer_words(p.W + int64_t(w.nt) * TN * row * kBlk, static_cast<uint32_t>(hw) * row * (kBlk * 2));
+    ra = buffer_words(p.A + int64_t(w.mt) * TM * row * kBlk, static_cast<uint32_t>(ha) * row * (kBlk * 2));
 #pragma unroll
-    for (int i = 0; i < DPW; ++i)
-      soff[i] = static_cast<uint32_t>((i < FW ? min(wave * FW + i, hw - 1) : min(wave * FA + i - FW, ha - 1)) * p.KC +
-                                      2 * w.s0) * (kBlk * 2);
+    for (int i = 0; i < DPW; ++i) {
+      const int b = i < FW ? wave * FW + i : wave * FA + i - FW;           // [tile][part]
+      const int tile = min(b / PARTS, (i < FW ? hw : ha) - 1);
+      soff[i] = static_cast<uint32_t>(tile * row + (b % PARTS) * p.KC + 2 * w.s0) * (kBlk * 2);
+    }
   };
   auto fetch = [&](int i, int buf) {
     if (i < FW)
@@ -776,14 +652,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
       dma16(ra, voff, soff[i], da + static_cast<uint32_t>((buf * BUF + (i - FW) * kBlk) * 2));
     soff[i] += kBlk * 2;
   };
-  const uint16_t* const wl = lds + wn * tn * kBlk + lane * 8;
-  const uint16_t* const al = lds + (TN + wm * tm) * kBlk + lane * 8;
-  uint4 fw[2][tn], fa[2][tm];
+  const uint16_t* const wl = lds + wn * tn * PARTS * kBlk + lane * 8;
+  const uint16_t* const al = lds + (TN + wm * tm) * PARTS * kBlk + lane * 8;
+  uint4 fw[2][tn * PARTS], fa[2][tm * PARTS];           // [set][tile, part]
   auto read = [&](int set, int buf, int k) {            // fragment k: A's first, all of which the first MFMAs need
-    if (k < tm)
+    if (k < tm * PARTS)
       fa[set][k] = *reinterpret_cast<const uint4*>(al + buf * BUF + k * kBlk);
     else
-      fw[set][k - tm] = *reinterpret_cast<const uint4*>(wl + buf * BUF + (k - tm) * kBlk);
+      fw[set][k - tm * PARTS] = *reinterpret_cast<const uint4*>(wl + buf * BUF + (k - tm * PARTS) * kBlk);
   };
   CeItem w = item_at(p, item);
   aim(w);
@@ -816,7 +692,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
       const int here = buf, next = buf == kBufs - 1 ? 0 : buf + 1;
       // Groups of four MFMAs, all but the last ones (LDS reads take time) with
       // their share of the DMAs and of the next stage's fragments.
-      constexpr int kGroups = tn * tm / 4, kLoaded = kGroups - kGroups / 4;
+      constexpr int kGroups = kPasses * tn * tm / 4, kLoaded = kGroups - kGroups / 4;
+      static_assert(tm % 4 == 0, "a group is within one row of tiles");
 #pragma unroll
       for (int g = 0; g < kGroups; ++g) {
         __builtin_amdgcn_sched_barrier(0);
@@ -824,10 +701,13 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
         for (int d = DPW * g / kLoaded; d < DPW * (g + 1) / kLoaded && d < DPW; ++d) fetch(d, here);
 #pragma unroll
         for (int k = kFrags * g / kLoaded; k < kFrags * (g + 1) / kLoaded && k < kFrags; ++k) read(half ^ 1, next, k);
+        // lo hi, hi lo, hi hi over a row of tiles
+        const int i = g * 4 / (kPasses * tm), pass = g * 4 / tm % kPasses;
+        const int pw = PARTS == 2 && pass == 0 ? 1 : 0, pa = PARTS == 2 && pass == 1 ? 1 : 0;
 #pragma unroll
         for (int q = 0; q < 4; ++q) {
-          const int i = (g * 4 + q) / tm, j = (g * 4 + q) % tm;
-          acc[i][j] = mma<1>(fw[half][i], fa[half][j], acc[i][j]);
+          const int j = g * 4 % tm + q;
+          acc[i][j] = mma<PARTS>(fw[half][i * PARTS + pw], fa[half][j * PARTS + pa], acc[i][j]);
         }
       }
       __builtin_amdgcn_sched_barrier(0);
@@ -851,7 +731,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(kPerEu, kPe
     stage(odd, false);
     stage(even, false);
     stage(odd, false);
-    ce_epilogue<T, 1, kEpi, TN, TM, tn, tm>(acc, mt0, nt0, split, wave, lane);
+    ce_epilogue<T, PARTS, kEpi, TN, TM, tn, tm>(acc, mt0, nt0, split, wave, lane);
     stored = mt0 + tm <= p.ta && nt0 + tn <= p.tw;      // every store was issued
     if (!more) break;
   }
@@ -1058,20 +938,20 @@ constexpr size_t kRowsLds = 65536;        // f's rows in LDS
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
 struct Sizes {
-  int64_t Rp, Kp, Vp;                     // padded to 64; Vp of the largest piece
+  int64_t Rp, Kp, Vp;                     // padded to 128; Vp of the largest piece
   int parts;
   size_t part, hit, maxima, scales, meta, f, fT, e, eT, G, GT, accf, acce, total;
 };
 
-// Accumulators of a product of m x n outputs over k columns whose stages are
-// shared out: at most max(tiles, 2 kFill) tiles (choose_splits), for either
-// size of tile.
-size_t acc_bytes(int64_t m, int64_t n, int64_t stages) {
+// Accumulators of a product of m x n outputs whose columns are shared out: at
+// most max(tiles, 2 kFill) tiles (choose_splits), of whichever size.
+size_t acc_bytes(int64_t m, int64_t n, int64_t columns) {
   int64_t most = 0;
-  for (int64_t side : {128, 256}) {
-    const int64_t tiles = up(m, side) / side * (up(n, side) / side);
-    most = std::max(most, std::max(tiles, std::min(tiles * stages, 2 * kFill)) * side * side);
-  }
+  for (int tm : {8, 16})
+    for (int tn : {8, 16}) {
+      const int64_t tiles = up(m, 16 * tm) / (16 * tm) * (up(n, 16 * tn) / (16 * tn));
+      most = std::max(most, std::max(tiles, std::min(tiles * (columns / 128), 2 * kFill)) * tm * tn * 256);
+    }
   return size_t(most) * 4;
 }
 
@@ -1081,11 +961,11 @@ int piece_of(const soma_ce_config& c) { return c.rows <= kLongRows ? kLongPiece 
 // workspace for many rows holds a call of fewer.
 Sizes sizes_of(const soma_ce_config& c, bool grad) {
   Sizes s{};
-  s.Rp = up(c.rows, 64);
-  s.Kp = up(c.width, 64);
-  s.Vp = up(std::min<int64_t>(c.vocab, piece_of(c)), 64);
+  s.Rp = up(c.rows, 128);
+  s.Kp = up(c.width, 128);
+  s.Vp = up(std::min<int64_t>(c.vocab, piece_of(c)), 128);
   s.parts = c.type == SOMA_FLOAT ? 2 : 1;
-  const int64_t longest = up(std::min<int64_t>(c.vocab, kLongPiece), 64);
+  const int64_t longest = up(std::min<int64_t>(c.vocab, kLongPiece), 128);
   const int64_t area = std::max(s.Rp * s.Vp, std::min<int64_t>(s.Rp, kLongRows) * longest);
   size_t at = 0;
   auto take = [&](size_t bytes) {
@@ -1109,8 +989,8 @@ Sizes sizes_of(const soma_ce_config& c, bool grad) {
     s.eT = take(size_t(longest) * s.Kp * half);
     s.G = take(size_t(area) * half);
     s.GT = take(size_t(area) * half);
-    s.accf = take(acc_bytes(s.Rp, s.Kp, longest / 32));
-    s.acce = take(acc_bytes(longest, s.Kp, s.Rp / 32));
+    s.accf = take(acc_bytes(s.Rp, s.Kp, longest));
+    s.acce = take(acc_bytes(longest, s.Kp, s.Rp));
   }
   s.total = at;
   return s;
@@ -1129,10 +1009,10 @@ int check_ce(const soma_ce_config* c) {
   return SOMA_OK;
 }
 
-// Shares of every tile's stages: as many as bring the items to `fill`, at
-// least four stages each.
+// Shares of every tile's columns: as many as bring the items to `fill`, at
+// least two pairs of stages each.
 int choose_splits(int64_t tiles, int64_t stages, int64_t fill) {
-  return int(std::max<int64_t>(1, std::min(fill / std::max<int64_t>(tiles, 1), stages / 4)));
+  return int(std::max<int64_t>(1, std::min(fill / std::max<int64_t>(tiles, 1), stages / 2)));
 }
 
 Divider divider(int d) {
@@ -1141,71 +1021,94 @@ Divider divider(int d) {
   return {uint32_t((uint64_t(1) << 32) * ((uint64_t(1) << l) - uint64_t(d)) / uint64_t(d)) + 1u, l, d};
 }
 
-// most: blocks that work through the items one after another; 0: a block each.
-int launch_items(const void* kern, CeMmArgs& p, int threads, int64_t most, unsigned lds, hipStream_t st) {
+// most: blocks that the card holds at once.
+int launch_items(const void* kern, CeMmArgs& p, int64_t most, unsigned lds, hipStream_t st) {
   const int64_t items = int64_t(p.ntm) * p.ntn * p.splits;
   if (items >= (int64_t(1) << 30)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
   p.items = int(items);
   p.by_tiles = divider(p.ntm * p.ntn), p.by_band = divider(8 * p.ntm), p.by_rest = divider(std::max(p.ntn % 8, 1));
   p.by_splits = divider(p.splits);
-  int64_t blocks = up(items, kXcd);
-  if (most) blocks = std::min(blocks, most);
+  const int64_t blocks = std::min(up(items, kXcd), most);
   hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
   if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
   void* args[] = {&p};
-  e = hipLaunchKernel(kern, dim3(unsigned(blocks)), dim3(threads), args, lds, st);
+  e = hipLaunchKernel(kern, dim3(unsigned(blocks)), dim3(256), args, lds, st);
   if (e != hipSuccess) return set_error(SOMA_EDEVICE, "k_ce_mm: %s", hipGetErrorString(e));
   return SOMA_OK;
 }
 
-// A product on tiles of 16 side x 16 side, side = 16 or 8; bf16 logits on large
-// tiles take 8 x 16.
+// Tiles in units of 16 rows of A and of W.
+struct Tile {
+  int tm, tn;
+};
+Tile tile_of(bool large, int parts, bool logits) {
+  if (!large) return {8, 8};
+  return {16, parts == 1 && !logits ? 16 : 8};
+}
+
 template <class T, int PARTS, int kEpi>
 int launch_mm(CeMmArgs& p, bool large, hipStream_t st) {
   constexpr bool kLogits = kEpi == kStats || kEpi == kGrad;
-  p.stages = p.KC / (PARTS == 1 ? 2 : 1);
-  const bool wide = PARTS == 1 && large && p.stages / p.splits >= 2;     // four stages of its own an item
-  const int tm = large ? 16 : 8, tn = wide && kLogits ? 8 : tm;
-  p.ntm = (p.ta + tm - 1) / tm;
-  p.ntn = (p.tw + tn - 1) / tn;
-  p.tile_subs = wide ? 1 : 2;
-  if constexpr (PARTS == 1 && kLogits) {
-    if (wide)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi, 8, 1, 3, 2>), p, 256, 2 * kFill, 73728, st);
-  } else if constexpr (PARTS == 1) {
-    if (wide)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm_wide<T, kEpi, 16, 2, 4, 1>), p, 256, kFill, 131072, st);
+  const Tile t = tile_of(large, PARTS, kLogits);
+  p.stages = p.KC / 2;
+  p.ntm = (p.ta + t.tm - 1) / t.tm;
+  p.ntn = (p.tw + t.tn - 1) / t.tn;
+  p.tile_subs = large ? 1 : 2;
+  if constexpr (PARTS == 1) {
+    if (!large)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 8, 8, 2, 4, 2>), p, 2 * kFill, 65536, st);
+    if constexpr (kLogits)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 8, 16, 1, 3, 2>), p, 2 * kFill, 73728, st);
+    else
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 16, 16, 2, 4, 1>), p, kFill, 131072, st);
+  } else {
+    if (!large)
+      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 2, kEpi, 8, 8, 2, 4, 1>), p, kFill, 131072, st);
+    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 2, kEpi, 8, 16, 1, 3, 1>), p, kFill, 147456, st);
   }
-  if (large)
-    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 16, 16, 2, 4, 2>), p, 512, kFill, 131072, st);
-  // One block a compute unit: its four buffers hide what a second block would.
-  if (int64_t(p.ntm) * p.ntn * p.splits <= kFill)
-    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 4>), p, 256, 0, 131072, st);
-  return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, PARTS, kEpi, 8, 8, 2, 2, 2>), p, 256, 0, 65536, st);
 }
 
-int64_t tiles_of(int64_t m, int64_t n, int64_t side) { return up(m, side) / side * (up(n, side) / side); }
+int64_t tiles_of(int64_t m, int64_t n, Tile t) { return (m + 16 * t.tm - 1) / (16 * t.tm) * ((n + 16 * t.tn - 1) / (16 * t.tn)); }
 
-// Logits on 256 x 256 tiles where they come to three quarters of the compute
-// units and their padding is no larger than a quarter.
-bool large_logits(int64_t m, int64_t n) {
-  return tiles_of(m, n, 256) >= kFill * 3 / 4 && up(m, 256) * up(n, 256) <= m * n * 5 / 4;
+// Microseconds of a product of m x n outputs over `columns` in `splits` shares,
+// from what the card reaches on many tiles (executed products: 1.1 PF/s on large
+// tiles, 0.9 on small ones) and the rounds that the items take, and from what
+// the sums of shares, or of pieces (`sums`), write and read at 5 TB/s.  It decides
+// between tiles and shares only.  Measured: fp32 logits 1,000 x 10,007 x 361, 316
+// large tiles in two rounds, 37.8 us, 632 small ones in three, 29.0; df 16,320 x
+// 512 over 256 columns, two shares of large tiles and their sum, 45 us, whole small
+// tiles 23.
+double product_us(int64_t m, int64_t n, int64_t columns, int parts, bool logits, bool large, int splits, bool sums) {
+  const Tile t = tile_of(large, parts, logits);
+  const int64_t hold = parts == 1 && (logits || !large) ? 2 * kFill : kFill;
+  const int64_t items = tiles_of(m, n, t) * splits, rounds = (items + hold - 1) / hold;
+  const double item = 2.0 * (parts == 1 ? 1 : 3) * t.tm * t.tn * 256.0 * double(columns) / splits;
+  return double(rounds) * double(hold) * item / (large ? 1.1e9 : 0.9e9) +
+         (sums || splits > 1 ? 8.0 * double(splits) * double(m) * double(n) / 5e6 : 0.0) + (splits > 1 ? 5.0 : 0.0);
 }
 
-// How the products with G are shared out, by the first and largest piece.
+bool large_logits(int64_t m, int64_t n, int64_t columns, int parts) {
+  return product_us(m, n, columns, parts, true, true, 1, false) < product_us(m, n, columns, parts, true, false, 1, false);
+}
+
+// How the products with G are shared out, by the first and largest piece:
+// whole tiles, or as many shares as fill the card, of either size.
 struct Shares {
   bool large;
   int splits;
 };
-Shares shares_of(int64_t m, int64_t n, int64_t columns, int parts) {
-  const int64_t stages = columns / (parts == 1 ? 64 : 32);
-  const int64_t large = tiles_of(m, n, 256), small = tiles_of(m, n, 128);
-  // Shares write and read their sums, 8 bytes an output each: with few columns
-  // that is longer than the product, and whole small tiles are better.
-  if (large < kFill && small >= kFill && columns <= 1024) return {false, 1};
-  const int s = choose_splits(large, stages, kFill);
-  if (large * s >= kFill * 3 / 4 && up(m, 256) * up(n, 256) <= m * n * 5 / 4) return {true, s};
-  return {false, choose_splits(small, stages, 2 * kFill)};
+Shares shares_of(int64_t m, int64_t n, int64_t columns, int parts, bool sums) {
+  Shares best{};
+  double least = 0.0;
+  for (const bool large : {true, false}) {
+    const int most = choose_splits(tiles_of(m, n, tile_of(large, parts, false)), columns / 64, large || parts == 2 ? kFill : 2 * kFill);
+    for (int s = 1;; s = most) {
+      const double us = product_us(m, n, columns, parts, false, large, s, sums);
+      if (best.splits == 0 || us < least) best = {large, s}, least = us;
+      if (s == most) break;
+    }
+  }
+  return best;
 }
 
 // One product with G.  `single`: it alone gives the result; else the result
@@ -1215,14 +1118,15 @@ template <class T, int PARTS>
 int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipStream_t st) {
   p.splits = sh.splits;
   if (single && p.splits == 1) return launch_mm<T, PARTS, kOut>(p, sh.large, st);
-  // A last piece of fewer stages than shares adds to the first ones only.
-  p.splits = std::min(sh.splits, p.KC / (PARTS == 1 ? 2 : 1));
+  // A last piece of fewer columns than shares need adds to the first ones only.
+  p.splits = std::max(1, std::min(sh.splits, p.KC / 4));
   if (int rc = launch_mm<T, PARTS, kPart>(p, sh.large, st)) return rc;
   if (!finish) return SOMA_OK;
   p.splits = sh.splits;
   const unsigned tiles = unsigned(p.ntm * p.ntn);
+  constexpr Tile t = {16, PARTS == 1 ? 16 : 8};           // tile_of(true, PARTS, false)
   if (sh.large)
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 16, 16>), dim3(tiles, 64), dim3(256), 0, st, p);
+    hipLaunchKernelGGL((k_ce_sum<T, PARTS, t.tn, t.tm>), dim3(tiles, t.tn * t.tm / 4), dim3(256), 0, st, p);
   else
     hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8>), dim3(tiles, 16), dim3(256), 0, st, p);
   return launched("k_ce_sum");
@@ -1277,7 +1181,7 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     stride = int(s.Rp);
     const int piece = piece_of(c);
     for (int v0 = 0; v0 < c.vocab; v0 += piece) {
-      const int n = std::min(piece, c.vocab - v0), np = int(up(n, 64));
+      const int n = std::min(piece, c.vocab - v0), np = int(up(n, 128));
       PackArgs b{};
       b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
       b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.nmax = nmax, b.which = 1;
@@ -1285,7 +1189,7 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       CeMmArgs p{};
       p.A = fp, p.W = ep, p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
       p.part = part, p.part_stride = stride, p.sub0 = subs, p.hit = hit, p.targets = targets, p.R = c.rows, p.V = n, p.v0 = v0;
-      const bool large = large_logits(s.Rp, np);
+      const bool large = large_logits(s.Rp, np, s.Kp, PARTS);
       p.splits = 1;
       if (int rc = launch_mm<T, PARTS, kStats>(p, large, st)) return rc;
       subs += p.tile_subs * p.ntn;
@@ -1317,10 +1221,10 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = nmax;
   a.scales = scales, a.meta = meta, a.lse = lse, a.w = w, a.V = c.vocab;
   if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
-  const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp, PARTS);
+  const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp, PARTS, c.vocab > piece_of(c));
   const int piece = piece_of(c);
   for (int v0 = 0; v0 < c.vocab; v0 += piece) {
-    const int n = std::min(piece, c.vocab - v0), np = int(up(n, 64));
+    const int n = std::min(piece, c.vocab - v0), np = int(up(n, 128));
     PackArgs b{};
     b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
     b.np = np, b.Kp = int(s.Kp), b.frag = at(s.e), b.fragT = df ? at(s.eT) : nullptr;
@@ -1330,7 +1234,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     p.A = at(s.f), p.W = at(s.e), p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
     p.meta = meta, p.G = at(s.G), p.GT = at(s.GT), p.V = n, p.v0 = v0;
     p.splits = 1;
-    if (int rc = launch_mm<T, PARTS, kGrad>(p, large_logits(s.Rp, np), st)) return rc;
+    if (int rc = launch_mm<T, PARTS, kGrad>(p, large_logits(s.Rp, np, s.Kp, PARTS), st)) return rc;
     if (df) {
       CeMmArgs q{};
       q.A = at(s.G), q.W = at(s.eT), q.ta = int(s.Rp / 16), q.tw = int(s.Kp / 16), q.KC = np / 32, q.scales = scales;
@@ -1342,7 +1246,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       q.A = at(s.GT), q.W = at(s.fT), q.ta = np / 16, q.tw = int(s.Kp / 16), q.KC = int(s.Rp / 32), q.scales = scales;
       q.out = static_cast<T*>(dE) + int64_t(v0) * c.width, q.M = n, q.N = c.width, q.is_de = 1;
       q.acc = reinterpret_cast<float4*>(ws + s.acce);
-      if (int rc = launch_product<T, PARTS>(q, shares_of(np, s.Kp, s.Rp, PARTS), true, true, st)) return rc;
+      if (int rc = launch_product<T, PARTS>(q, shares_of(np, s.Kp, s.Rp, PARTS, false), true, true, st)) return rc;
     }
   }
   return SOMA_OK;
