@@ -6,8 +6,8 @@
 // With a_t = s(f_t), b_t = s(i_t) tanh(g_t) a run of rows is one affine map of
 // the state in front of it, c -> A c + B, and maps of neighbouring runs
 // compose: (A2, B2) after (A1, B1) is (A2 A1, A2 B1 + B2).  So time runs side by
-// side.  A block takes 64 lanes of channels and walks over tiles of 64 rows: its 8
-// waves hold 8 rows each in registers, form the map of their rows, exchange the
+// side.  A block takes 64 lanes of channels and walks over tiles of 64 rows (backward: 32): its 8
+// waves hold 8 (4) rows each in registers, form the map of their rows, exchange the
 // maps through LDS and start from the state that the earlier waves' maps give.
 // The gates are read once; the next tile's are on their way meanwhile.  The
 // state in front of every 64th row is kept for the backward pass, which forms the
@@ -17,13 +17,16 @@
 // l_t = u_t + q_{t+1}, and what it passes on is q_t = s(f_t) l_t: the same affine
 // maps from the last row to the first, q -> A q + B.
 //
-// Work is split by sequence and channels where that fills the card.  Else the
-// rows are cut into pieces of whole tiles: a first launch forms the map of every
-// piece, and each block of the second starts from the maps of the pieces in front
-// of it.  That reads the gates twice (the second time largely from the last-level
-// cache), and is bound by memory like the first way.
+// Work is split by sequence and channels where that fills the card.  Else tiles are
+// dealt out one by one, in order (a counter), to blocks that publish their tile's
+// map, look back over the maps before it until they meet a state, publish the
+// state behind their own tile, and write their rows: the gates are still read
+// once, and a tile waits only for tiles that were dealt out earlier, so that some
+// block can always go on.  Values travel between compute units as 32- and 64-bit
+// words of agent scope that are their own flags (a word of ones: not there yet).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
 
 #include "soma.h"
@@ -33,11 +36,12 @@
 namespace soma {
 namespace {
 
-constexpr int kTile = 64;             // rows of a tile: SOMA_SCAN_BLOCK
 constexpr int kWaves = 8;
-constexpr int kRows = kTile / kWaves; // rows of a wave
+// Rows of a tile.  Backward holds twice as much of a row in registers, and takes
+// half as many.
+constexpr int kForward = 64, kBackward = 32;
 constexpr float kL2e = 1.4426950408889634f;
-static_assert(kTile == SOMA_SCAN_BLOCK, "the states' spacing is part of the interface");
+static_assert(kBackward == SOMA_SCAN_BLOCK && kForward == 2 * SOMA_SCAN_BLOCK, "the states' spacing is part of the interface");
 
 struct ScanArgs {
   const void* gates;
@@ -48,25 +52,29 @@ struct ScanArgs {
   const float* c0;          // [S][H] or NULL: zeros
   float* last;              // forward: cT [S][H]; backward: dc0 [S][H]; or NULL
   const float* dcT;         // backward: [S][H] or NULL: zeros
-  float* states;            // [ceil(rows / 64)][H]: the state in front of row 64 j; or NULL
-  float* start;             // pieces: c0 as it was (cT may be the same array), [S][H]
-  float2* maps;             // pieces: [pieces][H]
+  float* states;            // [ceil(rows / 32)][H]: the state in front of row 32 j; or NULL
   int rows, H, S, length;
-  int piece;                // rows of a piece, a multiple of 64 (0: split by sequence)
+  // tiles dealt out one by one
+  unsigned* ticket;         // the counter
+  struct TileInfo* info;    // [tiles]
+  uint64_t* maps;           // [tiles][H]
+  uint32_t* tile_state;     // [tiles][H]: behind a tile, in the order in which they are dealt out
+  int tile;                 // rows of one
+  int tiles, groups;
 };
 
-// An affine map x -> a x + b of the state.  a < 0 marks a map that forgets x
-// (a sequence starts inside): 0 * x would let another sequence's NaN through.
-__device__ __forceinline__ float apply_map(float2 m, float x) {
-  return m.x < 0.0f ? m.y : __builtin_fmaf(m.x, x, m.y);
-}
+// The sequence of a tile's first row, and that sequence's rows.
+struct TileInfo {
+  int s, first, to, pad;
+};
 
 __device__ __forceinline__ float sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kL2e * x));
 }
+// 1 - 2 / (1 + e^2x): fewer operations than the quotient of e^-2|x|, off by 2 u
+// where tanh is small; e^2x = inf gives 1.
 __device__ __forceinline__ float tanh_of(float x) {
-  const float e = __builtin_amdgcn_exp2f(-2.0f * kL2e * __builtin_fabsf(x));
-  return __builtin_copysignf((1.0f - e) * __builtin_amdgcn_rcpf(1.0f + e), x);
+  return __builtin_fmaf(-2.0f, __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(2.0f * kL2e * x)), 1.0f);
 }
 
 // VEC neighbouring channels of a row as 32 bits (bf16 pair, fp32, or one bf16).
@@ -125,13 +133,13 @@ __device__ __forceinline__ int sequence_of(const ScanArgs& a, int r) {
   return lo;
 }
 
-// This block's channels.
+// The channels of a group.
 template <int VEC>
 struct Channels {
   int ch;
   bool on;
-  __device__ __forceinline__ explicit Channels(const ScanArgs& a)
-      : ch((blockIdx.x * 64 + (threadIdx.x & 63)) * VEC), on(ch < a.H) {}
+  __device__ __forceinline__ Channels(const ScanArgs& a, int group)
+      : ch((group * 64 + (threadIdx.x & 63)) * VEC), on(ch < a.H) {}
 };
 
 template <int VEC>
@@ -152,7 +160,6 @@ __device__ __forceinline__ void store_state(float* p, int64_t row, const ScanArg
 // A run of rows of one sequence inside one tile.
 struct Run {
   int lo, hi;      // rows lo .. hi - 1
-  __device__ __forceinline__ int base() const { return lo & ~(kTile - 1); }
 };
 
 // The maps of a tile's waves, exchanged through LDS (two buffers in turn, so
@@ -163,40 +170,42 @@ struct Exchange {
 };
 
 // ---------------------------------------------------------------------------
-// Forward.  kMaps: only the map of the rows (piece mode's first launch).
+// Forward: maps() forms the maps of a run's rows and shares them, fold() brings
+// the state through them, rows_out() writes h.
 // ---------------------------------------------------------------------------
-template <class T, int VEC, bool kMaps>
+template <class T, int VEC>
 struct Forward {
   typedef Lane<T, VEC> L;
+  static constexpr int kTile = kForward, kRows = kTile / kWaves;
   const ScanArgs& a;
   Channels<VEC> c;
   Exchange<VEC>& x;
   int wave, lane, buf = 0;
+  float pa[kRows][VEC], pb[kRows][VEC];       // the map of the wave's rows up to each
+  float in[VEC];                              // the state in front of the wave's rows
 
-  __device__ __forceinline__ Forward(const ScanArgs& a_, Exchange<VEC>& x_)
-      : a(a_), c(a_), x(x_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {}
+  __device__ __forceinline__ Forward(const ScanArgs& a_, Exchange<VEC>& x_, int group)
+      : a(a_), c(a_, group), x(x_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {}
 
   struct Raw {
     typename L::raw g[4][kRows];
   };
 
-  __device__ __forceinline__ void load(const Run& r, Raw& raw) const {
-    const int row0 = r.base() + wave * kRows;
+  __device__ __forceinline__ void load(const Channels<VEC>& c, const Run& r, Raw& raw) const {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int row = row0 + u;
       if (c.on && row >= r.lo && row < r.hi) {
         const int64_t at = int64_t(row) * a.gate_stride + c.ch;
 #pragma unroll
-        for (int k = 0; k < (kMaps ? 3 : 4); ++k) raw.g[k][u] = L::load(a.gates, at + int64_t(k) * a.H);
+        for (int k = 0; k < 4; ++k) raw.g[k][u] = L::load(a.gates, at + int64_t(k) * a.H);
       }
     }
   }
 
-  // Advances the state (or, for kMaps, the map (A, state)) over a run.
-  __device__ __forceinline__ void advance(const Run& r, const Raw& raw, float (&state)[VEC], float (&A)[VEC]) {
-    const int row0 = r.base() + wave * kRows;
-    float pa[kRows][VEC], pb[kRows][VEC];     // the map of the wave's rows up to each
+  __device__ __forceinline__ void maps(const Run& r, const Raw& raw) {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float ma = 1.0f, mb = 0.0f;
@@ -215,7 +224,26 @@ struct Forward {
       x.m[buf][wave][lane * VEC + v] = make_float2(ma, mb);
     }
     __syncthreads();
-    float in[VEC];
+  }
+
+  // The map of the whole run.
+  __device__ __forceinline__ void whole_map(float (&A)[VEC], float (&B)[VEC]) const {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      A[v] = 1.0f, B[v] = 0.0f;
+#pragma unroll
+      for (int w = 0; w < kWaves; ++w) {
+        const float2 m = x.m[buf][w][lane * VEC + v];
+        A[v] *= m.x;
+        B[v] = __builtin_fmaf(m.x, B[v], m.y);
+      }
+    }
+  }
+
+  // Also keeps the states in front of every 32nd row.
+  __device__ __forceinline__ void fold(const Run& r, float (&state)[VEC]) {
+    if (wave == 0 && r.lo % SOMA_SCAN_BLOCK == 0) store_state<VEC>(a.states, r.lo / SOMA_SCAN_BLOCK, a, c, state);
+
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float s = state[v];
@@ -224,151 +252,296 @@ struct Forward {
         if (w == wave) in[v] = s;
         const float2 m = x.m[buf][w][lane * VEC + v];
         s = __builtin_fmaf(m.x, s, m.y);
-        if constexpr (kMaps) A[v] = A[v] < 0.0f ? A[v] : A[v] * m.x;
       }
       state[v] = s;
     }
     buf ^= 1;
-    if constexpr (!kMaps) {
+    const int half = (r.lo & ~(kTile - 1)) + SOMA_SCAN_BLOCK;
+    if (wave == kWaves / 2 && r.lo < half && half < r.hi) store_state<VEC>(a.states, half / SOMA_SCAN_BLOCK, a, c, in);
+  }
+
+  __device__ __forceinline__ void rows_out(const Run& r, const Raw& raw) const {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
-      for (int u = 0; u < kRows; ++u) {
-        const int row = row0 + u;
-        if (c.on && row >= r.lo && row < r.hi) {
-          float h[VEC];
+    for (int u = 0; u < kRows; ++u) {
+      const int row = row0 + u;
+      if (c.on && row >= r.lo && row < r.hi) {
+        float h[VEC];
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            const float cell = __builtin_fmaf(pa[u][v], in[v], pb[u][v]);
-            h[v] = sigmoid(L::get(raw.g[3][u], v)) * tanh_of(cell);
-          }
-          L::store(a.out, int64_t(row) * a.H + c.ch, h);
+        for (int v = 0; v < VEC; ++v) {
+          const float cell = __builtin_fmaf(pa[u][v], in[v], pb[u][v]);
+          h[v] = sigmoid(L::get(raw.g[3][u], v)) * tanh_of(cell);
         }
+        L::store(a.out, int64_t(row) * a.H + c.ch, h);
       }
     }
   }
 };
 
-// Rows [lo, hi) of sequence s from `state`, which is left as the state behind
-// them.  (kMaps: A is the map's factor.)
-template <class T, int VEC, bool kMaps>
-__device__ __forceinline__ void forward_rows(Forward<T, VEC, kMaps>& f, int lo, int hi, float (&state)[VEC],
-                                             float (&A)[VEC]) {
-  typedef typename Forward<T, VEC, kMaps>::Raw Raw;
-  if (lo >= hi) return;
-  Run r{lo, min(hi, (lo & ~(kTile - 1)) + kTile)};
-  Raw raw;
-  f.load(r, raw);
-  for (;;) {
-    const Run next{r.hi, min(hi, r.hi + kTile)};
-    Raw ahead;
-    if (next.lo < hi) f.load(next, ahead);
-    if constexpr (!kMaps)
-      if (f.wave == 0 && (r.lo & (kTile - 1)) == 0) store_state<VEC>(f.a.states, r.lo / kTile, f.a, f.c, state);
-    f.advance(r, raw, state, A);
-    if (next.lo >= hi) break;
-    r = next;
-    raw = ahead;
-  }
-}
-
+// By sequence: a block walks over the tiles of one.
 template <class T, int VEC>
 __global__ __launch_bounds__(64 * kWaves) void k_scan_forward(ScanArgs a) {
   __shared__ Exchange<VEC> x;
-  Forward<T, VEC, false> f(a, x);
-  float state[VEC], unused[VEC];
-  if (a.piece == 0) {
-    const int s = blockIdx.y;
-    const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
-    load_state<VEC>(a.c0, s, a, f.c, state);
-    forward_rows(f, lo, hi, state, unused);
-    if (f.wave == 0) store_state<VEC>(a.last, s, a, f.c, state);
-    return;
-  }
-  // Rows [lo, hi) of all sequences together.
-  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  int lo = max(p * a.piece, begin);
-  const int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
-  if (p == 0 && f.wave == 0 && a.last)        // sequences without a row keep their state
-    for (int s = 0; s < a.S; ++s)
-      if (first_row(a, s + 1) <= first_row(a, s)) {
-        load_state<VEC>(a.start, s, a, f.c, state);
-        store_state<VEC>(a.last, s, a, f.c, state);
-      }
-  if (lo >= hi) return;
-  int s = sequence_of(a, lo);
-  if (first_row(a, s) == lo) {
-    load_state<VEC>(a.start, s, a, f.c, state);
-  } else {
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) state[v] = 0.0f;
-    for (int q = 0; q < p; ++q)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (f.c.on) state[v] = apply_map(a.maps[int64_t(q) * a.H + f.c.ch + v], state[v]);
-  }
-  for (;;) {
-    const int to = clamp_row(first_row(a, s + 1), lo, hi);
-    forward_rows(f, lo, to, state, unused);
-    if (f.wave == 0 && to == first_row(a, s + 1) && to > first_row(a, s)) store_state<VEC>(a.last, s, a, f.c, state);
-    lo = to;
-    if (lo >= hi || s + 1 >= a.S) break;
-    ++s;
-    if (first_row(a, s) == lo && first_row(a, s + 1) > lo) load_state<VEC>(a.start, s, a, f.c, state);
-  }
-}
-
-// Piece mode's first launch: the map of every piece's rows, and the initial
-// states as they are now (the second launch may overwrite them with the last).
-template <class T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_forward_maps(ScanArgs a) {
-  __shared__ Exchange<VEC> x;
-  Forward<T, VEC, true> f(a, x);
-  float state[VEC], A[VEC];
-  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  if (f.wave == 0)
-    for (int s = p; s < a.S; s += gridDim.y) {
-      load_state<VEC>(a.c0, s, a, f.c, state);
-      store_state<VEC>(a.start, s, a, f.c, state);
-    }
-  const int lo = max(p * a.piece, begin);
-  const int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, state[v] = 0.0f;
+  Forward<T, VEC> f(a, x, blockIdx.x);
+  typedef typename Forward<T, VEC>::Raw Raw;
+  const int s = blockIdx.y;
+  const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
+  float state[VEC];
+  load_state<VEC>(a.c0, s, a, f.c, state);
   if (lo < hi) {
-    // Only the rows from the last start on matter.
-    const int s = sequence_of(a, hi - 1), from = first_row(a, s);
-    if (from >= lo) {
-      load_state<VEC>(a.c0, s, a, f.c, state);
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) A[v] = -1.0f;
+    Run r{lo, min(hi, (lo & ~(kForward - 1)) + kForward)};
+    Raw raw;
+    f.load(f.c, r, raw);
+    for (;;) {
+      const Run next{r.hi, min(hi, r.hi + kForward)};
+      Raw ahead;
+      if (next.lo < hi) f.load(f.c, next, ahead);
+      f.maps(r, raw);
+      f.fold(r, state);
+      f.rows_out(r, raw);
+      if (next.lo >= hi) break;
+      r = next;
+      raw = ahead;
     }
-    forward_rows(f, max(lo, from), hi, state, A);
   }
-  if (f.wave == 0 && f.c.on)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) a.maps[int64_t(p) * a.H + f.c.ch + v] = make_float2(A[v], state[v]);
+  if (f.wave == 0) store_state<VEC>(a.last, s, a, f.c, state);
 }
 
 // ---------------------------------------------------------------------------
-// Backward.
+// Tiles dealt out one by one.
 // ---------------------------------------------------------------------------
-template <class T, int VEC, bool kMaps>
+constexpr uint32_t kNone = 0xFFFFFFFFu;       // not there yet
+constexpr unsigned kPolls = 1u << 20;         // about a second; then the rows are NaN (no wait is without an end)
+
+__device__ __forceinline__ uint32_t word_of(float x) {
+  const uint32_t b = __float_as_uint(x);
+  return b == kNone ? 0x7FC00000u : b;        // that NaN in another form
+}
+
+template <int VEC>
+__device__ __forceinline__ void publish_map(const ScanArgs& a, const Channels<VEC>& c, int tile, const float (&A)[VEC],
+                                            const float (&B)[VEC]) {
+  if (!c.on) return;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    __hip_atomic_store(a.maps + int64_t(tile) * a.H + c.ch + v, uint64_t(__float_as_uint(B[v])) << 32 | word_of(A[v]),
+                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+template <int VEC>
+__device__ __forceinline__ void publish_state(const ScanArgs& a, const Channels<VEC>& c, int tile, const float (&x)[VEC]) {
+  if (!c.on) return;
+#pragma unroll
+  for (int v = 0; v < VEC; ++v)
+    __hip_atomic_store(a.tile_state + int64_t(tile) * a.H + c.ch + v, word_of(x[v]), __ATOMIC_RELAXED,
+                       __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// One wave: the state that the tiles from `tile` + kDir on bring, by way of their
+// maps, four at a time.
+template <int VEC, int kDir>
+__device__ __forceinline__ void look_back(const ScanArgs& a, const Channels<VEC>& c, int tile, float (&state)[VEC]) {
+  float A[VEC], B[VEC];
+#pragma unroll
+  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, B[v] = 0.0f, state[v] = __builtin_nanf("");
+  int q = tile + kDir;
+  for (unsigned polls = 0; polls < kPolls;) {
+    uint32_t st[4][VEC];
+    uint64_t mp[4][VEC];
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const int64_t at = int64_t(min(max(q + kDir * k, 0), a.tiles - 1)) * a.H + c.ch;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        st[k][v] = c.on ? __hip_atomic_load(a.tile_state + at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+        mp[k][v] = c.on ? __hip_atomic_load(a.maps + at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
+      }
+    }
+    int used = 0;
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      if (used < k) break;                    // one before was not there
+      const int at = q + kDir * k;
+      if (at < 0 || at >= a.tiles) break;
+      bool has_state = true, has_map = true;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        has_state = has_state && st[k][v] != kNone;
+        has_map = has_map && static_cast<uint32_t>(mp[k][v]) != kNone;
+      }
+      if (__all(has_state)) {
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) state[v] = __builtin_fmaf(A[v], __uint_as_float(st[k][v]), B[v]);
+        return;
+      }
+      if (!__all(has_map)) break;
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) {
+        B[v] = __builtin_fmaf(A[v], __uint_as_float(static_cast<uint32_t>(mp[k][v] >> 32)), B[v]);
+        A[v] *= __uint_as_float(static_cast<uint32_t>(mp[k][v]));
+      }
+      used = k + 1;
+    }
+    q += kDir * used;
+    if (used == 0) {
+      ++polls;
+      __builtin_amdgcn_s_sleep(1);
+    }
+  }
+}
+
+// Clears the words and the counter, finds every tile's sequence, and copies the
+// states of sequences without a row (from -> last).
+__global__ __launch_bounds__(256) void k_scan_begin(ScanArgs a, const float* from) {
+  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, n = int64_t(gridDim.x) * 256;
+  const int64_t words = int64_t(a.tiles) * a.H;
+  for (int64_t k = i; k < words; k += n) {
+    a.maps[k] = ~uint64_t(0);
+    a.tile_state[k] = kNone;
+  }
+  if (i == 0) *a.ticket = 0u;
+  for (int64_t k = i; k < a.tiles; k += n) {
+    const int s = sequence_of(a, static_cast<int>(k) * a.tile);
+    a.info[k] = TileInfo{s, first_row(a, s), first_row(a, s + 1), 0};
+  }
+  if (a.last)
+    for (int64_t k = i; k < int64_t(a.S) * a.H; k += n) {
+      const int s = static_cast<int>(k / a.H);
+      if (first_row(a, s + 1) <= first_row(a, s)) a.last[k] = from ? from[k] : 0.0f;
+    }
+}
+
+// The tickets of a block: the tile that it works on, and the one after, whose
+// rows are already on their way.
+template <int kDir>
+struct Tickets {
+  const ScanArgs& a;
+  unsigned* shared;           // [2]
+  int items, par = 0;
+  __device__ __forceinline__ Tickets(const ScanArgs& a_, unsigned* shared_)
+      : a(a_), shared(shared_), items(a_.tiles * a_.groups) {}
+  __device__ __forceinline__ void ask() {
+    if (threadIdx.x == 0)
+      shared[par] = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+  }
+  // Behind a barrier.
+  __device__ __forceinline__ int answer() {
+    const unsigned t = __builtin_amdgcn_readfirstlane(shared[par]);
+    par ^= 1;
+    return t < static_cast<unsigned>(items) ? static_cast<int>(t) : items;
+  }
+  __device__ __forceinline__ int tile(int t) const {
+    const int p = t / a.groups;
+    return kDir < 0 ? p : a.tiles - 1 - p;
+  }
+  __device__ __forceinline__ int group(int t) const { return t % a.groups; }
+};
+
+template <class T, int VEC>
+__global__ __launch_bounds__(64 * kWaves) void k_scan_forward_tiles(ScanArgs a) {
+  __shared__ Exchange<VEC> x;
+  __shared__ float carry[64 * VEC];
+  __shared__ unsigned next[2];
+  Forward<T, VEC> f(a, x, 0);
+  typedef typename Forward<T, VEC>::Raw Raw;
+  const int begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+  Tickets<-1> tickets(a, next);
+  auto rows_of = [&](int t) {
+    const int lo = tickets.tile(t) * kForward;
+    return Run{max(lo, begin), min(lo + kForward, end)};
+  };
+  tickets.ask();
+  __syncthreads();
+  int t = tickets.answer();
+  tickets.ask();
+  __syncthreads();
+  int after = tickets.answer();
+  Raw raw;
+  if (t < tickets.items) f.load(Channels<VEC>(a, tickets.group(t)), rows_of(t), raw);
+  while (t < tickets.items) {
+    Raw ahead;
+    if (after < tickets.items) f.load(Channels<VEC>(a, tickets.group(after)), rows_of(after), ahead);
+    tickets.ask();
+    const int p = tickets.tile(t);
+    const Run tile = rows_of(t);
+    f.c = Channels<VEC>(a, tickets.group(t));
+    if (tile.lo < tile.hi) {
+      const TileInfo info = a.info[p];
+      // The first run began in a tile before.  Every tile with rows publishes the
+      // state behind its last, wanted or not: no offsets can make a tile wait for
+      // one that has nothing to say.
+      const bool continued = info.first < tile.lo && tile.lo > begin;
+      // The runs that begin here, then the one that goes on from a tile before.
+      int lo = continued ? min(info.to, tile.hi) : tile.lo;
+      for (bool last = !continued && lo >= tile.hi; !last;) {
+        const bool goes_on = lo >= tile.hi;
+        const int s = goes_on || lo == tile.lo ? info.s : sequence_of(a, lo);
+        const int to = goes_on ? info.to : max(first_row(a, s + 1), lo + 1);
+        const Run r{goes_on ? tile.lo : lo, min(to, tile.hi)};
+        last = goes_on || (!continued && r.hi >= tile.hi);
+        lo = goes_on ? lo : r.hi;
+        float state[VEC];
+        // In front of maps' barrier: behind it a faster wave may write cT, which
+        // may be c0.
+        load_state<VEC>(goes_on ? nullptr : a.c0, s, a, f.c, state);
+        f.maps(r, raw);
+        if (goes_on) {
+          if (f.wave == 0) {
+            if (r.hi == tile.hi) {
+              float A[VEC], B[VEC];
+              f.whole_map(A, B);
+              publish_map<VEC>(a, f.c, p, A, B);
+            }
+            look_back<VEC, -1>(a, f.c, p, state);
+#pragma unroll
+            for (int v = 0; v < VEC; ++v) carry[f.lane * VEC + v] = state[v];
+          }
+          __syncthreads();
+#pragma unroll
+          for (int v = 0; v < VEC; ++v) state[v] = carry[f.lane * VEC + v];
+        }
+        f.fold(r, state);
+        if (f.wave == 0 && r.hi == tile.hi) publish_state<VEC>(a, f.c, p, state);
+        f.rows_out(r, raw);
+        if (f.wave == 0 && to == r.hi) store_state<VEC>(a.last, s, a, f.c, state);
+      }
+    }
+    __syncthreads();
+    raw = ahead;
+    t = after;
+    after = tickets.answer();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Backward: maps() forms the cells of a run again and the maps of its rows, fold()
+// brings what the rows behind pass on through them, rows_out() writes dgates.
+// ---------------------------------------------------------------------------
+template <class T, int VEC>
 struct Backward {
   typedef Lane<T, VEC> L;
+  static constexpr int kTile = kBackward, kRows = kTile / kWaves;
   const ScanArgs& a;
   Channels<VEC> c;
   Exchange<VEC>&x, &y;
   int wave, lane, buf = 0;
+  // The transcendental unit bounds this pass (a quarter of the rate, ten of its
+  // instructions an element): every gate is formed once and kept.
+  float f[kRows][VEC], i[kRows][VEC], g[kRows][VEC];
+  float pq[kRows][VEC];                    // l of each row, without what comes from behind the wave
+  float prev[kRows][VEC];                  // the cell in front of each row
+  float go[kRows][VEC];                    // dh t s(o) (1 - s(o))
+  float in[VEC];                           // what the rows behind the wave's pass on
 
-  __device__ __forceinline__ Backward(const ScanArgs& a_, Exchange<VEC>& x_, Exchange<VEC>& y_)
-      : a(a_), c(a_), x(x_), y(y_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {}
+  __device__ __forceinline__ Backward(const ScanArgs& a_, Exchange<VEC>& x_, Exchange<VEC>& y_, int group)
+      : a(a_), c(a_, group), x(x_), y(y_), wave(__builtin_amdgcn_readfirstlane(threadIdx.x >> 6)), lane(threadIdx.x & 63) {}
 
   struct Raw {
     typename L::raw g[5][kRows];
-    float entry[VEC];      // the state in front of the run
   };
 
-  __device__ __forceinline__ void load(const Run& r, int s, int first, Raw& raw) const {
-    const int row0 = r.base() + wave * kRows;
+  __device__ __forceinline__ void load(const Channels<VEC>& c, const Run& r, Raw& raw) const {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
       const int row = row0 + u;
@@ -379,17 +552,18 @@ struct Backward {
         raw.g[4][u] = L::load(a.dh, int64_t(row) * a.H + c.ch);
       }
     }
-    if (r.lo == first)
-      load_state<VEC>(a.c0, s, a, c, raw.entry);
-    else
-      load_state<VEC>(a.states, r.lo / kTile, a, c, raw.entry);
   }
 
-  // From q = the gradient that the rows behind pass on to the one that this
-  // run passes on (or, for kMaps, the map (A, q)).
-  __device__ __forceinline__ void advance(const Run& r, const Raw& raw, float (&q)[VEC], float (&A)[VEC]) {
-    const int row0 = r.base() + wave * kRows;
-    float f[kRows][VEC], cell[kRows][VEC], before[VEC];
+  // The state in front of row `lo` of sequence s, which starts at `first`.
+  __device__ __forceinline__ void entry_state(const Channels<VEC>& c, int lo, int s, int first, float (&x)[VEC]) const {
+    if (lo == first)
+      load_state<VEC>(a.c0, s, a, c, x);
+    else
+      load_state<VEC>(a.states, lo / SOMA_SCAN_BLOCK, a, c, x);
+  }
+
+  __device__ __forceinline__ void maps(const Run& r, const Raw& raw, const float (&entry)[VEC]) {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float ma = 1.0f, mb = 0.0f;
@@ -398,34 +572,34 @@ struct Backward {
         const int row = row0 + u;
         if (row >= r.lo && row < r.hi) {
           f[u][v] = sigmoid(L::get(raw.g[1][u], v));
-          cell[u][v] = sigmoid(L::get(raw.g[0][u], v)) * tanh_of(L::get(raw.g[2][u], v));
+          i[u][v] = sigmoid(L::get(raw.g[0][u], v));
+          g[u][v] = tanh_of(L::get(raw.g[2][u], v));
           ma *= f[u][v];
-          mb = __builtin_fmaf(f[u][v], mb, cell[u][v]);
+          mb = __builtin_fmaf(f[u][v], mb, i[u][v] * g[u][v]);
         }
       }
       x.m[buf][wave][lane * VEC + v] = make_float2(ma, mb);
     }
     __syncthreads();
-    float pq[kRows][VEC];                  // q in front of each row, from 0 behind the wave's last
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      float s = raw.entry[v];
+      float s = entry[v];
 #pragma unroll
       for (int w = 0; w < kWaves - 1; ++w)
         if (w < wave) {
           const float2 m = x.m[buf][w][lane * VEC + v];
           s = __builtin_fmaf(m.x, s, m.y);
         }
-      before[v] = s;
       float u_of[kRows];
 #pragma unroll
       for (int u = 0; u < kRows; ++u) {
         const int row = row0 + u;
         if (row >= r.lo && row < r.hi) {
-          s = __builtin_fmaf(f[u][v], s, cell[u][v]);
-          cell[u][v] = s;
-          const float t = tanh_of(s);
-          u_of[u] = L::get(raw.g[4][u], v) * sigmoid(L::get(raw.g[3][u], v)) * (1.0f - t * t);
+          prev[u][v] = s;
+          s = __builtin_fmaf(f[u][v], s, i[u][v] * g[u][v]);
+          const float t = tanh_of(s), o = sigmoid(L::get(raw.g[3][u], v)), dho = L::get(raw.g[4][u], v) * o;
+          u_of[u] = dho * __builtin_fmaf(-t, t, 1.0f);
+          go[u][v] = dho * t * (1.0f - o);
         }
       }
       float ma = 1.0f, mb = 0.0f;
@@ -434,7 +608,7 @@ struct Backward {
         const int row = row0 + u;
         pq[u][v] = 0.0f;
         if (row >= r.lo && row < r.hi) {
-          pq[u][v] = mb + u_of[u];         // l of the row, without what comes from behind the wave
+          pq[u][v] = mb + u_of[u];
           mb = f[u][v] * pq[u][v];
           ma *= f[u][v];
         }
@@ -442,7 +616,22 @@ struct Backward {
       y.m[buf][wave][lane * VEC + v] = make_float2(ma, mb);
     }
     __syncthreads();
-    float in[VEC];
+  }
+
+  __device__ __forceinline__ void whole_map(float (&A)[VEC], float (&B)[VEC]) const {
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) {
+      A[v] = 1.0f, B[v] = 0.0f;
+#pragma unroll
+      for (int w = kWaves - 1; w >= 0; --w) {
+        const float2 m = y.m[buf][w][lane * VEC + v];
+        A[v] *= m.x;
+        B[v] = __builtin_fmaf(m.x, B[v], m.y);
+      }
+    }
+  }
+
+  __device__ __forceinline__ void fold(float (&q)[VEC]) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
       float s = q[v];
@@ -451,142 +640,148 @@ struct Backward {
         if (w == wave) in[v] = s;
         const float2 m = y.m[buf][w][lane * VEC + v];
         s = __builtin_fmaf(m.x, s, m.y);
-        if constexpr (kMaps) A[v] = A[v] < 0.0f ? A[v] : A[v] * m.x;
       }
       q[v] = s;
     }
     buf ^= 1;
-    if constexpr (!kMaps) {
-      float fac[VEC];                      // product of the f of the rows behind
+  }
+
+  __device__ __forceinline__ void rows_out(const Run& r) const {
+    const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
+    float fac[VEC];                        // what the rows behind pass on, through the f of those in between
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) fac[v] = in[v];
+    for (int v = 0; v < VEC; ++v) fac[v] = in[v];
 #pragma unroll
-      for (int u = kRows - 1; u >= 0; --u) {
-        const int row = row0 + u;
-        if (row >= r.lo && row < r.hi) {
-          float d[4][VEC];
+    for (int u = kRows - 1; u >= 0; --u) {
+      const int row = row0 + u;
+      if (row >= r.lo && row < r.hi) {
+        float d[4][VEC];
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) {
-            const float l = pq[u][v] + fac[v];
-            fac[v] *= f[u][v];
-            const float i = sigmoid(L::get(raw.g[0][u], v)), g = tanh_of(L::get(raw.g[2][u], v));
-            const float o = sigmoid(L::get(raw.g[3][u], v)), t = tanh_of(cell[u][v]);
-            const float prev = u > 0 && row > r.lo ? cell[u > 0 ? u - 1 : 0][v] : before[v];
-            d[0][v] = l * g * (i * (1.0f - i));
-            d[1][v] = l * prev * (f[u][v] * (1.0f - f[u][v]));
-            d[2][v] = l * i * (1.0f - g * g);
-            d[3][v] = L::get(raw.g[4][u], v) * t * (o * (1.0f - o));
-          }
-          if (c.on) {
-            const int64_t at = int64_t(row) * 4 * a.H + c.ch;
+        for (int v = 0; v < VEC; ++v) {
+          const float l = pq[u][v] + fac[v], lf = l * f[u][v], li = l * i[u][v];
+          fac[v] *= f[u][v];
+          d[0][v] = li * g[u][v] * (1.0f - i[u][v]);
+          d[1][v] = lf * prev[u][v] * (1.0f - f[u][v]);
+          d[2][v] = li * __builtin_fmaf(-g[u][v], g[u][v], 1.0f);
+          d[3][v] = go[u][v];
+        }
+        if (c.on) {
+          const int64_t at = int64_t(row) * 4 * a.H + c.ch;
 #pragma unroll
-            for (int k = 0; k < 4; ++k) L::store(a.out, at + int64_t(k) * a.H, d[k]);
-          }
+          for (int k = 0; k < 4; ++k) L::store(a.out, at + int64_t(k) * a.H, d[k]);
         }
       }
     }
   }
 };
 
-// Rows [lo, hi) of sequence s (which starts at row `first`), last to first.
-template <class T, int VEC, bool kMaps>
-__device__ __forceinline__ void backward_rows(Backward<T, VEC, kMaps>& b, int lo, int hi, int s, int first,
-                                              float (&q)[VEC], float (&A)[VEC]) {
-  typedef typename Backward<T, VEC, kMaps>::Raw Raw;
-  if (lo >= hi) return;
-  Run r{max(lo, (hi - 1) & ~(kTile - 1)), hi};
-  Raw raw;
-  b.load(r, s, first, raw);
-  for (;;) {
-    const Run next{max(lo, r.lo - kTile), r.lo};
-    Raw ahead;
-    if (next.hi > lo) b.load(next, s, first, ahead);
-    b.advance(r, raw, q, A);
-    if (next.hi <= lo) break;
-    r = next;
-    raw = ahead;
-  }
-}
-
 template <class T, int VEC>
 __global__ __launch_bounds__(64 * kWaves) void k_scan_backward(ScanArgs a) {
   __shared__ Exchange<VEC> x, y;
-  Backward<T, VEC, false> b(a, x, y);
-  float q[VEC], unused[VEC];
-  if (a.piece == 0) {
-    const int s = blockIdx.y;
-    const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
-    load_state<VEC>(a.dcT, s, a, b.c, q);
-    backward_rows(b, lo, hi, s, lo, q, unused);
-    if (b.wave == 0) store_state<VEC>(a.last, s, a, b.c, q);
-    return;
-  }
-  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  const int lo = max(p * a.piece, begin);
-  int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
-  if (p == 0 && b.wave == 0 && a.last)
-    for (int s = 0; s < a.S; ++s)
-      if (first_row(a, s + 1) <= first_row(a, s)) {
-        load_state<VEC>(a.start, s, a, b.c, q);
-        store_state<VEC>(a.last, s, a, b.c, q);
+  Backward<T, VEC> b(a, x, y, blockIdx.x);
+  typedef typename Backward<T, VEC>::Raw Raw;
+  const int s = blockIdx.y;
+  const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
+  float q[VEC];
+  load_state<VEC>(a.dcT, s, a, b.c, q);
+  if (lo < hi) {
+    Run r{max(lo, (hi - 1) & ~(kBackward - 1)), hi};
+    Raw raw;
+    float entry[VEC];
+    b.load(b.c, r, raw);
+    b.entry_state(b.c, r.lo, s, lo, entry);
+    for (;;) {
+      const Run next{max(lo, r.lo - kBackward), r.lo};
+      Raw ahead;
+      float entry_ahead[VEC];
+      if (next.hi > lo) {
+        b.load(b.c, next, ahead);
+        b.entry_state(b.c, next.lo, s, lo, entry_ahead);
       }
-  if (lo >= hi) return;
-  int s = sequence_of(a, hi - 1);
-  if (first_row(a, s + 1) == hi) {
-    load_state<VEC>(a.start, s, a, b.c, q);
-  } else {
+      b.maps(r, raw, entry);
+      b.fold(q);
+      b.rows_out(r);
+      if (next.hi <= lo) break;
+      r = next;
+      raw = ahead;
 #pragma unroll
-    for (int v = 0; v < VEC; ++v) q[v] = 0.0f;
-    for (int n = static_cast<int>(gridDim.y) - 1; n > p; --n)
-#pragma unroll
-      for (int v = 0; v < VEC; ++v)
-        if (b.c.on) q[v] = apply_map(a.maps[int64_t(n) * a.H + b.c.ch + v], q[v]);
+      for (int v = 0; v < VEC; ++v) entry[v] = entry_ahead[v];
+    }
   }
-  for (;;) {
-    const int first = first_row(a, s), from = max(first, lo);
-    backward_rows(b, from, hi, s, first, q, unused);
-    if (b.wave == 0 && from == first && from < hi) store_state<VEC>(a.last, s, a, b.c, q);
-    hi = from;
-    if (hi <= lo) break;
-    s = sequence_of(a, hi - 1);
-    load_state<VEC>(a.start, s, a, b.c, q);
-  }
+  if (b.wave == 0) store_state<VEC>(a.last, s, a, b.c, q);
 }
 
 template <class T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_backward_maps(ScanArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void k_scan_backward_tiles(ScanArgs a) {
   __shared__ Exchange<VEC> x, y;
-  Backward<T, VEC, true> b(a, x, y);
-  float q[VEC], A[VEC];
-  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  if (b.wave == 0)
-    for (int s = p; s < a.S; s += gridDim.y) {
-      load_state<VEC>(a.dcT, s, a, b.c, q);
-      store_state<VEC>(a.start, s, a, b.c, q);
-    }
-  const int lo = max(p * a.piece, begin);
-  const int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
+  __shared__ float carry[64 * VEC];
+  __shared__ unsigned next[2];
+  Backward<T, VEC> b(a, x, y, 0);
+  typedef typename Backward<T, VEC>::Raw Raw;
+  const int begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+  Tickets<1> tickets(a, next);
+  auto rows_of = [&](int t) {
+    const int lo = tickets.tile(t) * kBackward;
+    return Run{max(lo, begin), min(lo + kBackward, end)};
+  };
+  tickets.ask();
+  __syncthreads();
+  int t = tickets.answer();
+  tickets.ask();
+  __syncthreads();
+  int after = tickets.answer();
+  Raw raw;
+  if (t < tickets.items) b.load(Channels<VEC>(a, tickets.group(t)), rows_of(t), raw);
+  while (t < tickets.items) {
+    Raw ahead;
+    if (after < tickets.items) b.load(Channels<VEC>(a, tickets.group(after)), rows_of(after), ahead);
+    tickets.ask();
+    const int p = tickets.tile(t);
+    const Run tile = rows_of(t);
+    b.c = Channels<VEC>(a, tickets.group(t));
+    if (tile.lo < tile.hi) {
+      const TileInfo info = a.info[p];
+      // The runs from the first on; the last one may go on behind the tile.
+      for (int lo = tile.lo; lo < tile.hi;) {
+        const int s = lo == tile.lo ? info.s : sequence_of(a, lo);
+        const int first = lo == tile.lo ? info.first : lo;
+        const int to = max(first_row(a, s + 1), lo + 1);
+        const Run r{lo, min(to, tile.hi)};
+        const bool front = lo == tile.lo;                       // the tile before may wait for what this passes on
+        float entry[VEC], q[VEC];
+        const bool goes_on = to > r.hi && r.hi < end;           // the tile behind has rows, and publishes
+        b.entry_state(b.c, lo, s, first, entry);
+        // In front of maps' barriers: behind them a faster wave may write dc0,
+        // which may be dcT.
+        load_state<VEC>(goes_on ? nullptr : a.dcT, s, a, b.c, q);
+        b.maps(r, raw, entry);
+        if (goes_on) {
+          if (b.wave == 0) {
+            if (front) {
+              float A[VEC], B[VEC];
+              b.whole_map(A, B);
+              publish_map<VEC>(a, b.c, p, A, B);
+            }
+            look_back<VEC, 1>(a, b.c, p, q);
 #pragma unroll
-  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, q[v] = 0.0f;
-  if (lo < hi) {
-    // Only the rows up to the end of the sequence that the piece begins in
-    // matter to the pieces in front of it.
-    const int s = sequence_of(a, lo), first = first_row(a, s), to = first_row(a, s + 1);
-    if (first == lo) {
+            for (int v = 0; v < VEC; ++v) carry[b.lane * VEC + v] = q[v];
+          }
+          __syncthreads();
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) A[v] = -1.0f;   // nothing is passed on
-    } else {
-      if (to <= hi) {
-        load_state<VEC>(a.dcT, s, a, b.c, q);
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) A[v] = -1.0f;
+          for (int v = 0; v < VEC; ++v) q[v] = carry[b.lane * VEC + v];
+        }
+        b.fold(q);
+        if (b.wave == 0 && front) publish_state<VEC>(a, b.c, p, q);
+        b.rows_out(r);
+        if (b.wave == 0 && first == lo) store_state<VEC>(a.last, s, a, b.c, q);
+        lo = r.hi;
       }
-      backward_rows(b, lo, min(hi, to), s, first, q, A);
     }
+    __syncthreads();
+    raw = ahead;
+    t = after;
+    after = tickets.answer();
   }
-  if (b.wave == 0 && b.c.on)
-#pragma unroll
-    for (int v = 0; v < VEC; ++v) a.maps[int64_t(p) * a.H + b.c.ch + v] = make_float2(A[v], q[v]);
 }
 
 // ---------------------------------------------------------------------------
@@ -609,7 +804,9 @@ __global__ __launch_bounds__(256) void k_scan_step(const T* gates, int64_t gate_
 // ---------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------
-constexpr int kMostPieces = 256;
+constexpr int64_t kTileBlocks = 512;      // blocks that work through the tiles: two a compute unit
+
+int64_t tiles_of(const soma_scan_config& c, int tile) { return (int64_t(c.rows) + tile - 1) / tile; }
 
 int check_shape(const soma_scan_config* c) {
   if (!c) return set_error(SOMA_EINVAL, "cfg is NULL");
@@ -617,6 +814,7 @@ int check_shape(const soma_scan_config* c) {
   if (c->rows < 0 || c->rows > (1 << 30)) return set_error(SOMA_ESHAPE, "rows must be in [0, 2^30]");
   if (c->width < 1 || c->width > (1 << 20)) return set_error(SOMA_ESHAPE, "width must be in [1, 2^20]");
   if (c->sequences < 1 || c->sequences > 65535) return set_error(SOMA_ESHAPE, "sequences must be in [1, 65535]");
+  if (int64_t(c->rows) * c->width > (int64_t(1) << 40)) return set_error(SOMA_ESHAPE, "rows times width must be at most 2^40");
   if (c->gate_stride < 4 * int64_t(c->width) || c->gate_stride > (int64_t(1) << 32))
     return set_error(SOMA_ESHAPE, "gate_stride must be at least 4 width");
   return SOMA_OK;
@@ -626,32 +824,32 @@ int vec_of(const soma_scan_config& c) { return c.type == SOMA_BFLOAT && c.width 
 
 int groups_of(const soma_scan_config& c, int vec) { return (c.width + 64 * vec - 1) / (64 * vec); }
 
-// Rows of a piece, or 0: split by sequence.  A block for every sequence and
-// group of channels reads its gates once; it is the better way where those
-// blocks fill the card's 256 compute units.  Below that the rows are cut into
-// about 512 blocks' pieces, at least one tile each.
-int piece_rows(const soma_scan_config& c, int vec) {
-  const int groups = groups_of(c, vec);
-  if (int64_t(c.sequences) * groups >= 256) return 0;
-  const int64_t tiles = (int64_t(c.rows) + kTile - 1) / kTile;
-  int64_t pieces = 512 / groups;
-  pieces = pieces < 1 ? 1 : (pieces > kMostPieces ? kMostPieces : pieces);
-  if (pieces <= c.sequences || tiles <= c.sequences) return 0;
-  const int64_t each = (tiles + pieces - 1) / pieces;
-  return static_cast<int>(each * kTile);
+// Whether tiles are dealt out one by one.  A block for every sequence and group of
+// channels needs no words and no other launch, and is the better way where those
+// blocks fill the card's 256 compute units, or where a sequence has a few hundred rows.
+bool by_tiles(const soma_scan_config& c, int vec) {
+  return int64_t(c.sequences) * groups_of(c, vec) < 256 && int64_t(c.rows) > 256 * int64_t(c.sequences);
 }
 
 size_t scan_workspace(const soma_scan_config& c) {
-  return up256(size_t(kMostPieces) * c.width * sizeof(float2)) + up256(size_t(c.sequences) * c.width * sizeof(float));
+  const size_t tiles = size_t(tiles_of(c, kBackward)), words = tiles * c.width;
+  return 256 + up256(tiles * sizeof(TileInfo)) + up256(words * 8) + up256(words * 4);
 }
 
-// The pieces' share of the arguments; returns the grid's second dimension.
-int split(const soma_scan_config& c, int vec, void* ws, ScanArgs* a) {
-  a->piece = piece_rows(c, vec);
-  if (a->piece == 0) return c.sequences;
-  a->maps = static_cast<float2*>(ws);
-  a->start = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(size_t(kMostPieces) * c.width * sizeof(float2)));
-  return (c.rows + a->piece - 1) / a->piece;
+// The workspace's parts, cleared.  `from`: the states that empty sequences keep.
+int begin_tiles(const soma_scan_config& c, int vec, int tile, void* ws, const float* from, ScanArgs* a, hipStream_t st) {
+  char* at = static_cast<char*>(ws);
+  const size_t tiles = size_t(tiles_of(c, tile)), words = tiles * c.width;
+  a->tile = tile;
+  a->tiles = int(tiles);
+  a->groups = groups_of(c, vec);
+  a->ticket = reinterpret_cast<unsigned*>(at);
+  a->info = reinterpret_cast<TileInfo*>(at + 256);
+  a->maps = reinterpret_cast<uint64_t*>(at + 256 + up256(tiles * sizeof(TileInfo)));
+  a->tile_state = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a->maps) + up256(words * 8));
+  const size_t blocks = std::min<size_t>((std::max(words, size_t(c.sequences) * c.width) + 255) / 256, 2048);
+  hipLaunchKernelGGL(k_scan_begin, dim3(unsigned(blocks)), dim3(256), 0, st, *a, from);
+  return launched("k_scan_begin");
 }
 
 int fill(const soma_scan_config& c, const void* gates, const int32_t* offsets, const float* c0, ScanArgs* a) {
@@ -699,17 +897,21 @@ int soma_scan_forward(const soma_scan_config* cfg, const void* gates, const int3
   a.last = cT;
   a.states = states;
   const int vec = vec_of(c) == 2 && is_aligned(gates, 4) && is_aligned(h, 4) ? 2 : 1;
-  const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
+  const dim3 block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
-  if (a.piece) {
+  if (by_tiles(c, vec)) {
+    if (int rc = begin_tiles(c, vec, kForward, workspace, c0, &a, st)) return rc;
+    const dim3 grid(unsigned(std::min<int64_t>(int64_t(a.tiles) * a.groups, kTileBlocks)));
     if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_forward_maps<float, 1>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_forward_tiles<float, 1>), grid, block, 0, st, a);
     else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 2>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_forward_tiles<bf16, 2>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_forward_maps")) return rc;
+      hipLaunchKernelGGL((k_scan_forward_tiles<bf16, 1>), grid, block, 0, st, a);
+    if (int rc = launched("k_scan_forward_tiles")) return rc;
+    return set_ok();
   }
+  const dim3 grid(groups_of(c, vec), c.sequences);
   if (c.type == SOMA_FLOAT)
     hipLaunchKernelGGL((k_scan_forward<float, 1>), grid, block, 0, st, a);
   else if (vec == 2)
@@ -741,17 +943,21 @@ int soma_scan_backward(const soma_scan_config* cfg, const void* gates, const int
   a.states = const_cast<float*>(states);
   const int vec =
       vec_of(c) == 2 && is_aligned(gates, 4) && is_aligned(dh, 4) && is_aligned(dgates, 4) ? 2 : 1;
-  const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
+  const dim3 block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
-  if (a.piece) {
+  if (by_tiles(c, vec)) {
+    if (int rc = begin_tiles(c, vec, kBackward, workspace, dcT, &a, st)) return rc;
+    const dim3 grid(unsigned(std::min<int64_t>(int64_t(a.tiles) * a.groups, kTileBlocks)));
     if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_backward_maps<float, 1>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_backward_tiles<float, 1>), grid, block, 0, st, a);
     else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 2>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_backward_tiles<bf16, 2>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_backward_maps")) return rc;
+      hipLaunchKernelGGL((k_scan_backward_tiles<bf16, 1>), grid, block, 0, st, a);
+    if (int rc = launched("k_scan_backward_tiles")) return rc;
+    return set_ok();
   }
+  const dim3 grid(groups_of(c, vec), c.sequences);
   if (c.type == SOMA_FLOAT)
     hipLaunchKernelGGL((k_scan_backward<float, 1>), grid, block, 0, st, a);
   else if (vec == 2)

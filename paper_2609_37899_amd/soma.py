@@ -79,7 +79,7 @@ class Config(ctypes.Structure):
 
 
 TYPE_FLOAT, TYPE_BFLOAT = 0, 1
-SCAN_BLOCK = 64             # rows between the states that a backward scan starts from
+SCAN_BLOCK = 32             # rows between the states that a backward scan starts from
 ADAMW_BLOCK = 256           # elements that share the scales of 8-bit moments
 
 
