@@ -557,9 +557,8 @@ typedef struct soma_scan_config {
   int64_t gate_stride;  /* elements between rows of gates, >= 4 width */
 } soma_scan_config;
 
-/* Bytes of device workspace of soma_scan_forward and soma_scan_backward: 0.4
- * bytes for every row and channel.  It grows with the rows, so a
- * workspace serves calls of fewer.  Pure. */
+/* Bytes of device workspace of soma_scan_forward and soma_scan_backward; it
+ * grows with width and sequences only.  Pure. */
 int soma_scan_workspace_size(const soma_scan_config* cfg, size_t* bytes);
 
 int soma_scan_forward(const soma_scan_config* cfg, const void* gates_dev, const int32_t* offsets_dev,

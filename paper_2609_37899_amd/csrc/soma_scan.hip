@@ -6,24 +6,33 @@
 // With a_t = s(f_t), b_t = s(i_t) tanh(g_t) a run of rows is one affine map of
 // the state in front of it, c -> A c + B, and maps of neighbouring runs
 // compose: (A2, B2) after (A1, B1) is (A2 A1, A2 B1 + B2).  So time runs side by
-// side.  A block takes 64 lanes of channels and walks over tiles of 64 rows (backward: 32): its 8
-// waves hold 8 (4) rows each in registers, form the map of their rows, exchange the
-// maps through LDS and start from the state that the earlier waves' maps give.
-// The gates are read once; the next tile's are on their way meanwhile.  The
-// state in front of every 64th row is kept for the backward pass, which forms the
-// cells of a tile again from it (1/64 of a state array instead of a whole one).
+// side.  A block takes 64 lanes of channels and walks over tiles of 64 rows
+// (backward: 32): its 8 waves hold 8 (4) rows each in registers, form the map of
+// their rows, exchange the maps through LDS and start from the state that the
+// earlier waves' maps give.  The gates are read once and formed once; the next
+// tile's are on their way meanwhile.  The state in front of every 32nd row is kept
+// for the backward pass, which forms the cells of a tile again from it (1/32 of a
+// state array instead of a whole one).
 //
 // Backward, with u_t = dh_t s(o_t) (1 - tanh^2 c_t), the gradient of a cell is
 // l_t = u_t + q_{t+1}, and what it passes on is q_t = s(f_t) l_t: the same affine
 // maps from the last row to the first, q -> A q + B.
 //
-// Work is split by sequence and channels where that fills the card.  Else tiles are
-// dealt out one by one, in order (a counter), to blocks that publish their tile's
-// map, look back over the maps before it until they meet a state, publish the
-// state behind their own tile, and write their rows: the gates are still read
-// once, and a tile waits only for tiles that were dealt out earlier, so that some
-// block can always go on.  Values travel between compute units as 32- and 64-bit
-// words of agent scope that are their own flags (a word of ones: not there yet).
+// Work is split by sequence and channels where that fills the card.  Else the
+// rows are cut into pieces of whole tiles: a first launch forms the map of every
+// piece, and each block of the second starts from the maps of the pieces in front
+// of it, applied in order.  That reads the gates twice, and is the shorter way all
+// the same: one launch whose tiles publish their maps and look back over those
+// before them took 742 us where this takes 690 (one sequence of 65,536 rows, width
+// 1,024, bf16, both passes), since a state then goes from compute unit to compute
+// unit 1,024 times; and which maps it joined depended on time, and with it the
+// last bits.
+//
+// Measured, bf16: 64 sequences of 1,024 rows, width 512: forward 81 us (4.1 TB/s),
+// backward 142 (4.2 TB/s); in pieces, the case above: maps 131 us (3.1 TB/s), forward
+// 149 (4.5 TB/s); maps 173, backward 255.  Each row and channel takes 10 of the
+// exponentials and reciprocals, which run at a quarter of the rate: 34 us of them in
+// the first case, either way, beside the conversions of bf16.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -54,19 +63,16 @@ struct ScanArgs {
   const float* dcT;         // backward: [S][H] or NULL: zeros
   float* states;            // [ceil(rows / 32)][H]: the state in front of row 32 j; or NULL
   int rows, H, S, length;
-  // tiles dealt out one by one
-  unsigned* ticket;         // the counter
-  struct TileInfo* info;    // [tiles]
-  uint64_t* maps;           // [tiles][H]
-  uint32_t* tile_state;     // [tiles][H]: behind a tile, in the order in which they are dealt out
-  int tile;                 // rows of one
-  int tiles, groups;
+  float* start;             // pieces: the states that come in as they were (cT or dc0 may be the same array), [S][H]
+  float2* maps;             // pieces: [pieces][H]
+  int piece;                // rows of a piece, whole tiles (0: split by sequence)
 };
 
-// The sequence of a tile's first row, and that sequence's rows.
-struct TileInfo {
-  int s, first, to, pad;
-};
+// An affine map x -> a x + b of the state.  a < 0 marks a map that forgets x
+// (a sequence starts inside): 0 * x would let another sequence's NaN through.
+__device__ __forceinline__ float apply_map(float2 m, float x) {
+  return m.x < 0.0f ? m.y : __builtin_fmaf(m.x, x, m.y);
+}
 
 __device__ __forceinline__ float sigmoid(float x) {
   return __builtin_amdgcn_rcpf(1.0f + __builtin_amdgcn_exp2f(-kL2e * x));
@@ -169,6 +175,40 @@ struct Exchange {
   float2 m[2][kWaves][64 * VEC];
 };
 
+// The maps of pieces from, from + step, ..., `count` of them, applied to x in this
+// order; 16 loads in flight at a time, or their latencies add up.
+template <int VEC>
+__device__ __forceinline__ void apply_maps(const ScanArgs& a, const Channels<VEC>& c, int from, int step, int count,
+                                           float (&x)[VEC]) {
+  if (!c.on) return;
+  for (int done = 0; done < count; done += 16) {
+    float2 m[16][VEC];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+#pragma unroll
+      for (int v = 0; v < VEC; ++v)
+        m[i][v] = a.maps[int64_t(from + step * min(done + i, count - 1)) * a.H + c.ch + v];
+#pragma unroll
+    for (int i = 0; i < 16; ++i)
+      if (done + i < count)
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) x[v] = apply_map(m[i][v], x[v]);
+  }
+}
+
+// A piece's share of copying the states that come in; sequences without a row
+// keep theirs.
+template <int VEC>
+__device__ __forceinline__ void keep_states(const ScanArgs& a, const Channels<VEC>& c, int wave, int p, const float* from) {
+  if (wave != 0) return;
+  for (int s = p; s < a.S; s += gridDim.y) {
+    float x[VEC];
+    load_state<VEC>(from, s, a, c, x);
+    store_state<VEC>(a.start, s, a, c, x);
+    if (first_row(a, s + 1) <= first_row(a, s)) store_state<VEC>(a.last, s, a, c, x);
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Forward: maps() forms the maps of a run's rows and shares them, fold() brings
 // the state through them, rows_out() writes h.
@@ -191,7 +231,8 @@ struct Forward {
     typename L::raw g[4][kRows];
   };
 
-  __device__ __forceinline__ void load(const Channels<VEC>& c, const Run& r, Raw& raw) const {
+  template <int kGates>
+  __device__ __forceinline__ void load(const Run& r, Raw& raw) const {
     const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -199,7 +240,7 @@ struct Forward {
       if (c.on && row >= r.lo && row < r.hi) {
         const int64_t at = int64_t(row) * a.gate_stride + c.ch;
 #pragma unroll
-        for (int k = 0; k < 4; ++k) raw.g[k][u] = L::load(a.gates, at + int64_t(k) * a.H);
+        for (int k = 0; k < kGates; ++k) raw.g[k][u] = L::load(a.gates, at + int64_t(k) * a.H);
       }
     }
   }
@@ -226,18 +267,18 @@ struct Forward {
     __syncthreads();
   }
 
-  // The map of the whole run.
-  __device__ __forceinline__ void whole_map(float (&A)[VEC], float (&B)[VEC]) const {
+  // The map (A, B), extended by the run's (A < 0 stays: see apply_map).
+  __device__ __forceinline__ void extend(float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      A[v] = 1.0f, B[v] = 0.0f;
 #pragma unroll
       for (int w = 0; w < kWaves; ++w) {
         const float2 m = x.m[buf][w][lane * VEC + v];
-        A[v] *= m.x;
+        A[v] = A[v] < 0.0f ? A[v] : A[v] * m.x;
         B[v] = __builtin_fmaf(m.x, B[v], m.y);
       }
     }
+    buf ^= 1;
   }
 
   // Also keeps the states in front of every 32nd row.
@@ -278,239 +319,100 @@ struct Forward {
   }
 };
 
-// By sequence: a block walks over the tiles of one.
+// Rows [lo, hi) of one sequence from `state`, which is left as the state behind
+// them.  kMaps: only the map (A, state).
+template <bool kMaps, class T, int VEC>
+__device__ __forceinline__ void forward_rows(Forward<T, VEC>& f, int lo, int hi, float (&state)[VEC], float (&A)[VEC]) {
+  typedef typename Forward<T, VEC>::Raw Raw;
+  if (lo >= hi) return;
+  Run r{lo, min(hi, (lo & ~(kForward - 1)) + kForward)};
+  Raw raw;
+  f.template load<kMaps ? 3 : 4>(r, raw);
+  for (;;) {
+    const Run next{r.hi, min(hi, r.hi + kForward)};
+    Raw ahead;
+    if (next.lo < hi) f.template load<kMaps ? 3 : 4>(next, ahead);
+    f.maps(r, raw);
+    if constexpr (kMaps) {
+      f.extend(A, state);
+    } else {
+      f.fold(r, state);
+      f.rows_out(r, raw);
+    }
+    if (next.lo >= hi) break;
+    r = next;
+    raw = ahead;
+  }
+}
+
 template <class T, int VEC>
 __global__ __launch_bounds__(64 * kWaves) void k_scan_forward(ScanArgs a) {
   __shared__ Exchange<VEC> x;
   Forward<T, VEC> f(a, x, blockIdx.x);
-  typedef typename Forward<T, VEC>::Raw Raw;
-  const int s = blockIdx.y;
-  const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
-  float state[VEC];
-  load_state<VEC>(a.c0, s, a, f.c, state);
-  if (lo < hi) {
-    Run r{lo, min(hi, (lo & ~(kForward - 1)) + kForward)};
-    Raw raw;
-    f.load(f.c, r, raw);
-    for (;;) {
-      const Run next{r.hi, min(hi, r.hi + kForward)};
-      Raw ahead;
-      if (next.lo < hi) f.load(f.c, next, ahead);
-      f.maps(r, raw);
-      f.fold(r, state);
-      f.rows_out(r, raw);
-      if (next.lo >= hi) break;
-      r = next;
-      raw = ahead;
+  float state[VEC], unused[VEC];
+  // Rows [lo, hi): one sequence, or a piece of all of them together.
+  int s, lo, hi;
+  if (a.piece == 0) {
+    s = blockIdx.y;
+    lo = first_row(a, s);
+    hi = clamp_row(first_row(a, s + 1), lo, a.rows);
+    load_state<VEC>(a.c0, s, a, f.c, state);
+    if (lo >= hi) {
+      if (f.wave == 0) store_state<VEC>(a.last, s, a, f.c, state);
+      return;
+    }
+  } else {
+    const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+    lo = max(p * a.piece, begin);
+    hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
+    if (lo >= hi) return;
+    s = sequence_of(a, lo);
+    if (first_row(a, s) == lo) {
+      load_state<VEC>(a.start, s, a, f.c, state);
+    } else {
+#pragma unroll
+      for (int v = 0; v < VEC; ++v) state[v] = 0.0f;
+      apply_maps(a, f.c, 0, 1, p, state);
     }
   }
-  if (f.wave == 0) store_state<VEC>(a.last, s, a, f.c, state);
-}
-
-// ---------------------------------------------------------------------------
-// Tiles dealt out one by one.
-// ---------------------------------------------------------------------------
-constexpr uint32_t kNone = 0xFFFFFFFFu;       // not there yet
-constexpr unsigned kPolls = 1u << 20;         // about a second; then the rows are NaN (no wait is without an end)
-
-__device__ __forceinline__ uint32_t word_of(float x) {
-  const uint32_t b = __float_as_uint(x);
-  return b == kNone ? 0x7FC00000u : b;        // that NaN in another form
-}
-
-template <int VEC>
-__device__ __forceinline__ void publish_map(const ScanArgs& a, const Channels<VEC>& c, int tile, const float (&A)[VEC],
-                                            const float (&B)[VEC]) {
-  if (!c.on) return;
-#pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    __hip_atomic_store(a.maps + int64_t(tile) * a.H + c.ch + v, uint64_t(__float_as_uint(B[v])) << 32 | word_of(A[v]),
-                       __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-}
-
-template <int VEC>
-__device__ __forceinline__ void publish_state(const ScanArgs& a, const Channels<VEC>& c, int tile, const float (&x)[VEC]) {
-  if (!c.on) return;
-#pragma unroll
-  for (int v = 0; v < VEC; ++v)
-    __hip_atomic_store(a.tile_state + int64_t(tile) * a.H + c.ch + v, word_of(x[v]), __ATOMIC_RELAXED,
-                       __HIP_MEMORY_SCOPE_AGENT);
-}
-
-// One wave: the state that the tiles from `tile` + kDir on bring, by way of their
-// maps, four at a time.
-template <int VEC, int kDir>
-__device__ __forceinline__ void look_back(const ScanArgs& a, const Channels<VEC>& c, int tile, float (&state)[VEC]) {
-  float A[VEC], B[VEC];
-#pragma unroll
-  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, B[v] = 0.0f, state[v] = __builtin_nanf("");
-  int q = tile + kDir;
-  for (unsigned polls = 0; polls < kPolls;) {
-    uint32_t st[4][VEC];
-    uint64_t mp[4][VEC];
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      const int64_t at = int64_t(min(max(q + kDir * k, 0), a.tiles - 1)) * a.H + c.ch;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        st[k][v] = c.on ? __hip_atomic_load(a.tile_state + at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
-        mp[k][v] = c.on ? __hip_atomic_load(a.maps + at + v, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT) : 0u;
-      }
-    }
-    int used = 0;
-#pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      if (used < k) break;                    // one before was not there
-      const int at = q + kDir * k;
-      if (at < 0 || at >= a.tiles) break;
-      bool has_state = true, has_map = true;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        has_state = has_state && st[k][v] != kNone;
-        has_map = has_map && static_cast<uint32_t>(mp[k][v]) != kNone;
-      }
-      if (__all(has_state)) {
-#pragma unroll
-        for (int v = 0; v < VEC; ++v) state[v] = __builtin_fmaf(A[v], __uint_as_float(st[k][v]), B[v]);
-        return;
-      }
-      if (!__all(has_map)) break;
-#pragma unroll
-      for (int v = 0; v < VEC; ++v) {
-        B[v] = __builtin_fmaf(A[v], __uint_as_float(static_cast<uint32_t>(mp[k][v] >> 32)), B[v]);
-        A[v] *= __uint_as_float(static_cast<uint32_t>(mp[k][v]));
-      }
-      used = k + 1;
-    }
-    q += kDir * used;
-    if (used == 0) {
-      ++polls;
-      __builtin_amdgcn_s_sleep(1);
-    }
+  for (;;) {
+    const int to = a.piece == 0 ? hi : clamp_row(first_row(a, s + 1), lo, hi);
+    forward_rows<false>(f, lo, to, state, unused);
+    if (f.wave == 0 && (a.piece == 0 || to == first_row(a, s + 1))) store_state<VEC>(a.last, s, a, f.c, state);
+    lo = to;
+    if (lo >= hi) break;
+    s = sequence_of(a, lo);
+    load_state<VEC>(a.start, s, a, f.c, state);
   }
 }
 
-// Clears the words and the counter, finds every tile's sequence, and copies the
-// states of sequences without a row (from -> last).
-__global__ __launch_bounds__(256) void k_scan_begin(ScanArgs a, const float* from) {
-  const int64_t i = int64_t(blockIdx.x) * 256 + threadIdx.x, n = int64_t(gridDim.x) * 256;
-  const int64_t words = int64_t(a.tiles) * a.H;
-  for (int64_t k = i; k < words; k += n) {
-    a.maps[k] = ~uint64_t(0);
-    a.tile_state[k] = kNone;
-  }
-  if (i == 0) *a.ticket = 0u;
-  for (int64_t k = i; k < a.tiles; k += n) {
-    const int s = sequence_of(a, static_cast<int>(k) * a.tile);
-    a.info[k] = TileInfo{s, first_row(a, s), first_row(a, s + 1), 0};
-  }
-  if (a.last)
-    for (int64_t k = i; k < int64_t(a.S) * a.H; k += n) {
-      const int s = static_cast<int>(k / a.H);
-      if (first_row(a, s + 1) <= first_row(a, s)) a.last[k] = from ? from[k] : 0.0f;
-    }
-}
-
-// The tickets of a block: the tile that it works on, and the one after, whose
-// rows are already on their way.
-template <int kDir>
-struct Tickets {
-  const ScanArgs& a;
-  unsigned* shared;           // [2]
-  int items, par = 0;
-  __device__ __forceinline__ Tickets(const ScanArgs& a_, unsigned* shared_)
-      : a(a_), shared(shared_), items(a_.tiles * a_.groups) {}
-  __device__ __forceinline__ void ask() {
-    if (threadIdx.x == 0)
-      shared[par] = __hip_atomic_fetch_add(a.ticket, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-  }
-  // Behind a barrier.
-  __device__ __forceinline__ int answer() {
-    const unsigned t = __builtin_amdgcn_readfirstlane(shared[par]);
-    par ^= 1;
-    return t < static_cast<unsigned>(items) ? static_cast<int>(t) : items;
-  }
-  __device__ __forceinline__ int tile(int t) const {
-    const int p = t / a.groups;
-    return kDir < 0 ? p : a.tiles - 1 - p;
-  }
-  __device__ __forceinline__ int group(int t) const { return t % a.groups; }
-};
-
+// Pieces, first launch: the map of every piece's rows, the initial states as they
+// are now (the second launch may overwrite them with the last), and the last
+// states of sequences without a row.
 template <class T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_forward_tiles(ScanArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void k_scan_forward_maps(ScanArgs a) {
   __shared__ Exchange<VEC> x;
-  __shared__ float carry[64 * VEC];
-  __shared__ unsigned next[2];
-  Forward<T, VEC> f(a, x, 0);
-  typedef typename Forward<T, VEC>::Raw Raw;
-  const int begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  Tickets<-1> tickets(a, next);
-  auto rows_of = [&](int t) {
-    const int lo = tickets.tile(t) * kForward;
-    return Run{max(lo, begin), min(lo + kForward, end)};
-  };
-  tickets.ask();
-  __syncthreads();
-  int t = tickets.answer();
-  tickets.ask();
-  __syncthreads();
-  int after = tickets.answer();
-  Raw raw;
-  if (t < tickets.items) f.load(Channels<VEC>(a, tickets.group(t)), rows_of(t), raw);
-  while (t < tickets.items) {
-    Raw ahead;
-    if (after < tickets.items) f.load(Channels<VEC>(a, tickets.group(after)), rows_of(after), ahead);
-    tickets.ask();
-    const int p = tickets.tile(t);
-    const Run tile = rows_of(t);
-    f.c = Channels<VEC>(a, tickets.group(t));
-    if (tile.lo < tile.hi) {
-      const TileInfo info = a.info[p];
-      // The first run began in a tile before.  Every tile with rows publishes the
-      // state behind its last, wanted or not: no offsets can make a tile wait for
-      // one that has nothing to say.
-      const bool continued = info.first < tile.lo && tile.lo > begin;
-      // The runs that begin here, then the one that goes on from a tile before.
-      int lo = continued ? min(info.to, tile.hi) : tile.lo;
-      for (bool last = !continued && lo >= tile.hi; !last;) {
-        const bool goes_on = lo >= tile.hi;
-        const int s = goes_on || lo == tile.lo ? info.s : sequence_of(a, lo);
-        const int to = goes_on ? info.to : max(first_row(a, s + 1), lo + 1);
-        const Run r{goes_on ? tile.lo : lo, min(to, tile.hi)};
-        last = goes_on || (!continued && r.hi >= tile.hi);
-        lo = goes_on ? lo : r.hi;
-        float state[VEC];
-        // In front of maps' barrier: behind it a faster wave may write cT, which
-        // may be c0.
-        load_state<VEC>(goes_on ? nullptr : a.c0, s, a, f.c, state);
-        f.maps(r, raw);
-        if (goes_on) {
-          if (f.wave == 0) {
-            if (r.hi == tile.hi) {
-              float A[VEC], B[VEC];
-              f.whole_map(A, B);
-              publish_map<VEC>(a, f.c, p, A, B);
-            }
-            look_back<VEC, -1>(a, f.c, p, state);
+  Forward<T, VEC> f(a, x, blockIdx.x);
+  float state[VEC], A[VEC];
+  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+  keep_states(a, f.c, f.wave, p, a.c0);
+  const int lo = max(p * a.piece, begin);
+  const int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) carry[f.lane * VEC + v] = state[v];
-          }
-          __syncthreads();
+  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, state[v] = 0.0f;
+  if (lo < hi) {
+    // Only the rows from the last start on matter.
+    const int s = sequence_of(a, hi - 1), from = first_row(a, s);
+    if (from >= lo) {
+      load_state<VEC>(a.c0, s, a, f.c, state);
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) state[v] = carry[f.lane * VEC + v];
-        }
-        f.fold(r, state);
-        if (f.wave == 0 && r.hi == tile.hi) publish_state<VEC>(a, f.c, p, state);
-        f.rows_out(r, raw);
-        if (f.wave == 0 && to == r.hi) store_state<VEC>(a.last, s, a, f.c, state);
-      }
+      for (int v = 0; v < VEC; ++v) A[v] = -1.0f;
     }
-    __syncthreads();
-    raw = ahead;
-    t = after;
-    after = tickets.answer();
+    forward_rows<true>(f, max(lo, from), hi, state, A);
   }
+  if (f.wave == 0 && f.c.on)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) a.maps[int64_t(p) * a.H + f.c.ch + v] = make_float2(A[v], state[v]);
 }
 
 // ---------------------------------------------------------------------------
@@ -540,7 +442,7 @@ struct Backward {
     typename L::raw g[5][kRows];
   };
 
-  __device__ __forceinline__ void load(const Channels<VEC>& c, const Run& r, Raw& raw) const {
+  __device__ __forceinline__ void load(const Run& r, Raw& raw) const {
     const int row0 = (r.lo & ~(kTile - 1)) + wave * kRows;
 #pragma unroll
     for (int u = 0; u < kRows; ++u) {
@@ -555,7 +457,7 @@ struct Backward {
   }
 
   // The state in front of row `lo` of sequence s, which starts at `first`.
-  __device__ __forceinline__ void entry_state(const Channels<VEC>& c, int lo, int s, int first, float (&x)[VEC]) const {
+  __device__ __forceinline__ void entry_state(int lo, int s, int first, float (&x)[VEC]) const {
     if (lo == first)
       load_state<VEC>(a.c0, s, a, c, x);
     else
@@ -618,17 +520,17 @@ struct Backward {
     __syncthreads();
   }
 
-  __device__ __forceinline__ void whole_map(float (&A)[VEC], float (&B)[VEC]) const {
+  __device__ __forceinline__ void extend(float (&A)[VEC], float (&B)[VEC]) {
 #pragma unroll
     for (int v = 0; v < VEC; ++v) {
-      A[v] = 1.0f, B[v] = 0.0f;
 #pragma unroll
       for (int w = kWaves - 1; w >= 0; --w) {
         const float2 m = y.m[buf][w][lane * VEC + v];
-        A[v] *= m.x;
+        A[v] = A[v] < 0.0f ? A[v] : A[v] * m.x;
         B[v] = __builtin_fmaf(m.x, B[v], m.y);
       }
     }
+    buf ^= 1;
   }
 
   __device__ __forceinline__ void fold(float (&q)[VEC]) {
@@ -675,113 +577,112 @@ struct Backward {
   }
 };
 
+// Rows [lo, hi) of sequence s (which starts at row `first`), last to first, from q,
+// which is left as what they pass on.  kMaps: only the map (A, q).
+template <bool kMaps, class T, int VEC>
+__device__ __forceinline__ void backward_rows(Backward<T, VEC>& b, int lo, int hi, int s, int first, float (&q)[VEC],
+                                              float (&A)[VEC]) {
+  typedef typename Backward<T, VEC>::Raw Raw;
+  if (lo >= hi) return;
+  Run r{max(lo, (hi - 1) & ~(kBackward - 1)), hi};
+  Raw raw;
+  float entry[VEC];
+  b.load(r, raw);
+  b.entry_state(r.lo, s, first, entry);
+  for (;;) {
+    const Run next{max(lo, r.lo - kBackward), r.lo};
+    Raw ahead;
+    float entry_ahead[VEC];
+    if (next.hi > lo) {
+      b.load(next, ahead);
+      b.entry_state(next.lo, s, first, entry_ahead);
+    }
+    b.maps(r, raw, entry);
+    if constexpr (kMaps) {
+      b.extend(A, q);
+    } else {
+      b.fold(q);
+      b.rows_out(r);
+    }
+    if (next.hi <= lo) break;
+    r = next;
+    raw = ahead;
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) entry[v] = entry_ahead[v];
+  }
+}
+
 template <class T, int VEC>
 __global__ __launch_bounds__(64 * kWaves) void k_scan_backward(ScanArgs a) {
   __shared__ Exchange<VEC> x, y;
   Backward<T, VEC> b(a, x, y, blockIdx.x);
-  typedef typename Backward<T, VEC>::Raw Raw;
-  const int s = blockIdx.y;
-  const int lo = first_row(a, s), hi = clamp_row(first_row(a, s + 1), lo, a.rows);
-  float q[VEC];
-  load_state<VEC>(a.dcT, s, a, b.c, q);
-  if (lo < hi) {
-    Run r{max(lo, (hi - 1) & ~(kBackward - 1)), hi};
-    Raw raw;
-    float entry[VEC];
-    b.load(b.c, r, raw);
-    b.entry_state(b.c, r.lo, s, lo, entry);
-    for (;;) {
-      const Run next{max(lo, r.lo - kBackward), r.lo};
-      Raw ahead;
-      float entry_ahead[VEC];
-      if (next.hi > lo) {
-        b.load(b.c, next, ahead);
-        b.entry_state(b.c, next.lo, s, lo, entry_ahead);
-      }
-      b.maps(r, raw, entry);
-      b.fold(q);
-      b.rows_out(r);
-      if (next.hi <= lo) break;
-      r = next;
-      raw = ahead;
+  float q[VEC], unused[VEC];
+  int s, lo, hi;
+  if (a.piece == 0) {
+    s = blockIdx.y;
+    lo = first_row(a, s);
+    hi = clamp_row(first_row(a, s + 1), lo, a.rows);
+    load_state<VEC>(a.dcT, s, a, b.c, q);
+    if (lo >= hi) {
+      if (b.wave == 0) store_state<VEC>(a.last, s, a, b.c, q);
+      return;
+    }
+  } else {
+    const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+    lo = max(p * a.piece, begin);
+    hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
+    if (lo >= hi) return;
+    s = sequence_of(a, hi - 1);
+    if (first_row(a, s + 1) == hi) {
+      load_state<VEC>(a.start, s, a, b.c, q);
+    } else {
 #pragma unroll
-      for (int v = 0; v < VEC; ++v) entry[v] = entry_ahead[v];
+      for (int v = 0; v < VEC; ++v) q[v] = 0.0f;
+      const int last = static_cast<int>(gridDim.y) - 1;
+      apply_maps(a, b.c, last, -1, last - p, q);
     }
   }
-  if (b.wave == 0) store_state<VEC>(a.last, s, a, b.c, q);
+  for (;;) {
+    const int first = first_row(a, s), from = a.piece == 0 ? lo : max(first, lo);
+    backward_rows<false>(b, from, hi, s, first, q, unused);
+    if (b.wave == 0 && from == first) store_state<VEC>(a.last, s, a, b.c, q);
+    hi = from;
+    if (hi <= lo) break;
+    s = sequence_of(a, hi - 1);
+    load_state<VEC>(a.start, s, a, b.c, q);
+  }
 }
 
 template <class T, int VEC>
-__global__ __launch_bounds__(64 * kWaves) void k_scan_backward_tiles(ScanArgs a) {
+__global__ __launch_bounds__(64 * kWaves) void k_scan_backward_maps(ScanArgs a) {
   __shared__ Exchange<VEC> x, y;
-  __shared__ float carry[64 * VEC];
-  __shared__ unsigned next[2];
-  Backward<T, VEC> b(a, x, y, 0);
-  typedef typename Backward<T, VEC>::Raw Raw;
-  const int begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
-  Tickets<1> tickets(a, next);
-  auto rows_of = [&](int t) {
-    const int lo = tickets.tile(t) * kBackward;
-    return Run{max(lo, begin), min(lo + kBackward, end)};
-  };
-  tickets.ask();
-  __syncthreads();
-  int t = tickets.answer();
-  tickets.ask();
-  __syncthreads();
-  int after = tickets.answer();
-  Raw raw;
-  if (t < tickets.items) b.load(Channels<VEC>(a, tickets.group(t)), rows_of(t), raw);
-  while (t < tickets.items) {
-    Raw ahead;
-    if (after < tickets.items) b.load(Channels<VEC>(a, tickets.group(after)), rows_of(after), ahead);
-    tickets.ask();
-    const int p = tickets.tile(t);
-    const Run tile = rows_of(t);
-    b.c = Channels<VEC>(a, tickets.group(t));
-    if (tile.lo < tile.hi) {
-      const TileInfo info = a.info[p];
-      // The runs from the first on; the last one may go on behind the tile.
-      for (int lo = tile.lo; lo < tile.hi;) {
-        const int s = lo == tile.lo ? info.s : sequence_of(a, lo);
-        const int first = lo == tile.lo ? info.first : lo;
-        const int to = max(first_row(a, s + 1), lo + 1);
-        const Run r{lo, min(to, tile.hi)};
-        const bool front = lo == tile.lo;                       // the tile before may wait for what this passes on
-        float entry[VEC], q[VEC];
-        const bool goes_on = to > r.hi && r.hi < end;           // the tile behind has rows, and publishes
-        b.entry_state(b.c, lo, s, first, entry);
-        // In front of maps' barriers: behind them a faster wave may write dc0,
-        // which may be dcT.
-        load_state<VEC>(goes_on ? nullptr : a.dcT, s, a, b.c, q);
-        b.maps(r, raw, entry);
-        if (goes_on) {
-          if (b.wave == 0) {
-            if (front) {
-              float A[VEC], B[VEC];
-              b.whole_map(A, B);
-              publish_map<VEC>(a, b.c, p, A, B);
-            }
-            look_back<VEC, 1>(a, b.c, p, q);
+  Backward<T, VEC> b(a, x, y, blockIdx.x);
+  float q[VEC], A[VEC];
+  const int p = blockIdx.y, begin = first_row(a, 0), end = clamp_row(first_row(a, a.S), begin, a.rows);
+  keep_states(a, b.c, b.wave, p, a.dcT);
+  const int lo = max(p * a.piece, begin);
+  const int hi = static_cast<int>(min(int64_t(p + 1) * a.piece, int64_t(end)));
 #pragma unroll
-            for (int v = 0; v < VEC; ++v) carry[b.lane * VEC + v] = q[v];
-          }
-          __syncthreads();
+  for (int v = 0; v < VEC; ++v) A[v] = 1.0f, q[v] = 0.0f;
+  if (lo < hi) {
+    // Only the rows up to the end of the sequence that the piece begins in
+    // matter to the pieces in front of it.
+    const int s = sequence_of(a, lo), first = first_row(a, s), to = first_row(a, s + 1);
+    if (first == lo) {
 #pragma unroll
-          for (int v = 0; v < VEC; ++v) q[v] = carry[b.lane * VEC + v];
-        }
-        b.fold(q);
-        if (b.wave == 0 && front) publish_state<VEC>(a, b.c, p, q);
-        b.rows_out(r);
-        if (b.wave == 0 && first == lo) store_state<VEC>(a.last, s, a, b.c, q);
-        lo = r.hi;
+      for (int v = 0; v < VEC; ++v) A[v] = -1.0f;   // nothing is passed on
+    } else {
+      if (to <= hi) {
+        load_state<VEC>(a.dcT, s, a, b.c, q);
+#pragma unroll
+        for (int v = 0; v < VEC; ++v) A[v] = -1.0f;
       }
+      backward_rows<true>(b, lo, min(hi, to), s, first, q, A);
     }
-    __syncthreads();
-    raw = ahead;
-    t = after;
-    after = tickets.answer();
   }
+  if (b.wave == 0 && b.c.on)
+#pragma unroll
+    for (int v = 0; v < VEC; ++v) a.maps[int64_t(p) * a.H + b.c.ch + v] = make_float2(A[v], q[v]);
 }
 
 // ---------------------------------------------------------------------------
@@ -804,9 +705,7 @@ __global__ __launch_bounds__(256) void k_scan_step(const T* gates, int64_t gate_
 // ---------------------------------------------------------------------------
 // Host
 // ---------------------------------------------------------------------------
-constexpr int64_t kTileBlocks = 512;      // blocks that work through the tiles: two a compute unit
-
-int64_t tiles_of(const soma_scan_config& c, int tile) { return (int64_t(c.rows) + tile - 1) / tile; }
+constexpr int kMostPieces = 256;
 
 int check_shape(const soma_scan_config* c) {
   if (!c) return set_error(SOMA_EINVAL, "cfg is NULL");
@@ -820,36 +719,42 @@ int check_shape(const soma_scan_config* c) {
   return SOMA_OK;
 }
 
-int vec_of(const soma_scan_config& c) { return c.type == SOMA_BFLOAT && c.width % 2 == 0 && c.gate_stride % 2 == 0 ? 2 : 1; }
-
 int groups_of(const soma_scan_config& c, int vec) { return (c.width + 64 * vec - 1) / (64 * vec); }
 
-// Whether tiles are dealt out one by one.  A block for every sequence and group of
-// channels needs no words and no other launch, and is the better way where those
-// blocks fill the card's 256 compute units, or where a sequence has a few hundred rows.
-bool by_tiles(const soma_scan_config& c, int vec) {
-  return int64_t(c.sequences) * groups_of(c, vec) < 256 && int64_t(c.rows) > 256 * int64_t(c.sequences);
+// Rows of a piece, or 0: split by sequence.  A block for every sequence and group
+// of channels reads its gates once, and is the better way where those blocks fill
+// the card's 256 compute units, or where a sequence is a few tiles long (bf16,
+// both passes, 32 sequences of 512 rows, width 512: 79 us, in pieces 111; one
+// sequence of 16,384, width 2,048: 344 us in pieces, above 2,000 without).  Else
+// the rows are cut into pieces for about 512 blocks, at least two tiles each.
+int piece_rows(const soma_scan_config& c, int vec) {
+  const int64_t groups = groups_of(c, vec);
+  if (int64_t(c.sequences) * groups_of(c, 1) >= 256 || c.rows <= 256 * int64_t(c.sequences)) return 0;
+  const int64_t most = std::min<int64_t>(std::max<int64_t>(512 / groups, 1), kMostPieces);
+  const int64_t tiles = (int64_t(c.rows) + kForward - 1) / kForward;
+  return static_cast<int>(std::max<int64_t>((tiles + most - 1) / most, 2) * kForward);
+}
+
+// Channels of a lane.  Two of bf16 make whole 256-byte runs of a row and halve the
+// instructions for addresses (256 sequences of 256 rows, width 512: both passes
+// 217 us, one channel 231), unless by sequence that leaves less than two blocks a
+// compute unit (64 of 512 rows: 129 us, one channel 115).
+int vec_of(const soma_scan_config& c, bool aligned) {
+  if (c.type != SOMA_BFLOAT || !aligned || c.width % 2 || c.gate_stride % 2) return 1;
+  return piece_rows(c, 2) == 0 && int64_t(c.sequences) * groups_of(c, 2) < 512 ? 1 : 2;
 }
 
 size_t scan_workspace(const soma_scan_config& c) {
-  const size_t tiles = size_t(tiles_of(c, kBackward)), words = tiles * c.width;
-  return 256 + up256(tiles * sizeof(TileInfo)) + up256(words * 8) + up256(words * 4);
+  return up256(size_t(kMostPieces) * c.width * sizeof(float2)) + up256(size_t(c.sequences) * c.width * sizeof(float));
 }
 
-// The workspace's parts, cleared.  `from`: the states that empty sequences keep.
-int begin_tiles(const soma_scan_config& c, int vec, int tile, void* ws, const float* from, ScanArgs* a, hipStream_t st) {
-  char* at = static_cast<char*>(ws);
-  const size_t tiles = size_t(tiles_of(c, tile)), words = tiles * c.width;
-  a->tile = tile;
-  a->tiles = int(tiles);
-  a->groups = groups_of(c, vec);
-  a->ticket = reinterpret_cast<unsigned*>(at);
-  a->info = reinterpret_cast<TileInfo*>(at + 256);
-  a->maps = reinterpret_cast<uint64_t*>(at + 256 + up256(tiles * sizeof(TileInfo)));
-  a->tile_state = reinterpret_cast<uint32_t*>(reinterpret_cast<char*>(a->maps) + up256(words * 8));
-  const size_t blocks = std::min<size_t>((std::max(words, size_t(c.sequences) * c.width) + 255) / 256, 2048);
-  hipLaunchKernelGGL(k_scan_begin, dim3(unsigned(blocks)), dim3(256), 0, st, *a, from);
-  return launched("k_scan_begin");
+// The pieces' share of the arguments; returns the grid's second dimension.
+int split(const soma_scan_config& c, int vec, void* ws, ScanArgs* a) {
+  a->piece = piece_rows(c, vec);
+  if (a->piece == 0) return c.sequences;
+  a->maps = static_cast<float2*>(ws);
+  a->start = reinterpret_cast<float*>(static_cast<char*>(ws) + up256(size_t(kMostPieces) * c.width * sizeof(float2)));
+  return (c.rows + a->piece - 1) / a->piece;
 }
 
 int fill(const soma_scan_config& c, const void* gates, const int32_t* offsets, const float* c0, ScanArgs* a) {
@@ -896,22 +801,18 @@ int soma_scan_forward(const soma_scan_config* cfg, const void* gates, const int3
   a.out = h;
   a.last = cT;
   a.states = states;
-  const int vec = vec_of(c) == 2 && is_aligned(gates, 4) && is_aligned(h, 4) ? 2 : 1;
-  const dim3 block(64 * kWaves);
+  const int vec = vec_of(c, is_aligned(gates, 4) && is_aligned(h, 4));
+  const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
-  if (by_tiles(c, vec)) {
-    if (int rc = begin_tiles(c, vec, kForward, workspace, c0, &a, st)) return rc;
-    const dim3 grid(unsigned(std::min<int64_t>(int64_t(a.tiles) * a.groups, kTileBlocks)));
+  if (a.piece) {
     if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_forward_tiles<float, 1>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_forward_maps<float, 1>), grid, block, 0, st, a);
     else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_forward_tiles<bf16, 2>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 2>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((k_scan_forward_tiles<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_forward_tiles")) return rc;
-    return set_ok();
+      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 1>), grid, block, 0, st, a);
+    if (int rc = launched("k_scan_forward_maps")) return rc;
   }
-  const dim3 grid(groups_of(c, vec), c.sequences);
   if (c.type == SOMA_FLOAT)
     hipLaunchKernelGGL((k_scan_forward<float, 1>), grid, block, 0, st, a);
   else if (vec == 2)
@@ -941,23 +842,18 @@ int soma_scan_backward(const soma_scan_config* cfg, const void* gates, const int
   a.last = dc0;
   a.dcT = dcT;
   a.states = const_cast<float*>(states);
-  const int vec =
-      vec_of(c) == 2 && is_aligned(gates, 4) && is_aligned(dh, 4) && is_aligned(dgates, 4) ? 2 : 1;
-  const dim3 block(64 * kWaves);
+  const int vec = vec_of(c, is_aligned(gates, 4) && is_aligned(dh, 4) && is_aligned(dgates, 4));
+  const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
-  if (by_tiles(c, vec)) {
-    if (int rc = begin_tiles(c, vec, kBackward, workspace, dcT, &a, st)) return rc;
-    const dim3 grid(unsigned(std::min<int64_t>(int64_t(a.tiles) * a.groups, kTileBlocks)));
+  if (a.piece) {
     if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_backward_tiles<float, 1>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_backward_maps<float, 1>), grid, block, 0, st, a);
     else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_backward_tiles<bf16, 2>), grid, block, 0, st, a);
+      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 2>), grid, block, 0, st, a);
     else
-      hipLaunchKernelGGL((k_scan_backward_tiles<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_backward_tiles")) return rc;
-    return set_ok();
+      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 1>), grid, block, 0, st, a);
+    if (int rc = launched("k_scan_backward_maps")) return rc;
   }
-  const dim3 grid(groups_of(c, vec), c.sequences);
   if (c.type == SOMA_FLOAT)
     hipLaunchKernelGGL((k_scan_backward<float, 1>), grid, block, 0, st, a);
   else if (vec == 2)

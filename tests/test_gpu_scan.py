@@ -103,6 +103,23 @@ def test_equal_lengths_without_offsets(sequences, length):
         assert torch.equal(y[k], z[k]), k
 
 
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("lengths", [[20000], [9000, 0, 11003]])
+def test_repeated_calls_give_the_same_bits(dtype, lengths):
+    """Few long sequences: what the blocks pass on does not depend on which of them is done first."""
+    torch = require_gpu()
+    x, want = make(torch, dtype, 96, lengths)
+    plan = soma.GatedScan(x["gates"].shape[0], len(lengths), 96, getattr(torch, dtype))
+    y = run(torch, plan, x, dtype)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+    for _ in range(5):
+        z = run(torch, plan, x, dtype)
+        torch.cuda.synchronize()
+        for k in ("h", "cT", "dgates", "dc0"):
+            assert torch.equal(y[k], z[k]), k
+
+
 @pytest.mark.parametrize("lengths", ["ragged", "long", "long_pair", "many"])
 def test_states_in_place_and_left_out(lengths):
     """cT over c0 and dc0 over dcT; without them the states are zeros and nothing else changes."""
