@@ -632,7 +632,8 @@ int soma_ce_grad(const soma_ce_config* cfg, const void* f_dev, const void* E_dev
  * rounded to nearest even, with the block's largest magnitude at the largest
  * code (448; 1.9375).  A v that is not 0 keeps at least code 1.  All zeros is
  * the state before the first update.  A gradient that is not finite makes its
- * own element's param and moments so, and no other's. */
+ * own element's param and moments so, and no other's (v's 8 bits have no code
+ * for it: they stay at the largest). */
 #define SOMA_ADAMW_BLOCK 256
 
 typedef struct soma_adamw_tensor {

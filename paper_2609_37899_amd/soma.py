@@ -679,6 +679,7 @@ class AdamW(_Plan):
             table[i] = AdamWTensor(pp, pg, *px, self._ptr(c, f"copies[{i}]", torch.bfloat16, p.shape, optional=True),
                                    p.numel(), float(w), _type_of(p.dtype), _type_of(g.dtype), bits, 0)
         self.params, self.grads, self.copies = params, grads, copies
+        self._shapes = [p.shape for p in params]
         out = ctypes.c_size_t()
         _check(load().soma_adamw_workspace_size(table, n, ctypes.byref(out)))
         self._start(out.value, self.device)
@@ -721,10 +722,12 @@ class AdamW(_Plan):
         n = len(self.params)
         if len(m_out) != n or len(v_out) != n:
             raise ValueError(f"m_out and v_out must hold {n} tensors")
-        arrays = []
+        arrays, index = [], self.device.index
         for name, x in (("m_out", m_out), ("v_out", v_out)):
-            a = (ctypes.c_void_p * n)()
-            for i, (t, p) in enumerate(zip(x, self.params)):
-                a[i] = self._ptr(t, f"{name}[{i}]", torch.float32, p.shape)
-            arrays.append(a)
+            for i, (t, shape) in enumerate(zip(x, self._shapes)):
+                # hundreds of tensors: the full check, a microsecond each, only for what is not plainly right
+                if not (isinstance(t, torch.Tensor) and t.dtype is torch.float32 and t.get_device() == index
+                        and t.shape == shape and t.is_contiguous()):
+                    self._ptr(t, f"{name}[{i}]", torch.float32, shape)
+            arrays.append((ctypes.c_void_p * n)(*[t.data_ptr() for t in x]))
         self._call(stream, load().soma_adamw_moments, self._h, *arrays)

@@ -132,6 +132,40 @@ def test_from_zero_moments(bits):
     assert ((p - before).abs() <= 1e-3 * 1.2).all()
 
 
+@pytest.mark.parametrize("ptype", ["float32", "bfloat16"])
+def test_ordinary_blocks_as_any_other(ptype):
+    """Moments in 8 bits take a shorter way where a block of 256 holds ordinary values only.  The same tensors, aligned
+    and one element further on (which never takes it), blocks of every kind side by side."""
+    torch = require_gpu()
+    n = 4096 * 3 + 77
+    x, y = (make(torch, ptype, ptype, 8, [n], shift) for shift in (0, 1))
+    for z in (x, y):
+        m, v, _, _ = z["state"][0]
+        v.clamp_(min=1)                                   # no code 0
+        g = z["g"][0]
+        for k, (gv, mv, vv) in enumerate([(0.0, 0, 0), (1e-30, 0, 0), (1e18, 1, 1), (0.0, 40, 30), (float("inf"), 1, 1),
+                                          (float("nan"), 1, 1), (1e-12, 0, 1), (3e38, 126, 255), (1e-14, 0, 0)]):
+            b = slice(256 * (3 * k + 1), 256 * (3 * k + 2) if k % 2 else 256 * (3 * k + 1) + 5)
+            g[b], m[b], v[b] = gv, mv, vv
+    before = x["p"][0].double()
+    plans = [soma.AdamW(z["p"], z["g"], bits=8, weight_decay=0.1, moments=z["state"]) for z in (x, y)]
+    for t in (1, 2):
+        for plan in plans:
+            plan.step(t, 1e-2)
+        torch.cuda.synchronize()
+        a, b = x["p"][0].double(), y["p"][0].double()
+        # the quotients differ by a reciprocal's 2 u and two roundings, the products by two, the root by 2 u at most,
+        # then p's own roundings (its type's whole step where one falls the other way), and the first update's again
+        tol = t * (8 * ref.U * (b - before).abs() + (2 * ref.U + 2 * ref.half_step(ptype)) * b.abs())
+        same = torch.isfinite(b)
+        assert torch.equal(torch.isfinite(a), same)
+        assert ((a - b).abs()[same] <= tol[same]).all()
+        for u, w in zip(x["state"][0][:2], y["state"][0][:2]):
+            assert torch.equal(u, w)
+        for u, w in zip(x["state"][0][2:], y["state"][0][2:]):
+            assert ((u - w).abs() <= 4 * ref.U * w).all()
+
+
 def test_non_finite_gradients_stay_their_own():
     torch = require_gpu()
     for bits in (32, 8):
