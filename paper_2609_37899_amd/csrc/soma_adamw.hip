@@ -74,7 +74,9 @@ struct Rates {
 // A block's scale from its largest magnitude, and the factor that brings its
 // values onto the code's range (0 for a block of zeros, or one whose largest
 // has no finite factor).
-__device__ __forceinline__ float code_factor(float top, float largest) { return top > 1e-35f ? largest / top : 0.0f; }
+__device__ __forceinline__ float code_factor(float top, float largest) {
+  return top > 1e-35f ? largest * (1.0f / top) : 0.0f;
+}
 
 __device__ __forceinline__ uint32_t root_code(float y) {
   const uint32_t b = __float_as_uint(y);
@@ -121,10 +123,10 @@ __device__ __forceinline__ float ordinary_root(float x) {
   return __builtin_fmaf(__builtin_fmaf(-s, s, x), 0.5f * y, s);
 }
 
-// a / b, to nearest but for as few, a and b well inside the range.
-__device__ __forceinline__ float ordinary_quotient(float a, float b) {
-  const float y = __builtin_amdgcn_rcpf(b), q = a * y;
-  return __builtin_fmaf(__builtin_fmaf(-b, q, a), y, q);
+// 1 / x, to nearest but for as few, x well inside the range.
+__device__ __forceinline__ float ordinary_inverse(float x) {
+  const float y = __builtin_amdgcn_rcpf(x);
+  return __builtin_fmaf(__builtin_fmaf(-x, y, 1.0f), y, y);
 }
 
 // Four consecutive values as they lie in memory.
@@ -315,7 +317,7 @@ __device__ __forceinline__ bool adamw_ordinary(const Tensor& t, int64_t block, c
     p[i] = p[i] * keep - r.size * (m[i] * __builtin_amdgcn_rcpf(root[i] * r.root + r.delta));
   }
   const float top_r = wave_max(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3])));
-  const float fm = ordinary_quotient(kTopM, top_m), fr = ordinary_quotient(kTopRoot, top_r);
+  const float fm = kTopM * ordinary_inverse(top_m), fr = kTopRoot * ordinary_inverse(top_r);
   int mw = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * fm, m[1] * fm, 0, false);
   mw = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * fm, m[3] * fm, mw, true);
   uint32_t vw = 0;
