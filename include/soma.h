@@ -557,8 +557,8 @@ typedef struct soma_scan_config {
   int64_t gate_stride;  /* elements between rows of gates, >= 4 width */
 } soma_scan_config;
 
-/* Bytes of device workspace of soma_scan_forward and soma_scan_backward; it
- * grows with width and sequences only.  Pure. */
+/* Bytes of device workspace of soma_scan_forward and soma_scan_backward (0: none
+ * is needed); it does not shrink with more rows.  Pure. */
 int soma_scan_workspace_size(const soma_scan_config* cfg, size_t* bytes);
 
 int soma_scan_forward(const soma_scan_config* cfg, const void* gates_dev, const int32_t* offsets_dev,
@@ -655,7 +655,8 @@ typedef struct soma_adamw_tensor {
 typedef struct soma_adamw soma_adamw;
 
 /* A plan holds the tensors' addresses: they must stay valid while it is used.
- * soma_adamw_create copies the table to the device and waits for the copy.
+ * soma_adamw_create copies the table to the device and waits for the copy.  No
+ * two arrays of a plan may overlap, but for gradients, which are only read.
  * `tensors` is a host array.  Pointers need only their elements' alignment; 16
  * bytes (fp32), 8 (bf16) and 4 (codes) are faster. */
 int soma_adamw_workspace_size(const soma_adamw_tensor* tensors, int32_t n, size_t* bytes);

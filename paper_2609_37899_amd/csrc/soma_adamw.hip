@@ -29,10 +29,9 @@
 // bits: 238 us (5.0 TB/s), their values in fp32 240 us (5.0 TB/s).
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cmath>
-#include <cstring>
 #include <new>
-#include <vector>
 
 #include "soma.h"
 #include "soma_host.hpp"
@@ -469,6 +468,44 @@ int check_tensors(const soma_adamw_tensor* x, int32_t n, int64_t* chunks) {
   return SOMA_OK;
 }
 
+struct Range {
+  uintptr_t at, end;
+  bool written;
+};
+
+// Whether an array that the step writes overlaps another (two tensors' blocks run
+// at the same time).
+int check_apart(const soma_adamw_tensor* x, int32_t n) {
+  Range* const r = new (std::nothrow) Range[7 * size_t(n)];
+  if (!r) return set_error(SOMA_EINVAL, "out of host memory");
+  size_t k = 0;
+  for (int32_t i = 0; i < n; ++i) {
+    const soma_adamw_tensor& t = x[i];
+    if (t.count == 0) continue;
+    const size_t count = size_t(t.count), blocks = (count + kStateBlock - 1) / kStateBlock;
+    const bool bytes = t.state_bits == 8;
+    const auto add = [&](const void* p, size_t n_bytes, bool written) {
+      if (p) r[k++] = Range{reinterpret_cast<uintptr_t>(p), reinterpret_cast<uintptr_t>(p) + n_bytes, written};
+    };
+    add(t.param, count * type_size(t.param_type), true);
+    add(t.grad, count * type_size(t.grad_type), false);
+    add(t.m, count * (bytes ? 1 : 4), true);
+    add(t.v, count * (bytes ? 1 : 4), true);
+    if (bytes) add(t.m_scale, blocks * 4, true), add(t.v_scale, blocks * 4, true);
+    add(t.copy, count * 2, true);
+  }
+  std::sort(r, r + k, [](const Range& a, const Range& b) { return a.at < b.at; });
+  uintptr_t read_end = 0, written_end = 0;
+  bool apart = true;
+  for (size_t i = 0; i < k; ++i) {
+    apart = apart && r[i].at >= written_end && (!r[i].written || r[i].at >= read_end);
+    uintptr_t& end = r[i].written ? written_end : read_end;
+    end = std::max(end, r[i].end);
+  }
+  delete[] r;
+  return apart ? SOMA_OK : set_error(SOMA_EINVAL, "two arrays of the plan overlap");
+}
+
 size_t table_bytes(int32_t n) { return up256(size_t(n) * sizeof(Tensor)); }
 
 }  // namespace
@@ -499,6 +536,7 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
   int64_t chunks = 0;
   if (int rc = check_tensors(tensors, n, &chunks)) return rc;
   if (!out) return set_error(SOMA_EINVAL, "out is NULL");
+  if (int rc = check_apart(tensors, n)) return rc;
   const size_t need = table_bytes(n) + up256(size_t(chunks) * sizeof(Block));
   if (int rc = check_workspace(workspace, ws_bytes, need)) return rc;
   char* host = new (std::nothrow) char[need]();

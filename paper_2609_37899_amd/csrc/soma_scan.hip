@@ -745,6 +745,7 @@ int vec_of(const soma_scan_config& c, bool aligned) {
 }
 
 size_t scan_workspace(const soma_scan_config& c) {
+  if (piece_rows(c, 1) == 0) return 0;               // with two channels a lane, or fewer rows, so too
   return up256(size_t(kMostPieces) * c.width * sizeof(float2)) + up256(size_t(c.sequences) * c.width * sizeof(float));
 }
 

@@ -455,19 +455,30 @@ class _Plan:
         if self.device.index is None:
             self.device = torch.device("cuda", torch.cuda.current_device())
         self.workspace = torch.empty(max(int(nbytes), 256), dtype=torch.uint8, device=self.device)
-        self._stream0 = torch.cuda.current_stream(self.device).cuda_stream
+        self._memory = [self.workspace]
+        st = torch.cuda.current_stream(self.device)
+        self._stream0 = st.cuda_stream
+        if not torch.cuda.is_current_stream_capturing():
+            st.synchronize()           # other streams may use the memory as well: nothing before is under way in it
         self._ws = ctypes.c_void_p(self.workspace.data_ptr())
 
     def _call(self, stream, fn, *args):
         """fn(*args, stream) with the plan's device current."""
         import torch
-        with torch.cuda.device(self.device):
-            st = stream if stream is not None else torch.cuda.current_stream(self.device)
-            if st.device != self.device:
-                raise ValueError(f"stream belongs to {st.device}, the plan to {self.device}")
-            if st.cuda_stream != self._stream0:
-                self.workspace.record_stream(st)      # not handed out again before this stream is done with it
-            _check(fn(*args, ctypes.c_void_p(st.cuda_stream)))
+        st = stream if stream is not None else torch.cuda.current_stream(self.device)
+        raw = st.cuda_stream
+        if stream is not None and st.device != self.device:
+            raise ValueError(f"stream belongs to {st.device}, the plan to {self.device}")
+        if raw != self._stream0:
+            for x in self._memory:
+                x.record_stream(st)                   # not handed out again before this stream is done with it
+        if torch.cuda.current_device() == self.device.index:
+            rc = fn(*args, raw)
+        else:
+            with torch.cuda.device(self.device):
+                rc = fn(*args, raw)
+        if rc != SOMA_OK:
+            _check(rc)
 
     def _ptr(self, t, name, dtype, shape, optional=False, strided=False):
         """The address of a tensor of this type and shape on the plan's device
@@ -475,18 +486,19 @@ class _Plan:
         import torch
         if t is None and optional:
             return None
-        if not isinstance(t, torch.Tensor) or t.device != self.device:
+        # get_device() is -1 for the CPU
+        if not isinstance(t, torch.Tensor) or t.get_device() != self.device.index or t.device.type != "cuda":
             raise TypeError(f"{name} must be a tensor on {self.device}")
         if t.dtype != dtype:
             raise TypeError(f"{name} must be {dtype}, got {t.dtype}")
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape:
             raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
-        if strided and t.dim() == 2:
+        if not t.is_contiguous():
+            if not strided or t.dim() != 2:
+                raise ValueError(f"{name} must be contiguous")
             if t.shape[1] > 1 and t.stride(1) != 1 or t.shape[0] > 1 and t.stride(0) < t.shape[1]:
                 raise ValueError(f"{name} must have contiguous rows that do not overlap")
-        elif not t.is_contiguous():
-            raise ValueError(f"{name} must be contiguous")
-        return ctypes.c_void_p(t.data_ptr())
+        return t.data_ptr()
 
 
 def _row_stride(t) -> int:
@@ -656,14 +668,22 @@ class AdamW(_Plan):
             raise TypeError("params must be device tensors")
         self.device, self.bits, self.betas, self.delta = params[0].device, bits, tuple(betas), float(delta)
         state = torch.float32 if bits == 32 else torch.uint8
+        self._own = None
         if moments is None:
-            moments = []
+            # one allocation, every array 256 bytes aligned
+            sizes = []
             for p in params:
                 blocks = -(-p.numel() // ADAMW_BLOCK)
-                x = [torch.zeros(p.numel(), dtype=state, device=self.device) for _ in range(2)]
-                if bits == 8:
-                    x += [torch.zeros(blocks, dtype=torch.float32, device=self.device) for _ in range(2)]
-                moments.append(tuple(x))
+                sizes += [p.numel()] * 2 if bits == 32 else [p.numel(), p.numel(), blocks, blocks]
+            types = [torch.float32] * 2 if bits == 32 else [torch.uint8, torch.uint8, torch.float32, torch.float32]
+            ends, end = [], 0
+            for i, k in enumerate(sizes):
+                end = -(-(end + k * types[i % len(types)].itemsize) // 256) * 256
+                ends.append(end)
+            self._own = torch.zeros(end, dtype=torch.uint8, device=self.device)
+            arrays = [self._own[at:at + k * types[i % len(types)].itemsize].view(types[i % len(types)])
+                      for i, (at, k) in enumerate(zip([0] + ends, sizes))]
+            moments = [tuple(arrays[i:i + len(types)]) for i in range(0, len(arrays), len(types))]
         self.state = [tuple(x) for x in moments]
         if len(self.state) != n or any(len(x) != (2 if bits == 32 else 4) for x in self.state):
             raise ValueError("moments must hold (m, v) for each tensor, or (m, v, m_scale, v_scale) for 8 bits")
@@ -683,6 +703,8 @@ class AdamW(_Plan):
         out = ctypes.c_size_t()
         _check(load().soma_adamw_workspace_size(table, n, ctypes.byref(out)))
         self._start(out.value, self.device)
+        if self._own is not None:
+            self._memory.append(self._own)
         plan = ctypes.c_void_p()
         with torch.cuda.device(self.device):
             st = stream if stream is not None else torch.cuda.current_stream(self.device)

@@ -216,3 +216,58 @@ def test_many_tensors_captured_and_on_another_stream():
     for k, s in enumerate(x["state"]):
         m, _ = ref.moments_of(*arrays(s))
         assert np.all(np.abs(outs[0][k].cpu().numpy() - m) <= ref.U * np.abs(m)), k
+
+
+def test_refusals_and_closed_plans():
+    torch = require_gpu()
+    x = make(torch, "float32", "float32", 32, [100, 7])
+    plan = soma.AdamW(x["p"], x["g"], moments=x["state"])
+    before = [p.clone() for p in x["p"]]
+    for bad in (dict(t=0, lr=1e-3), dict(t=1, lr=float("nan")), dict(t=1, lr=float("inf"))):
+        with pytest.raises(soma.SomaError):
+            plan.step(**bad)
+    for bad in (dict(betas=(1.0, 0.999)), dict(betas=(0.9, -0.1)), dict(delta=0.0), dict(delta=float("nan"))):
+        other = soma.AdamW(x["p"], x["g"], moments=x["state"], **bad)
+        with pytest.raises(soma.SomaError):
+            other.step(1, 1e-3)
+    with pytest.raises(TypeError):
+        plan.step(1, 1e-3, torch.ones(1, dtype=torch.float64, device="cuda"))
+    with pytest.raises(ValueError):
+        plan.step(1, 1e-3, torch.ones(2, device="cuda"))
+    out = [torch.zeros(100, device="cuda"), torch.zeros(7, device="cuda")]
+    for bad in (out[:1], [out[0], torch.zeros(8, device="cuda")], [out[0], torch.zeros(14, device="cuda")[::2]]):
+        with pytest.raises(ValueError):
+            plan.moments(bad, out)
+    with pytest.raises(TypeError):
+        plan.moments(out, [out[0], torch.zeros(7)])
+    with pytest.raises(TypeError):
+        plan.moments(out, [out[0].half(), out[1]])
+    with pytest.raises(soma.SomaError):                    # the same tensor twice
+        soma.AdamW(x["p"][:1] * 2, x["g"][:1] * 2)
+    with pytest.raises(soma.SomaError):
+        soma.AdamW(x["p"], x["p"])
+    with pytest.raises(ValueError):
+        soma.AdamW([torch.zeros(8, 8, device="cuda").t()], [torch.zeros(8, 8, device="cuda")])
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for p, q in zip(x["p"], before))
+    plan.close()
+    with pytest.raises(RuntimeError):
+        plan.step(1, 1e-3)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_moments_from_zeros_used_on_another_stream(bits):
+    """Moments that the plan makes itself, of many odd sizes, from the first step on on a stream of their own."""
+    torch = require_gpu()
+    sizes = [1, 0, 255, 300, 5000, 3]
+    x = make(torch, "float32", "float32", 32, sizes)
+    zero = [(torch.zeros(n, device="cuda"),) * 2 for n in sizes]
+    want = expect(dict(x, state=zero), [0.0] * len(sizes), 1, 1e-2, 1.0)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    plan = soma.AdamW(x["p"], x["g"], bits=bits, weight_decay=0.0, betas=(B1, B2), delta=DELTA)
+    plan.step(1, 1e-2, stream=st)
+    torch.cuda.synchronize()
+    for p, s, w in zip(x["p"], plan.state, want):
+        assert s[0].numel() == p.numel() and all(t.data_ptr() % 256 == 0 for t in s)
+        check_tensor(p, s, w, "float32", 1e-2)
