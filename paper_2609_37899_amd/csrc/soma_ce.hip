@@ -166,6 +166,13 @@ struct PackArgs {
   int V;
 };
 
+// f and the first piece of E in one launch, or a later piece alone: blocks from
+// `first` on (of the grid's x) take the second.
+struct PackPair {
+  PackArgs a[2];
+  int first;
+};
+
 __device__ __forceinline__ void split_rn(float x, uint16_t& hi, uint16_t& lo) {
   const _Float16 h = static_cast<_Float16>(x);
   hi = __builtin_bit_cast(uint16_t, h);
@@ -195,12 +202,14 @@ __device__ __forceinline__ void fragment_words(const float (&v)[8], float scale,
 // values are a word of the fragment as they come from memory.  For the transpose
 // the words go through LDS, where a lane picks eight rows of its column.
 template <class T, int PARTS>
-__global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
+__global__ __launch_bounds__(256) void k_ce_pack(PackPair pair) {
   constexpr int kRow = 64 + 8;               // halves: 16-byte rows, columns of 8 rows on different banks
   __shared__ __attribute__((aligned(16))) uint16_t tile[PARTS][64][kRow];
   __shared__ float red[4];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
-  const int r0 = blockIdx.x * 64, k0 = blockIdx.y * 64;
+  const bool second = int(blockIdx.x) >= pair.first;
+  const PackArgs& a = pair.a[second];
+  const int r0 = (int(blockIdx.x) - (second ? pair.first : 0)) * 64, k0 = blockIdx.y * 64;
   const T* x = static_cast<const T*>(a.x);
   const int row = r0 + wave * 16 + lr;
   float v[2][8] = {};
@@ -231,7 +240,7 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackArgs a) {
       if constexpr (PARTS == 2) {
         e = power_scale(maximum_of(a.maxima + kMaxima, a.nmax, red));
       }
-      if (blockIdx.x == 0 && threadIdx.x == 0) *a.scales = Scales{scale, e, c, 0.0f};
+      if (r0 == 0 && threadIdx.x == 0) *a.scales = Scales{scale, e, c, 0.0f};
     }
   }
   if (a.meta && blockIdx.y == 0 && threadIdx.x < 64) {
@@ -1132,10 +1141,13 @@ int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipSt
   return launched("k_ce_sum");
 }
 
+// Packs a, and b as well if it is not NULL, which has as many columns.
 template <class T, int PARTS>
-int launch_pack(PackArgs& a, hipStream_t st) {
-  a.eight = is_aligned(a.x, 4 * sizeof(T)) && a.stride % 4 == 0;
-  hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(unsigned(a.np / 64), unsigned(a.Kp / 64)), dim3(256), 0, st, a);
+int launch_pack(const PackArgs& a, const PackArgs* b, hipStream_t st) {
+  PackPair p{{a, b ? *b : a}, a.np / 64};
+  for (PackArgs& x : p.a) x.eight = is_aligned(x.x, 4 * sizeof(T)) && x.stride % 4 == 0;
+  const unsigned blocks = unsigned(p.first + (b ? b->np / 64 : 0));
+  hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(blocks, unsigned(a.Kp / 64)), dim3(256), 0, st, p);
   return launched("k_ce_pack");
 }
 
@@ -1177,7 +1189,6 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
     a.targets = targets, a.frag = fp, a.maxima = PARTS == 2 ? maxima : nullptr, a.nmax = nmax, a.scales = scales;
     a.V = c.vocab;
-    if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
     stride = int(s.Rp);
     const int piece = piece_of(c);
     for (int v0 = 0; v0 < c.vocab; v0 += piece) {
@@ -1185,7 +1196,7 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
       PackArgs b{};
       b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
       b.np = np, b.Kp = int(s.Kp), b.frag = ep, b.maxima = a.maxima, b.nmax = nmax, b.which = 1;
-      if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
+      if (int rc = v0 == 0 ? launch_pack<T, PARTS>(a, &b, st) : launch_pack<T, PARTS>(b, nullptr, st)) return rc;
       CeMmArgs p{};
       p.A = fp, p.W = ep, p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
       p.part = part, p.part_stride = stride, p.sub0 = subs, p.hit = hit, p.targets = targets, p.R = c.rows, p.V = n, p.v0 = v0;
@@ -1220,7 +1231,6 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
   a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = nmax;
   a.scales = scales, a.meta = meta, a.lse = lse, a.w = w, a.V = c.vocab;
-  if (int rc = launch_pack<T, PARTS>(a, st)) return rc;
   const Shares of_df = shares_of(s.Rp, s.Kp, s.Vp, PARTS, c.vocab > piece_of(c));
   const int piece = piece_of(c);
   for (int v0 = 0; v0 < c.vocab; v0 += piece) {
@@ -1229,7 +1239,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     b.x = static_cast<const T*>(E) + int64_t(v0) * c.e_stride, b.stride = c.e_stride, b.n = n, b.K = c.width;
     b.np = np, b.Kp = int(s.Kp), b.frag = at(s.e), b.fragT = df ? at(s.eT) : nullptr;
     b.maxima = PARTS == 2 ? maxima : nullptr, b.nmax = nmax, b.which = 1;
-    if (int rc = launch_pack<T, PARTS>(b, st)) return rc;
+    if (int rc = v0 == 0 ? launch_pack<T, PARTS>(a, &b, st) : launch_pack<T, PARTS>(b, nullptr, st)) return rc;
     CeMmArgs p{};
     p.A = at(s.f), p.W = at(s.e), p.ta = int(s.Rp / 16), p.tw = np / 16, p.KC = int(s.Kp / 32), p.scales = scales;
     p.meta = meta, p.G = at(s.G), p.GT = at(s.GT), p.V = n, p.v0 = v0;
