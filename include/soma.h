@@ -546,8 +546,8 @@ enum soma_type {
  *           needs, the state in front of every SOMA_SCAN_BLOCK-th row.  NULL:
  *           not wanted.
  * gates and h have `type`; states and arithmetic are fp32, sigma and tanh to
- * 2^-22 (of 1, not of a small value).  Constraints: rows
- * in [0, 2^30], width in [1, 2^20], sequences in [1, 65535]. */
+ * 2^-22 (of 1, not of a small value).  Constraints: rows in [0, 2^30], width in
+ * [1, 2^20], sequences in [1, 65535]. */
 #define SOMA_SCAN_BLOCK 32
 
 typedef struct soma_scan_config {
