@@ -778,32 +778,34 @@ __global__ __launch_bounds__(256) void k_ce_sum(CeMmArgs p) {
 }
 
 // ---------------------------------------------------------------------------
-// The loss of a few rows (up to 16): E is read once and is all there is to
+// The loss of a few rows: E is read once (twice, rows_of) and is all there is to
 // read.  A wave takes 16 vocabulary rows at a time straight from E into MFMA
-// operands (lane (lr, lg): row lr, 8 or 4 consecutive columns), the rows of f
-// wait in LDS; a lane keeps the running maximum and sum of its logits.  fp32
-// uses the fp32 matrix instruction.  A head of 50,257 x 1,024 in bf16, 103 MB: 22.5 us
-// (4.6 TB/s), and 4 for the join.
+// operands (lane (lr, lg): row lr, 8 or 4 consecutive columns), the rows of f, RT
+// tiles of 16, wait in LDS; a lane keeps the running maximum and sum of its
+// logits.  fp32 uses the fp32 matrix instruction.  A head of 50,257 x 1,024 in bf16, 103 MB: 21.3 us
+// (4.8 TB/s), and 4 for the join.
 // ---------------------------------------------------------------------------
 struct RowsArgs {
   const void *f, *E;
   int64_t f_stride, e_stride;
   const int32_t* targets;
   int R, V, K;
-  float2* part;             // [gridDim.x][16]
+  float2* part;             // [gridDim.x][part_stride]
+  int part_stride, part_rows;   // the rows of this pass that have a place in it
+  int wide;                 // f's rows allow 16-byte loads
   float* hit;
 };
 
 constexpr int kRowsWaves = 16;
 
-template <class T>
+template <class T, int RT>
 __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
   constexpr bool kB = sizeof(T) == 2;
   constexpr int kW = 16 / sizeof(T);                    // columns of a lane's 16 bytes
   constexpr int kChunk = 4 * kW;                        // columns of one step
   extern __shared__ __attribute__((aligned(16))) unsigned char ce_lds[];
-  T* const fl = reinterpret_cast<T*>(ce_lds);           // [chunk][lane][kW]
-  __shared__ float2 red[kRowsWaves][16];
+  T* const fl = reinterpret_cast<T*>(ce_lds);           // [chunk][row tile][lane][kW]
+  __shared__ float2 red[kRowsWaves][16 * RT];
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63, lr = lane & 15, lg = lane >> 4;
   const int chunks = (a.K + kChunk - 1) / kChunk;
   const T* f = static_cast<const T*>(a.f);
@@ -816,51 +818,87 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
   int t = static_cast<int>(int64_t(tiles) * blockIdx.x / gridDim.x) + wave;
   // rows past the end repeat the last and are masked below
   auto row_of = [&](int tile) { return E + min(tile * 16 + lr, a.V - 1) * a.e_stride + lg * kW; };
-  // Two batches of eight loads: one is multiplied while the other is on its way,
-  // the next tile's first behind the last of this one, the first of all before f
-  // is brought to LDS.
-  auto load = [&](uint4 (&x)[8], const T* e, int c) {
+  // Two batches of eight loads (four, where accumulators need the registers): one is
+  // multiplied while the other is on its way, the next tile's first behind the last
+  // of this one, the first of all before f is brought to LDS.
+  constexpr int U = RT == 1 ? 8 : 4;
+  auto load = [&](uint4 (&x)[U], const T* e, int c) {
 #pragma unroll
-    for (int u = 0; u < 8; ++u)
+    for (int u = 0; u < U; ++u)
       if (c + u < full) x[u] = *reinterpret_cast<const uint4*>(e + (c + u) * kChunk);
   };
-  uint4 x0[8], x1[8];
+  uint4 x0[U], x1[U];
   const T* e = row_of(t);
   if (t < last) load(x0, e, 0);
-  for (int c = wave; c < chunks; c += kRowsWaves)
+  bool on[RT];
 #pragma unroll
-    for (int j = 0; j < kW; ++j) {
-      const int k = c * kChunk + lg * kW + j;
-      const bool on = lr < a.R && k < a.K && a.targets[lr] >= 0;
-      T z{};
-      fl[(c * 64 + lane) * kW + j] = on ? f[lr * a.f_stride + k] : z;
+  for (int i = 0; i < RT; ++i) on[i] = 16 * i + lr < a.R && a.targets[16 * i + lr] >= 0;
+  for (int c = wave; c < chunks; c += kRowsWaves) {
+    const int k = c * kChunk + lg * kW;
+    uint4 y[RT];
+    if (a.wide && c < full) {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        y[i] = make_uint4(0, 0, 0, 0);
+        if (on[i]) y[i] = *reinterpret_cast<const uint4*>(f + (16 * i + lr) * a.f_stride + k);
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < RT; ++i) {
+        T one[kW] = {};
+#pragma unroll
+        for (int j = 0; j < kW; ++j)
+          if (on[i] && k + j < a.K) one[j] = f[(16 * i + lr) * a.f_stride + k + j];
+        __builtin_memcpy(&y[i], one, 16);
+      }
     }
+#pragma unroll
+    for (int i = 0; i < RT; ++i) *reinterpret_cast<uint4*>(fl + ((c * RT + i) * 64 + lane) * kW) = y[i];
+  }
   __syncthreads();
-  const int target = lr < a.R ? a.targets[lr] : -1;
-  float top = kLowest, sum = 0.0f;
+  int target[RT];
+  float top[RT], sum[RT];
+#pragma unroll
+  for (int i = 0; i < RT; ++i)
+    target[i] = 16 * i + lr < a.R ? a.targets[16 * i + lr] : -1, top[i] = kLowest, sum[i] = 0.0f;
   for (; t < last; t += kRowsWaves) {
-    f32x4 acc{0.f, 0.f, 0.f, 0.f}, acc2{0.f, 0.f, 0.f, 0.f};
+    f32x4 acc[RT], acc2{0.f, 0.f, 0.f, 0.f};            // acc2: one tile alone takes turns
+#pragma unroll
+    for (int i = 0; i < RT; ++i) acc[i] = f32x4{0.f, 0.f, 0.f, 0.f};
     auto step = [&](const uint4& x, int c, bool odd) {
-      const uint4 y = *reinterpret_cast<const uint4*>(fl + (c * 64 + lane) * kW);
-      f32x4& to = odd ? acc2 : acc;
-      if constexpr (kB)
-        to = mma<1>(x, y, to);
-      else
-        to = mfma_k16(__builtin_bit_cast(float4, x), __builtin_bit_cast(float4, y), to);
+      uint4 y[RT];
+#pragma unroll
+      for (int i = 0; i < RT; ++i) y[i] = *reinterpret_cast<const uint4*>(fl + ((c * RT + i) * 64 + lane) * kW);
+      if constexpr (kB) {
+#pragma unroll
+        for (int i = 0; i < RT; ++i) {
+          f32x4& to = RT == 1 && odd ? acc2 : acc[i];
+          to = mma<1>(x, y[i], to);
+        }
+      } else {
+        const f32x4 xf = __builtin_bit_cast(f32x4, x);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)                     // tile by tile: one's next product would wait for its last
+#pragma unroll
+          for (int i = 0; i < RT; ++i) {
+            f32x4& to = RT == 1 && odd ? acc2 : acc[i];
+            to = __builtin_amdgcn_mfma_f32_16x16x4f32(xf[j], __builtin_bit_cast(f32x4, y[i])[j], to, 0, 0, 0);
+          }
+      }
     };
     const T* ahead = row_of(t + kRowsWaves);
-    for (int c = 0; c < full; c += 16) {
-      load(x1, e, c + 8);
+    for (int c = 0; c < full; c += 2 * U) {
+      load(x1, e, c + U);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
+      for (int u = 0; u < U; ++u)
         if (c + u < full) step(x0[u], c + u, u & 1);
-      if (c + 16 < full)
-        load(x0, e, c + 16);
+      if (c + 2 * U < full)
+        load(x0, e, c + 2 * U);
       else if (t + kRowsWaves < last)
         load(x0, ahead, 0);
 #pragma unroll
-      for (int u = 0; u < 8; ++u)
-        if (c + 8 + u < full) step(x1[u], c + 8 + u, u & 1);
+      for (int u = 0; u < U; ++u)
+        if (c + U + u < full) step(x1[u], c + U + u, u & 1);
     }
     int c = full;
     if (c < chunks) {                                   // the tail, column by column
@@ -875,29 +913,36 @@ __global__ __launch_bounds__(64 * kRowsWaves) void k_ce_rows(RowsArgs a) {
       step(x, c, false);
     }
     e = ahead;
-    // acc[q] = logit of row lr, vocabulary row 16 t + 4 lg + q
-    float l[4], most = top;
+    // acc[i][q] = logit of row 16 i + lr, vocabulary row 16 t + 4 lg + q
 #pragma unroll
-    for (int q = 0; q < 4; ++q) {
-      const int v = t * 16 + 4 * lg + q;
-      l[q] = v < a.V ? acc[q] + acc2[q] : -__builtin_inff();
-      most = fmaxf(most, l[q]);
-      if (v == target && v < a.V) a.hit[lr] = l[q];
+    for (int i = 0; i < RT; ++i) {
+      float l[4], most = top[i];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        const int v = t * 16 + 4 * lg + q;
+        l[q] = v < a.V ? (RT == 1 ? acc[i][q] + acc2[q] : acc[i][q]) : -__builtin_inff();
+        most = fmaxf(most, l[q]);
+        if (v == target[i] && v < a.V) a.hit[16 * i + lr] = l[q];
+      }
+      sum[i] *= exp2_f(kLog2e * (top[i] - most));
+#pragma unroll
+      for (int q = 0; q < 4; ++q) sum[i] += exp2_f(kLog2e * (l[q] - most));
+      top[i] = most;
     }
-    sum *= exp2_f(kLog2e * (top - most));
-#pragma unroll
-    for (int q = 0; q < 4; ++q) sum += exp2_f(kLog2e * (l[q] - most));
-    top = most;
   }
-  const float all = group4_max(top);
-  sum = group4_sum(sum * exp2_f(kLog2e * (top - all)));
-  if (lg == 0) red[wave][lr] = make_float2(all, sum);
+#pragma unroll
+  for (int i = 0; i < RT; ++i) {
+    const float all = group4_max(top[i]);
+    const float of_all = group4_sum(sum[i] * exp2_f(kLog2e * (top[i] - all)));
+    if (lg == 0) red[wave][16 * i + lr] = make_float2(all, of_all);
+  }
   __syncthreads();
-  if (threadIdx.x < 16) {
+  const int r = threadIdx.x;
+  if (r < 16 * RT && r < a.part_rows) {
     float m = kLowest, s = 0.0f;
-    for (int w = 0; w < kRowsWaves; ++w) m = fmaxf(m, red[w][threadIdx.x].x);
-    for (int w = 0; w < kRowsWaves; ++w) s += red[w][threadIdx.x].y * exp2_f(kLog2e * (red[w][threadIdx.x].x - m));
-    a.part[blockIdx.x * 16 + threadIdx.x] = make_float2(m, s);
+    for (int w = 0; w < kRowsWaves; ++w) m = fmaxf(m, red[w][r].x);
+    for (int w = 0; w < kRowsWaves; ++w) s += red[w][r].y * exp2_f(kLog2e * (red[w][r].x - m));
+    a.part[int64_t(blockIdx.x) * a.part_stride + r] = make_float2(m, s);
   }
 }
 
@@ -955,7 +1000,9 @@ __global__ __launch_bounds__(256) void k_ce_zero(uint16_t* x, int64_t halves) {
 // ---------------------------------------------------------------------------
 constexpr int64_t kFill = 256;            // tiles that fill the card
 constexpr int kRowsBlocks = 256;          // blocks of k_ce_rows
-constexpr size_t kRowsLds = 65536;        // f's rows in LDS
+constexpr size_t kRowsLds = 147456;       // f's rows in LDS, beside 8 KiB of the waves' results
+constexpr int64_t kTwiceBytes = 1 << 24;  // of a head that k_ce_rows reads twice
+constexpr int kRowsMost = 128;            // rows that k_ce_rows takes at most: two passes of 64
 
 int64_t up(int64_t x, int64_t q) { return (x + q - 1) / q * q; }
 
@@ -997,7 +1044,7 @@ Sizes sizes_of(const soma_ce_config& c, bool grad) {
   };
   const size_t half = size_t(s.parts) * 2;
   if (!grad) {
-    s.part = take(std::max(size_t(up(c.vocab, 64) / 64 + 4 * (c.vocab / kPiece + 1)) * s.Rp, size_t(kRowsBlocks) * 16) * 8);
+    s.part = take(std::max(size_t(up(c.vocab, 64) / 64 + 4 * (c.vocab / kPiece + 1)) * s.Rp, size_t(kRowsBlocks) * std::min<int64_t>(up(c.rows, 16), kRowsMost)) * 8);
     s.hit = take(size_t(s.Rp) * 4);
   } else {
     s.meta = take(size_t(s.Rp) * sizeof(RowMeta));
@@ -1169,6 +1216,35 @@ int maxima_of(const soma_ce_config& c) {
   return int(std::min<int64_t>(kMaxima, up((std::max(c.rows, c.vocab) + 3) / 4, 4)));
 }
 
+size_t rows_lds(int width, size_t size, int tiles) { return size_t(up(width, 64)) * 16 * tiles * size; }
+
+// Row tiles of a pass of k_ce_rows, 0: not by it.  Its one or two readings of E
+// against a packed copy written and read as well (bf16, 50,257 x 1,024: 64 rows
+// 28.9 us, packed 97; 128 rows in two passes 54.7, packed 98).  Of a small head
+// nothing is bound by reading, and a second pass costs more than packing: 2,000 x
+// 768, 128 rows, 24.8 us, packed 17.3; 16,000 x 512 either way 21.6; 32,000 x 512
+// 25.7, packed 39.  fp32 takes 32 rows a pass: its matrix instruction is a
+// sixteenth as fast, and bounds 64 in one (107 us, 2 x 32: 103, packed 221).
+int rows_of(const soma_ce_config& c, size_t size) {
+  int most = size == 2 ? 4 : 2;
+  while (most > 0 && rows_lds(c.width, size, most) > kRowsLds) most /= 2;
+  if (most == 0 || c.rows > 32 * most) return 0;
+  const int passes = c.rows > 16 * most ? 2 : 1;
+  if (passes == 2 && int64_t(c.vocab) * c.width * int64_t(size) < kTwiceBytes) return 0;
+  int tiles = 1;
+  while (16 * tiles * passes < c.rows) tiles *= 2;
+  return tiles;
+}
+
+template <class T, int RT>
+int launch_rows(const RowsArgs& a, int blocks, hipStream_t st) {
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ce_rows<T, RT>),
+                                           hipFuncAttributeMaxDynamicSharedMemorySize, int(kRowsLds));
+  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
+  hipLaunchKernelGGL((k_ce_rows<T, RT>), dim3(blocks), dim3(64 * kRowsWaves), unsigned(rows_lds(a.K, sizeof(T), RT)), st, a);
+  return launched("k_ce_rows");
+}
+
 template <class T, int PARTS>
 int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int32_t* targets, float* loss, float* lse,
                char* ws, hipStream_t st) {
@@ -1176,17 +1252,23 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   float2* part = reinterpret_cast<float2*>(ws + s.part);
   float* hit = reinterpret_cast<float*>(ws + s.hit);
   int subs = 0, stride = 0;
-  // A few rows: E straight from memory, where its rows allow 16-byte loads.
-  const size_t rows_lds = size_t(up(c.width, 64)) * 16 * sizeof(T);
-  if (c.rows <= 16 && rows_lds <= kRowsLds && is_aligned(E, 16) && c.e_stride * sizeof(T) % 16 == 0) {
-    const RowsArgs a{f, E, c.f_stride, c.e_stride, targets, c.rows, c.vocab, c.width, part, hit};
-    subs = int(std::min<int64_t>(kRowsBlocks, (up(c.vocab, 16) / 16 + kRowsWaves - 1) / kRowsWaves));
-    stride = 16;
-    const hipError_t he = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ce_rows<T>),
-                                              hipFuncAttributeMaxDynamicSharedMemorySize, int(kRowsLds));
-    if (he != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(he));
-    hipLaunchKernelGGL(k_ce_rows<T>, dim3(subs), dim3(64 * kRowsWaves), unsigned(rows_lds), st, a);
-    if (int rc = launched("k_ce_rows")) return rc;
+  const int tiles = is_aligned(E, 16) && c.e_stride * sizeof(T) % 16 == 0 ? rows_of(c, sizeof(T)) : 0;
+  if (tiles) {
+    subs = int(std::min<int64_t>(kRowsBlocks, up(c.vocab, 16) / 16));
+    stride = int(up(c.rows, 16));
+    for (int r0 = 0; r0 < c.rows; r0 += 16 * tiles) {
+      const RowsArgs a{static_cast<const T*>(f) + r0 * c.f_stride, E, c.f_stride, c.e_stride, targets + r0,
+                       std::min(c.rows - r0, 16 * tiles), c.vocab, c.width, part + r0, stride, stride - r0,
+                       is_aligned(f, 16) && c.f_stride * sizeof(T) % 16 == 0, hit + r0};
+      int rc = SOMA_OK;
+      if (tiles == 1)
+        rc = launch_rows<T, 1>(a, subs, st);
+      else if (tiles == 2)
+        rc = launch_rows<T, 2>(a, subs, st);
+      else if constexpr (PARTS == 1)
+        rc = launch_rows<T, 4>(a, subs, st);
+      if (rc) return rc;
+    }
   } else {
     float* maxima = reinterpret_cast<float*>(ws + s.maxima);
     Scales* scales = reinterpret_cast<Scales*>(ws + s.scales);

@@ -231,3 +231,29 @@ def test_captured_on_another_stream_and_repeated(dtype):
         torch.cuda.synchronize()
         for name in y:
             assert torch.equal(y[name], e[name]), (k, name)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("R,V,K", [
+    (17, 100, 64), (32, 777, 512), (33, 1000, 136), (49, 20000, 8), (64, 1, 96), (65, 5003, 1024), (100, 50, 72),
+    (128, 3000, 64), (129, 3000, 64), (32, 300, 2304), (33, 300, 2304), (64, 70, 2304), (7, 65, 4616), (20, 65, 1200)])
+def test_loss_of_some_rows(dtype, R, V, K):
+    """Rows that take the head from memory as it lies, in one or two passes, and the numbers around those limits."""
+    torch = require_gpu()
+    x = make(torch, dtype, R, V, K, ignored=0.2)
+    x["f"][3] = torch.where(x["targets"][3] < 0, float("inf"), x["f"][3])
+    plan = soma.CrossEntropy(R, V, K, getattr(torch, dtype), grad=False)
+    y = {k: torch.full((R,), 7.0, device="cuda") for k in ("loss", "lse")}
+    plan.loss(x["f"], x["E"], x["targets"], y["loss"], y["lse"])
+    torch.cuda.synchronize()
+    want = ref.cross_entropy(host(x["f"]), host(x["E"]), host(x["targets"]).astype(np.int64))
+    # a product and every addition are off by 2 u: accumulators of at most K / 4 in a row, and those of the exponentials
+    for name in y:
+        assert np.all(np.abs(host(y[name]) - want[name]) <= (K / 4 + 40) * ref.U * want[name + "_fp32"] + 1e-37), name
+    # fewer rows in the same plan, to the same bits where the passes are alike, else within the bound
+    n = R - 1
+    loss, lse = torch.full((n,), 7.0, device="cuda"), torch.full((n,), 7.0, device="cuda")
+    plan.loss(x["f"][:n], x["E"], x["targets"][:n], loss, lse)
+    torch.cuda.synchronize()
+    assert np.all(np.abs(host(loss) - want["loss"][:n]) <= (K / 4 + 40) * ref.U * want["loss_fp32"][:n] + 1e-37)
+    assert np.all(np.abs(host(lse) - want["lse"][:n]) <= (K / 4 + 40) * ref.U * want["lse_fp32"][:n] + 1e-37)
