@@ -630,9 +630,9 @@ int soma_ce_grad(const soma_ce_config* cfg, const void* f_dev, const void* E_dev
  * SOMA_ADAMW_BLOCK elements, [ceil(count / SOMA_ADAMW_BLOCK)] each,
  *   m = e4m3(code) m_scale;  v = (r(code) v_scale)^2,
  *   r(0) = 0, r(k) = (16 + k % 16) 2^(k / 16 - 19),
- * rounded to nearest even, with the block's largest magnitude at the largest
- * code (448; 1.9375).  A v that is not 0 keeps at least code 1.  All zeros is
- * the state before the first update.  A gradient that is not finite makes its
+ * with the block's largest magnitude at the largest code (448; 1.9375), rounded
+ * to nearest even or at random (soma_adamw_set_rounding).  A v that is not 0
+ * keeps at least code 1.  All zeros is the state before the first update.  A gradient that is not finite makes its
  * own element's param and moments so, and no other's (v's 8 bits have no code
  * for it: they stay at the largest). */
 #define SOMA_ADAMW_BLOCK 256
@@ -664,6 +664,25 @@ int soma_adamw_workspace_size(const soma_adamw_tensor* tensors, int32_t n, size_
 int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspace_dev, size_t workspace_bytes,
                       void* stream, soma_adamw** out);
 void soma_adamw_destroy(soma_adamw* plan);
+
+/* How the plan rounds moments to 8 bits from its next step on (those of 32 are
+ * not concerned).
+ *   SOMA_ROUND_NEAREST  (a new plan's): the closest codes of one step.  Over many
+ *     steps v does not follow its average: an update below half a code, 3 to 6%
+ *     of v, is lost each time, and with beta2 = 0.999 most are.
+ *   SOMA_ROUND_RANDOM   what a training run needs: either neighbour, with the
+ *     probability at which the expected m and v are the exact ones, from element
+ *     i's word i % 4 of Philox4x32-10 with key (lo32(seed), hi32(seed) ^ hi32(t))
+ *     and counter (lo32(i / 4), tensor, lo32(t), hi32(i / 4)): with d the word's
+ *     upper 20 bits, v takes the larger root if (d + 1/2) 2^-20 is below
+ *     (root^2 - smaller^2) / (larger^2 - smaller^2); with its lower 12, m the
+ *     larger magnitude if (d + 1/2) 2^-12 is below (|m| - smaller) / (larger -
+ *     smaller).  The same seed, t and inputs give the same bits. */
+enum soma_rounding {
+  SOMA_ROUND_NEAREST = 0,
+  SOMA_ROUND_RANDOM = 1
+};
+int soma_adamw_set_rounding(soma_adamw* plan, int32_t rounding, uint64_t seed);
 
 /* Update number t >= 1 of every tensor.  grad_scale_dev: s, one fp32 value on
  * the device (loss scaling, clipping); NULL: 1. */

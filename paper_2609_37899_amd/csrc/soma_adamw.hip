@@ -16,6 +16,15 @@
 // e4m3's unit (2.2e-6 of the block's largest) becomes 0.  The update of p uses
 // the new moments before their rounding.
 //
+// To nearest, an update of less than half a code is lost, at every step again: with
+// beta2 = 0.999 v moves by a thousandth of its distance to g^2, its codes lie 6 to
+// 12% apart, so that an element falls only as its block's largest does.  (One element
+// of 256 keeps its gradient, the others' fall tenfold: their root is 7.8 times too
+// large after 5,000 updates.)  Random rounding (random_codes) keeps either neighbour
+// with the probability that makes the expected value the exact one, so the average of
+// many steps is followed; 64 bits of Philox for four elements serve it, drawn from
+// the element, its tensor and the number of the update.
+//
 // The step is bound by memory: every element is read and written once.  A
 // block takes 4096 consecutive elements of one tensor (a table of blocks, made
 // once with the plan, names the tensor), a wave 256 of them at a time, four a
@@ -26,7 +35,9 @@
 //
 // Measured: 24 tensors of 40 M fp32 elements in all, moments of 32 bits: 217 us,
 // 5.2 TB/s, as fast as a copy.  400 tensors of 120 M bf16 elements, moments of 8
-// bits: 238 us (5.0 TB/s), their values in fp32 240 us (5.0 TB/s).
+// bits: 238 us (5.0 TB/s), their values in fp32 240 us (5.0 TB/s).  Steps of the same
+// back to back take 272 us, rounded at random 343 (operations bound it: Philox is 40
+// multiplications for four elements); with fp32 parameters and gradients 365 and 389.
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
@@ -35,6 +46,7 @@
 
 #include "soma.h"
 #include "soma_host.hpp"
+#include "soma_rng.hpp"
 #include "soma_types.hpp"
 
 namespace soma {
@@ -75,6 +87,12 @@ struct Rates {
   double lr;
 };
 
+// Random rounding: Philox's key and the update's part of its counter, the tensor.
+struct Draw {
+  uint2 key;
+  uint32_t t, tensor;
+};
+
 // A block's scale from its largest magnitude, and the factor that brings its
 // values onto the code's range (0 for a block of zeros, or one whose largest
 // has no finite factor).
@@ -107,6 +125,48 @@ __device__ __forceinline__ uint32_t e4m3_four(const float (&y)[4]) {
 template <int kByte>
 __device__ __forceinline__ float e4m3_value(uint32_t w) {
   return __builtin_amdgcn_cvt_f32_fp8(static_cast<int>(w), kByte);
+}
+
+// Random rounding of four elements from element `at` on, a multiple of four.  Each has a
+// word of Philox4x32-10 with key stream_key(seed, t), counter (lo32(at / 4), tensor,
+// lo32(t), hi32(at / 4)): its upper 20 bits are v's draw, the lower 12 m's, both at the
+// middle of their interval, (draw + 1/2) 2^-20 and 2^-12.
+
+// y, |y| <= 448 up to a rounding, to one of the two e4m3 values beside it, away from 0
+// if the draw is below (|y| - lower) / (upper - lower).  Below 2^-6 the steps are
+// 2^-9, as they are in [2^-6, 2^-5): the value is moved there and back.
+__device__ __forceinline__ float random_e4m3(float y, uint32_t draw) {
+  const float a = __builtin_fabsf(y), shift = a < 0x1p-6f ? 0x1p-6f : 0.0f;
+  const uint32_t b = (__float_as_uint(a + shift) + 0xFFFFFu - (draw * 256u + 128u)) & ~0xFFFFFu;
+  return __builtin_copysignf(fminf(__uint_as_float(b) - shift, kTopM), y);
+}
+
+// The code of one of the two roots beside y, the larger one if the draw is below
+// (y^2 - lower^2) / (larger^2 - lower^2): it is v, the square, whose expected value
+// stays.  As to nearest, what is not 0 keeps code 1, and NaN and infinity have 255.
+__device__ __forceinline__ uint32_t random_root_code(float y, uint32_t draw) {
+  const uint32_t b = __float_as_uint(y) & 0x7FFFFFFFu, low = b & ~0x7FFFFu;
+  const float y0 = __uint_as_float(low), y1 = __uint_as_float(low + 0x80000u);
+  const float u = static_cast<float>(2u * draw + 1u) * 0x1p-21f;
+  int k = static_cast<int>(b >> 19) - kRootBias + (u * ((y1 - y0) * (y1 + y0)) < (y - y0) * (y + y0) ? 1 : 0);
+  k = k < 1 ? 1 : (k > 255 ? 255 : k);
+  return y == 0.0f ? 0u : static_cast<uint32_t>(k);
+}
+
+// ym: m over its scale, left rounded to e4m3's values; yr: the roots over theirs.
+// Returns the roots' codes.
+__device__ __forceinline__ uint32_t random_codes(const Draw& d, int64_t at, float (&ym)[4], const float (&yr)[4]) {
+  const uint64_t q = static_cast<uint64_t>(at) >> 2;
+  const uint4 x = philox4x32_10(make_uint4(static_cast<uint32_t>(q), d.tensor, d.t, static_cast<uint32_t>(q >> 32)), d.key);
+  const uint32_t w[4] = {x.x, x.y, x.z, x.w};
+  uint32_t codes = 0;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const float r = random_e4m3(ym[i], w[i] & 0xFFFu);
+    ym[i] = __builtin_fabsf(ym[i]) < 1e30f ? r : ym[i];
+    codes |= random_root_code(yr[i], w[i] >> 12) << (8 * i);
+  }
+  return codes;
 }
 
 // Largest finite magnitude of four.
@@ -204,8 +264,9 @@ __device__ __forceinline__ void decode(uint32_t mw, uint32_t vw, float ms, float
 }
 
 // The wave's 256 elements from `block` on, any length and alignment.
-template <class P, class G, bool kBytes>
-__device__ __forceinline__ void adamw_round(const Tensor& t, int64_t block, const Rates& r, float scale, float keep) {
+template <class P, class G, bool kBytes, bool kRandom>
+__device__ __forceinline__ void adamw_round(const Tensor& t, int64_t block, const Rates& r, const Draw& d, float scale,
+                                            float keep) {
   const int lane = threadIdx.x & 63;
   const bool wide = t.wide != 0;
   P* const param = static_cast<P*>(t.param);
@@ -244,10 +305,17 @@ __device__ __forceinline__ void adamw_round(const Tensor& t, int64_t block, cons
     const float fm = code_factor(top_m, kTopM), fr = code_factor(top_r, kTopRoot);
     float y[4];
     uint32_t vw = 0;
+    if constexpr (kRandom) {
+      float yr[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      y[i] = m[i] * fm;
-      vw |= root_code(root[i] * fr) << (8 * i);
+      for (int i = 0; i < 4; ++i) y[i] = m[i] * fm, yr[i] = root[i] * fr;
+      vw = random_codes(d, at, y, yr);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        y[i] = m[i] * fm;
+        vw |= root_code(root[i] * fr) << (8 * i);
+      }
     }
     store_codes(static_cast<uint8_t*>(t.m), at, n, wide, e4m3_four(y));
     store_codes(static_cast<uint8_t*>(t.v), at, n, wide, vw);
@@ -286,9 +354,9 @@ struct RawBytes {
 // any of the 256.  In those ranges nothing is subnormal, infinite or NaN, so the
 // root, the quotients and the codes need none of the steps that look for it: 54
 // operations for each element where there were 100.
-template <class P, class G>
-__device__ __forceinline__ bool adamw_ordinary(const Tensor& t, int64_t block, const Rates& r, float scale, float keep,
-                                               const RawBytes<P, G>& raw) {
+template <class P, class G, bool kRandom>
+__device__ __forceinline__ bool adamw_ordinary(const Tensor& t, int64_t block, const Rates& r, const Draw& d, float scale,
+                                               float keep, const RawBytes<P, G>& raw) {
   const int lane = threadIdx.x & 63;
   float p[4], g[4], m[4], v[4];
   Four<P>::values(raw.p, p);
@@ -322,17 +390,27 @@ __device__ __forceinline__ bool adamw_ordinary(const Tensor& t, int64_t block, c
   }
   const float top_r = wave_max(fmaxf(fmaxf(root[0], root[1]), fmaxf(root[2], root[3])));
   const float fm = kTopM * ordinary_inverse(top_m), fr = kTopRoot * ordinary_inverse(top_r);
-  int mw = __builtin_amdgcn_cvt_pk_fp8_f32(m[0] * fm, m[1] * fm, 0, false);
-  mw = __builtin_amdgcn_cvt_pk_fp8_f32(m[2] * fm, m[3] * fm, mw, true);
+  const int64_t at = block + lane * 4;
+  float y[4];
   uint32_t vw = 0;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const uint32_t b = __float_as_uint(root[i] * fr);
-    // negative codes are wanted: what is below code 1 becomes 1
-    const int k = static_cast<int>(b + ((b >> 19) & 1u) + (0x3FFFFu - (uint32_t(kRootBias) << 19))) >> 19;
-    vw |= static_cast<uint32_t>(k < 1 ? 1 : k) << (8 * i);
+  for (int i = 0; i < 4; ++i) y[i] = m[i] * fm;
+  if constexpr (kRandom) {
+    float yr[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) yr[i] = root[i] * fr;
+    vw = random_codes(d, at, y, yr);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t b = __float_as_uint(root[i] * fr);
+      // negative codes are wanted: what is below code 1 becomes 1
+      const int k = static_cast<int>(b + ((b >> 19) & 1u) + (0x3FFFFu - (uint32_t(kRootBias) << 19))) >> 19;
+      vw |= static_cast<uint32_t>(k < 1 ? 1 : k) << (8 * i);
+    }
   }
-  const int64_t at = block + lane * 4;
+  int mw = __builtin_amdgcn_cvt_pk_fp8_f32(y[0], y[1], 0, false);
+  mw = __builtin_amdgcn_cvt_pk_fp8_f32(y[2], y[3], mw, true);
   store_four(static_cast<P*>(t.param) + at, make_float4(p[0], p[1], p[2], p[3]));
   if (t.copy) store_four(static_cast<bf16*>(t.copy) + at, make_float4(p[0], p[1], p[2], p[3]));
   *reinterpret_cast<uint32_t*>(static_cast<uint8_t*>(t.m) + at) = static_cast<uint32_t>(mw);
@@ -345,8 +423,8 @@ __device__ __forceinline__ bool adamw_ordinary(const Tensor& t, int64_t block, c
   return true;
 }
 
-template <class P, class G, bool kBytes>
-__device__ __forceinline__ void adamw_chunk(const Tensor& t, int64_t first, const Rates& r, float scale) {
+template <class P, class G, bool kBytes, bool kRandom>
+__device__ __forceinline__ void adamw_chunk(const Tensor& t, int64_t first, const Rates& r, const Draw& d, float scale) {
   const int wave = threadIdx.x >> 6;
   const float keep = static_cast<float>(1.0 - r.lr * t.decay);
   first += wave * kStateBlock;
@@ -358,8 +436,8 @@ __device__ __forceinline__ void adamw_chunk(const Tensor& t, int64_t first, cons
       for (int k = 0; k < kRounds; ++k) raw[k].load(t, first + k * 4 * kStateBlock);
 #pragma unroll
       for (int k = 0; k < kRounds; ++k)
-        if (!adamw_ordinary<P, G>(t, first + k * 4 * kStateBlock, r, scale, keep, raw[k]))
-          adamw_round<P, G, true>(t, first + k * 4 * kStateBlock, r, scale, keep);
+        if (!adamw_ordinary<P, G, kRandom>(t, first + k * 4 * kStateBlock, r, d, scale, keep, raw[k]))
+          adamw_round<P, G, true, kRandom>(t, first + k * 4 * kStateBlock, r, d, scale, keep);
       return;
     }
   }
@@ -368,25 +446,27 @@ __device__ __forceinline__ void adamw_chunk(const Tensor& t, int64_t first, cons
   for (int k = 0; k < kRounds; ++k) {
     const int64_t block = first + k * 4 * kStateBlock;            // the wave's 256 elements
     if (block >= end) break;                                      // wave-uniform
-    adamw_round<P, G, kBytes>(t, block, r, scale, keep);
+    adamw_round<P, G, kBytes, kBytes && kRandom>(t, block, r, d, scale, keep);
   }
 }
 
-__global__ __launch_bounds__(kThreadsAdamw) void k_adamw(const Tensor* tensors, const Block* blocks, Rates r,
+template <bool kRandom>
+__global__ __launch_bounds__(kThreadsAdamw) void k_adamw(const Tensor* tensors, const Block* blocks, Rates r, Draw d,
                                                          const float* grad_scale) {
   const Block b = blocks[blockIdx.x];
   const Tensor t = tensors[b.tensor];
   const float scale = grad_scale ? *grad_scale : 1.0f;
   const int64_t first = int64_t(b.chunk) * r.chunk;
+  d.tensor = b.tensor;
   switch (t.kind) {
-    case 0: adamw_chunk<float, float, false>(t, first, r, scale); break;
-    case 1: adamw_chunk<float, float, true>(t, first, r, scale); break;
-    case 2: adamw_chunk<float, bf16, false>(t, first, r, scale); break;
-    case 3: adamw_chunk<float, bf16, true>(t, first, r, scale); break;
-    case 4: adamw_chunk<bf16, float, false>(t, first, r, scale); break;
-    case 5: adamw_chunk<bf16, float, true>(t, first, r, scale); break;
-    case 6: adamw_chunk<bf16, bf16, false>(t, first, r, scale); break;
-    default: adamw_chunk<bf16, bf16, true>(t, first, r, scale); break;
+    case 0: adamw_chunk<float, float, false, kRandom>(t, first, r, d, scale); break;
+    case 1: adamw_chunk<float, float, true, kRandom>(t, first, r, d, scale); break;
+    case 2: adamw_chunk<float, bf16, false, kRandom>(t, first, r, d, scale); break;
+    case 3: adamw_chunk<float, bf16, true, kRandom>(t, first, r, d, scale); break;
+    case 4: adamw_chunk<bf16, float, false, kRandom>(t, first, r, d, scale); break;
+    case 5: adamw_chunk<bf16, float, true, kRandom>(t, first, r, d, scale); break;
+    case 6: adamw_chunk<bf16, bf16, false, kRandom>(t, first, r, d, scale); break;
+    default: adamw_chunk<bf16, bf16, true, kRandom>(t, first, r, d, scale); break;
   }
 }
 
@@ -529,6 +609,8 @@ struct soma_adamw {
   const soma::Tensor* tensors;       // device
   const soma::Block* blocks;         // device
   int64_t* first_chunk;              // host, [n + 1]
+  int32_t rounding;                  // enum soma_rounding
+  uint64_t seed;
 };
 
 using namespace soma;
@@ -586,7 +668,8 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
     return set_error(SOMA_EDEVICE, "copying the tensors' table: %s", hipGetErrorString(e));
   }
   *plan = soma_adamw{n, chunk, chunks, static_cast<const Tensor*>(workspace),
-                     reinterpret_cast<const Block*>(static_cast<char*>(workspace) + table_bytes(n)), first};
+                     reinterpret_cast<const Block*>(static_cast<char*>(workspace) + table_bytes(n)), first,
+                     SOMA_ROUND_NEAREST, 0};
   *out = plan;
   return set_ok();
 }
@@ -595,6 +678,15 @@ void soma_adamw_destroy(soma_adamw* plan) {
   if (!plan) return;
   delete[] plan->first_chunk;
   delete plan;
+}
+
+int soma_adamw_set_rounding(soma_adamw* plan, int32_t rounding, uint64_t seed) {
+  if (!plan) return set_error(SOMA_EINVAL, "plan is NULL");
+  if (rounding != SOMA_ROUND_NEAREST && rounding != SOMA_ROUND_RANDOM)
+    return set_error(SOMA_EINVAL, "unknown rounding %d", rounding);
+  plan->rounding = rounding;
+  plan->seed = seed;
+  return set_ok();
 }
 
 int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double beta2, double delta,
@@ -610,8 +702,13 @@ int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double
   const double bc1 = 1.0 - std::pow(beta1, double(t)), bc2 = 1.0 - std::pow(beta2, double(t));
   const Rates r{float(beta1), float(1.0 - beta1), float(beta2), float(1.0 - beta2), float(lr / bc1),
                 float(1.0 / std::sqrt(bc2)), float(delta), 1.0 / std::sqrt(bc2) <= 0x1p30 && delta <= 0x1p30, plan->chunk, lr};
-  hipLaunchKernelGGL(k_adamw, dim3(unsigned(plan->chunks)), dim3(kThreadsAdamw), 0, stream_of(stream), plan->tensors,
-                     plan->blocks, r, grad_scale);
+  // stream_key(seed, t)
+  const Draw d{make_uint2(uint32_t(plan->seed), uint32_t(plan->seed >> 32) ^ uint32_t(uint64_t(t) >> 32)), uint32_t(t), 0};
+  const dim3 grid(unsigned(plan->chunks)), block(kThreadsAdamw);
+  if (plan->rounding == SOMA_ROUND_RANDOM)
+    hipLaunchKernelGGL(k_adamw<true>, grid, block, 0, stream_of(stream), plan->tensors, plan->blocks, r, d, grad_scale);
+  else
+    hipLaunchKernelGGL(k_adamw<false>, grid, block, 0, stream_of(stream), plan->tensors, plan->blocks, r, d, grad_scale);
   if (int rc = launched("k_adamw")) return rc;
   return set_ok();
 }

@@ -31,7 +31,7 @@ EXPORTS = ("soma_param_count", "soma_workspace_size", "soma_create", "soma_destr
            "soma_get_phase_times", "soma_get_narrow_projections", "soma_set_spin_limit", "soma_spsa_step_noalloc",
            "soma_scan_workspace_size", "soma_scan_forward", "soma_scan_backward", "soma_scan_step",
            "soma_ce_workspace_size", "soma_ce_loss", "soma_ce_grad", "soma_adamw_workspace_size", "soma_adamw_create",
-           "soma_adamw_destroy", "soma_adamw_step", "soma_adamw_moments", "soma_last_error")
+           "soma_adamw_destroy", "soma_adamw_set_rounding", "soma_adamw_step", "soma_adamw_moments", "soma_last_error")
 
 
 class SomaError(RuntimeError):
@@ -81,6 +81,7 @@ class Config(ctypes.Structure):
 TYPE_FLOAT, TYPE_BFLOAT = 0, 1
 SCAN_BLOCK = 32             # rows between the states that a backward scan starts from
 ADAMW_BLOCK = 256           # elements that share the scales of 8-bit moments
+ROUNDINGS = {"nearest": 0, "random": 1}
 
 
 class ScanConfig(ctypes.Structure):
@@ -155,6 +156,7 @@ def load():
             "soma_adamw_create": (ctypes.c_int, [ctypes.POINTER(AdamWTensor), ctypes.c_int32, vp, ctypes.c_size_t, vp,
                                                  ctypes.POINTER(vp)]),
             "soma_adamw_destroy": (None, [vp]),
+            "soma_adamw_set_rounding": (ctypes.c_int, [vp, ctypes.c_int32, ctypes.c_uint64]),
             "soma_adamw_step": (ctypes.c_int, [vp, ctypes.c_int64] + [ctypes.c_double] * 4 + [vp, vp]),
             "soma_adamw_moments": (ctypes.c_int, [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]),
             "soma_last_error": (ctypes.c_char_p, []),
@@ -650,10 +652,15 @@ class AdamW(_Plan):
     plan uses at every step: keep them in place.  bits: moments in 32 or in 8.
     weight_decay: one value, or one for each tensor.  moments: a list of (m, v),
     or for 8 bits (m, v, m_scale, v_scale), to go on from; None: zeros.  copies:
-    bfloat16 tensors (or None) that receive the new parameters too."""
+    bfloat16 tensors (or None) that receive the new parameters too.
+
+    rounding of moments in 8 bits: "random" for a training run, drawn from seed
+    and the update's number, or "nearest", the closest codes of a single step.  To
+    nearest, v does not follow its average over many steps, since updates of less
+    than half a code (3 to 6% of v) are lost."""
 
     def __init__(self, params, grads, bits: int = 32, weight_decay=0.01, betas=(0.9, 0.999), delta: float = 1e-8,
-                 moments=None, copies=None, stream=None):
+                 moments=None, copies=None, stream=None, rounding: str = "nearest", seed: int = 0):
         import torch
         self._h = ctypes.c_void_p()
         params, grads = list(params), list(grads)
@@ -664,6 +671,8 @@ class AdamW(_Plan):
             raise ValueError("params must not be empty; grads, copies and weight_decay must be as many")
         if bits not in (8, 32):
             raise ValueError("bits must be 8 or 32")
+        if rounding not in ROUNDINGS:
+            raise ValueError(f"rounding must be one of {sorted(ROUNDINGS)}")
         if not isinstance(params[0], torch.Tensor) or params[0].device.type != "cuda":
             raise TypeError("params must be device tensors")
         self.device, self.bits, self.betas, self.delta = params[0].device, bits, tuple(betas), float(delta)
@@ -711,6 +720,8 @@ class AdamW(_Plan):
             _check(load().soma_adamw_create(table, n, self._ws, out.value, ctypes.c_void_p(st.cuda_stream),
                                             ctypes.byref(plan)))
         self._h = plan
+        self.rounding, self.seed = rounding, int(seed)
+        _check(load().soma_adamw_set_rounding(plan, ROUNDINGS[rounding], self.seed & (2**64 - 1)))
 
     def close(self):
         if self._h.value:
