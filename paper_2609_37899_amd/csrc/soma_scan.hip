@@ -834,7 +834,7 @@ int soma_scan_backward(const soma_scan_config* cfg, const void* gates, const int
   if (!is_aligned(gates, e) || !is_aligned(dh, e) || !is_aligned(dgates, e) || !is_aligned(dcT, 4) ||
       !is_aligned(dc0, 4) || !is_aligned(states, 4))
     return set_error(SOMA_EINVAL, "a pointer is not aligned to its elements");
-  if (dgates == gates || (c.rows > 0 && dgates == dh)) return set_error(SOMA_EINVAL, "dgates must be an array of its own");
+  if (c.rows > 0 && (dgates == gates || dgates == dh)) return set_error(SOMA_EINVAL, "dgates must be an array of its own");
   if (int rc = check_workspace(workspace, ws_bytes, scan_workspace(c))) return rc;
   ScanArgs a{};
   if (int rc = fill(c, gates, offsets, c0, &a)) return rc;
