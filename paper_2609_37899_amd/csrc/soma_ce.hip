@@ -1401,7 +1401,7 @@ int soma_ce_grad(const soma_ce_config* cfg, const void* f, const void* E, const 
   if (int rc = check_ce(cfg)) return rc;
   const soma_ce_config& c = *cfg;
   const size_t e = type_size(c.type);
-  if (!df && !dE) return set_error(SOMA_EINVAL, "neither df nor dE is wanted");
+  if (c.rows > 0 && !df && !dE) return set_error(SOMA_EINVAL, "neither df nor dE is wanted");   // of no rows, df has no address
   if (c.rows > 0 && (!f || !E || !targets || !lse || !grad_loss)) return set_error(SOMA_EINVAL, "NULL device pointer");
   if (!is_aligned(f, e) || !is_aligned(E, e) || !is_aligned(targets, 4) || !is_aligned(lse, 4) ||
       !is_aligned(grad_loss, 4))
