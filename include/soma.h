@@ -545,8 +545,9 @@ enum soma_type {
  *   states  [ceil(rows / SOMA_SCAN_BLOCK)][width] fp32: what the backward pass
  *           needs, the state in front of every SOMA_SCAN_BLOCK-th row.  NULL:
  *           not wanted.
- * gates and h have `type`; states and arithmetic are fp32, sigma and tanh to
- * 2^-22 (of 1, not of a small value).  Constraints: rows in [0, 2^30], width in
+ * gates and h have `type`; states and arithmetic are fp32, tanh(x) to 2^-20 of the
+ * value (bf16 gates: 2^-15) and sigma(x) to (2 |x| + 6) 2^-24, the gradients'
+ * factors 1 - sigma and 1 - tanh^2 to as much of 1.  Constraints: rows in [0, 2^30], width in
  * [1, 2^20], sequences in [1, 65535]. */
 #define SOMA_SCAN_BLOCK 32
 
