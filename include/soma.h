@@ -613,8 +613,9 @@ int soma_ce_workspace_size(const soma_ce_config* cfg, int grad, size_t* bytes);
 int soma_ce_loss(const soma_ce_config* cfg, const void* f_dev, const void* E_dev, const int32_t* targets_dev,
                  float* loss_dev, float* lse_dev, void* workspace_dev, size_t workspace_bytes, void* stream);
 
-/* The gradients of sum_r w_r loss_r (w = grad_loss [rows] fp32, of any sign),
- * with the lse that soma_ce_loss gave:
+/* The gradients of sum_r w_r loss_r (w = grad_loss [rows] fp32, of any sign; one
+ * that is not finite makes its row of df so, and dE), with the lse that
+ * soma_ce_loss gave:
  *   df_r = w_r (sum_v p_rv E_v - E_{t_r}),  dE_v = sum_r w_r (p_rv - [v = t_r]) f_r.
  *   df [rows][width], dE [vocab][width], contiguous, 16-byte aligned; either
  *   may be NULL: not wanted. */

@@ -18,8 +18,9 @@
 // operand as two fp16 parts, x s = hi + lo to nearest with a power of two s that
 // brings its array's largest magnitude to 2^13 .. 2^14, and a b as lo hi + hi lo
 // + hi hi: 2^-22 of a value, or 2^-38 of its array's largest.  The weight w_r
-// enters as c (w_r / c) with c = max |w|, whose c is multiplied in fp32: under a
-// mean, the common case, the factor inside is exactly 1.
+// enters as c (w_r / c) with c the largest finite |w|, whose c is multiplied in fp32:
+// under a mean, the common case, the factor inside is exactly 1.  (A weight that is
+// not finite is its row's alone.)
 //
 // Fragment order: a matrix [rows][K] is blocks of 1 KiB, [row / 16][part][k / 32],
 // of 64 words of 8 halves, word 16 lg + lr holding row lr, k 8 lg .. + 7: what lane
@@ -57,7 +58,7 @@ struct RowMeta {
   int target, pad;
 };
 
-// Scales of the fp32 path (1 for bf16) and the largest weight.
+// Scales of the fp32 path (1 for bf16) and the largest finite weight.
 struct Scales {
   float f, e, c, pad;
 };
@@ -143,12 +144,8 @@ __global__ __launch_bounds__(256) void k_ce_max(MaxArgs a, int first) {
       for (int i = 0; i < 4 && k + i < a.K; ++i) top = fmaxf(top, finite_abs(load_value(p + k + i)));
     }
   } else if (a.w) {
-    // not finite: the largest is not either, and every gradient says so
     for (int r = blockIdx.x * 256 + threadIdx.x; r < a.R; r += gridDim.x * 256)
-      if (a.targets[r] >= 0) {
-        const float w = __builtin_fabsf(a.w[r]);
-        top = w <= 3.402823466e38f ? fmaxf(top, w) : __builtin_inff();
-      }
+      if (a.targets[r] >= 0) top = fmaxf(top, finite_abs(a.w[r]));
   }
   top = block_max(top, lds);
   if (threadIdx.x == 0) a.maxima[which * kMaxima + blockIdx.x] = top;
@@ -261,7 +258,7 @@ __global__ __launch_bounds__(256) void k_ce_pack(PackPair pair) {
       const int t = a.targets[r];
       if (t >= 0) {
         m.lse = a.lse[r];
-        m.rho = c > 0.0f ? a.w[r] / c : 0.0f;
+        m.rho = c > 0.0f ? a.w[r] / c : a.w[r];   // c = 0: 0, infinite or NaN
         m.target = t;
         if (t >= a.V) m.rho = __builtin_nanf("");
       }
