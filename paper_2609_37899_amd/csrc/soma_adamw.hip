@@ -101,7 +101,7 @@ __device__ __forceinline__ float code_factor(float top, float largest) {
 }
 
 __device__ __forceinline__ uint32_t root_code(float y) {
-  const uint32_t b = __float_as_uint(y);
+  const uint32_t b = __float_as_uint(y) & 0x7FFFFFFFu;   // NaN may have a sign, which the sum would carry past 2^32
   int k = static_cast<int>((b + 0x3FFFFu + ((b >> 19) & 1u)) >> 19) - kRootBias;
   k = k < 1 ? 1 : (k > 255 ? 255 : k);    // NaN and infinity: 255
   return y == 0.0f ? 0u : static_cast<uint32_t>(k);
