@@ -687,7 +687,8 @@ enum soma_rounding {
 int soma_adamw_set_rounding(soma_adamw* plan, int32_t rounding, uint64_t seed);
 
 /* Update number t >= 1 of every tensor.  grad_scale_dev: s, one fp32 value on
- * the device (loss scaling, clipping); NULL: 1. */
+ * the device (loss scaling, clipping); NULL: 1.  lr / (1 - beta1^t) and delta > 0
+ * must be so in fp32. */
 int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double beta2, double delta,
                     const float* grad_scale_dev, void* stream);
 

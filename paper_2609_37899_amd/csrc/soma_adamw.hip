@@ -696,10 +696,11 @@ int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double
   if (!std::isfinite(lr)) return set_error(SOMA_EINVAL, "lr must be finite");
   if (!(beta1 >= 0.0 && beta1 < 1.0 && beta2 >= 0.0 && beta2 < 1.0))
     return set_error(SOMA_EINVAL, "beta1 and beta2 must be in [0, 1)");
-  if (!(std::isfinite(delta) && delta > 0.0)) return set_error(SOMA_EINVAL, "delta must be finite and > 0");
+  if (!(std::isfinite(float(delta)) && float(delta) > 0.0f)) return set_error(SOMA_EINVAL, "delta must be finite and > 0 in fp32");
   if (!is_aligned(grad_scale, 4)) return set_error(SOMA_EINVAL, "grad_scale must be 4-byte aligned");
   if (plan->chunks == 0) return set_ok();
   const double bc1 = 1.0 - std::pow(beta1, double(t)), bc2 = 1.0 - std::pow(beta2, double(t));
+  if (!std::isfinite(float(lr / bc1))) return set_error(SOMA_EINVAL, "lr / (1 - beta1^t) must be finite in fp32");
   const Rates r{float(beta1), float(1.0 - beta1), float(beta2), float(1.0 - beta2), float(lr / bc1),
                 float(1.0 / std::sqrt(bc2)), float(delta), 1.0 / std::sqrt(bc2) <= 0x1p30 && delta <= 0x1p30, plan->chunk, lr};
   // stream_key(seed, t)

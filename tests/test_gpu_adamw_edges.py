@@ -24,3 +24,21 @@ def test_codes_of_gradients_that_are_not_finite(bits, rounding):
     m, v = (x.cpu().numpy() for x in plan.state[0][:2])
     assert m[300] & 127 == 127 and v[300] == 255
     assert not torch.isfinite(p[300]) and torch.isfinite(p[:300]).all() and torch.isfinite(p[301:]).all()
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_rates_that_fp32_does_not_hold_are_refused(bits):
+    """delta of 0 in fp32 would make 0 / 0 of an element without gradients; rates beyond fp32's range are infinite."""
+    torch = require_gpu()
+    p, grad = torch.ones(300, device="cuda"), torch.zeros(300, device="cuda")
+    for delta in (1e-46, 1e39):
+        plan = soma.AdamW([p], [grad], bits=bits, delta=delta)
+        with pytest.raises(soma.SomaError):
+            plan.step(1, 1e-3)
+    plan = soma.AdamW([p], [grad], bits=bits, delta=1e-44)       # fp32's smallest values are among them
+    for lr in (1e39, -1e39, 3e38):                               # 3e38 / (1 - 0.9)
+        with pytest.raises(soma.SomaError):
+            plan.step(1, lr)
+    plan.step(1, 1e-3)
+    torch.cuda.synchronize()
+    assert torch.allclose(p, torch.full_like(p, 1 - 1e-5))       # the decay alone
