@@ -515,8 +515,8 @@ int soma_get_narrow_projections(const soma_ctx* ctx, int32_t* launches);
  *     may;
  *   - every sum is formed in a fixed order in 32 bits or more: repeated calls
  *     give the same bits;
- *   - every call can be captured into a HIP graph (soma_adamw_create cannot:
- *     it waits for its copy to the device).
+ *   - every call can be captured into a HIP graph, with the scalars that it was
+ *     given (soma_adamw_create cannot: it waits for its copy to the device).
  * ------------------------------------------------------------------------- */
 
 /* Types of the operators' arrays. */
@@ -687,8 +687,10 @@ enum soma_rounding {
 int soma_adamw_set_rounding(soma_adamw* plan, int32_t rounding, uint64_t seed);
 
 /* Update number t >= 1 of every tensor.  grad_scale_dev: s, one fp32 value on
- * the device (loss scaling, clipping); NULL: 1.  lr / (1 - beta1^t) and delta > 0
- * must be so in fp32. */
+ * the device (loss scaling, clipping); NULL: 1.  lr / (1 - beta1^t) must be finite
+ * and delta > 0 in fp32.  t and the rates belong to the call: a captured step
+ * repeats them, and its random rounding, at every replay; a run that goes on
+ * calls the step anew, or captures it anew, for each update. */
 int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double beta2, double delta,
                     const float* grad_scale_dev, void* stream);
 

@@ -736,7 +736,8 @@ class AdamW(_Plan):
 
     def step(self, t: int, lr: float, grad_scale=None, stream=None):
         """Update number t >= 1.  grad_scale: one float32 value on the device
-        that every gradient is multiplied with (None: 1)."""
+        that every gradient is multiplied with (None: 1).  A captured step repeats
+        its t, its lr and its random rounding at every replay."""
         import torch
         if not self._h.value:
             raise RuntimeError("the plan is closed")
