@@ -635,6 +635,12 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
   if (int rc = check_apart(tensors, n)) return rc;
   const size_t need = table_bytes(n) + up256(size_t(chunks) * sizeof(Block));
   if (int rc = check_workspace(workspace, ws_bytes, need)) return rc;
+  const hipStream_t st = stream_of(stream);
+  // Waiting for a stream that records a graph would end the recording.
+  hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
+  hipError_t e = hipStreamIsCapturing(st, &recording);
+  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipStreamIsCapturing: %s", hipGetErrorString(e));
+  if (recording != hipStreamCaptureStatusNone) return set_error(SOMA_EINVAL, "a plan cannot be made on a stream that is captured");
   char* host = new (std::nothrow) char[need]();
   int64_t* first = new (std::nothrow) int64_t[size_t(n) + 1];
   soma_adamw* plan = new (std::nothrow) soma_adamw;
@@ -658,8 +664,7 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
     for (int64_t c = 0; c < chunks_of(x.count, chunk); ++c) bb[at++] = Block{i, int32_t(c)};
   }
   first[n] = at;
-  const hipStream_t st = stream_of(stream);
-  hipError_t e = hipMemcpyAsync(workspace, host, need, hipMemcpyHostToDevice, st);
+  e = hipMemcpyAsync(workspace, host, need, hipMemcpyHostToDevice, st);
   if (e == hipSuccess) e = hipStreamSynchronize(st);
   delete[] host;
   if (e != hipSuccess) {

@@ -42,3 +42,25 @@ def test_rates_that_fp32_does_not_hold_are_refused(bits):
     plan.step(1, 1e-3)
     torch.cuda.synchronize()
     assert torch.allclose(p, torch.full_like(p, 1 - 1e-5))       # the decay alone
+
+
+def test_a_plan_is_not_made_in_a_capture_and_leaves_it_whole():
+    torch = require_gpu()
+    n = 300
+    p, grad = torch.ones(n, device="cuda"), torch.ones(n, device="cuda")
+    q = p.clone()
+    moments = [(torch.zeros(n, device="cuda"), torch.zeros(n, device="cuda")) for _ in range(2)]
+    plan, eager = soma.AdamW([p], [grad], moments=moments[:1]), soma.AdamW([q], [grad], moments=moments[1:])
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        plan.step(1, 1e-3)
+        with pytest.raises(soma.SomaError, match="captured"):
+            soma.AdamW([p], [grad], moments=moments[:1])
+        plan.step(2, 1e-3)
+    for _ in range(3):
+        graph.replay()
+        for t in (1, 2):
+            eager.step(t, 1e-3)
+        torch.cuda.synchronize()
+        assert torch.equal(p, q) and all(torch.equal(a, b) for a, b in zip(*moments))
