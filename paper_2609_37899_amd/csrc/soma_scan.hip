@@ -779,8 +779,7 @@ int fill(const soma_scan_config& c, const void* gates, const int32_t* offsets, c
   a->rows = c.rows;
   a->H = c.width;
   a->S = c.sequences;
-  a->length = c.rows / c.sequences;
-  if (!offsets && a->length == 0) a->length = 1;       // rows == 0: every sequence is empty (first_row is clamped)
+  a->length = c.rows / c.sequences;                    // 0: every sequence is empty
   return SOMA_OK;
 }
 

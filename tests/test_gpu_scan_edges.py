@@ -5,6 +5,7 @@ import pytest
 import train_reference as ref
 from gpu_common import require_gpu
 from paper_2609_37899_amd import soma
+from test_gpu_scan import check, make, run
 
 pytestmark = pytest.mark.gpu
 
@@ -74,3 +75,37 @@ def test_small_states_keep_their_digits(dtype, lengths, scale):
         tol = tol * (1 + 2.0**-8) + (ref.half_step(dtype) if y.dtype != torch.float32 else 0)
         rel = np.abs(y.double().cpu().numpy() - exact) / np.abs(exact)
         assert rel.max() <= tol, (name, rel.max(), tol)
+
+
+@pytest.mark.parametrize("behind", [0, 9])
+def test_many_ragged_sequences_two_channels_a_lane(behind):
+    """600 sequences in one launch: enough blocks for two bf16 channels a lane without pieces."""
+    torch = require_gpu()
+    H = 130
+    lengths = [int(k) for k in np.random.default_rng(7).integers(0, 70, 600)]
+    x, want = make(torch, "bfloat16", H, lengths, behind=behind)
+    plan = soma.GatedScan(x["gates"].shape[0], len(lengths), H, torch.bfloat16)
+    y = run(torch, plan, x, "bfloat16")
+    torch.cuda.synchronize()
+    check(y, want, "bfloat16")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("off", [[0, 500, 4000, 1 << 30], [-5, 600, 200, 2000], [0, 0, 0, -1], [1900, 100, 50, 2000],
+                                 [0, 1500, 700, 1000]])
+def test_offsets_that_break_the_rules_in_pieces_stay_inside(dtype, off):
+    """Rows enough for pieces: both walks over a piece's sequences go on at every step whatever the offsets say, and rows
+    behind the arrays stay as they were."""
+    torch = require_gpu()
+    H, rows, dt = 64, 2000, getattr(torch, dtype)
+    plan = soma.GatedScan(rows, 3, H, dt)
+    assert plan._bytes > 0                                # pieces
+    gates = torch.randn(rows, 4 * H, device="cuda").to(dt)
+    guard = torch.full((rows + 64, H), 7.0, device="cuda", dtype=dt)
+    dguard = torch.full((rows + 64, 4 * H), 7.0, device="cuda", dtype=dt)
+    o = torch.tensor(off, dtype=torch.int32, device="cuda")
+    states = torch.zeros_like(plan.new_states())
+    plan.forward(gates, guard[:rows], None, None, states, o)
+    plan.backward(gates, states, guard[:rows].clone(), dguard[:rows], None, None, None, o)
+    torch.cuda.synchronize()
+    assert (guard[rows:] == 7).all() and (dguard[rows:] == 7).all()
