@@ -5,6 +5,8 @@ import pytest
 import train_reference as ref
 from gpu_common import require_gpu
 from paper_2609_37899_amd import soma
+from test_gpu_adamw import B1, B2, DELTA, SIZES, arrays, check_tensor, expect, make
+from test_gpu_adamw_rounding import chunk_of
 
 pytestmark = pytest.mark.gpu
 
@@ -64,3 +66,80 @@ def test_a_plan_is_not_made_in_a_capture_and_leaves_it_whole():
             eager.step(t, 1e-3)
         torch.cuda.synchronize()
         assert torch.equal(p, q) and all(torch.equal(a, b) for a, b in zip(*moments))
+
+
+MANY = [1] * 1030                   # tensors of one element: a block each, so that all blocks take 4,096 elements
+
+
+@pytest.mark.parametrize("ptype,gtype", [("float32", "float32"), ("float32", "bfloat16"), ("bfloat16", "float32"),
+                                         ("bfloat16", "bfloat16")])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("shift", [0, 1])
+def test_blocks_of_4096_match_the_reference(ptype, gtype, bits, shift):
+    torch = require_gpu()
+    sizes = SIZES + [8192, 12288 + 255] + MANY
+    x = make(torch, ptype, gtype, bits, sizes, shift)
+    if bits == 8:
+        for s in x["state"][1::2]:
+            s[1].clamp_(min=1)                           # no code 0: the short way
+    decay = [0.1 * (k % 3) for k in range(len(sizes))]
+    copies = [torch.zeros(n, dtype=torch.bfloat16, device="cuda") if k % 3 else None for k, n in enumerate(sizes)]
+    plan = soma.AdamW(x["p"], x["g"], bits=bits, weight_decay=decay, betas=(B1, B2), delta=DELTA, moments=x["state"],
+                      copies=copies)
+    assert chunk_of(plan, sizes) == 4096
+    scale = torch.tensor([0.5], device="cuda")
+    for t in (1, 2, 1000):
+        want = expect(x, decay, t, 1e-2, 0.5)
+        plan.step(t, 1e-2, scale)
+        torch.cuda.synchronize()
+        for p, s, w in zip(x["p"], x["state"], want):
+            check_tensor(p, s, w, ptype, 1e-2)
+    outs = [[torch.zeros(n, device="cuda") for n in sizes] for _ in range(2)]
+    plan.moments(*outs)
+    torch.cuda.synchronize()
+    for k, s in enumerate(x["state"]):
+        m, v = ref.moments_of(*arrays(s))
+        assert np.all(np.abs(outs[0][k].cpu().numpy() - m) <= ref.U * np.abs(m))
+        assert np.all(np.abs(outs[1][k].cpu().numpy() - v) <= 3 * ref.U * v + 1e-44)
+        if copies[k] is not None:
+            c, p = copies[k].double().cpu().numpy(), x["p"][k].double().cpu().numpy()
+            assert np.all(np.abs(c - p) <= (2.0 ** -8 + ref.U) * np.abs(p))
+
+
+@pytest.mark.parametrize("rounding", ["nearest", "random"])
+@pytest.mark.parametrize("ptype,gtype", [("float32", "float32"), ("float32", "bfloat16"), ("bfloat16", "float32"),
+                                         ("bfloat16", "bfloat16")])
+def test_short_way_of_ordinary_blocks(ptype, gtype, rounding):
+    """Blocks of 4,096 aligned elements with moments in 8 bits take a shorter way where 256 hold ordinary values only.
+    The same tensors, aligned and one element further on (which never takes it), blocks of every kind side by side."""
+    torch = require_gpu()
+    n = 4096 * 50 + 77
+    x, y = (make(torch, ptype, gtype, 8, [n] + MANY, shift) for shift in (0, 1))
+    for z in (x, y):
+        m, v, _, _ = z["state"][0]
+        v.clamp_(min=1)                                   # no code 0
+        g = z["g"][0]
+        for k, (gv, mv, vv) in enumerate([(0.0, 0, 0), (1e-30, 0, 0), (1e18, 1, 1), (0.0, 40, 30), (float("inf"), 1, 1),
+                                          (float("nan"), 1, 1), (1e-12, 0, 1), (3e38, 126, 255), (1e-14, 0, 0),
+                                          (-float("inf"), 1, 1), (1e19, 3, 3), (0.0, 128, 1)]):
+            b = slice(256 * (3 * k + 1), 256 * (3 * k + 2) if k % 2 else 256 * (3 * k + 1) + 5)
+            g[b], m[b], v[b] = gv, mv, vv
+    before = x["p"][0].double()
+    plans = [soma.AdamW(z["p"], z["g"], bits=8, weight_decay=0.1, moments=z["state"], rounding=rounding, seed=6)
+             for z in (x, y)]
+    assert all(chunk_of(plan, [n] + MANY) == 4096 for plan in plans)
+    for t in (1, 2):
+        for plan in plans:
+            plan.step(t, 1e-2)
+        torch.cuda.synchronize()
+        a, b = x["p"][0].double(), y["p"][0].double()
+        # the quotients differ by a reciprocal's 2 u and two roundings, the products by two, the root by 2 u at most,
+        # then p's own roundings (its type's whole step where one falls the other way), and the first update's again
+        tol = t * (8 * ref.U * (b - before).abs() + (2 * ref.U + 2 * ref.half_step(ptype)) * b.abs())
+        same = torch.isfinite(b)
+        assert torch.equal(torch.isfinite(a), same)
+        assert ((a - b).abs()[same] <= tol[same]).all()
+        for u, w in zip(x["state"][0][:2], y["state"][0][:2]):
+            assert torch.equal(u, w)
+        for u, w in zip(x["state"][0][2:], y["state"][0][2:]):
+            assert ((u - w).abs() <= 4 * ref.U * w).all()
