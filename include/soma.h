@@ -547,7 +547,13 @@ enum soma_type {
  *           not wanted.
  * gates and h have `type`; states and arithmetic are fp32, tanh(x) to 2^-20 of the
  * value (bf16 gates: 2^-15) and sigma(x) to (2 |x| + 6) 2^-24, the gradients'
- * factors 1 - sigma and 1 - tanh^2 to as much of 1.  Constraints: rows in [0, 2^30], width in
+ * factors 1 - sigma and 1 - tanh^2 to as much of 1.  How the rows are shared out
+ * goes by the numbers of rows and sequences alone, since the lengths are on the
+ * device: with 256 or more sequences and groups of 64 channels, or up to 256 rows a
+ * sequence on average, each sequence is one block's, and one that is far longer
+ * than the others takes as long as its rows in a row do (60,000 rows beside 15 of
+ * 300, width 1,024, bf16: both passes 7.5 ms, as a call of its own 0.75).
+ * Constraints: rows in [0, 2^30], width in
  * [1, 2^20], sequences in [1, 65535]. */
 #define SOMA_SCAN_BLOCK 32
 
@@ -582,19 +588,22 @@ int soma_scan_step(const soma_scan_config* cfg, const void* gates_dev, const flo
                    void* stream);
 
 /* Softmax cross entropy of a linear head over a vocabulary of any size, and
- * its gradients, without the logits in memory:
+ * its gradients, without the logits in memory (a piece of the vocabulary at a
+ * time; for the gradients that piece of their softmax's part is, see
+ * soma_ce_workspace_size):
  *   l_rv = f_r . E_v,  lse_r = log sum_v exp(l_rv),  loss_r = lse_r - l_{r,t_r}.
  *   f       [rows][width], decoder inputs, rows f_stride elements apart.
  *   E       [vocab][width], the head, rows e_stride elements apart.
  *   targets [rows] int32.  A negative one: the row has no target; its loss and
- *           lse are 0, its gradient is zeros, and nothing that its f holds
- *           (infinities, NaN) reaches any result.  One >= vocab: the row's loss
+ *           lse are 0, its gradient is zeros (as long as E is finite), and
+ *           nothing that its f holds (infinities, NaN) reaches any result.  One >= vocab: the row's loss
  *           is NaN, and so are the gradients that it enters.
  * f, E and their gradients have `type`.  Products accumulate in fp32; fp32
  * operands enter as two fp16 parts with a power of two as scale for each array:
  * 2^-22 of a value, or 2^-38 of the array's largest finite magnitude where that
- * is more; bf16 operands enter as they are, and the softmax's part of a gradient
- * is rounded to bf16 (2^-8) before its products.
+ * is more, and so does the softmax's part of a gradient, w (p - [v = t]), whose
+ * largest counts as the largest |w|; bf16 operands enter as they are, and the
+ * softmax's part is rounded to bf16 (2^-8) before its products.
  * Constraints: rows in [0, 2^20], vocab in [1, 2^24], width in [1, 2^16]. */
 typedef struct soma_ce_config {
   int32_t rows;
@@ -606,7 +615,13 @@ typedef struct soma_ce_config {
 } soma_ce_config;
 
 /* Bytes of device workspace of soma_ce_loss, or (grad != 0) of both calls.  It
- * does not shrink with more rows, so a workspace serves calls of fewer.  Pure. */
+ * does not shrink with more rows, so a workspace serves calls of fewer.  The loss
+ * needs its operands, padded, and 8 bytes for every row and 64 of the vocabulary;
+ * the gradients keep the softmax's part of a piece of 16,384 of the vocabulary
+ * (8,192 of more than 8,192 rows) and its transpose, 4 bytes a value (fp32: 8): a
+ * vocabulary of one piece takes more than its logits would (16,320 rows, 256 x 512,
+ * fp32: 236 MB, the logits 17), a longer one less (8,192 rows, 131,072 x 1,024,
+ * bf16: 906 MB, its logits 2,147).  Pure. */
 int soma_ce_workspace_size(const soma_ce_config* cfg, int grad, size_t* bytes);
 
 /* loss [rows] and lse [rows] (fp32); either may be NULL. */

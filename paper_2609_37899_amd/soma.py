@@ -447,7 +447,8 @@ class _Plan:
     """What the operators' classes share: one device, a workspace on it, and
     the checks of their arguments.  A plan must not be used by two streams at
     once, nor by two captured graphs that may run at once: its workspace is
-    shared."""
+    shared.  A captured graph holds the addresses of the plan's memory, not the
+    plan: keep the plan as long as the graph."""
 
     def _start(self, nbytes: int, device):
         import torch
@@ -524,7 +525,8 @@ class GatedScan(_Plan):
     gates [n][4 width] hold the pre-activations in blocks i, f, g, o; rows may be
     strided.  offsets [sequences + 1] (int32, on the device) gives each
     sequence's first row; None: all sequences have n / sequences rows.  Rows
-    behind the last sequence are neither read nor written."""
+    behind the last sequence are neither read nor written.  A sequence far longer
+    than the others of its batch is best given a call of its own (soma.h)."""
 
     def __init__(self, rows: int, sequences: int, width: int, dtype, device="cuda"):
         self.rows, self.sequences, self.width, self.dtype = int(rows), int(sequences), int(width), dtype
