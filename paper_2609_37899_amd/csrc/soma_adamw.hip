@@ -639,7 +639,7 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
   // Waiting for a stream that records a graph would end the recording.
   hipStreamCaptureStatus recording = hipStreamCaptureStatusNone;
   hipError_t e = hipStreamIsCapturing(st, &recording);
-  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipStreamIsCapturing: %s", hipGetErrorString(e));
+  if (e != hipSuccess) return device_error("hipStreamIsCapturing", e);
   if (recording != hipStreamCaptureStatusNone) return set_error(SOMA_EINVAL, "a plan cannot be made on a stream that is captured");
   char* host = new (std::nothrow) char[need]();
   int64_t* first = new (std::nothrow) int64_t[size_t(n) + 1];
@@ -670,7 +670,7 @@ int soma_adamw_create(const soma_adamw_tensor* tensors, int32_t n, void* workspa
   if (e != hipSuccess) {
     delete[] first;
     delete plan;
-    return set_error(SOMA_EDEVICE, "copying the tensors' table: %s", hipGetErrorString(e));
+    return device_error("copying the tensors' table", e);
   }
   *plan = soma_adamw{n, chunk, chunks, static_cast<const Tensor*>(workspace),
                      reinterpret_cast<const Block*>(static_cast<char*>(workspace) + table_bytes(n)), first,
@@ -711,11 +711,9 @@ int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double
   // stream_key(seed, t)
   const Draw d{make_uint2(uint32_t(plan->seed), uint32_t(plan->seed >> 32) ^ uint32_t(uint64_t(t) >> 32)), uint32_t(t), 0};
   const dim3 grid(unsigned(plan->chunks)), block(kThreadsAdamw);
-  if (plan->rounding == SOMA_ROUND_RANDOM)
-    hipLaunchKernelGGL(k_adamw<true>, grid, block, 0, stream_of(stream), plan->tensors, plan->blocks, r, d, grad_scale);
-  else
-    hipLaunchKernelGGL(k_adamw<false>, grid, block, 0, stream_of(stream), plan->tensors, plan->blocks, r, d, grad_scale);
-  if (int rc = launched("k_adamw")) return rc;
+  const auto kernel = plan->rounding == SOMA_ROUND_RANDOM ? k_adamw<true> : k_adamw<false>;
+  if (int rc = launch("k_adamw", kernel, grid, block, 0, stream_of(stream), plan->tensors, plan->blocks, r, d, grad_scale))
+    return rc;
   return set_ok();
 }
 
@@ -732,9 +730,9 @@ int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_ou
     if (chunks == 0) continue;
     Outputs o{};
     for (int32_t k = i; k < end; ++k) o.m[k - i] = m_out[k], o.v[k - i] = v_out[k];
-    hipLaunchKernelGGL(k_adamw_moments, dim3(unsigned(chunks)), dim3(kThreadsAdamw), 0, stream_of(stream),
-                       plan->tensors, plan->blocks + plan->first_chunk[i], i, plan->chunk, o);
-    if (int rc = launched("k_adamw_moments")) return rc;
+    if (int rc = launch("k_adamw_moments", k_adamw_moments, dim3(unsigned(chunks)), dim3(kThreadsAdamw), 0,
+                        stream_of(stream), plan->tensors, plan->blocks + plan->first_chunk[i], i, plan->chunk, o))
+      return rc;
   }
   return set_ok();
 }

@@ -1095,19 +1095,16 @@ Divider divider(int d) {
 }
 
 // most: blocks that the card holds at once.
-int launch_items(const void* kern, CeMmArgs& p, int64_t most, unsigned lds, hipStream_t st) {
+int launch_items(void (*kernel)(CeMmArgs), CeMmArgs& p, int64_t most, unsigned lds, hipStream_t st) {
   const int64_t items = int64_t(p.ntm) * p.ntn * p.splits;
   if (items >= (int64_t(1) << 30)) return set_error(SOMA_ESHAPE, "too many tiles in one launch");
   p.items = int(items);
   p.by_tiles = divider(p.ntm * p.ntn), p.by_band = divider(8 * p.ntm), p.by_rest = divider(std::max(p.ntn % 8, 1));
   p.by_splits = divider(p.splits);
   const int64_t blocks = std::min(up(items, kXcd), most);
-  hipError_t e = hipFuncSetAttribute(kern, hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
-  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-  void* args[] = {&p};
-  e = hipLaunchKernel(kern, dim3(unsigned(blocks)), dim3(256), args, lds, st);
-  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "k_ce_mm: %s", hipGetErrorString(e));
-  return SOMA_OK;
+  const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(kernel), hipFuncAttributeMaxDynamicSharedMemorySize, int(lds));
+  if (e != hipSuccess) return device_error("hipFuncSetAttribute", e);
+  return launch("k_ce_mm", kernel, dim3(unsigned(blocks)), dim3(256), lds, st, p);
 }
 
 // Tiles in units of 16 rows of A and of W.
@@ -1129,15 +1126,15 @@ int launch_mm(CeMmArgs& p, bool large, hipStream_t st) {
   p.tile_subs = large ? 1 : 2;
   if constexpr (PARTS == 1) {
     if (!large)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 8, 8, 2, 4, 2>), p, 2 * kFill, 65536, st);
+      return launch_items(k_ce_mm<T, 1, kEpi, 8, 8, 2, 4, 2>, p, 2 * kFill, 65536, st);
     if constexpr (kLogits)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 8, 16, 1, 3, 2>), p, 2 * kFill, 73728, st);
+      return launch_items(k_ce_mm<T, 1, kEpi, 8, 16, 1, 3, 2>, p, 2 * kFill, 73728, st);
     else
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 1, kEpi, 16, 16, 2, 4, 1>), p, kFill, 131072, st);
+      return launch_items(k_ce_mm<T, 1, kEpi, 16, 16, 2, 4, 1>, p, kFill, 131072, st);
   } else {
     if (!large)
-      return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 2, kEpi, 8, 8, 2, 4, 1>), p, kFill, 131072, st);
-    return launch_items(reinterpret_cast<const void*>(&k_ce_mm<T, 2, kEpi, 8, 16, 1, 3, 1>), p, kFill, 147456, st);
+      return launch_items(k_ce_mm<T, 2, kEpi, 8, 8, 2, 4, 1>, p, kFill, 131072, st);
+    return launch_items(k_ce_mm<T, 2, kEpi, 8, 16, 1, 3, 1>, p, kFill, 147456, st);
   }
 }
 
@@ -1198,11 +1195,8 @@ int launch_product(CeMmArgs p, const Shares& sh, bool single, bool finish, hipSt
   p.splits = sh.splits;
   const unsigned tiles = unsigned(p.ntm * p.ntn);
   constexpr Tile t = {16, PARTS == 1 ? 16 : 8};           // tile_of(true, PARTS, false)
-  if (sh.large)
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, t.tn, t.tm>), dim3(tiles, t.tn * t.tm / 4), dim3(256), 0, st, p);
-  else
-    hipLaunchKernelGGL((k_ce_sum<T, PARTS, 8, 8>), dim3(tiles, 16), dim3(256), 0, st, p);
-  return launched("k_ce_sum");
+  if (sh.large) return launch("k_ce_sum", k_ce_sum<T, PARTS, t.tn, t.tm>, dim3(tiles, t.tn * t.tm / 4), dim3(256), 0, st, p);
+  return launch("k_ce_sum", k_ce_sum<T, PARTS, 8, 8>, dim3(tiles, 16), dim3(256), 0, st, p);
 }
 
 // Packs a, and b as well if it is not NULL, which has as many columns.
@@ -1210,8 +1204,7 @@ template <class T, int PARTS>
 int launch_pack(const PackArgs& a, const PackArgs* b, hipStream_t st) {
   const PackPair p{{a, b ? *b : a}, a.np / 64};
   const unsigned blocks = unsigned(p.first + (b ? b->np / 64 : 0));
-  hipLaunchKernelGGL((k_ce_pack<T, PARTS>), dim3(blocks, unsigned(a.Kp / 64)), dim3(256), 0, st, p);
-  return launched("k_ce_pack");
+  return launch("k_ce_pack", k_ce_pack<T, PARTS>, dim3(blocks, unsigned(a.Kp / 64)), dim3(256), 0, st, p);
 }
 
 // Partial maxima of each array: a block for every four rows of the larger one.
@@ -1243,9 +1236,8 @@ template <class T, int RT>
 int launch_rows(const RowsArgs& a, int blocks, hipStream_t st) {
   const hipError_t e = hipFuncSetAttribute(reinterpret_cast<const void*>(&k_ce_rows<T, RT>),
                                            hipFuncAttributeMaxDynamicSharedMemorySize, int(kRowsLds));
-  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "hipFuncSetAttribute: %s", hipGetErrorString(e));
-  hipLaunchKernelGGL((k_ce_rows<T, RT>), dim3(blocks), dim3(64 * kRowsWaves), unsigned(rows_lds(a.K, sizeof(T), RT)), st, a);
-  return launched("k_ce_rows");
+  if (e != hipSuccess) return device_error("hipFuncSetAttribute", e);
+  return launch("k_ce_rows", k_ce_rows<T, RT>, dim3(blocks), dim3(64 * kRowsWaves), unsigned(rows_lds(a.K, sizeof(T), RT)), st, a);
 }
 
 template <class T, int PARTS>
@@ -1280,8 +1272,7 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
     const int nmax = maxima_of(c);
     if (PARTS == 2) {
       const MaxArgs m{f, E, nullptr, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
-      hipLaunchKernelGGL(k_ce_max<T>, dim3(nmax, 3), dim3(256), 0, st, m, 0);
-      if (int rc = launched("k_ce_max")) return rc;
+      if (int rc = launch("k_ce_max", k_ce_max<T>, dim3(nmax, 3), dim3(256), 0, st, m, 0)) return rc;
     }
     PackArgs a{};
     a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
@@ -1306,11 +1297,8 @@ int loss_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   }
   const dim3 jgrid((c.rows + 15) / 16);
   if (subs <= 32)
-    hipLaunchKernelGGL(k_ce_join<8>, jgrid, dim3(128), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss, lse);
-  else
-    hipLaunchKernelGGL(k_ce_join<64>, jgrid, dim3(1024), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss,
-                       lse);
-  return launched("k_ce_join");
+    return launch("k_ce_join", k_ce_join<8>, jgrid, dim3(128), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss, lse);
+  return launch("k_ce_join", k_ce_join<64>, jgrid, dim3(1024), 0, st, part, subs, stride, targets, hit, c.rows, c.vocab, loss, lse);
 }
 
 template <class T, int PARTS>
@@ -1323,8 +1311,7 @@ int grad_typed(const soma_ce_config& c, const void* f, const void* E, const int3
   auto at = [&](size_t o) { return reinterpret_cast<uint16_t*>(ws + o); };
   const MaxArgs m{f, E, w, targets, c.f_stride, c.e_stride, c.rows, c.vocab, c.width, maxima};
   const int nmax = PARTS == 2 ? maxima_of(c) : 64;
-  hipLaunchKernelGGL(k_ce_max<T>, dim3(nmax, PARTS == 2 ? 3 : 1), dim3(256), 0, st, m, PARTS == 2 ? 0 : 2);
-  if (int rc = launched("k_ce_max")) return rc;
+  if (int rc = launch("k_ce_max", k_ce_max<T>, dim3(nmax, PARTS == 2 ? 3 : 1), dim3(256), 0, st, m, PARTS == 2 ? 0 : 2)) return rc;
   PackArgs a{};
   a.x = f, a.stride = c.f_stride, a.n = c.rows, a.K = c.width, a.np = int(s.Rp), a.Kp = int(s.Kp);
   a.targets = targets, a.frag = at(s.f), a.fragT = dE ? at(s.fT) : nullptr, a.maxima = maxima, a.nmax = nmax;
@@ -1409,8 +1396,7 @@ int soma_ce_grad(const soma_ce_config* cfg, const void* f, const void* E, const 
   if (c.rows == 0) {                      // no row: dE is a sum of nothing
     if (dE) {
       const int64_t halves = int64_t(c.vocab) * c.width * int64_t(e) / 2;
-      hipLaunchKernelGGL(k_ce_zero, dim3(1024), dim3(256), 0, st, static_cast<uint16_t*>(dE), halves);
-      if (int rc = launched("k_ce_zero")) return rc;
+      if (int rc = launch("k_ce_zero", k_ce_zero, dim3(1024), dim3(256), 0, st, static_cast<uint16_t*>(dE), halves)) return rc;
     }
     return set_ok();
   }

@@ -6,6 +6,8 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <tuple>
+
 #include "soma.h"
 
 namespace soma {
@@ -19,10 +21,24 @@ inline hipStream_t stream_of(void* s) { return reinterpret_cast<hipStream_t>(s);
 
 inline bool is_aligned(const void* p, size_t a) { return reinterpret_cast<uintptr_t>(p) % a == 0; }
 
-inline int launched(const char* what) {
-  const hipError_t e = hipGetLastError();
-  if (e != hipSuccess) return set_error(SOMA_EDEVICE, "%s: %s", what, hipGetErrorString(e));
-  return SOMA_OK;
+// A device call's failure; the runtime's record of it is cleared, for it is told here.
+inline int device_error(const char* what, hipError_t e) {
+  (void)hipGetLastError();
+  return set_error(SOMA_EDEVICE, "%s: %s", what, hipGetErrorString(e));
+}
+
+// Launches and reports the launch's own status: the runtime's last error may be of
+// a call that the caller made before.
+template <class... P, class... A>
+int launch(const char* what, void (*kernel)(P...), dim3 grid, dim3 block, unsigned lds, hipStream_t st, const A&... args) {
+  std::tuple<P...> values(args...);
+  const hipError_t e = std::apply(
+      [&](P&... x) {
+        void* at[] = {const_cast<void*>(static_cast<const void*>(&x))...};
+        return hipLaunchKernel(reinterpret_cast<const void*>(kernel), grid, block, at, lds, st);
+      },
+      values);
+  return e == hipSuccess ? SOMA_OK : device_error(what, e);
 }
 
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }

@@ -815,21 +815,15 @@ int soma_scan_forward(const soma_scan_config* cfg, const void* gates, const int3
   const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
   if (a.piece) {
-    if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_forward_maps<float, 1>), grid, block, 0, st, a);
-    else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 2>), grid, block, 0, st, a);
-    else
-      hipLaunchKernelGGL((k_scan_forward_maps<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_forward_maps")) return rc;
+    const auto kernel = c.type == SOMA_FLOAT ? k_scan_forward_maps<float, 1>
+                        : vec == 2           ? k_scan_forward_maps<bf16, 2>
+                                             : k_scan_forward_maps<bf16, 1>;
+    if (int rc = launch("k_scan_forward_maps", kernel, grid, block, 0, st, a)) return rc;
   }
-  if (c.type == SOMA_FLOAT)
-    hipLaunchKernelGGL((k_scan_forward<float, 1>), grid, block, 0, st, a);
-  else if (vec == 2)
-    hipLaunchKernelGGL((k_scan_forward<bf16, 2>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_scan_forward<bf16, 1>), grid, block, 0, st, a);
-  if (int rc = launched("k_scan_forward")) return rc;
+  const auto kernel = c.type == SOMA_FLOAT ? k_scan_forward<float, 1>
+                      : vec == 2           ? k_scan_forward<bf16, 2>
+                                           : k_scan_forward<bf16, 1>;
+  if (int rc = launch("k_scan_forward", kernel, grid, block, 0, st, a)) return rc;
   return set_ok();
 }
 
@@ -856,21 +850,15 @@ int soma_scan_backward(const soma_scan_config* cfg, const void* gates, const int
   const dim3 grid(groups_of(c, vec), split(c, vec, workspace, &a)), block(64 * kWaves);
   const hipStream_t st = stream_of(stream);
   if (a.piece) {
-    if (c.type == SOMA_FLOAT)
-      hipLaunchKernelGGL((k_scan_backward_maps<float, 1>), grid, block, 0, st, a);
-    else if (vec == 2)
-      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 2>), grid, block, 0, st, a);
-    else
-      hipLaunchKernelGGL((k_scan_backward_maps<bf16, 1>), grid, block, 0, st, a);
-    if (int rc = launched("k_scan_backward_maps")) return rc;
+    const auto kernel = c.type == SOMA_FLOAT ? k_scan_backward_maps<float, 1>
+                        : vec == 2           ? k_scan_backward_maps<bf16, 2>
+                                             : k_scan_backward_maps<bf16, 1>;
+    if (int rc = launch("k_scan_backward_maps", kernel, grid, block, 0, st, a)) return rc;
   }
-  if (c.type == SOMA_FLOAT)
-    hipLaunchKernelGGL((k_scan_backward<float, 1>), grid, block, 0, st, a);
-  else if (vec == 2)
-    hipLaunchKernelGGL((k_scan_backward<bf16, 2>), grid, block, 0, st, a);
-  else
-    hipLaunchKernelGGL((k_scan_backward<bf16, 1>), grid, block, 0, st, a);
-  if (int rc = launched("k_scan_backward")) return rc;
+  const auto kernel = c.type == SOMA_FLOAT ? k_scan_backward<float, 1>
+                      : vec == 2           ? k_scan_backward<bf16, 2>
+                                           : k_scan_backward<bf16, 1>;
+  if (int rc = launch("k_scan_backward", kernel, grid, block, 0, st, a)) return rc;
   return set_ok();
 }
 
@@ -883,13 +871,13 @@ int soma_scan_step(const soma_scan_config* cfg, const void* gates, const float* 
   if (!is_aligned(gates, e) || !is_aligned(h, e) || !is_aligned(cT, 4) || !is_aligned(c0, 4))
     return set_error(SOMA_EINVAL, "a pointer is not aligned to its elements");
   const dim3 grid((c.width + 255) / 256, c.sequences), block(256);
-  if (c.type == SOMA_FLOAT)
-    hipLaunchKernelGGL(k_scan_step<float>, grid, block, 0, stream_of(stream), static_cast<const float*>(gates),
-                       c.gate_stride, c0, cT, static_cast<float*>(h), c.width);
-  else
-    hipLaunchKernelGGL(k_scan_step<bf16>, grid, block, 0, stream_of(stream), static_cast<const bf16*>(gates),
-                       c.gate_stride, c0, cT, static_cast<bf16*>(h), c.width);
-  if (int rc = launched("k_scan_step")) return rc;
+  const hipStream_t st = stream_of(stream);
+  if (int rc = c.type == SOMA_FLOAT
+                   ? launch("k_scan_step", k_scan_step<float>, grid, block, 0, st, static_cast<const float*>(gates),
+                            c.gate_stride, c0, cT, static_cast<float*>(h), c.width)
+                   : launch("k_scan_step", k_scan_step<bf16>, grid, block, 0, st, static_cast<const bf16*>(gates),
+                            c.gate_stride, c0, cT, static_cast<bf16*>(h), c.width))
+    return rc;
   return set_ok();
 }
 
