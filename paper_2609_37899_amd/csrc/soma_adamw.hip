@@ -22,8 +22,8 @@
 // of 256 keeps its gradient, the others' fall tenfold: their root is 7.8 times too
 // large after 5,000 updates.)  Random rounding (random_codes) keeps either neighbour
 // with the probability that makes the expected value the exact one, so the average of
-// many steps is followed; 64 bits of Philox for four elements serve it, drawn from
-// the element, its tensor and the number of the update.
+// many steps is followed; a word of Philox for each element serves it, drawn from the
+// element, its tensor and the number of the update.
 //
 // The step is bound by memory: every element is read and written once.  A
 // block takes 4096 consecutive elements of one tensor (a table of blocks, made
