@@ -713,6 +713,67 @@ int soma_adamw_step(soma_adamw* plan, int64_t t, double lr, double beta1, double
  * v_out[i] (host arrays of device pointers) receive tensor i's [count]. */
 int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_out, void* stream);
 
+/* Linear attention with a decay for each head: a recurrence whose state is a
+ * matrix, over sequences that lie behind one another in one array of rows,
+ *   S_t = a_h S_{t-1} + k_t v_t^T,   o_t = scale q_t^T S_t,   a_h = exp(log_decay[h]).
+ *   q       [rows][heads key_width], k [rows][kv_heads key_width], v [rows]
+ *           [kv_heads value_width], of `type`, rows q_stride, k_stride and
+ *           v_stride elements apart.  Head h reads keys and values of head
+ *           h / (heads / kv_heads).
+ *   log_decay [heads] fp32, <= 0 (0: nothing is forgotten; -infinity: a_h = 0 and
+ *           a_h^0 = 1).  Constants of the layer: there is no gradient.
+ *   offsets as soma_scan_forward's.
+ *   s0, sT  [sequences][heads][key_width][value_width] fp32, the states in front
+ *           of the first row and behind the last.  s0 NULL: zeros; sT NULL: not
+ *           wanted.  They may be the same array.  An empty sequence keeps its
+ *           state.
+ *   o       [rows][heads value_width] of `type`, rows contiguous.
+ * States, sums and decays are fp32.  bf16 operands enter the products as they are;
+ * what is formed from them (q k^T, the states) as bf16 parts that hold 2^-15 of it,
+ * in a state's own update all 24 bits; fp32 operands as they are.  A decay's power over n rows is
+ * off by (|n log_decay| + 2) 2^-23 of itself.  A value that is not finite makes what it enters not
+ * finite (an infinity may become NaN), and nothing else: rows in front of it
+ * and other sequences and heads never see it.
+ * Constraints: rows in [0, 2^30], sequences in [1, 65535], heads in [1, 1024],
+ * kv_heads a divisor of heads, both widths in [1, 256]. */
+typedef struct soma_la_config {
+  int32_t rows;
+  int32_t sequences;
+  int32_t heads;
+  int32_t kv_heads;
+  int32_t key_width;
+  int32_t value_width;
+  int32_t type;      /* enum soma_type */
+  float scale;       /* finite */
+  int64_t q_stride;  /* elements, >= heads key_width */
+  int64_t k_stride;
+  int64_t v_stride;
+} soma_la_config;
+
+/* Bytes of device workspace of soma_la_forward, or (grad != 0) of both calls (0:
+ * none is needed); it does not shrink with more rows.  Pure. */
+int soma_la_workspace_size(const soma_la_config* cfg, int grad, size_t* bytes);
+
+int soma_la_forward(const soma_la_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,
+                    const float* log_decay_dev, const int32_t* offsets_dev, const float* s0_dev, void* o_dev, float* sT_dev,
+                    void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The gradients of soma_la_forward's inputs from those of its outputs, with the
+ * inputs of that call.
+ *   do      [rows][heads value_width] of `type`, rows contiguous; dsT as sT, NULL: zeros.
+ *   dq, dk, dv [rows][..] as q, k and v, rows contiguous, arrays of their own.
+ *           Those of shared keys and values are summed in fp32.
+ *   ds0     as s0, NULL: not wanted; may be dsT. */
+int soma_la_backward(const soma_la_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,
+                     const float* log_decay_dev, const int32_t* offsets_dev, const float* s0_dev, const void* do_dev,
+                     const float* dsT_dev, void* dq_dev, void* dk_dev, void* dv_dev, float* ds0_dev, void* workspace_dev,
+                     size_t workspace_bytes, void* stream);
+
+/* One row for every sequence (rows = sequences), as when text is generated: sT
+ * from s0 (which may be the same array; NULL: zeros) and o. */
+int soma_la_step(const soma_la_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,
+                 const float* log_decay_dev, const float* s0_dev, float* sT_dev, void* o_dev, void* stream);
+
 /* Thread-local description of the last error ("" if none). */
 const char* soma_last_error(void);
 

@@ -6,6 +6,7 @@
 #include <stddef.h>
 #include <stdint.h>
 
+#include <initializer_list>
 #include <tuple>
 
 #include "soma.h"
@@ -52,6 +53,30 @@ inline int check_workspace(const void* ws, size_t have, size_t need) {
   if (!is_aligned(ws, 256)) return set_error(SOMA_EWORKSPACE, "workspace must be 256-byte aligned");
   if (have < need) return set_error(SOMA_EWORKSPACE, "workspace too small: %zu < %zu bytes", have, need);
   return SOMA_OK;
+}
+
+// Bytes of an array that a call reads or writes.
+struct Span {
+  const void* p;
+  size_t n;
+};
+inline Span span_of(const void* p, int64_t rows, int64_t width, int64_t stride, size_t size) {
+  return {p, rows > 0 ? static_cast<size_t>((rows - 1) * stride + width) * size : 0};
+}
+
+// Whether outputs share no byte with one another nor with an input.
+inline bool are_apart(std::initializer_list<Span> outs, std::initializer_list<Span> ins) {
+  const auto meet = [](const Span& a, const Span& b) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a.p), y = reinterpret_cast<uintptr_t>(b.p);
+    return a.p && b.p && a.n && b.n && x < y + b.n && y < x + a.n;
+  };
+  for (const Span* a = outs.begin(); a != outs.end(); ++a) {
+    for (const Span* b = outs.begin(); b != a; ++b)
+      if (meet(*a, *b)) return false;
+    for (const Span& b : ins)
+      if (meet(*a, b)) return false;
+  }
+  return true;
 }
 
 }  // namespace soma

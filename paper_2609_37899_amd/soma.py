@@ -31,7 +31,8 @@ EXPORTS = ("soma_param_count", "soma_workspace_size", "soma_create", "soma_destr
            "soma_get_phase_times", "soma_get_narrow_projections", "soma_set_spin_limit", "soma_spsa_step_noalloc",
            "soma_scan_workspace_size", "soma_scan_forward", "soma_scan_backward", "soma_scan_step",
            "soma_ce_workspace_size", "soma_ce_loss", "soma_ce_grad", "soma_adamw_workspace_size", "soma_adamw_create",
-           "soma_adamw_destroy", "soma_adamw_set_rounding", "soma_adamw_step", "soma_adamw_moments", "soma_last_error")
+           "soma_adamw_destroy", "soma_adamw_set_rounding", "soma_adamw_step", "soma_adamw_moments",
+           "soma_la_workspace_size", "soma_la_forward", "soma_la_backward", "soma_la_step", "soma_last_error")
 
 
 class SomaError(RuntimeError):
@@ -100,6 +101,11 @@ class AdamWTensor(ctypes.Structure):
         (n, ctypes.c_int32) for n in ("param_type", "grad_type", "state_bits", "reserved")]
 
 
+class LinearAttentionConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "sequences", "heads", "kv_heads", "key_width", "value_width", "type")] + [
+        ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
+
+
 _lib = None
 
 
@@ -159,6 +165,11 @@ def load():
             "soma_adamw_set_rounding": (ctypes.c_int, [vp, ctypes.c_int32, ctypes.c_uint64]),
             "soma_adamw_step": (ctypes.c_int, [vp, ctypes.c_int64] + [ctypes.c_double] * 4 + [vp, vp]),
             "soma_adamw_moments": (ctypes.c_int, [vp, ctypes.POINTER(vp), ctypes.POINTER(vp), vp]),
+            "soma_la_workspace_size": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig), ctypes.c_int,
+                                                      ctypes.POINTER(ctypes.c_size_t)]),
+            "soma_la_forward": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
+            "soma_la_backward": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 13 + [ctypes.c_size_t, vp]),
+            "soma_la_step": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 8),
             "soma_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -767,3 +778,79 @@ class AdamW(_Plan):
                     self._ptr(t, f"{name}[{i}]", torch.float32, shape)
             arrays.append((ctypes.c_void_p * n)(*[t.data_ptr() for t in x]))
         self._call(stream, load().soma_adamw_moments, self._h, *arrays)
+
+
+class LinearAttention(_Plan):
+    """Linear attention with a decay for each head, S_t = a_h S_{t-1} + k_t v_t^T, o_t = scale q_t^T S_t, over
+    ``sequences`` sequences that lie behind one another in at most ``rows`` rows.  ``dtype`` (float32 or bfloat16) is the
+    type of q, k, v, o and their gradients; states are float32.
+
+    q [n][heads key_width], k [n][kv_heads key_width] and v [n][kv_heads value_width]; rows may be strided (parts of one
+    projection).  kv_heads: heads of k and v, each shared by heads / kv_heads (None: heads).  log_decay [heads]
+    (float32, on the device): log a_h <= 0, constants of the layer.  scale: None is key_width ** -0.5.  offsets as
+    GatedScan's.  States are [sequences][heads][key_width][value_width]."""
+
+    def __init__(self, rows: int, sequences: int, heads: int, key_width: int, value_width: int, dtype, kv_heads=None,
+                 scale=None, grad: bool = True, device="cuda"):
+        self.rows, self.sequences, self.heads = int(rows), int(sequences), int(heads)
+        self.kv_heads = self.heads if kv_heads is None else int(kv_heads)
+        self.key_width, self.value_width, self.dtype, self.with_grad = int(key_width), int(value_width), dtype, bool(grad)
+        self._type = _type_of(dtype)
+        _check_sizes(rows=self.rows, sequences=self.sequences, heads=self.heads, kv_heads=self.kv_heads,
+                     key_width=self.key_width, value_width=self.value_width)
+        self.scale = float(max(1, self.key_width) ** -0.5 if scale is None else scale)
+        self._widths = (self.heads * self.key_width, self.kv_heads * self.key_width, self.kv_heads * self.value_width)
+        out = ctypes.c_size_t()
+        _check(load().soma_la_workspace_size(ctypes.byref(self._cfg(self.rows, self._widths)), int(self.with_grad),
+                                             ctypes.byref(out)))
+        self._bytes = out.value
+        self._state = (self.sequences, self.heads, self.key_width, self.value_width)
+        self._start(out.value, device)
+
+    def _cfg(self, rows, strides):
+        return LinearAttentionConfig(rows, self.sequences, self.heads, self.kv_heads, self.key_width, self.value_width,
+                                     self._type, self.scale, *strides)
+
+    def _inputs(self, q, k, v, log_decay):
+        import torch
+        if not isinstance(q, torch.Tensor) or q.dim() != 2:
+            raise TypeError("q must be a tensor [rows][heads key_width]")
+        n = q.shape[0]
+        if n > self.rows:
+            raise ValueError(f"{n} rows, but the plan was made for {self.rows}")
+        ptrs = [self._ptr(t, name, self.dtype, (n, w), strided=True) for t, name, w in zip((q, k, v), "qkv", self._widths)]
+        cfg = self._cfg(n, [_row_stride(t) for t in (q, k, v)])
+        return n, [ctypes.byref(cfg), *ptrs, self._ptr(log_decay, "log_decay", torch.float32, (self.heads,))]
+
+    def _of_state(self, t, name, optional=True):
+        import torch
+        return self._ptr(t, name, torch.float32, self._state, optional=optional)
+
+    def _of_rows(self, t, name, n, width):
+        return self._ptr(t, name, self.dtype, (n, width))
+
+    def _offsets(self, offsets):
+        import torch
+        return self._ptr(offsets, "offsets", torch.int32, (self.sequences + 1,), optional=True)
+
+    def forward(self, q, k, v, log_decay, o, s0=None, sT=None, offsets=None, stream=None):
+        """o [n][heads value_width]; sT receives the states behind the last rows (it may be s0)."""
+        n, args = self._inputs(q, k, v, log_decay)
+        self._call(stream, load().soma_la_forward, *args, self._offsets(offsets), self._of_state(s0, "s0"),
+                   self._of_rows(o, "o", n, self.heads * self.value_width), self._of_state(sT, "sT"), self._ws, self._bytes)
+
+    def backward(self, q, k, v, log_decay, do, dq, dk, dv, s0=None, dsT=None, ds0=None, offsets=None, stream=None):
+        """dq, dk, dv and ds0 (which may be dsT) from do [n][heads value_width] and dsT, with forward's inputs."""
+        if not self.with_grad:
+            raise ValueError("the plan was made without gradients")
+        n, args = self._inputs(q, k, v, log_decay)
+        self._call(stream, load().soma_la_backward, *args, self._offsets(offsets), self._of_state(s0, "s0"),
+                   self._of_rows(do, "do", n, self.heads * self.value_width), self._of_state(dsT, "dsT"),
+                   *[self._of_rows(t, name, n, w) for t, name, w in zip((dq, dk, dv), ("dq", "dk", "dv"), self._widths)],
+                   self._of_state(ds0, "ds0"), self._ws, self._bytes)
+
+    def step(self, q, k, v, log_decay, s0, sT, o, stream=None):
+        """One row for every sequence: sT (it may be s0) and o [sequences][heads value_width]."""
+        n, args = self._inputs(q, k, v, log_decay)
+        self._call(stream, load().soma_la_step, *args, self._of_state(s0, "s0"), self._of_state(sT, "sT", optional=False),
+                   self._of_rows(o, "o", n, self.heads * self.value_width))

@@ -1,0 +1,364 @@
+"""Linear attention with a decay for each head against every pair of rows in 64 bits: widths, heads, lengths, types,
+strides, states, gradients, decays at the ends of their range, values that are not finite, captured and repeated calls."""
+import numpy as np
+import pytest
+
+import block_reference as ref
+from gpu_common import require_gpu
+from paper_2609_37899_amd import soma
+
+pytestmark = pytest.mark.gpu
+
+LENGTHS = {
+    "one": [1], "empty": [0, 1, 0, 2, 0], "chunk": [64, 32], "around": [63, 65, 1, 33], "ragged": [200, 0, 7, 129, 0, 1, 90],
+    "long": [1500], "all_empty": [0, 0],
+}
+WIDTHS = {"1": (1, 1, 1, 1), "64": (2, 1, 64, 64), "odd": (3, 3, 45, 77), "128": (2, 1, 128, 128), "wide": (4, 2, 130, 256),
+          "keys": (2, 2, 256, 5), "values": (2, 1, 9, 200)}
+OUT = ("o", "sT", "dq", "dk", "dv", "ds0")
+
+
+def make(torch, dtype, widths, lengths, behind=3, pad=0, seed=0, log_decay=None, scale=0.3):
+    """Inputs (rows `pad` elements longer than needed) on the GPU, and their exact results."""
+    g = np.random.default_rng(seed)
+    dt = getattr(torch, dtype)
+    H, K, dk, dv = widths
+    rows, S = sum(lengths) + behind, len(lengths)
+
+    def both(x, t):
+        y = torch.from_numpy(x.astype(np.float32)).to(t).cuda()
+        return y, y.double().cpu().numpy()
+
+    x, w = {}, {}
+    for name, width in (("q", H * dk), ("k", K * dk), ("v", K * dv)):
+        whole, exact = both(g.standard_normal((rows, width + pad)), dt)
+        x[name], w[name] = whole[:, :width], exact[:, :width]
+    x["do"], w["do"] = both(g.standard_normal((rows, H * dv)), dt)
+    for name in ("s0", "dsT"):
+        x[name], w[name] = both(g.standard_normal((S, H, dk, dv)), torch.float32)
+    if log_decay is None:
+        log_decay = np.log1p(-2.0 ** -np.linspace(1, 9, H))
+    x["log_decay"], w["log_decay"] = both(np.resize(np.asarray(log_decay, dtype=np.float64), H), torch.float32)
+    x["offsets"] = torch.tensor([0] + list(np.cumsum(lengths)), dtype=torch.int32).cuda()
+    heads = {"q": (H, dk), "k": (K, dk), "v": (K, dv), "do": (H, dv)}
+    q, k, v, do = (w[n].reshape(rows, *heads[n]) for n in ("q", "k", "v", "do"))
+    want = ref.linear_attention(q, k, v, w["log_decay"], lengths, w["s0"], np.float64(np.float32(scale)), dtype, do, w["dsT"])
+    return x, want
+
+
+def plan_of(torch, dtype, widths, x, S, scale=0.3):
+    H, K, dk, dv = widths
+    return soma.LinearAttention(x["q"].shape[0], S, H, dk, dv, getattr(torch, dtype), kv_heads=K, scale=scale)
+
+
+def run(torch, plan, x, stream=None, offsets=True, out=None):
+    rows = x["q"].shape[0]
+    H, K, dk, dv, dt = plan.heads, plan.kv_heads, plan.key_width, plan.value_width, plan.dtype
+    if out is None:
+        out = {n: torch.full((rows, w), 7.0, dtype=dt, device="cuda") for n, w in (("o", H * dv), ("dq", H * dk), ("dk", K * dk),
+                                                                                   ("dv", K * dv))}
+        out.update(sT=torch.full_like(x["s0"], 7.0), ds0=torch.full_like(x["s0"], 7.0))
+        torch.cuda.synchronize()
+    off = x["offsets"] if offsets else None
+    plan.forward(x["q"], x["k"], x["v"], x["log_decay"], out["o"], x["s0"], out["sT"], off, stream=stream)
+    plan.backward(x["q"], x["k"], x["v"], x["log_decay"], x["do"], out["dq"], out["dk"], out["dv"], x["s0"], x["dsT"], out["ds0"],
+                  off, stream=stream)
+    return out
+
+
+def check(y, want, dtype, names=OUT):
+    for name in names:
+        exact = want[name].reshape(y[name].shape)
+        got, err = y[name].double().cpu().numpy(), want[name + "_err"].reshape(exact.shape)
+        step = ref.half_step("float32" if name in ("sT", "ds0") else dtype)
+        outside = np.isnan(exact)
+        assert np.all(got[outside] == 7.0), f"{name}: rows behind the last sequence were written"
+        tol = err * (1 + step) + step * np.abs(np.nan_to_num(exact)) + 1e-37
+        bad = ~(np.abs(got - exact) <= tol)            # NaN counts as wrong
+        bad[outside] = False
+        assert not bad.any(), (f"{name}: {bad.sum()} of {bad.size}, worst {np.nanmax(np.abs(got - exact) / tol):.2f} "
+                               f"of the bound, first at {np.argwhere(bad)[0]}")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("lengths", sorted(LENGTHS))
+@pytest.mark.parametrize("widths", sorted(WIDTHS))
+def test_matches_reference(dtype, lengths, widths):
+    torch = require_gpu()
+    x, want = make(torch, dtype, WIDTHS[widths], LENGTHS[lengths])
+    y = run(torch, plan_of(torch, dtype, WIDTHS[widths], x, len(LENGTHS[lengths])), x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("pad,shift", [(1, 0), (2, 1), (64, 3), (8, 8)])
+def test_strides_and_alignment(dtype, pad, shift):
+    """Rows further apart than their length, starting at any element."""
+    torch = require_gpu()
+    lengths, widths = [70, 3, 40], (2, 1, 64, 48)
+    x, want = make(torch, dtype, widths, lengths)
+    rows = x["q"].shape[0]
+    for n in ("q", "k", "v"):
+        w = x[n].shape[1]
+        flat = torch.full((rows * (w + pad) + shift + 8,), float("nan"), dtype=x[n].dtype, device="cuda")
+        view = flat[shift:shift + rows * (w + pad)].view(rows, w + pad)[:, :w]
+        view.copy_(x[n])
+        x[n] = view
+    y = run(torch, plan_of(torch, dtype, widths, x, 3), x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+
+
+def test_parts_of_one_projection():
+    """q, k and v side by side in one array."""
+    torch = require_gpu()
+    lengths, widths = [50, 90], (4, 2, 32, 64)
+    x, want = make(torch, "bfloat16", widths, lengths)
+    whole = torch.cat([x["q"], x["k"], x["v"]], 1)
+    a, b = x["q"].shape[1], x["q"].shape[1] + x["k"].shape[1]
+    x["q"], x["k"], x["v"] = whole[:, :a], whole[:, a:b], whole[:, b:]
+    y = run(torch, plan_of(torch, "bfloat16", widths, x, 2), x)
+    torch.cuda.synchronize()
+    check(y, want, "bfloat16")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("sequences,length", [(1, 1), (4, 100), (300, 3), (1, 700), (200, 1)])
+def test_equal_lengths_without_offsets(dtype, sequences, length):
+    """The same bits as with offsets."""
+    torch = require_gpu()
+    widths, lengths = (2, 1, 20, 36), [length] * sequences
+    x, want = make(torch, dtype, widths, lengths, behind=0)
+    plan = plan_of(torch, dtype, widths, x, sequences)
+    y, z = run(torch, plan, x, offsets=False), run(torch, plan, x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+    for k in OUT:
+        assert torch.equal(y[k], z[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("lengths", [[6000], [2500, 0, 3003, 0], [300] * 7 + [0, 1, 2000, 64, 0, 700]])
+@pytest.mark.parametrize("widths", ["64", "odd", "wide"])
+def test_pieces(dtype, lengths, widths):
+    """Rows enough for pieces, whose borders fall into sequences, between them and on empty ones; the same bits again."""
+    torch = require_gpu()
+    x, want = make(torch, dtype, WIDTHS[widths], lengths)
+    plan = plan_of(torch, dtype, WIDTHS[widths], x, len(lengths))
+    assert plan._bytes > 0
+    y = run(torch, plan, x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+    for _ in range(3):
+        z = run(torch, plan, x)
+        torch.cuda.synchronize()
+        for k in OUT:
+            assert torch.equal(y[k], z[k]), k
+
+
+@pytest.mark.parametrize("lengths", [LENGTHS["ragged"], [3000], [1300, 0, 1700]])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_states_in_place_and_left_out(dtype, lengths):
+    """sT over s0 and ds0 over dsT; without them the states are zeros and nothing else changes."""
+    torch = require_gpu()
+    widths = (2, 1, 33, 70)
+    x, _ = make(torch, dtype, widths, lengths)
+    plan = plan_of(torch, dtype, widths, x, len(lengths))
+    y = run(torch, plan, x)
+    z = {k: torch.full_like(v, 7.0) for k, v in y.items()}
+    s, d = x["s0"].clone(), x["dsT"].clone()
+    args = x["q"], x["k"], x["v"], x["log_decay"]
+    plan.forward(*args, z["o"], s, s, x["offsets"])
+    plan.backward(*args, x["do"], z["dq"], z["dk"], z["dv"], x["s0"], d, d, x["offsets"])
+    torch.cuda.synchronize()
+    z["sT"], z["ds0"] = s, d
+    for k in OUT:
+        assert torch.equal(y[k], z[k]), k
+    zero = torch.zeros_like(x["s0"])
+    x["s0"] = x["dsT"] = zero
+    y = run(torch, plan, x)
+    z = {k: torch.full_like(v, 7.0) for k, v in y.items()}
+    plan.forward(*args, z["o"], None, None, x["offsets"])
+    plan.backward(*args, x["do"], z["dq"], z["dk"], z["dv"], None, None, None, x["offsets"])
+    torch.cuda.synchronize()
+    for k in ("o", "dq", "dk", "dv"):
+        assert torch.equal(y[k], z[k]), k
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("log_decay", [0.0, -1e-6, -1.0, -30.0, -1e4, float("-inf")])
+@pytest.mark.parametrize("lengths", [[150, 1, 33], [2100]])
+def test_decays_at_the_ends_of_their_range(dtype, log_decay, lengths):
+    torch = require_gpu()
+    widths = (2, 2, 24, 40)
+    x, want = make(torch, dtype, widths, lengths, log_decay=[log_decay, -0.1])
+    y = run(torch, plan_of(torch, dtype, widths, x, len(lengths)), x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+
+
+@pytest.mark.parametrize("scale", [0.0, -2.0, 1e-3])
+def test_scales(scale):
+    torch = require_gpu()
+    widths, lengths = (2, 1, 40, 16), [100, 0, 31]
+    x, want = make(torch, "float32", widths, lengths, scale=scale)
+    y = run(torch, plan_of(torch, "float32", widths, x, 3, scale), x)
+    torch.cuda.synchronize()
+    check(y, want, "float32")
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), float("-inf")])
+@pytest.mark.parametrize("where", [0, 5, 30, 31, 77, 127, 128, 149])
+def test_what_is_not_finite_reaches_no_row_in_front(dtype, value, where):
+    """One value of k or v: rows of its sequence in front of it, other sequences and heads are bit for bit as without it,
+    rows behind it are not finite where it enters.  The same for gradients, from the back."""
+    torch = require_gpu()
+    widths, lengths = (2, 2, 40, 72), [20, 150, 20]
+    x, _ = make(torch, dtype, widths, lengths, log_decay=[-0.01, -0.3])
+    plan = plan_of(torch, dtype, widths, x, 3)
+    y = run(torch, plan, x)
+    row = 20 + where
+    for name, col in (("v", 72 + 17), ("k", 40 + 3)):           # of head 1
+        x2 = dict(x)
+        x2[name] = x[name].clone()
+        x2[name][row, col] = value
+        z = run(torch, plan, x2)
+        torch.cuda.synchronize()
+        assert torch.equal(y["o"][:row], z["o"][:row]) and torch.equal(y["o"][170:], z["o"][170:])
+        assert torch.equal(y["o"][:, :72], z["o"][:, :72])
+        hit = z["o"][row:170, 72 + 17] if name == "v" else z["o"][row:170, 72:]
+        assert not torch.isfinite(hit).any()
+        if name == "v":
+            rest = torch.ones(72, dtype=torch.bool)
+            rest[17] = False
+            assert torch.equal(y["o"][:, 72:][:, rest.cuda()], z["o"][:, 72:][:, rest.cuda()])
+        # dq of rows in front does not see it; dk and dv of rows behind do not
+        assert torch.equal(y["dq"][:row], z["dq"][:row])
+        assert torch.equal(y["dk"][row + 1:], z["dk"][row + 1:]) and torch.equal(y["dv"][row + 1:], z["dv"][row + 1:])
+    x2 = dict(x)
+    x2["q"] = x["q"].clone()
+    x2["q"][row, 41] = value
+    z = run(torch, plan, x2)
+    torch.cuda.synchronize()
+    keep = torch.arange(193) != row
+    assert torch.equal(y["o"][keep.cuda()], z["o"][keep.cuda()]) and not torch.isfinite(z["o"][row, 72:]).any()
+    assert torch.equal(y["dk"][row + 1:], z["dk"][row + 1:]) and torch.equal(y["dv"][row + 1:], z["dv"][row + 1:])
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("off", [[0, 500, 4000, 1 << 30], [-5, 600, 200, 2000], [0, 0, 0, -1], [1900, 100, 50, 2000],
+                                 [0, 1500, 700, 1000]])
+@pytest.mark.parametrize("rows", [2000, 300])
+def test_offsets_that_break_the_rules_stay_inside(dtype, off, rows):
+    torch = require_gpu()
+    dt = getattr(torch, dtype)
+    H, K, dk, dv = 2, 1, 16, 24
+    plan = soma.LinearAttention(rows, 3, H, dk, dv, dt, kv_heads=K)
+    assert (plan._bytes > 2 * 4 * rows * H * dv) == (rows == 2000)     # pieces, beside the shared heads' gradients
+    q, k, v, do = (torch.randn(rows, w, device="cuda").to(dt) for w in (H * dk, K * dk, K * dv, H * dv))
+    l, o = torch.full((H,), -0.1, device="cuda"), torch.tensor(off, dtype=torch.int32, device="cuda")
+    s = torch.zeros(4, H, dk, dv, device="cuda")
+    guards = {n: torch.full((rows + 64, w), 7.0, device="cuda", dtype=dt) for n, w in (("o", H * dv), ("dq", H * dk), ("dk", K * dk),
+                                                                                       ("dv", K * dv))}
+    s[3] = 7.0
+    plan.forward(q, k, v, l, guards["o"][:rows], None, s[:3], o)
+    plan.backward(q, k, v, l, do, *[guards[n][:rows] for n in ("dq", "dk", "dv")], None, None, s[:3], o)
+    torch.cuda.synchronize()
+    assert all((x[rows:] == 7).all() for x in guards.values()) and (s[3] == 7).all()
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("widths", sorted(WIDTHS))
+def test_step(dtype, widths):
+    """One row for every sequence: the reference's, in place as well, and without a state; three in a row are a prompt's."""
+    torch = require_gpu()
+    W, S = WIDTHS[widths], 5
+    x, want = make(torch, dtype, W, [1] * S, behind=0)
+    plan = plan_of(torch, dtype, W, x, S)
+    args = x["q"], x["k"], x["v"], x["log_decay"]
+    y = {"o": torch.zeros(S, W[0] * W[3], dtype=plan.dtype, device="cuda"), "sT": torch.zeros_like(x["s0"])}
+    plan.step(*args, x["s0"], y["sT"], y["o"])
+    torch.cuda.synchronize()
+    check(y, want, dtype, ("o", "sT"))
+    s, o = x["s0"].clone(), torch.zeros_like(y["o"])
+    plan.step(*args, s, s, o)
+    torch.cuda.synchronize()
+    assert torch.equal(s, y["sT"]) and torch.equal(o, y["o"])
+    plan.step(*args, None, s, o)
+    z, u = torch.zeros_like(s), torch.zeros_like(o)
+    plan.step(*args, torch.zeros_like(s), z, u)
+    torch.cuda.synchronize()
+    assert torch.equal(s, z) and torch.equal(o, u)
+    x3, want3 = make(torch, dtype, W, [3] * S, behind=0, seed=4)
+    s = x3["s0"].clone()
+    rows = torch.empty(3 * S, W[0] * W[3], dtype=plan.dtype, device="cuda")
+    for t in range(3):
+        plan.step(x3["q"][t::3], x3["k"][t::3], x3["v"][t::3], x3["log_decay"], s, s, o)
+        rows[t::3] = o
+    torch.cuda.synchronize()
+    check({"o": rows, "sT": s}, want3, dtype, ("o", "sT"))
+
+
+@pytest.mark.parametrize("lengths", [[100, 0, 37], [2000, 300]])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+def test_captured_and_on_another_stream(dtype, lengths):
+    """Replays see new inputs; eager work lies between them."""
+    torch = require_gpu()
+    widths = (2, 1, 32, 48)
+    x, _ = make(torch, dtype, widths, lengths)
+    plan, eager = (plan_of(torch, dtype, widths, x, len(lengths)) for _ in range(2))
+    side = torch.cuda.Stream()
+    out = run(torch, plan, x)
+    torch.cuda.synchronize()
+    z = run(torch, eager, x, stream=side)
+    side.synchronize()
+    for k in OUT:
+        assert torch.equal(out[k], z[k]), k
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        run(torch, plan, x, out=out)
+    for seed in (1, 2, 3):
+        y, _ = make(torch, dtype, widths, lengths, seed=seed)
+        for k in x:
+            x[k].copy_(y[k])
+        for k in OUT:
+            out[k].fill_(7.0)
+        graph.replay()
+        z = run(torch, eager, y)
+        torch.cuda.synchronize()
+        for k in OUT:
+            assert torch.equal(out[k], z[k]), k
+
+
+def test_beyond_2_31_elements():
+    """The last sequences of arrays of more than 2^31 elements, against a call of their own."""
+    torch = require_gpu()
+    H, d, n = 32, 64, 2**20 + 4100
+    x = torch.zeros(n, H * d, dtype=torch.bfloat16, device="cuda")
+    q, k, v, do = (torch.zeros_like(x) for _ in range(4))
+    for t in (q, k, v, do):
+        t[-5000:].normal_()
+    l = torch.full((H,), -0.05, device="cuda")
+    off = torch.tensor([0, n - 5000, n - 2000, n - 3], dtype=torch.int32, device="cuda")
+    o, dq, dk, dv = (torch.full_like(x, 7.0) for _ in range(4))
+    del x
+    plan = soma.LinearAttention(n, 3, H, d, d, torch.bfloat16)
+    s = torch.zeros(3, H, d, d, device="cuda")
+    plan.forward(q, k, v, l, o, None, s, off)
+    plan.backward(q, k, v, l, do, dq, dk, dv, None, None, None, off)
+    small = soma.LinearAttention(5000, 2, H, d, d, torch.bfloat16)
+    so, sq, sk, sv = (torch.zeros(5000, H * d, dtype=torch.bfloat16, device="cuda") for _ in range(4))
+    tail = [t[-5000:] for t in (q, k, v, do)]
+    offs = torch.tensor([0, 3000, 4997], dtype=torch.int32, device="cuda")
+    s2 = torch.zeros(2, H, d, d, device="cuda")
+    small.forward(*tail[:3], l, so, None, s2, offs)
+    small.backward(*tail[:3], l, tail[3], sq, sk, sv, None, None, None, offs)
+    torch.cuda.synchronize()
+    for big, part in ((o, so), (dq, sq), (dk, sk), (dv, sv)):
+        a, b = big[-5000:-3].float(), part[:-3].float()
+        # two splits into pieces: each within 2^-8 and the roundings of a value that may cancel
+        assert (big[-3:] == 7).all() and (a - b).abs().max() <= 2**-7 * b.abs().max()
+        assert (big[:n - 5000] == 0).all()
+    assert (s[1:] - s2).abs().max() <= 1e-5 * s2.abs().max()
