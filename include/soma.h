@@ -774,6 +774,124 @@ int soma_la_backward(const soma_la_config* cfg, const void* q_dev, const void* k
 int soma_la_step(const soma_la_config* cfg, const void* q_dev, const void* k_dev, const void* v_dev,
                  const float* log_decay_dev, const float* s0_dev, float* sT_dev, void* o_dev, void* stream);
 
+/* Dropout.  Element i of an array of rows, i = row width + column whatever its row
+ * stride, has 16 bits of Philox4x32-10: half i % 2 (0: the lower) of word (i / 2) % 4
+ * of block b = i / 8, with key (lo32(seed), hi32(seed) ^ hi32(t)) and counter (lo32(b),
+ * layer, lo32(t), hi32(b)), t = step + *step_dev.  With cut = p 65536, rounded, an
+ * element whose bits are below cut is dropped, whatever its value: it counts as 0; what
+ * is kept is multiplied with 65536 / (65536 - cut).  The mask is not stored: a gradient
+ * forms it again from the same numbers.  `layer` tells masks of one step apart. */
+typedef struct soma_drop {
+  double p;                 /* in [0, 1), rounded to 2^-16; below 1 - 2^-17 */
+  uint64_t seed;
+  uint64_t step;
+  const uint64_t* step_dev; /* on the device, read when the call runs: a captured call
+                               whose caller counts it up draws anew at every replay.
+                               NULL: 0 */
+  uint32_t layer;
+  uint32_t reserved;        /* 0 */
+} soma_drop;
+
+/* y = drop(x), or residual + drop(x); y's gradient goes back through the same call.
+ *   x, residual [rows][width] of `type`, rows x_stride and residual_stride elements
+ *   apart (residual NULL: none); y [rows][width], rows contiguous; it may be x or
+ *   residual where their rows are so too.  drop NULL: p = 0.
+ * In fp32, rounded once.  Constraints: rows in [0, 2^30], width in [1, 2^20], at most
+ * 2^40 elements. */
+typedef struct soma_dropout_config {
+  int32_t rows;
+  int32_t width;
+  int32_t type;             /* enum soma_type */
+  int32_t reserved;         /* 0 */
+  int64_t x_stride;         /* elements, >= width */
+  int64_t residual_stride;
+} soma_dropout_config;
+
+int soma_dropout(const soma_dropout_config* cfg, const void* x_dev, const void* residual_dev, const soma_drop* drop,
+                 void* y_dev, void* stream);
+
+/* Root-mean-square norm with the residual's addition, and dropout of the branch:
+ *   total_r = residual_r + drop(x)_r,
+ *   y_r = gain total_r / rms_r,   rms_r = sqrt(mean(total_r^2) + eps).
+ *   x       [rows][width] of `type`, rows x_stride elements apart.
+ *   residual [rows][width] of `sum_type`, rows residual_stride elements apart; NULL:
+ *           none.
+ *   gain    [width] fp32.
+ *   total   [rows][width] of `sum_type`, rows contiguous, what the backward pass
+ *           needs; NULL: not wanted.  It may be residual where that has contiguous
+ *           rows.
+ *   y       [rows][width] of `type`, rows contiguous.
+ * sum_type is `type` or fp32.  drop NULL: p = 0.  Sums are fp32; y is formed from
+ * total before that is rounded.
+ * Constraints: rows in [0, 2^30], width in [1, 2^14], eps finite and >= 0. */
+typedef struct soma_norm_config {
+  int32_t rows;
+  int32_t width;
+  int32_t type;             /* enum soma_type */
+  int32_t sum_type;
+  float eps;
+  int32_t reserved;         /* 0 */
+  int64_t x_stride;         /* elements, >= width */
+  int64_t residual_stride;
+} soma_norm_config;
+
+/* Bytes of device workspace of soma_norm_backward with dgain; it does not shrink with
+ * more rows.  Pure. */
+int soma_norm_workspace_size(const soma_norm_config* cfg, size_t* bytes);
+
+int soma_norm_forward(const soma_norm_config* cfg, const void* x_dev, const void* residual_dev, const float* gain_dev,
+                      const soma_drop* drop, void* total_dev, void* y_dev, void* stream);
+
+/* The same with y in 8 bits: codes [rows][width], e4m3, and scales [rows] fp32,
+ * y = code scale, scale = max |y_r| / 448 (a row of zeros: 0; a row that holds a NaN:
+ * NaN), codes rounded to nearest even. */
+int soma_norm_forward_codes(const soma_norm_config* cfg, const void* x_dev, const void* residual_dev,
+                            const float* gain_dev, const soma_drop* drop, void* total_dev, void* codes_dev,
+                            float* scales_dev, void* stream);
+
+/* The gradients from dy [rows][width] of `type` and dtotal [rows][width] of `sum_type`
+ * (what else reads total; NULL: zeros), rows contiguous, with the total that the
+ * forward call gave, its gain and its drop:
+ *   dresidual [rows][width] of `sum_type`; may be dtotal.
+ *   dx      [rows][width] of `type`: drop(dresidual), before that is rounded.
+ *   dgain   [width] fp32.
+ * Any of the three may be NULL: not wanted; the workspace is dgain's alone. */
+int soma_norm_backward(const soma_norm_config* cfg, const void* total_dev, const float* gain_dev, const void* dy_dev,
+                       const void* dtotal_dev, const soma_drop* drop, void* dresidual_dev, void* dx_dev, float* dgain_dev,
+                       void* workspace_dev, size_t workspace_bytes, void* stream);
+
+/* The next token of every row of logits.
+ *   logits  [rows][vocab] of `type`, rows logit_stride elements apart.  NaN counts as
+ *           -infinity: never drawn.
+ *   u       [rows] fp32, random numbers in [0, 1) (others are taken as the closest).
+ *   temperature [rows] fp32, NULL: 1.  One that is not > 0: the likeliest token.
+ *   top_k   [rows] int32, NULL or <= 0: off.
+ *   top_p   [rows] fp32, NULL, >= 1 or NaN: off.
+ *   min_p   [rows] fp32, NULL, <= 0 or NaN: off; above 1: 1.
+ * Tokens are ranked by their logits, the lower index first among equals, and weigh
+ * w_v = exp((l_v - max l) / temperature) (a logit that is the maximum: 1, an infinite
+ * one among them).  top_k keeps the first k; of these, top_p keeps every one in front
+ * of which less than top_p of their weight lies (the first one always); min_p keeps
+ * w >= min_p.  The token is the first, by index, of those left up to which more than u
+ * of their weight lies.  Weights are formed in fp64 and summed as multiples of 2^-s,
+ * s = 62 - ceil(log2 vocab) (50,257: 2^-46), in whatever order the same: a token whose
+ * weight is below half of that is never drawn.
+ *   tokens  [rows] int32; -1 where every logit is -infinity or NaN.
+ *   logprob [rows] fp32, log of the token's share in what was left (-1: -infinity);
+ *           NULL: not wanted.
+ * Constraints: rows in [0, 2^20], vocab in [1, 2^20]. */
+typedef struct soma_sample_config {
+  int32_t rows;
+  int32_t vocab;
+  int32_t type;             /* enum soma_type */
+  int32_t reserved;         /* 0 */
+  int64_t logit_stride;     /* elements, >= vocab */
+} soma_sample_config;
+
+int soma_sample(const soma_sample_config* cfg, const void* logits_dev, const float* u_dev, const float* temperature_dev,
+                const int32_t* top_k_dev, const float* top_p_dev, const float* min_p_dev, int32_t* tokens_dev,
+                float* logprob_dev, void* stream);
+
 /* Thread-local description of the last error ("" if none). */
 const char* soma_last_error(void);
 

@@ -32,7 +32,9 @@ EXPORTS = ("soma_param_count", "soma_workspace_size", "soma_create", "soma_destr
            "soma_scan_workspace_size", "soma_scan_forward", "soma_scan_backward", "soma_scan_step",
            "soma_ce_workspace_size", "soma_ce_loss", "soma_ce_grad", "soma_adamw_workspace_size", "soma_adamw_create",
            "soma_adamw_destroy", "soma_adamw_set_rounding", "soma_adamw_step", "soma_adamw_moments",
-           "soma_la_workspace_size", "soma_la_forward", "soma_la_backward", "soma_la_step", "soma_last_error")
+           "soma_la_workspace_size", "soma_la_forward", "soma_la_backward", "soma_la_step", "soma_dropout",
+           "soma_norm_workspace_size", "soma_norm_forward", "soma_norm_forward_codes", "soma_norm_backward", "soma_sample",
+           "soma_last_error")
 
 
 class SomaError(RuntimeError):
@@ -106,6 +108,26 @@ class LinearAttentionConfig(ctypes.Structure):
         ("scale", ctypes.c_float)] + [(n, ctypes.c_int64) for n in ("q_stride", "k_stride", "v_stride")]
 
 
+class Drop(ctypes.Structure):
+    """soma_drop: which elements are dropped."""
+    _fields_ = [("p", ctypes.c_double), ("seed", ctypes.c_uint64), ("step", ctypes.c_uint64), ("step_dev", ctypes.c_void_p),
+                ("layer", ctypes.c_uint32), ("reserved", ctypes.c_uint32)]
+
+
+class DropoutConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "width", "type", "reserved")] + [
+        (n, ctypes.c_int64) for n in ("x_stride", "residual_stride")]
+
+
+class NormConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "width", "type", "sum_type")] + [
+        ("eps", ctypes.c_float), ("reserved", ctypes.c_int32)] + [(n, ctypes.c_int64) for n in ("x_stride", "residual_stride")]
+
+
+class SampleConfig(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("rows", "vocab", "type", "reserved")] + [("logit_stride", ctypes.c_int64)]
+
+
 _lib = None
 
 
@@ -170,6 +192,13 @@ def load():
             "soma_la_forward": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 9 + [ctypes.c_size_t, vp]),
             "soma_la_backward": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 13 + [ctypes.c_size_t, vp]),
             "soma_la_step": (ctypes.c_int, [ctypes.POINTER(LinearAttentionConfig)] + [vp] * 8),
+            "soma_dropout": (ctypes.c_int, [ctypes.POINTER(DropoutConfig), vp, vp, ctypes.POINTER(Drop), vp, vp]),
+            "soma_norm_workspace_size": (ctypes.c_int, [ctypes.POINTER(NormConfig), ctypes.POINTER(ctypes.c_size_t)]),
+            "soma_norm_forward": (ctypes.c_int, [ctypes.POINTER(NormConfig), vp, vp, vp, ctypes.POINTER(Drop)] + [vp] * 3),
+            "soma_norm_forward_codes": (ctypes.c_int, [ctypes.POINTER(NormConfig), vp, vp, vp, ctypes.POINTER(Drop)] + [vp] * 4),
+            "soma_norm_backward": (ctypes.c_int, [ctypes.POINTER(NormConfig)] + [vp] * 4 + [ctypes.POINTER(Drop)] + [vp] * 4
+                                   + [ctypes.c_size_t, vp]),
+            "soma_sample": (ctypes.c_int, [ctypes.POINTER(SampleConfig)] + [vp] * 9),
             "soma_last_error": (ctypes.c_char_p, []),
         }
         for name, (res, args) in sig.items():
@@ -854,3 +883,138 @@ class LinearAttention(_Plan):
         n, args = self._inputs(q, k, v, log_decay)
         self._call(stream, load().soma_la_step, *args, self._of_state(s0, "s0"), self._of_state(sT, "sT", optional=False),
                    self._of_rows(o, "o", n, self.heads * self.value_width))
+
+
+class _Dropping(_Plan):
+    """What the operators share that drop elements with probability ``drop`` (rounded to 2^-16): seed, step and layer of
+    a call name the mask, and a backward pass gives the same.  step may be an int64 tensor of one element on the device,
+    which is read when the call runs, so that a captured call draws anew once its program has counted it up."""
+
+    def _set_drop(self, drop):
+        self.drop = float(drop)
+        if not 0.0 <= self.drop < 1.0 or round(self.drop * 65536) > 65535:
+            raise ValueError("drop must be in [0, 1) and leave at least 1 of 65,536 elements")
+
+    def _mask(self, seed, step, layer):
+        import torch
+        if self.drop == 0.0:
+            return None
+        where = None
+        if isinstance(step, torch.Tensor):
+            where, step = self._ptr(step.view(-1) if step.is_contiguous() else step, "step", torch.int64, (1,)), 0
+        if not 0 <= int(layer) < 2**32:
+            raise ValueError("layer must be in [0, 2^32)")
+        return ctypes.byref(Drop(self.drop, int(seed) & (2**64 - 1), int(step) & (2**64 - 1), where, int(layer), 0))
+
+    def _rows_of(self, x, name):
+        import torch
+        if not isinstance(x, torch.Tensor) or x.dim() != 2:
+            raise TypeError(f"{name} must be a tensor [rows][{self.width}]")
+        if x.shape[0] > self.rows:
+            raise ValueError(f"{x.shape[0]} rows, but the plan was made for {self.rows}")
+        return x.shape[0]
+
+
+class Dropout(_Dropping):
+    """Dropout of at most ``rows`` rows of ``width`` elements of ``dtype`` (float32 or bfloat16), its mask formed from a
+    counter and never stored."""
+
+    def __init__(self, rows: int, width: int, dtype, drop: float, device="cuda"):
+        self.rows, self.width, self.dtype = int(rows), int(width), dtype
+        self._type = _type_of(dtype)
+        _check_sizes(rows=self.rows, width=self.width)
+        self._set_drop(drop)
+        self._start(0, device)
+
+    def forward(self, x, y, residual=None, seed=0, step=0, layer=0, stream=None):
+        """y [n][width] = residual + drop(x) (None: drop(x)); it may be x or residual.  x and residual may be strided."""
+        n = self._rows_of(x, "x")
+        px = self._ptr(x, "x", self.dtype, (n, self.width), strided=True)
+        pr = self._ptr(residual, "residual", self.dtype, (n, self.width), optional=True, strided=True)
+        cfg = DropoutConfig(n, self.width, self._type, 0, _row_stride(x), self.width if residual is None else _row_stride(residual))
+        self._call(stream, load().soma_dropout, ctypes.byref(cfg), px, pr, self._mask(seed, step, layer),
+                   self._ptr(y, "y", self.dtype, (n, self.width)))
+
+    def backward(self, dy, dx, seed=0, step=0, layer=0, stream=None):
+        """dx [n][width] (it may be dy) from dy, with the numbers that forward had; the residual's gradient is dy."""
+        self.forward(dy, dx, None, seed, step, layer, stream)
+
+
+class RmsNorm(_Dropping):
+    """Root-mean-square norm with the residual's addition, total = residual + drop(x), y = gain total / rms(total), of at
+    most ``rows`` rows of ``width``.  ``dtype`` (float32 or bfloat16) is the type of x and y, ``sum_dtype`` (dtype or
+    float32; None: dtype) that of residual and total; gains are float32."""
+
+    def __init__(self, rows: int, width: int, dtype, sum_dtype=None, eps: float = 1e-5, drop: float = 0.0, device="cuda"):
+        self.rows, self.width, self.dtype = int(rows), int(width), dtype
+        self.sum_dtype = dtype if sum_dtype is None else sum_dtype
+        self._types, self.eps = (_type_of(dtype), _type_of(self.sum_dtype)), float(eps)
+        _check_sizes(rows=self.rows, width=self.width)
+        self._set_drop(drop)
+        out = ctypes.c_size_t()
+        _check(load().soma_norm_workspace_size(ctypes.byref(self._cfg(self.rows, self.width, self.width)), ctypes.byref(out)))
+        self._bytes = out.value
+        self._start(out.value, device)
+
+    def _cfg(self, rows, x_stride, residual_stride):
+        return NormConfig(rows, self.width, *self._types, self.eps, 0, x_stride, residual_stride)
+
+    def forward(self, x, gain, y, residual=None, total=None, scale=None, seed=0, step=0, layer=0, stream=None):
+        """y [n][width] and total [n][width] (None: not wanted; it may be residual) from x, residual (None: none) and
+        gain [width].  With scale [n] (float32), y is torch.float8_e4m3fn codes and its values are y scale."""
+        import torch
+        n = self._rows_of(x, "x")
+        px = self._ptr(x, "x", self.dtype, (n, self.width), strided=True)
+        pr = self._ptr(residual, "residual", self.sum_dtype, (n, self.width), optional=True, strided=True)
+        cfg = self._cfg(n, _row_stride(x), self.width if residual is None else _row_stride(residual))
+        args = [ctypes.byref(cfg), px, pr, self._ptr(gain, "gain", torch.float32, (self.width,)), self._mask(seed, step, layer),
+                self._ptr(total, "total", self.sum_dtype, (n, self.width), optional=True)]
+        if scale is None:
+            self._call(stream, load().soma_norm_forward, *args, self._ptr(y, "y", self.dtype, (n, self.width)))
+        else:
+            self._call(stream, load().soma_norm_forward_codes, *args, self._ptr(y, "y", torch.float8_e4m3fn, (n, self.width)),
+                       self._ptr(scale, "scale", torch.float32, (n,)))
+
+    def backward(self, total, gain, dy, dtotal=None, dresidual=None, dx=None, dgain=None, seed=0, step=0, layer=0, stream=None):
+        """dresidual [n][width] (it may be dtotal), dx [n][width] and dgain [width] (float32), any of which may be None,
+        from dy and dtotal (None: zeros), with the total that forward gave and the numbers that it had."""
+        import torch
+        n = self._rows_of(total, "total")
+        shape = (n, self.width)
+        cfg = self._cfg(n, self.width, self.width)
+        self._call(stream, load().soma_norm_backward, ctypes.byref(cfg), self._ptr(total, "total", self.sum_dtype, shape),
+                   self._ptr(gain, "gain", torch.float32, (self.width,)), self._ptr(dy, "dy", self.dtype, shape),
+                   self._ptr(dtotal, "dtotal", self.sum_dtype, shape, optional=True), self._mask(seed, step, layer),
+                   self._ptr(dresidual, "dresidual", self.sum_dtype, shape, optional=True),
+                   self._ptr(dx, "dx", self.dtype, shape, optional=True),
+                   self._ptr(dgain, "dgain", torch.float32, (self.width,), optional=True), self._ws, self._bytes)
+
+
+class Sampler(_Plan):
+    """The next token of at most ``rows`` rows of ``vocab`` logits of ``dtype`` (float32 or bfloat16), from random numbers
+    that the caller gives."""
+
+    def __init__(self, rows: int, vocab: int, dtype, device="cuda"):
+        self.rows, self.vocab, self.dtype = int(rows), int(vocab), dtype
+        self._type = _type_of(dtype)
+        _check_sizes(rows=self.rows, vocab=self.vocab)
+        self._start(0, device)
+
+    def sample(self, logits, u, tokens, logprob=None, temperature=None, top_k=None, top_p=None, min_p=None, stream=None):
+        """tokens [n] (int32) and logprob [n] (float32) of logits [n][vocab], whose rows may be strided, and u [n] in
+        [0, 1).  temperature, top_p, min_p [n] (float32) and top_k [n] (int32): None is off.  A temperature of 0 takes the
+        likeliest token; a row without a logit above -infinity gives -1."""
+        import torch
+        if not isinstance(logits, torch.Tensor) or logits.dim() != 2:
+            raise TypeError("logits must be a tensor [rows][vocab]")
+        n = logits.shape[0]
+        if n > self.rows:
+            raise ValueError(f"{n} rows, but the plan was made for {self.rows}")
+        pl = self._ptr(logits, "logits", self.dtype, (n, self.vocab), strided=True)
+        cfg = SampleConfig(n, self.vocab, self._type, 0, _row_stride(logits))
+        f, i = torch.float32, torch.int32
+        self._call(stream, load().soma_sample, ctypes.byref(cfg), pl, self._ptr(u, "u", f, (n,)),
+                   self._ptr(temperature, "temperature", f, (n,), optional=True),
+                   self._ptr(top_k, "top_k", i, (n,), optional=True), self._ptr(top_p, "top_p", f, (n,), optional=True),
+                   self._ptr(min_p, "min_p", f, (n,), optional=True), self._ptr(tokens, "tokens", i, (n,)),
+                   self._ptr(logprob, "logprob", f, (n,), optional=True))

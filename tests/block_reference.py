@@ -81,3 +81,96 @@ def linear_attention(q, k, v, log_decay, lengths, s0, scale, dtype="float32", do
             out["ds0"][n, h] = whole * G + (qh * front[:, None]).T @ g
             out["ds0_err"][n, h] = ew * a(G) + (a(qh) * (off(t + 1) * a(front))[:, None]).T @ a(g)
     return out
+
+
+def philox(ctr, key):
+    """Philox4x32-10 of counters [n][4] and one key, uint64 arrays of 32-bit words."""
+    x = [ctr[:, i].astype(np.uint64) for i in range(4)]
+    k0, k1 = int(key[0]), int(key[1])
+    low = np.uint64(0xFFFFFFFF)
+    for _ in range(10):
+        a, b = x[0] * np.uint64(0xD2511F53), x[2] * np.uint64(0xCD9E8D57)
+        x = [(b >> np.uint64(32)) ^ x[1] ^ np.uint64(k0), b & low, (a >> np.uint64(32)) ^ x[3] ^ np.uint64(k1), a & low]
+        k0, k1 = (k0 + 0x9E3779B9) & 0xFFFFFFFF, (k1 + 0xBB67AE85) & 0xFFFFFFFF
+    return np.stack(x, 1)
+
+
+def keep(rows, width, p, seed, step, layer, first=0):
+    """The factor of every element of rows first .. first + rows - 1: 0, or 65536 / (65536 - cut)."""
+    cut = round(p * 65536)
+    lo, hi = first * width, (first + rows) * width
+    b = np.arange(lo // 8, -(-hi // 8), dtype=np.uint64)
+    s, t = int(seed) % 2**64, int(step) % 2**64
+    ctr = np.stack([b & np.uint64(0xFFFFFFFF), np.full_like(b, layer), np.full_like(b, t & 0xFFFFFFFF), b >> np.uint64(32)], 1)
+    w = philox(ctr, (s & 0xFFFFFFFF, (s >> 32) ^ (t >> 32)))
+    fields = np.stack([w & np.uint64(0xFFFF), w >> np.uint64(16)], 2).reshape(-1)
+    kept = fields[lo - lo // 8 * 8:][:hi - lo] >= cut
+    return (kept * (65536 / (65536 - cut))).reshape(rows, width)
+
+
+def drop(x, factor):
+    """What is dropped counts as 0, whatever it is."""
+    return np.where(factor == 0, 0.0, x) * factor
+
+
+def norm(x, residual, gain, eps, factor):
+    """total and y, and their bounds before they are rounded to their types.
+
+    The factor carries 1 u, its product and the sum 1 each; the mean of squares at most 64 u (sums of up to 40 terms a
+    lane and 10 halvings), half of it in the root; root, division, products: 6."""
+    t = drop(x, factor) + (0 if residual is None else residual)
+    et = U * (2 * np.abs(drop(x, factor)) + np.abs(t))
+    n = x.shape[1]
+    square = (t * t).mean(1, keepdims=True) + eps
+    inv = 1 / np.sqrt(square)
+    y = gain * t * inv
+    ei = 40 * U + (np.abs(t) * et).sum(1, keepdims=True) / n / square
+    return {"total": t, "total_err": et, "y": y, "y_err": np.abs(gain) * inv * et + (ei + 6 * U) * np.abs(y)}
+
+
+def norm_backward(t, gain, dy, dtotal, eps, factor):
+    """From the total as it is stored: dresidual, dx, dgain and their bounds."""
+    rows, n = t.shape
+    inv = 1 / np.sqrt((t * t).mean(1, keepdims=True) + eps)
+    x, h = t * inv, dy * gain
+    m, ma = (h * x).mean(1, keepdims=True), np.abs(h * x).mean(1, keepdims=True)
+    d = (0 if dtotal is None else dtotal) + inv * (h - x * m)
+    size = inv * (np.abs(h) + np.abs(x) * np.abs(m))
+    e = U * (100 * size + 2 * np.abs(d) + 120 * inv * np.abs(x) * ma)
+    # a lane's rows one after another, waves, blocks in 16 columns
+    return {"dresidual": d, "dresidual_err": e, "dx": drop(d, factor), "dx_err": (e + 2 * U * np.abs(d)) * factor,
+            "dgain": (dy * x).sum(0), "dgain_err": U * (100 + rows / 512 + 64) * np.abs(dy * x).sum(0)}
+
+
+def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
+    """One row: (token, its share's logarithm, how near u comes to another token, in shares)."""
+    l = np.where(np.isnan(logits), -np.inf, logits.astype(np.float64))
+    top = l.max()
+    if top == -np.inf:
+        return -1, -np.inf, 1.0
+    order = np.argsort(-l, kind="stable")
+    if not temperature > 0:
+        return int(order[0]), 0.0, 1.0
+    with np.errstate(invalid="ignore", over="ignore"):
+        w = np.where(l == top, 1.0, np.where((l == -np.inf) | (top == np.inf), 0.0, np.exp((l - top) / temperature)))
+    order = order[l[order] > -np.inf]
+    near = 1.0
+    if top_k > 0:
+        order = order[:top_k]
+    if top_p < 1:
+        before = np.cumsum(w[order]) - w[order]
+        limit = max(float(top_p), 0.0) * w[order].sum()
+        if order.size > 1:                 # the first stays whatever the limit
+            near = min(near, np.abs(before[1:] - limit).min() / w[order].sum())
+        stay = before < limit
+        stay[0] = True
+        order = order[stay]
+    if min_p > 0:
+        order = order[w[order] >= min(float(min_p), 1.0)]
+    order = np.sort(order)
+    run = np.cumsum(w[order])
+    share = run / run[-1]
+    u = min(max(float(u), 0.0), 1.0)
+    at = min(int(np.searchsorted(share, u, side="right")), int(np.nonzero(w[order])[0][-1]))
+    near = min(near, np.abs(share[:-1] - u).min() if share.size > 1 else 1.0)
+    return int(order[at]), float(np.log(w[order[at]] / run[-1])), near

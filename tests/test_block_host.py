@@ -139,6 +139,167 @@ def test_linear_attention_of_no_rows_is_no_error(lib, dtype):
     assert passed(forward(lib, c, None, 0, **none)) and passed(backward(lib, c, None, 0, **none))
 
 
+def drop(**kw):
+    d = soma.Drop(0.1, 1, 2, None, 3, 0)
+    for k, v in kw.items():
+        setattr(d, k, v)
+    return ctypes.byref(d)
+
+
+DROPS = (dict(p=-0.1), dict(p=1.0), dict(p=float("nan")), dict(p=1 - 2.0**-18), dict(step_dev=0x1004), dict(reserved=1))
+
+
+def dropout(lib, cfg, x=ptr(0), residual=ptr(1), d=None, y=ptr(2)):
+    return lib.soma_dropout(cfg, x, residual, d if d is not None else drop(), y, None)
+
+
+def dropout_cfg(**kw):
+    c = soma.DropoutConfig(10, 20, 0, 0, 24, 20)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return ctypes.byref(c)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("rows", -1, soma.SOMA_ESHAPE), ("rows", 2**30 + 1, soma.SOMA_ESHAPE), ("width", 0, soma.SOMA_ESHAPE),
+    ("width", 2**20 + 1, soma.SOMA_ESHAPE), ("type", 2, soma.SOMA_EINVAL), ("reserved", 1, soma.SOMA_EINVAL),
+    ("x_stride", 19, soma.SOMA_ESHAPE), ("residual_stride", 19, soma.SOMA_ESHAPE), ("x_stride", 2**33, soma.SOMA_ESHAPE)])
+def test_dropout_shapes(lib, field, value, code):
+    assert dropout(lib, dropout_cfg(**{field: value})) == code and lib.soma_last_error()
+
+
+def test_dropout_arguments(lib):
+    c = dropout_cfg()
+    assert lib.soma_dropout(None, ptr(0), None, None, ptr(1), None) == soma.SOMA_EINVAL
+    for kw in (dict(x=None), dict(y=None), dict(x=at(ptr(0), 2)), dict(residual=at(ptr(0), 2)), dict(y=at(ptr(0), 2))):
+        assert dropout(lib, c, **kw) == soma.SOMA_EINVAL, kw
+    for kw in DROPS:
+        assert dropout(lib, c, d=drop(**kw)) == soma.SOMA_EINVAL, kw
+    # y over part of x, over strided x, over part of the residual, over the step
+    for y in (at(ptr(0), 4 * (9 * 24 + 19)), ptr(0), at(ptr(1), 796), at(ptr(1), -796)):
+        assert dropout(lib, c, y=y) == soma.SOMA_EINVAL and b"overlap" in lib.soma_last_error()
+    assert dropout(lib, c, d=drop(step_dev=ptr(2).value + 8)) == soma.SOMA_EINVAL
+    assert dropout(lib, dropout_cfg(rows=2**30, width=2**20, x_stride=2**20, residual_stride=2**20)) == soma.SOMA_ESHAPE
+    assert passed(dropout(lib, c, y=ptr(1)))                      # in place of the residual
+    assert lib.soma_dropout(dropout_cfg(rows=0), None, None, None, None, None) == soma.SOMA_OK
+
+
+def norm_cfg(**kw):
+    c = soma.NormConfig(10, 20, 1, 0, 1e-5, 0, 20, 20)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return ctypes.byref(c)
+
+
+N = {n: ptr(i) for i, n in enumerate(("x", "residual", "gain", "total", "y", "scales", "dy", "dtotal", "dresidual", "dx", "dgain"))}
+
+
+def norm_forward(lib, cfg, d=None, **kw):
+    x = dict(N, **kw)
+    return lib.soma_norm_forward(cfg, x["x"], x["residual"], x["gain"], d, x["total"], x["y"], None)
+
+
+def norm_codes(lib, cfg, d=None, **kw):
+    x = dict(N, **kw)
+    return lib.soma_norm_forward_codes(cfg, x["x"], x["residual"], x["gain"], d, x["total"], x["y"], x["scales"], None)
+
+
+def norm_backward(lib, cfg, d=None, ws=WS, n=BIG, **kw):
+    x = dict(N, **kw)
+    return lib.soma_norm_backward(cfg, x["total"], x["gain"], x["dy"], x["dtotal"], d, x["dresidual"], x["dx"], x["dgain"], ws, n, None)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("rows", -1, soma.SOMA_ESHAPE), ("rows", 2**30 + 1, soma.SOMA_ESHAPE), ("width", 0, soma.SOMA_ESHAPE),
+    ("width", 2**14 + 1, soma.SOMA_ESHAPE), ("type", 2, soma.SOMA_EINVAL), ("sum_type", -1, soma.SOMA_EINVAL),
+    ("reserved", 1, soma.SOMA_EINVAL), ("eps", -1e-5, soma.SOMA_EINVAL), ("eps", float("nan"), soma.SOMA_EINVAL),
+    ("eps", float("inf"), soma.SOMA_EINVAL), ("x_stride", 19, soma.SOMA_ESHAPE), ("residual_stride", 19, soma.SOMA_ESHAPE),
+    ("residual_stride", 2**33, soma.SOMA_ESHAPE)])
+def test_norm_shapes(lib, field, value, code):
+    c, out = norm_cfg(**{field: value}), ctypes.c_size_t()
+    assert lib.soma_norm_workspace_size(c, ctypes.byref(out)) == code
+    for call in (norm_forward, norm_codes, norm_backward):
+        assert call(lib, c) == code and lib.soma_last_error()
+
+
+def test_norm_arguments(lib):
+    out, c = ctypes.c_size_t(), norm_cfg()
+    assert lib.soma_norm_workspace_size(None, ctypes.byref(out)) == soma.SOMA_EINVAL
+    assert lib.soma_norm_workspace_size(c, None) == soma.SOMA_EINVAL
+    assert norm_forward(lib, norm_cfg(type=0, sum_type=1)) == soma.SOMA_EINVAL
+    last = 0
+    for rows in (0, 1, 3, 4, 5, 1000, 4096, 4097, 10**6, 2**30):
+        assert lib.soma_norm_workspace_size(norm_cfg(rows=rows), ctypes.byref(out)) == soma.SOMA_OK
+        assert out.value >= last
+        last = out.value
+    for call, names in ((norm_forward, ("x", "gain", "y")), (norm_codes, ("x", "gain", "y", "scales")), (norm_backward, ("total", "gain", "dy"))):
+        for name in names:
+            assert call(lib, c, **{name: None}) == soma.SOMA_EINVAL, name
+        for kw in DROPS:
+            assert call(lib, c, drop(**kw)) == soma.SOMA_EINVAL, kw
+    assert norm_backward(lib, c, dresidual=None, dx=None, dgain=None) == soma.SOMA_EINVAL
+    for call, names in ((norm_forward, ("x", "residual", "gain", "total", "y")), (norm_codes, ("x", "residual", "gain", "total", "scales")),
+                        (norm_backward, ("total", "gain", "dy", "dtotal", "dresidual", "dx", "dgain"))):
+        for name in names:
+            assert call(lib, c, **{name: at(N[name], 1)}) == soma.SOMA_EINVAL, name
+    # bytes of 10 x 20 elements of bf16 or fp32
+    size = dict(x=400, residual=800, gain=80, total=800, y=400, scales=40, dy=400, dtotal=800, dresidual=800, dx=400, dgain=80)
+    for call, outs, ins in ((norm_forward, ("total", "y"), ("x", "residual", "gain")),
+                            (norm_codes, ("total", "scales"), ("x", "residual", "gain")),
+                            (norm_backward, ("dresidual", "dx", "dgain"), ("total", "gain", "dy", "dtotal"))):
+        for o in outs:
+            for i in ins + tuple(x for x in outs if x != o):
+                assert call(lib, c, **{o: at(N[i], size[i] - 4)}) == soma.SOMA_EINVAL, (o, i)
+                assert b"overlap" in lib.soma_last_error()
+    # in place of strided rows
+    assert norm_forward(lib, norm_cfg(residual_stride=24), total=N["residual"]) == soma.SOMA_EINVAL
+    assert passed(norm_forward(lib, c, total=N["residual"])) and passed(norm_backward(lib, c, dresidual=N["dtotal"]))
+    assert lib.soma_norm_workspace_size(c, ctypes.byref(out)) == soma.SOMA_OK
+    for kw in (dict(ws=None), dict(ws=at(WS, 128)), dict(n=out.value - 1)):
+        assert norm_backward(lib, c, **kw) == soma.SOMA_EWORKSPACE, kw
+    none = dict.fromkeys(("x", "residual", "total", "y", "scales"))
+    assert norm_forward(lib, norm_cfg(rows=0), **none) == soma.SOMA_OK and norm_codes(lib, norm_cfg(rows=0), **none) == soma.SOMA_OK
+    none = dict.fromkeys(("total", "dy", "dtotal", "dresidual", "dx"))
+    assert passed(norm_backward(lib, norm_cfg(rows=0), **none))
+
+
+def sample_cfg(**kw):
+    c = soma.SampleConfig(10, 1000, 0, 0, 1000)
+    for k, v in kw.items():
+        setattr(c, k, v)
+    return ctypes.byref(c)
+
+
+SAMPLE = ("logits", "u", "temperature", "top_k", "top_p", "min_p", "tokens", "logprob")
+
+
+def sample(lib, cfg, **kw):
+    x = dict({n: ptr(i) for i, n in enumerate(SAMPLE)}, **kw)
+    return lib.soma_sample(cfg, *(x[n] for n in SAMPLE), None)
+
+
+@pytest.mark.parametrize("field,value,code", [
+    ("rows", -1, soma.SOMA_ESHAPE), ("rows", 2**20 + 1, soma.SOMA_ESHAPE), ("vocab", 0, soma.SOMA_ESHAPE),
+    ("vocab", 2**20 + 1, soma.SOMA_ESHAPE), ("type", 2, soma.SOMA_EINVAL), ("reserved", 1, soma.SOMA_EINVAL),
+    ("logit_stride", 999, soma.SOMA_ESHAPE), ("logit_stride", 2**33, soma.SOMA_ESHAPE)])
+def test_sample_shapes(lib, field, value, code):
+    assert sample(lib, sample_cfg(**{field: value})) == code and lib.soma_last_error()
+
+
+def test_sample_arguments(lib):
+    c = sample_cfg()
+    assert sample(lib, None) == soma.SOMA_EINVAL
+    for name in ("logits", "u", "tokens"):
+        assert sample(lib, c, **{name: None}) == soma.SOMA_EINVAL, name
+    for i, name in enumerate(SAMPLE):
+        assert sample(lib, c, **{name: at(ptr(i), 2)}) == soma.SOMA_EINVAL, name
+    for o in ("tokens", "logprob"):
+        for i, name in enumerate(SAMPLE):
+            if name != o:
+                assert sample(lib, c, **{o: at(ptr(i), 36)}) == soma.SOMA_EINVAL and b"overlap" in lib.soma_last_error()
+    assert sample(lib, sample_cfg(rows=0), **dict.fromkeys(SAMPLE)) == soma.SOMA_OK
+
+
 def test_classes_refuse_on_the_host():
     torch = pytest.importorskip("torch")
     soma.load()
@@ -156,3 +317,24 @@ def test_classes_refuse_on_the_host():
         soma.LinearAttention(10, 1, 4, 8, 8, torch.float32, kv_heads=3)
     with pytest.raises(soma.SomaError):
         soma.LinearAttention(10, 1, 4, 8, 8, torch.float32, scale=float("nan"))
+    for bad in (-0.1, 1.0, float("nan"), 1 - 2.0**-18):
+        with pytest.raises(ValueError):
+            soma.Dropout(10, 8, torch.float32, bad)
+        with pytest.raises(ValueError):
+            soma.RmsNorm(10, 8, torch.float32, drop=bad)
+    with pytest.raises(TypeError):
+        soma.Dropout(10, 8, torch.float16, 0.1)
+    with pytest.raises(TypeError):
+        soma.RmsNorm(10, 8, torch.bfloat16, torch.float16)
+    with pytest.raises(soma.SomaError):
+        soma.RmsNorm(10, 8, torch.float32, torch.bfloat16)
+    with pytest.raises(soma.SomaError):
+        soma.RmsNorm(10, 2**14 + 1, torch.float32)
+    for make in (lambda: soma.Dropout(10, 8, torch.float32, 0.1, device="cpu"), lambda: soma.RmsNorm(10, 8, torch.float32, device="cpu"),
+                 lambda: soma.Sampler(10, 8, torch.float32, device="cpu"), lambda: soma.Sampler(10, 8, torch.float16)):
+        with pytest.raises(TypeError):
+            make()
+    for make in (lambda: soma.Sampler(-1, 8, torch.float32), lambda: soma.Dropout(10, -8, torch.float32, 0.1),
+                 lambda: soma.RmsNorm(2**31, 8, torch.float32)):
+        with pytest.raises(ValueError):
+            make()

@@ -46,3 +46,46 @@ def test_linear_attention_is_its_recurrence_and_its_gradients_are_differences(he
             z[name][i] -= 1e-4
             # quadratic and cubic terms: the difference is exact up to 64-bit roundings and 1e-8 of the third order
             assert abs((loss(y) - loss(z)) / 2e-4 - out[grad][i]) < 1e-6 * (1 + abs(out[grad][i])), (name, i)
+
+
+def test_norm_gradients_are_differences():
+    g = np.random.default_rng(5)
+    x, r, gain = g.standard_normal((4, 7)), g.standard_normal((4, 7)), 1 + 0.1 * g.standard_normal(7)
+    dy, dt = g.standard_normal((4, 7)), g.standard_normal((4, 7))
+    factor = ref.keep(4, 7, 0.4, 12345, 3, 1)
+    out = ref.norm_backward(ref.norm(x, r, gain, 1e-3, factor)["total"], gain, dy, dt, 1e-3, factor)
+
+    def loss(x, r, gain):
+        y = ref.norm(x, r, gain, 1e-3, factor)
+        return (y["y"] * dy).sum() + (y["total"] * dt).sum()
+
+    for name, which in (("dx", 0), ("dresidual", 1), ("dgain", 2)):
+        for i in np.ndindex(out[name].shape):
+            a = [x.copy(), r.copy(), gain.copy()]
+            b = [x.copy(), r.copy(), gain.copy()]
+            a[which][i] += 1e-5
+            b[which][i] -= 1e-5
+            # third derivatives of a root of O(1): 1e-10 times some hundred, and 64-bit roundings over 1e-5
+            assert abs((loss(*a) - loss(*b)) / 2e-5 - out[name][i]) < 1e-7
+
+
+def test_mask_is_the_framework_s_philox(oracle_mod):
+    """The generator's words against the oracle's."""
+    g = np.random.default_rng(1)
+    ctr = g.integers(0, 2**32, (50, 4), dtype=np.uint64)
+    key = g.integers(0, 2**32, 2, dtype=np.uint64)
+    mine = ref.philox(ctr, key)
+    theirs = np.array([oracle_mod.philox(tuple(int(v) for v in c), tuple(int(v) for v in key)) for c in ctr], dtype=np.uint64)
+    assert np.array_equal(mine, theirs)
+
+
+def test_sample_by_hand():
+    l = np.log(np.array([0.1, 0.4, 0.1, 0.4]))
+    assert [ref.sample(l, u)[0] for u in (0.0, 0.099, 0.101, 0.499, 0.501, 0.599, 0.601, 0.999, 1.0)] == [0, 0, 1, 1, 2, 2, 3, 3, 3]
+    assert ref.sample(l, 0.7, temperature=0)[0] == 1
+    assert ref.sample(l, 0.999, top_k=1)[0] == 1 and ref.sample(l, 0.999, top_k=3)[0] == 3
+    assert ref.sample(l, 0.01, top_k=3)[0] == 0 and ref.sample(l, 0.5, top_k=2, top_p=0.4)[0] == 1
+    assert ref.sample(l, 0.999, top_p=0.3)[0] == 1 and ref.sample(l, 0.001, top_p=0.85)[0] == 0
+    assert ref.sample(l, 0.999, min_p=0.5)[0] == 3 and ref.sample(l, 0.0, min_p=0.5)[0] == 1
+    assert ref.sample(np.full(3, -np.inf), 0.5)[0] == -1 and ref.sample(np.array([np.nan, 1.0, -np.inf]), 0.9)[0] == 1
+    assert [ref.sample(np.array([np.inf, 1.0, np.inf]), u)[0] for u in (0.2, 0.9)] == [0, 2]
