@@ -735,7 +735,7 @@ int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_ou
  * finite (an infinity may become NaN), and nothing else: rows in front of it
  * and other sequences and heads never see it.
  * Constraints: rows in [0, 2^30], sequences in [1, 65535], heads in [1, 1024],
- * kv_heads a divisor of heads, both widths in [1, 256]. */
+ * kv_heads a divisor of heads, both widths in [1, 256], strides up to 2^22. */
 typedef struct soma_la_config {
   int32_t rows;
   int32_t sequences;

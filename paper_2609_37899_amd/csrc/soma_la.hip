@@ -102,9 +102,9 @@ struct Walk {
   int64_t x_stride, y_stride, z_stride;     // elements between rows
   int x_share, y_share, z_share;            // heads that share one of x's, y's or z's
   int inner, outer;                         // columns of a head of x and y; of z and out
-  int x_vec, y_vec, z_vec;                  // 16-byte loads
+  int vec;                                  // every array aligned: through buffers
   void* out;                                // [rows][heads outer] of T, or fp32
-  int out_float, out_vec;
+  int out_float;
   const float *begin, *log_decay;           // states [sequences][heads][..], or NULL: zeros
   float* end;                               // the same, or NULL: not wanted
   int64_t row_stride, col_stride;           // of begin and end, an inner and an outer index
@@ -114,7 +114,6 @@ struct Walk {
   float p_scale, in_scale, front_scale;     // of P, of the state's update, of what R gives
   int piece, pieces;                        // rows a piece (0: a block a sequence), pieces
   float* slots;                             // [pieces][heads][slices][a block's state]
-  int2* info;                               // [pieces]: rows of a piece's map, sequence it begins in (-1: in front of it)
 };
 
 __device__ __forceinline__ int first_row(const Walk& a, int s) {
@@ -145,36 +144,19 @@ __device__ __forceinline__ int sequence_before(const Walk& a, int row) {
   return lo - 1;
 }
 
-// kEl elements of a row of T from column c on, zeros from `width` on.
-template <class T>
-__device__ __forceinline__ uint4 load_unit(const T* row, int c, int width, bool there, int vec) {
-  uint4 u = make_uint4(0, 0, 0, 0);
-  if (!there) return u;
-  if (vec) {
-    if (c < width) u = *reinterpret_cast<const uint4*>(row + c);
-    return u;
-  }
-  uint32_t w[4] = {0, 0, 0, 0};
-  if constexpr (sizeof(T) == 2) {
-    const uint16_t* p = reinterpret_cast<const uint16_t*>(row);
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c + i < width) w[i / 2] |= static_cast<uint32_t>(p[c + i]) << (16 * (i & 1));
-  } else {
-    const uint32_t* p = reinterpret_cast<const uint32_t*>(row);
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-      if (c + i < width) w[i] = p[c + i];
-  }
-  return make_uint4(w[0], w[1], w[2], w[3]);
-}
-
 // A value that is not finite, told by its exponent's carry into the bit above.
 template <class T>
 __device__ __forceinline__ uint32_t not_finite(const uint4& u) {
   constexpr uint32_t e = sizeof(T) == 2 ? 0x7F807F80u : 0x7F800000u, one = sizeof(T) == 2 ? 0x00800080u : 0x00800000u,
                      top = sizeof(T) == 2 ? 0x80008000u : 0x80000000u;
   return (((u.x & e) + one) | ((u.y & e) + one) | ((u.z & e) + one) | ((u.w & e) + one)) & top;
+}
+
+// A value that the compiler takes for another every time: what is seldom used and formed
+// from it is formed again there, not kept over a loop in registers.
+__device__ __forceinline__ int fresh(int x) {
+  asm volatile("" : "+v"(x));
+  return x;
 }
 
 // A fragment with zeros in the place of what is not finite.
@@ -195,19 +177,65 @@ __device__ __forceinline__ f4 finite_part(const f4& f) {
   return r;
 }
 
+typedef uint32_t u4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u2 __attribute__((ext_vector_type(2)));
+
+// A buffer from p on; what is read behind `bytes` is 0, what is written there is lost.
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, uint32_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(bytes), 0x00020000);
+}
+constexpr uint32_t kNowhere = 0xFFFFFFFFu;
+
 // Rows of one array on their way to LDS: kRows x kCols, kThreads lanes side by side.
-template <class T, int kRows, int kCols>
+// They come through a buffer that ends with the chunk's last row: row r lies at r
+// strides (walking back, at kRows - 1 - r less the rows that the chunk is short of,
+// which wraps for those), and what is not there lies behind the end.  kVec: 16 bytes
+// at a time, else element by element.
+template <class T, int kRows, int kCols, bool kVec>
 struct Tile {
   typedef Kind<T> K;
   static constexpr int kUnits = kCols / K::kEl, kMine = kRows * kUnits / kThreads, kStride = kCols + K::kPad;
   static_assert(kMine * kThreads == kRows * kUnits, "every lane has as many units");
   uint4 u[kMine];
+  uint32_t off[kMine];
+  const T* base;              // of the head's columns
+  int64_t stride;
+  int c0, width, back;
 
-  __device__ __forceinline__ void load(const T* base, int64_t stride, int row0, int dir, int m, int c0, int width, int vec) {
+  __device__ __forceinline__ void start(const void* p, int64_t row_stride, int head, int columns, int from, int backward) {
+    base = static_cast<const T*>(p) + static_cast<int64_t>(head) * columns;
+    stride = row_stride, c0 = from, width = columns, back = backward;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
       const int at = threadIdx.x + kThreads * k, r = at / kUnits, c = c0 + at % kUnits * K::kEl;
-      u[k] = load_unit(base + static_cast<int64_t>(row0 + (r < m ? dir * r : 0)) * stride, c, width, r < m, vec);
+      const uint32_t line = static_cast<uint32_t>(back ? kRows - 1 - r : r) * static_cast<uint32_t>(stride);
+      off[k] = c < width ? (line + c) * static_cast<uint32_t>(sizeof(T)) : kNowhere;
+    }
+  }
+  // m rows from `row` on, or back.
+  __device__ __forceinline__ void load(int row, int m) {
+    const T* const p = base + static_cast<int64_t>(back ? row - (m - 1) : row) * stride;
+    const auto buffer = buffer_of(p, (static_cast<uint32_t>(m - 1) * static_cast<uint32_t>(stride) + width) * static_cast<uint32_t>(sizeof(T)));
+    const uint32_t less = back ? static_cast<uint32_t>(kRows - m) * static_cast<uint32_t>(stride) * static_cast<uint32_t>(sizeof(T)) : 0u;
+#pragma unroll
+    for (int k = 0; k < kMine; ++k) {
+      if constexpr (kVec) {
+        u[k] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(buffer, off[k] - less, 0, 0));
+      } else {
+        const int left = width - (c0 + static_cast<int>(threadIdx.x + kThreads * k) % kUnits * K::kEl);   // elements of the row
+        uint32_t w[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if constexpr (sizeof(T) == 4) {
+            w[i] = __builtin_amdgcn_raw_buffer_load_b32(buffer, i < left ? off[k] - less + 4 * i : kNowhere, 0, 0);
+          } else {
+            const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(buffer, 2 * i < left ? off[k] - less + 4 * i : kNowhere, 0, 0);
+            const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(buffer, 2 * i + 1 < left ? off[k] - less + 4 * i + 2 : kNowhere, 0, 0);
+            w[i] = (lo & 0xFFFFu) | hi << 16;
+          }
+        }
+        u[k] = make_uint4(w[0], w[1], w[2], w[3]);
+      }
     }
   }
   __device__ __forceinline__ uint32_t store(typename K::Word* lds) const {
@@ -246,7 +274,7 @@ __device__ __forceinline__ f4 across(const float* lds, int stride, int k, int co
 
 // kInner: columns of X and Y, filled up; kTiles: 16-column tiles of Z a wave.  kMap:
 // only what a piece adds to the state behind it.
-template <class T, int kInner, int kTiles, bool kMap>
+template <class T, int kInner, int kTiles, bool kMap, bool kVec>
 struct Walker {
   typedef Kind<T> K;
   typedef typename K::Word Word;
@@ -293,7 +321,7 @@ struct Walker {
   static __device__ __forceinline__ int outer_of(int wave, int n, int lane) { return (wave * kTiles + n) * 16 + (lane & 15); }
 
   __device__ __forceinline__ void read_state(const Walk& a, const float* p, int col0) {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int l = fresh(threadIdx.x), lane = l & 63, wave = l >> 6;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -307,7 +335,7 @@ struct Walker {
         }
   }
   __device__ __forceinline__ void write_state(const Walk& a, float* p, int col0) const {
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int l = fresh(threadIdx.x), lane = l & 63, wave = l >> 6;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -340,15 +368,12 @@ struct Walker {
   }
 
   // Rows lo .. hi - 1 of the arrays.
-  __device__ void part(const Walk& a, int lo, int hi, int head, int col0, Word* lds) {
+  __device__ __forceinline__ void part(const Walk& a, int lo, int hi, int head, int col0, Word* lds) {
     Word* const ly = lds;
     Word* const lz = ly + kC * kXs;
     Word* const lx = lz + kC * kZs;
     Word* const lp = lx + kC * kXs;
     uint32_t* const flags = reinterpret_cast<uint32_t*>(kMap ? lx : lp + kPWords);
-    const T* const x = static_cast<const T*>(a.x) + static_cast<int64_t>(head / a.x_share) * a.inner;
-    const T* const y = static_cast<const T*>(a.y) + static_cast<int64_t>(head / a.y_share) * a.inner;
-    const T* const z = static_cast<const T*>(a.z) + static_cast<int64_t>(head / a.z_share) * a.outer;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
     const int dir = a.back ? -1 : 1, n = hi - lo, row0 = a.back ? hi - 1 : lo;
 
@@ -368,14 +393,25 @@ struct Walker {
       }
     }
 
-    Tile<T, kC, kInner> tx, ty;
-    Tile<T, kC, kCols> tz;
+    Tile<T, kC, kInner, kVec> tx, ty;
+    Tile<T, kC, kCols, kVec> tz;
+    if constexpr (!kMap) tx.start(a.x, a.x_stride, head / a.x_share, a.inner, 0, a.back);
+    ty.start(a.y, a.y_stride, head / a.y_share, a.inner, 0, a.back);
+    tz.start(a.z, a.z_stride, head / a.z_share, a.outer, col0, a.back);
     const auto fetch = [&](int c) {
       const int m = min(kC, n - c), row = row0 + dir * c;
-      if constexpr (!kMap) tx.load(x, a.x_stride, row, dir, m, 0, a.inner, a.x_vec);
-      ty.load(y, a.y_stride, row, dir, m, 0, a.inner, a.y_vec);
-      tz.load(z, a.z_stride, row, dir, m, col0, a.outer, a.z_vec);
+      if constexpr (!kMap) tx.load(row, m);
+      ty.load(row, m);
+      tz.load(row, m);
     };
+    // out's rows, the same way
+    const uint32_t size = a.out_float ? 4 : sizeof(T), line = static_cast<uint32_t>(a.heads) * a.outer * size;
+    uint32_t out_off[kTiles];
+#pragma unroll
+    for (int k = 0; k < kTiles; ++k) {
+      const int col = col0 + (wave * kTiles + k) * 16 + 4 * g;
+      out_off[k] = col < a.outer ? (a.back ? kC - 1 - li : li) * line + col * size : kNowhere;
+    }
     fetch(0);
     for (int c = 0; c < n; c += kC) {
       const int m = min(kC, n - c), flag = (c / kC) & 1;
@@ -527,6 +563,8 @@ struct Walker {
 
       if constexpr (!kMap) {
         if (slow) {
+          const int l = fresh(threadIdx.x);
+          const int wave = l >> 6, g = (l & 63) >> 4, li = l & 15;
           for (int j = 0; j < m; ++j)
 #pragma unroll
             for (int k = 0; k < kTiles; ++k) {
@@ -552,39 +590,43 @@ struct Walker {
               }
             }
         }
+        unsigned char* const to = static_cast<unsigned char*>(a.out) +
+                                  static_cast<int64_t>(a.back ? row0 - c - (m - 1) : row0 + c) * line +
+                                  static_cast<int64_t>(head) * a.outer * size;
+        const auto buffer = buffer_of(to, (m - 1) * line + a.outer * size);
+        const uint32_t less = a.back ? (kC - m) * line : 0u;
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i) {
-          if (16 * i + li < m) {
-            const int64_t row = row0 + dir * (c + 16 * i + li);
-            const int64_t to = row * a.heads * a.outer + static_cast<int64_t>(head) * a.outer;
+        for (int i = 0; i < kRowTiles; ++i)
 #pragma unroll
-            for (int k = 0; k < kTiles; ++k) {
-              const int col = col0 + (wave * kTiles + k) * 16 + 4 * g;
-              if (a.out_vec) {
-                if (col < a.outer) {
-                  const float4 v = make_float4(o[i][k][0], o[i][k][1], o[i][k][2], o[i][k][3]);
-                  if (a.out_float) store_four(static_cast<float*>(a.out) + to + col, v);
-                  else store_four(static_cast<T*>(a.out) + to + col, v);
-                }
-              } else {
+          for (int k = 0; k < kTiles; ++k) {
+            const f4& v = o[i][k];
+            const uint32_t at = out_off[k] + (a.back ? -(16 * i * line) : 16 * i * line) - less;
+            const uint32_t pair[2] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+            const bool wide = sizeof(T) == 4 || a.out_float;
+            if constexpr (kVec) {
+              const uint32_t there = out_off[k] == kNowhere ? kNowhere : at;
+              if (wide) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), buffer, there, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b64(u2{pair[0], pair[1]}, buffer, there, 0, 0);
+            } else {
+              const int left = a.outer - (col0 + (wave * kTiles + k) * 16 + 4 * g);
 #pragma unroll
-                for (int e = 0; e < 4; ++e)
-                  if (col + e < a.outer) {
-                    if (a.out_float) static_cast<float*>(a.out)[to + col + e] = o[i][k][e];
-                    else store_value(static_cast<T*>(a.out) + to + col + e, o[i][k][e]);
-                  }
+              for (int e = 0; e < 4; ++e) {
+                if (wide) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), buffer, e < left ? at + 4 * e : kNowhere, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(static_cast<short>(pair[e / 2] >> (16 * (e & 1))), buffer, e < left ? at + 2 * e : kNowhere, 0, 0);
               }
             }
           }
-        }
       }
     }
   }
 };
 
-template <class T, int kInner, int kTiles, bool kMap>
-__global__ __launch_bounds__(kThreads) void k_la_walk(const Walk a) {
-  typedef Walker<T, kInner, kTiles, kMap> W;
+// Blocks that share a compute unit: what the state's registers leave room for.
+constexpr int blocks_of(int size, int inner, int tiles) { return inner * tiles >= 256 && (size == 2 || inner == 256) ? 1 : 2; }
+
+template <class T, int kInner, int kTiles, bool kMap, bool kVec>
+__global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kInner, kTiles)) void k_la_walk(const Walk a) {
+  typedef Walker<T, kInner, kTiles, kMap, kVec> W;
   __shared__ __align__(16) unsigned char memory[W::kLds];
   typename W::Word* const lds = reinterpret_cast<typename W::Word*>(memory);
   const int units = a.heads * a.slices;
@@ -605,28 +647,21 @@ __global__ __launch_bounds__(kThreads) void k_la_walk(const Walk a) {
     // what the piece adds to the state of the sequence that crosses its far border
     const int border = a.back ? p * a.piece : min((p + 1) * a.piece, a.rows);
     const int s = border > 0 && border < a.rows ? sequence_before(a, border) : -1;
-    int lo = 0, hi = 0, begins = -1;
+    int lo = 0, hi = 0;
     if (s >= 0 && first_row(a, s + 1) > border) {
       const int b = first_row(a, s), e = first_row(a, s + 1), far = min(p + 1 < a.pieces ? (p + 1) * a.piece : a.rows, a.rows);
       lo = a.back ? border : max(b, p * a.piece);
       hi = a.back ? min(e, far) : border;
-      if (a.back ? e <= far : b >= p * a.piece) begins = s;
     }
-    if (unit == 0 && threadIdx.x == 0) a.info[p] = make_int2(max(hi - lo, 0), begins);
     if (hi <= lo) return;
     w.zero();
     w.part(a, lo, hi, head, col0, lds);
     w.write_slot(a.slots + (static_cast<int64_t>(p) * units + unit) * W::kState);
-  } else if (!a.piece) {
-    const int b = first_row(a, p), e = first_row(a, p + 1);
-    const int64_t at = (static_cast<int64_t>(p) * a.heads + head) * state;
-    w.read_state(a, a.begin ? a.begin + at : nullptr, col0);
-    if (e > b) w.part(a, b, e, head, col0, lds);
-    if (a.end) w.write_state(a, a.end + at, col0);
   } else {
-    const bool last = p + 1 == a.pieces;
-    const int lo = p * a.piece, hi = last ? a.rows : lo + a.piece;
-    const int s0 = sequence_from(a, lo), s1 = last ? a.sequences - 1 : sequence_before(a, hi);
+    // one sequence, or those of a piece
+    const bool whole = !a.piece, last = whole || p + 1 == a.pieces;
+    const int lo = whole ? 0 : p * a.piece, hi = last ? a.rows : lo + a.piece;
+    const int s0 = whole ? p : sequence_from(a, lo), s1 = whole ? p : last ? a.sequences - 1 : sequence_before(a, hi);
     for (int i = s0; i <= s1; ++i) {
       const int s = a.back ? s1 - (i - s0) : i;
       const int b = first_row(a, s), e = max(first_row(a, s + 1), b);
@@ -642,44 +677,48 @@ __global__ __launch_bounds__(kThreads) void k_la_walk(const Walk a) {
   }
 }
 
-// From what every piece adds to the state with which the next is entered, in the
-// slot of the piece that is left.
+// From what every piece adds to the state with which the next is entered, in the slot
+// of the piece that is left: for every sequence, one after another over its pieces.
 template <class T, int kInner, int kTiles>
 __global__ __launch_bounds__(kThreads) void k_la_join(const Walk a) {
-  typedef Walker<T, kInner, kTiles, true> W;
-  const int units = a.heads * a.slices, per = W::kState / 4;
-  const int64_t id = static_cast<int64_t>(blockIdx.x) * kThreads + threadIdx.x;
-  const int unit = static_cast<int>(id / per), at = static_cast<int>(id % per);
-  if (unit >= units) return;
+  typedef Walker<T, kInner, kTiles, true, true> W;
+  constexpr int kPer = W::kState / 4, kAhead = 8;
+  const int units = a.heads * a.slices, blocks = (units * kPer + kThreads - 1) / kThreads;
+  const int s = blockIdx.x / blocks, id = static_cast<int>(blockIdx.x % blocks) * kThreads + static_cast<int>(threadIdx.x);
+  const int unit = id / kPer, at = id % kPer;
+  const int b = first_row(a, s), e = first_row(a, s + 1);
+  if (e <= b || unit >= units) return;
+  const int front = b / a.piece, back = (e - 1) / a.piece, count = back - front;
+  if (count == 0) return;
   const int head = unit / a.slices, slice = unit % a.slices;
-  const int lane = at & 63, wave = (at >> 6) & 3, tile = at / kThreads;
-  const int n = tile % kTiles, s = tile / kTiles % W::kSub, t = tile / kTiles / W::kSub;
-  const int c = slice * W::kCols + W::outer_of(wave, n, lane), d = W::inner_of(t, s, lane);
   float l = a.log_decay[head] * kL2e;
   l = l < -1e30f ? -1e30f : l;
   f4 state = {0, 0, 0, 0};
-  constexpr int kAhead = 8;
-  for (int k0 = 0; k0 < a.pieces; k0 += kAhead) {
+  if (a.begin) {
+    const int lane = at & 63, wave = (at >> 6) & 3, tile = at / kThreads;
+    const int n = tile % kTiles, sub = tile / kTiles % W::kSub, t = tile / kTiles / W::kSub;
+    const int c = slice * W::kCols + W::outer_of(wave, n, lane), d = W::inner_of(t, sub, lane);
+    const float* p = a.begin + (static_cast<int64_t>(s) * a.heads + head) * a.inner * a.outer;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (c < a.outer && d + i < a.inner) state[i] = p[(d + i) * a.row_stride + c * a.col_stride];
+  }
+  const auto slot = [&](int i) {
+    const int p = a.back ? back - i : front + i;
+    return reinterpret_cast<f4*>(a.slots + (static_cast<int64_t>(p) * units + unit) * W::kState + at * 4);
+  };
+  for (int i0 = 0; i0 < count; i0 += kAhead) {
     f4 add[kAhead];
-    int2 info[kAhead];
+#pragma unroll
+    for (int k = 0; k < kAhead; ++k)
+      if (i0 + k < count) add[k] = *slot(i0 + k);
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
-      const int i = k0 + k, p = a.back ? a.pieces - 1 - i : i;
-      info[k] = i < a.pieces ? a.info[p] : make_int2(0, -1);
-      if (info[k].x > 0) add[k] = *reinterpret_cast<const f4*>(a.slots + (static_cast<int64_t>(p) * units + unit) * W::kState + at * 4);
-    }
-#pragma unroll
-    for (int k = 0; k < kAhead; ++k) {
-      if (info[k].x <= 0) continue;
-      const int p = a.back ? a.pieces - 1 - (k0 + k) : k0 + k;
-      if (info[k].y >= 0) {
-        const float* b = a.begin ? a.begin + (static_cast<int64_t>(info[k].y) * a.heads + head) * a.inner * a.outer : nullptr;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          state[i] = b && c < a.outer && d + i < a.inner ? b[(d + i) * a.row_stride + c * a.col_stride] : 0.0f;
-      }
-      state = state * __builtin_amdgcn_exp2f(l * static_cast<float>(info[k].x)) + add[k];
-      *reinterpret_cast<f4*>(a.slots + (static_cast<int64_t>(p) * units + unit) * W::kState + at * 4) = state;
+      if (i0 + k >= count) break;
+      const int p = a.back ? back - (i0 + k) : front + i0 + k;
+      const int rows = min(e, (p + 1) * a.piece) - max(b, p * a.piece);
+      state = state * __builtin_amdgcn_exp2f(l * static_cast<float>(rows)) + add[k];
+      *slot(i0 + k) = state;
     }
   }
 }
@@ -774,7 +813,8 @@ __global__ __launch_bounds__(kThreads) void k_la_step(const Step a) {
 // Host
 
 constexpr int kMostPieces = 256;
-constexpr int kEnough = 1024;      // blocks that fill the card
+constexpr int kEnough = 512;       // blocks that fill the card
+constexpr int64_t kMostStride = 1 << 22;   // a chunk's offsets in a buffer stay below 2^31
 
 int check_shape(const soma_la_config* cfg) {
   if (!cfg) return set_error(SOMA_EINVAL, "cfg is NULL");
@@ -789,7 +829,7 @@ int check_shape(const soma_la_config* cfg) {
   if (c.value_width < 1 || c.value_width > 256) return set_error(SOMA_ESHAPE, "value_width %d is out of range", c.value_width);
   if (!std::isfinite(c.scale)) return set_error(SOMA_EINVAL, "scale must be finite");
   for (int64_t stride : {c.q_stride, c.k_stride, c.v_stride})
-    if (stride > (int64_t{1} << 32)) return set_error(SOMA_ESHAPE, "a row stride is out of range");
+    if (stride > kMostStride) return set_error(SOMA_ESHAPE, "a row stride is out of range");
   if (c.q_stride < static_cast<int64_t>(c.heads) * c.key_width || c.k_stride < static_cast<int64_t>(c.kv_heads) * c.key_width ||
       c.v_stride < static_cast<int64_t>(c.kv_heads) * c.value_width)
     return set_error(SOMA_ESHAPE, "a row stride is shorter than its row");
@@ -803,7 +843,7 @@ struct Shape {
 Shape shape_of(int inner, int outer) {
   Shape s;
   s.inner = inner <= 64 ? 64 : inner <= 128 ? 128 : 256;
-  s.tiles = outer <= 64 || s.inner == 256 ? 1 : 2;
+  s.tiles = outer <= 64 || s.inner >= 128 ? 1 : 2;
   s.slices = (outer + 64 * s.tiles - 1) / (64 * s.tiles);
   return s;
 }
@@ -813,14 +853,14 @@ Shape shape_of(int inner, int outer) {
 int most_pieces(const soma_la_config& c, const Shape& s) {
   const int64_t units = static_cast<int64_t>(c.heads) * s.slices;
   if (units * c.sequences >= kEnough || c.rows <= static_cast<int64_t>(c.sequences) * 256) return 0;
-  return static_cast<int>(std::min<int64_t>(kMostPieces, (2 * kEnough + units - 1) / units));
+  return static_cast<int>(std::min<int64_t>(kMostPieces, (kEnough + units - 1) / units));
 }
 
 size_t slots_size(const soma_la_config& c, int inner, int outer) {
   const Shape s = shape_of(inner, outer);
   const int most = most_pieces(c, s);
   if (!most) return 0;
-  return up256(sizeof(float) * most * c.heads * s.slices * s.inner * 64 * s.tiles) + up256(sizeof(int2) * most);
+  return up256(sizeof(float) * most * c.heads * s.slices * s.inner * 64 * s.tiles);
 }
 
 // A copy of the states that a walk begins with, where it ends with the same array and
@@ -854,17 +894,17 @@ size_t la_workspace(const soma_la_config& c, bool grad) {
 template <class T, int kInner, int kTiles>
 int walk_as(const Walk& a, hipStream_t st) {
   const int units = a.heads * a.slices, parts = a.piece ? a.pieces : a.sequences;
+  const dim3 grid(static_cast<unsigned>(units) * parts), block(kThreads);
   if (a.piece) {
-    if (int rc = launch("k_la_walk (maps)", k_la_walk<T, kInner, kTiles, true>, dim3(static_cast<unsigned>(units) * parts),
-                        dim3(kThreads), 0, st, a))
+    if (int rc = launch("k_la_walk (maps)", a.vec ? k_la_walk<T, kInner, kTiles, true, true> : k_la_walk<T, kInner, kTiles, true, false>,
+                        grid, block, 0, st, a))
       return rc;
-    const int64_t n = static_cast<int64_t>(units) * Walker<T, kInner, kTiles, true>::kState / 4;
-    if (int rc = launch("k_la_join", k_la_join<T, kInner, kTiles>, dim3(static_cast<unsigned>((n + kThreads - 1) / kThreads)),
-                        dim3(kThreads), 0, st, a))
+    const unsigned blocks = (units * (kInner * 64 * kTiles / 4) + kThreads - 1) / kThreads;
+    if (int rc = launch("k_la_join", k_la_join<T, kInner, kTiles>, dim3(blocks * a.sequences), block, 0, st, a))
       return rc;
   }
-  return launch("k_la_walk", k_la_walk<T, kInner, kTiles, false>, dim3(static_cast<unsigned>(units) * parts), dim3(kThreads), 0,
-                st, a);
+  return launch("k_la_walk", a.vec ? k_la_walk<T, kInner, kTiles, false, true> : k_la_walk<T, kInner, kTiles, false, false>, grid,
+                block, 0, st, a);
 }
 
 template <class T>
@@ -892,10 +932,9 @@ int walk(const soma_la_config& c, const Array& x, const Array& y, const Array& z
   a.x_stride = x.stride, a.y_stride = y.stride, a.z_stride = z.stride;
   a.x_share = x.share, a.y_share = y.share, a.z_share = z.share;
   a.inner = inner, a.outer = outer;
-  a.x_vec = vec(x, inner), a.y_vec = vec(y, inner), a.z_vec = vec(z, outer);
+  a.vec = vec(x, inner) && vec(y, inner) && vec(z, outer) && outer % 4 == 0 && is_aligned(out, out_float ? 16 : 4 * e);
   a.out = out;
   a.out_float = out_float;
-  a.out_vec = outer % 4 == 0 && is_aligned(out, out_float ? 16 : 4 * e);
   a.begin = begin, a.end = end, a.log_decay = log_decay;
   a.row_stride = transposed ? 1 : outer;
   a.col_stride = transposed ? inner : 1;
@@ -909,7 +948,6 @@ int walk(const soma_la_config& c, const Array& x, const Array& y, const Array& z
     a.piece = ((c.rows + most - 1) / most + 63) / 64 * 64;
     a.pieces = (c.rows + a.piece - 1) / a.piece;
     a.slots = reinterpret_cast<float*>(ws);
-    a.info = reinterpret_cast<int2*>(ws + up256(sizeof(float) * most * c.heads * s.slices * s.inner * 64 * s.tiles));
   }
   return c.type == SOMA_FLOAT ? walk_of<float>(a, s, st) : walk_of<bf16>(a, s, st);
 }

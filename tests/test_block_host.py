@@ -67,7 +67,8 @@ def step(lib, cfg, **kw):
     ("key_width", 0, soma.SOMA_ESHAPE), ("key_width", 257, soma.SOMA_ESHAPE), ("value_width", 0, soma.SOMA_ESHAPE),
     ("value_width", 257, soma.SOMA_ESHAPE), ("type", 2, soma.SOMA_EINVAL), ("type", -1, soma.SOMA_EINVAL),
     ("scale", float("nan"), soma.SOMA_EINVAL), ("scale", float("inf"), soma.SOMA_EINVAL), ("q_stride", 63, soma.SOMA_ESHAPE),
-    ("k_stride", 31, soma.SOMA_ESHAPE), ("v_stride", 47, soma.SOMA_ESHAPE), ("q_stride", 2**33, soma.SOMA_ESHAPE)])
+    ("k_stride", 31, soma.SOMA_ESHAPE), ("v_stride", 47, soma.SOMA_ESHAPE), ("q_stride", 2**33, soma.SOMA_ESHAPE),
+    ("v_stride", 2**22 + 1, soma.SOMA_ESHAPE)])
 def test_linear_attention_shapes(lib, field, value, code):
     c, out = la_cfg(**{field: value}), ctypes.c_size_t()
     assert lib.soma_la_workspace_size(c, 1, ctypes.byref(out)) == code
