@@ -874,8 +874,8 @@ int soma_norm_backward(const soma_norm_config* cfg, const void* total_dev, const
  * of which less than top_p of their weight lies (the first one always); min_p keeps
  * w >= min_p.  The token is the first, by index, of those left up to which more than u
  * of their weight lies.  Weights are formed in fp64 and summed as multiples of 2^-s,
- * s = 62 - ceil(log2 vocab) (50,257: 2^-46), in whatever order the same: a token whose
- * weight is below half of that is never drawn.
+ * rounded down, s = 62 - ceil(log2 vocab) (50,257: 2^-46), in whatever order the same:
+ * a token whose weight is below that is never drawn.
  *   tokens  [rows] int32; -1 where every logit is -infinity or NaN.
  *   logprob [rows] fp32, log of the token's share in what was left (-1: -infinity);
  *           NULL: not wanted.

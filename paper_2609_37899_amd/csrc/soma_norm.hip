@@ -365,8 +365,16 @@ __global__ __launch_bounds__(1024) void k_norm_gain(const float* partial, int bl
   __shared__ float sums[16][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
   float x = 0.0f;
-  if (c < width)
-    for (int b = w; b < blocks; b += 16) x += partial[static_cast<int64_t>(b) * width + c];
+  if (c < width) {
+    // sixteen on their way at once
+    for (int b0 = w; b0 < blocks; b0 += 256) {
+      float p[16];
+#pragma unroll
+      for (int k = 0; k < 16; ++k) p[k] = b0 + 16 * k < blocks ? partial[static_cast<int64_t>(b0 + 16 * k) * width + c] : 0.0f;
+#pragma unroll
+      for (int k = 0; k < 16; ++k) x += p[k];
+    }
+  }
   sums[w][threadIdx.x & 63] = x;
   __syncthreads();
   if (w == 0 && c < width) {
