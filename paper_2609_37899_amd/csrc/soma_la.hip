@@ -102,7 +102,7 @@ struct Walk {
   int64_t x_stride, y_stride, z_stride;     // elements between rows
   int x_share, y_share, z_share;            // heads that share one of x's, y's or z's
   int inner, outer;                         // columns of a head of x and y; of z and out
-  int vec;                                  // every array aligned: through buffers
+  int whole;                                // both widths are whole units of 16 bytes
   void* out;                                // [rows][heads outer] of T, or fp32
   int out_float;
   const float *begin, *log_decay;           // states [sequences][heads][..], or NULL: zeros
@@ -189,13 +189,15 @@ constexpr uint32_t kNowhere = 0xFFFFFFFFu;
 // Rows of one array on their way to LDS: kRows x kCols, kThreads lanes side by side.
 // They come through a buffer that ends with the chunk's last row: row r lies at r
 // strides (walking back, at kRows - 1 - r less the rows that the chunk is short of,
-// which wraps for those), and what is not there lies behind the end.  kVec: 16 bytes
-// at a time, else element by element.
-template <class T, int kRows, int kCols, bool kVec>
+// which wraps for those), and what is not there lies behind the end.  Loads of 16 bytes
+// take any element's alignment.  A row's last unit may reach into what follows, which
+// becomes 0, and a buffer ends in whole words: the last of an odd number of bf16 comes
+// by itself.
+template <class T, int kRows, int kCols, bool kWhole>
 struct Tile {
   typedef Kind<T> K;
   static constexpr int kUnits = kCols / K::kEl, kMine = kRows * kUnits / kThreads, kStride = kCols + K::kPad;
-  static_assert(kMine * kThreads == kRows * kUnits, "every lane has as many units");
+  static_assert(kMine * kThreads == kRows * kUnits && kThreads % kUnits == 0, "every lane has as many units, of the same columns");
   uint4 u[kMine];
   uint32_t off[kMine];
   const T* base;              // of the head's columns
@@ -218,22 +220,18 @@ struct Tile {
     const auto buffer = buffer_of(p, (static_cast<uint32_t>(m - 1) * static_cast<uint32_t>(stride) + width) * static_cast<uint32_t>(sizeof(T)));
     const uint32_t less = back ? static_cast<uint32_t>(kRows - m) * static_cast<uint32_t>(stride) * static_cast<uint32_t>(sizeof(T)) : 0u;
 #pragma unroll
-    for (int k = 0; k < kMine; ++k) {
-      if constexpr (kVec) {
-        u[k] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(buffer, off[k] - less, 0, 0));
-      } else {
-        const int left = width - (c0 + static_cast<int>(threadIdx.x + kThreads * k) % kUnits * K::kEl);   // elements of the row
-        uint32_t w[4];
+    for (int k = 0; k < kMine; ++k) u[k] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(buffer, off[k] - less, 0, 0));
+    const int left = width % K::kEl;        // elements of a row's last unit, where it is not full
+    if (!kWhole && left) {
+      const int at = width - left - c0, words = left * static_cast<int>(sizeof(T)) / 4;
+      const bool mine = static_cast<int>(threadIdx.x) % kUnits * K::kEl == at;     // (of every unit of a lane: kThreads is a multiple)
 #pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if constexpr (sizeof(T) == 4) {
-            w[i] = __builtin_amdgcn_raw_buffer_load_b32(buffer, i < left ? off[k] - less + 4 * i : kNowhere, 0, 0);
-          } else {
-            const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(buffer, 2 * i < left ? off[k] - less + 4 * i : kNowhere, 0, 0);
-            const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(buffer, 2 * i + 1 < left ? off[k] - less + 4 * i + 2 : kNowhere, 0, 0);
-            w[i] = (lo & 0xFFFFu) | hi << 16;
-          }
-        }
+      for (int k = 0; k < kMine; ++k) {
+        uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, last = 0;
+        if (sizeof(T) == 2 && left % 2) last = __builtin_amdgcn_raw_buffer_load_b16(buffer, mine ? off[k] - less + 2 * (left - 1) : kNowhere, 0, 0) & 0xFFFF;
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (i >= words && mine) w[i] = i == words ? last : 0;
         u[k] = make_uint4(w[0], w[1], w[2], w[3]);
       }
     }
@@ -274,7 +272,7 @@ __device__ __forceinline__ f4 across(const float* lds, int stride, int k, int co
 
 // kInner: columns of X and Y, filled up; kTiles: 16-column tiles of Z a wave.  kMap:
 // only what a piece adds to the state behind it.
-template <class T, int kInner, int kTiles, bool kMap, bool kVec>
+template <class T, int kInner, int kTiles, bool kMap, bool kWhole>
 struct Walker {
   typedef Kind<T> K;
   typedef typename K::Word Word;
@@ -378,7 +376,7 @@ struct Walker {
     const int dir = a.back ? -1 : 1, n = hi - lo, row0 = a.back ? hi - 1 : lo;
     // fp32 widths that nobody rounded: no products of columns that are filled up, which
     // the fp32 MFMA's rate makes worth the branches (45 x 77: walks 88 -> 68 us)
-    constexpr bool kSkip = !kVec && sizeof(T) == 4 && kInner < 256;
+    constexpr bool kSkip = !kWhole && sizeof(T) == 4 && kInner < 256;
     const int own_wave = __builtin_amdgcn_readfirstlane(wave);
     const auto step_out = [&](int t) { return kSkip && t * K::kKw >= a.inner; };
     const auto tile_out = [&](int k) { return kSkip && col0 + (k * 4 + own_wave) * 16 >= a.outer; };
@@ -399,8 +397,8 @@ struct Walker {
       }
     }
 
-    Tile<T, kC, kInner, kVec> tx, ty;
-    Tile<T, kC, kCols, kVec> tz;
+    Tile<T, kC, kInner, kWhole> tx, ty;
+    Tile<T, kC, kCols, kWhole> tz;
     if constexpr (!kMap) tx.start(a.x, a.x_stride, head / a.x_share, a.inner, 0, a.back);
     ty.start(a.y, a.y_stride, head / a.y_share, a.inner, 0, a.back);
     tz.start(a.z, a.z_stride, head / a.z_share, a.outer, col0, a.back);
@@ -617,16 +615,16 @@ struct Walker {
             const uint32_t at = out_off[k] + (a.back ? -(16 * i * line) : 16 * i * line) - less;
             const uint32_t pair[2] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
             const bool wide = sizeof(T) == 4 || a.out_float;
-            if constexpr (kVec) {
-              const uint32_t there = out_off[k] == kNowhere ? kNowhere : at;
-              if (wide) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), buffer, there, 0, 0);
-              else __builtin_amdgcn_raw_buffer_store_b64(u2{pair[0], pair[1]}, buffer, there, 0, 0);
-            } else {
-              const int left = a.outer - (col0 + (k * 4 + wave) * 16 + 4 * g);
+            const int left = a.outer - (col0 + (k * 4 + wave) * 16 + 4 * g);
+            const uint32_t there = left >= 4 ? at : kNowhere;
+            if (wide) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), buffer, there, 0, 0);
+            else __builtin_amdgcn_raw_buffer_store_b64(u2{pair[0], pair[1]}, buffer, there, 0, 0);
+            if (!kWhole && a.outer % 4) {
+              const bool some = left > 0 && left < 4;
 #pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                if (wide) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), buffer, e < left ? at + 4 * e : kNowhere, 0, 0);
-                else __builtin_amdgcn_raw_buffer_store_b16(static_cast<short>(pair[e / 2] >> (16 * (e & 1))), buffer, e < left ? at + 2 * e : kNowhere, 0, 0);
+              for (int e = 0; e < 3; ++e) {
+                if (wide) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), buffer, some && e < left ? at + 4 * e : kNowhere, 0, 0);
+                else __builtin_amdgcn_raw_buffer_store_b16(static_cast<short>(pair[e / 2] >> (16 * (e & 1))), buffer, some && e < left ? at + 2 * e : kNowhere, 0, 0);
               }
             }
           }
@@ -638,9 +636,9 @@ struct Walker {
 // Blocks that share a compute unit: what the state's registers leave room for.
 constexpr int blocks_of(int inner) { return inner == 256 ? 1 : 2; }
 
-template <class T, int kInner, int kTiles, bool kMap, bool kVec>
+template <class T, int kInner, int kTiles, bool kMap, bool kWhole>
 __global__ __launch_bounds__(kThreads, blocks_of(kInner)) void k_la_walk(const Walk a) {
-  typedef Walker<T, kInner, kTiles, kMap, kVec> W;
+  typedef Walker<T, kInner, kTiles, kMap, kWhole> W;
   __shared__ __align__(16) unsigned char memory[W::kLds];
   typename W::Word* const lds = reinterpret_cast<typename W::Word*>(memory);
   const int units = a.heads * a.slices;
@@ -868,7 +866,8 @@ Shape shape_of(int inner, int outer) {
 // Their number goes by the heads alone, so that a workspace serves fewer rows too.
 int most_pieces(const soma_la_config& c, const Shape& s) {
   const int64_t units = static_cast<int64_t>(c.heads) * s.slices;
-  if (units * c.sequences >= kEnough || c.rows <= static_cast<int64_t>(c.sequences) * 256) return 0;
+  const int few = c.type == SOMA_FLOAT ? 4 * Kind<float>::kC : 4 * Kind<bf16>::kC;
+  if (units * c.sequences >= kEnough || c.rows <= static_cast<int64_t>(c.sequences) * few) return 0;
   return static_cast<int>(std::min<int64_t>(kMostPieces, (kEnough + units - 1) / units));
 }
 
@@ -912,14 +911,14 @@ int walk_as(const Walk& a, hipStream_t st) {
   const int units = a.heads * a.slices, parts = a.piece ? a.pieces : a.sequences;
   const dim3 grid(static_cast<unsigned>(units) * parts), block(kThreads);
   if (a.piece) {
-    if (int rc = launch("k_la_walk (maps)", a.vec ? k_la_walk<T, kInner, kTiles, true, true> : k_la_walk<T, kInner, kTiles, true, false>,
+    if (int rc = launch("k_la_walk (maps)", a.whole ? k_la_walk<T, kInner, kTiles, true, true> : k_la_walk<T, kInner, kTiles, true, false>,
                         grid, block, 0, st, a))
       return rc;
     const unsigned blocks = (units * (kInner * 64 * kTiles / 4) + kThreads - 1) / kThreads;
     if (int rc = launch("k_la_join", k_la_join<T, kInner, kTiles>, dim3(blocks * a.sequences), block, 0, st, a))
       return rc;
   }
-  return launch("k_la_walk", a.vec ? k_la_walk<T, kInner, kTiles, false, true> : k_la_walk<T, kInner, kTiles, false, false>, grid,
+  return launch("k_la_walk", a.whole ? k_la_walk<T, kInner, kTiles, false, true> : k_la_walk<T, kInner, kTiles, false, false>, grid,
                 block, 0, st, a);
 }
 
@@ -941,14 +940,12 @@ int walk(const soma_la_config& c, const Array& x, const Array& y, const Array& z
          const float* log_decay, const int32_t* offsets, const float* begin, float* end, bool transposed, void* out,
          bool out_float, unsigned char* ws, hipStream_t st) {
   const Shape s = shape_of(inner, outer);
-  const int64_t e = static_cast<int64_t>(type_size(c.type));
-  const auto vec = [&](const Array& a, int width) { return is_aligned(a.p, 16) && a.stride * e % 16 == 0 && width * e % 16 == 0; };
   Walk a{};
   a.x = x.p, a.y = y.p, a.z = z.p;
   a.x_stride = x.stride, a.y_stride = y.stride, a.z_stride = z.stride;
   a.x_share = x.share, a.y_share = y.share, a.z_share = z.share;
   a.inner = inner, a.outer = outer;
-  a.vec = vec(x, inner) && vec(y, inner) && vec(z, outer) && outer % 4 == 0 && is_aligned(out, out_float ? 16 : 4 * e);
+  a.whole = inner * type_size(c.type) % 16 == 0 && outer * type_size(c.type) % 16 == 0;
   a.out = out;
   a.out_float = out_float;
   a.begin = begin, a.end = end, a.log_decay = log_decay;

@@ -87,7 +87,7 @@ def test_linear_attention_arguments(lib):
         need.append(out.value)
     assert 0 < need[0] < need[1]
     # blocks enough, or rows too few for pieces: no workspace
-    for kw in (dict(sequences=500), dict(rows=512)):
+    for kw in (dict(sequences=500), dict(rows=512, type=1), dict(rows=256)):
         assert lib.soma_la_workspace_size(la_cfg(**kw), 0, ctypes.byref(out)) == soma.SOMA_OK and out.value == 0
     for call, names in ((forward, ("q", "k", "v", "log_decay", "o")), (backward, ("q", "k", "v", "log_decay", "do", "dq", "dk", "dv"))):
         for name in names:
