@@ -66,7 +66,7 @@ __device__ __forceinline__ V wave_before(V v, V* all) {
 }
 
 constexpr int kIndexBits = 20;              // of a vocabulary
-constexpr int kHeld = 110 * 1024;           // bytes of a row that LDS holds
+constexpr size_t kLds = 160 * 1024;         // of a compute unit: more than that must not be asked for
 
 // kBins bins; kInLds: the row is held in LDS.
 template <class T, int kThreads, int kBins, bool kInLds>
@@ -588,13 +588,22 @@ __global__ __launch_bounds__(kFew) void k_sample_few(const Sample a) {
   }
 }
 
+// The instance that holds a row in LDS beside what it shares, if there is room.
+template <class T, int kThreads, int kBins>
+int sample_held(const Sample& a, int rows, hipStream_t st, bool* fits) {
+  // from the 16 bytes that it begins in, in whole groups of eight
+  const size_t lds = (static_cast<size_t>(a.vocab) + (16 / sizeof(T) - 1) + 7) / 8 * 8 * sizeof(T);
+  *fits = sizeof(typename Row<T, kThreads, kBins, true>::Shared) + lds <= kLds;
+  if (!*fits) return SOMA_OK;
+  return launch("k_sample", k_sample<T, kThreads, kBins, true>, dim3(rows), dim3(kThreads), static_cast<unsigned>(lds), st, a);
+}
+
 template <class T>
 int sample_as(const Sample& a, int rows, hipStream_t st) {
-  const size_t bytes = (static_cast<size_t>(a.vocab) + 16 / sizeof(T)) * sizeof(T);
-  const unsigned lds = static_cast<unsigned>((bytes + 15) / 16 * 16);
   if (a.vocab <= kFew) return launch("k_sample_few", k_sample_few<T>, dim3(rows), dim3(kFew), 0, st, a);
-  if (a.vocab <= 4096) return launch("k_sample", k_sample<T, 256, 512, true>, dim3(rows), dim3(256), lds, st, a);
-  if (bytes <= kHeld) return launch("k_sample", k_sample<T, 1024, 2048, true>, dim3(rows), dim3(1024), lds, st, a);
+  bool fits = false;
+  const int rc = a.vocab <= 4096 ? sample_held<T, 256, 512>(a, rows, st, &fits) : sample_held<T, 1024, 2048>(a, rows, st, &fits);
+  if (fits) return rc;
   return launch("k_sample", k_sample<T, 1024, 2048, false>, dim3(rows), dim3(1024), 0, st, a);
 }
 

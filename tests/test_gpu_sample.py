@@ -65,7 +65,7 @@ def test_matches_reference(dtype, vocab, filters):
 
 
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
-@pytest.mark.parametrize("vocab", [100, 5000])
+@pytest.mark.parametrize("vocab", [100, 256, 257, 1000, 5000])
 def test_equal_logits(dtype, vocab):
     """Ties go to the lowest index: rows of one value, of two, and of small whole numbers."""
     torch = require_gpu()
@@ -129,6 +129,30 @@ def test_strides_and_alignment(dtype, pad, shift):
     for kw in ({}, {"top_k": np.full(20, 50), "top_p": np.full(20, 0.8)}):
         a, b = draw(torch, logits, u, **kw), draw(torch, view, u, **kw)
         assert np.array_equal(a[0], b[0]) and np.array_equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bfloat16", 56175), ("bfloat16", 70001), ("float32", 28090), ("float32", 131072)])
+def test_rows_too_long_for_lds(dtype, vocab):
+    """Both sides of the length that a row is held up to, and beyond; rows of any alignment."""
+    torch = require_gpu()
+    logits, u, g = make(torch, 6, vocab, dtype, seed=14)
+    for V in (vocab, vocab - 11):
+        kw = {"temperature": g.uniform(0.5, 1.5, 6), "top_k": np.exp(g.uniform(0, np.log(V), 6)).astype(np.int32)}
+        check(torch, logits[:, :V], u, **kw)
+        check(torch, logits[:, vocab - V:], u, top_p=g.uniform(0.3, 1.0, 6), **kw)
+        check(torch, logits[:, :V], u, most_near=1)
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("spread", [1e-3, 0.05, 100.0])
+def test_narrow_and_wide_logits(dtype, spread):
+    """Bins of many equal logits, and logits so far apart that few count."""
+    torch = require_gpu()
+    logits, u, g = make(torch, 8, 20000, dtype, seed=15, spread=spread)
+    logits[::2, 5] = 60.0                    # one far above the rest
+    for kw in ({"top_k": np.array([1, 2, 17, 500, 3000, 9000, 19999, 20000])}, {"top_p": g.uniform(0.2, 1.0, 8)},
+               {"top_k": np.full(8, 4000), "top_p": np.full(8, 0.7), "temperature": np.full(8, 1.7)}):
+        check(torch, logits, u, **kw)
 
 
 def test_shares():
