@@ -36,6 +36,8 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
+#include <type_traits>
 
 #include "soma.h"
 #include "soma_host.hpp"
@@ -116,6 +118,15 @@ struct Walk {
   float* slots;                             // [pieces][heads][slices][a block's state]
 };
 
+// Walks of one launch, of equal widths (as instances go), rows and direction's pieces.
+// Those of a head and part lie side by side on one XCD, whose L2 then gives the second
+// and third what they share.
+constexpr int kMostWalks = 3, kXcds = 8;
+struct Walks {
+  Walk walk[kMostWalks];
+  int count, parts;                         // sequences or pieces
+};
+
 __device__ __forceinline__ int first_row(const Walk& a, int s) {
   if (!a.offsets) return s * a.length;
   const int b = a.offsets[s];
@@ -184,7 +195,8 @@ typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t buffer_of(const void* p, uint32_t bytes) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, static_cast<int>(bytes), 0x00020000);
 }
-constexpr uint32_t kNowhere = 0xFFFFFFFFu;
+// (16 bytes from here on do not wrap, nor less the 2^30 that a chunk is short of)
+constexpr uint32_t kNowhere = 0xC0000000u;
 
 // Rows of one array on their way to LDS: kRows x kCols, kThreads lanes side by side.
 // They come through a buffer that ends with the chunk's last row: row r lies at r
@@ -200,31 +212,35 @@ struct Tile {
   static_assert(kMine * kThreads == kRows * kUnits && kThreads % kUnits == 0, "every lane has as many units, of the same columns");
   uint4 u[kMine];
   uint32_t off[kMine];
-  const T* base;              // of the head's columns
-  int64_t stride;
+  uint64_t at;                // of the chunk's first row in memory, if it were full
+  uint32_t line, bytes;       // between rows; of a full chunk
   int c0, width, back;
 
-  __device__ __forceinline__ void start(const void* p, int64_t row_stride, int head, int columns, int from, int backward) {
-    base = static_cast<const T*>(p) + static_cast<int64_t>(head) * columns;
-    stride = row_stride, c0 = from, width = columns, back = backward;
+  // `row`: the first one walked over
+  __device__ __forceinline__ void start(const void* p, int64_t stride, int head, int columns, int from, int backward, int row) {
+    c0 = from, width = columns, back = backward;
+    line = static_cast<uint32_t>(stride) * static_cast<uint32_t>(sizeof(T));
+    bytes = (kRows - 1) * line + width * static_cast<uint32_t>(sizeof(T));
+    at = reinterpret_cast<uint64_t>(static_cast<const T*>(p) + static_cast<int64_t>(head) * columns) +
+         static_cast<int64_t>(back ? row - (kRows - 1) : row) * line;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) {
-      const int at = threadIdx.x + kThreads * k, r = at / kUnits, c = c0 + at % kUnits * K::kEl;
-      const uint32_t line = static_cast<uint32_t>(back ? kRows - 1 - r : r) * static_cast<uint32_t>(stride);
-      off[k] = c < width ? (line + c) * static_cast<uint32_t>(sizeof(T)) : kNowhere;
+      const int i = threadIdx.x + kThreads * k, r = i / kUnits, c = c0 + i % kUnits * K::kEl;
+      off[k] = c < width ? static_cast<uint32_t>(back ? kRows - 1 - r : r) * line + c * static_cast<uint32_t>(sizeof(T)) : kNowhere;
     }
   }
-  // m rows from `row` on, or back.
-  __device__ __forceinline__ void load(int row, int m) {
-    const T* const p = base + static_cast<int64_t>(back ? row - (m - 1) : row) * stride;
-    const auto buffer = buffer_of(p, (static_cast<uint32_t>(m - 1) * static_cast<uint32_t>(stride) + width) * static_cast<uint32_t>(sizeof(T)));
-    const uint32_t less = back ? static_cast<uint32_t>(kRows - m) * static_cast<uint32_t>(stride) * static_cast<uint32_t>(sizeof(T)) : 0u;
+  // The next m rows.
+  __device__ __forceinline__ void load(int m) {
+    const uint32_t few = static_cast<uint32_t>(kRows - m) * line, less = back ? few : 0u;
+    const auto buffer = buffer_of(reinterpret_cast<const void*>(at + less), bytes - few);
+    const int step = static_cast<int>(kRows * line);
+    at += back ? -step : step;
 #pragma unroll
     for (int k = 0; k < kMine; ++k) u[k] = __builtin_bit_cast(uint4, __builtin_amdgcn_raw_buffer_load_b128(buffer, off[k] - less, 0, 0));
     const int left = width % K::kEl;        // elements of a row's last unit, where it is not full
     if (!kWhole && left) {
-      const int at = width - left - c0, words = left * static_cast<int>(sizeof(T)) / 4;
-      const bool mine = static_cast<int>(threadIdx.x) % kUnits * K::kEl == at;     // (of every unit of a lane: kThreads is a multiple)
+      const int from = width - left - c0, words = left * static_cast<int>(sizeof(T)) / 4;
+      const bool mine = static_cast<int>(threadIdx.x) % kUnits * K::kEl == from;   // (of every unit of a lane: kThreads is a multiple)
 #pragma unroll
       for (int k = 0; k < kMine; ++k) {
         uint32_t w[4] = {u[k].x, u[k].y, u[k].z, u[k].w}, last = 0;
@@ -349,20 +365,22 @@ struct Walker {
   // A slot holds the registers as they lie.
   static __device__ __forceinline__ int in_slot(int t, int s, int n) { return (((t * kSub + s) * kTiles + n) * kThreads) * 4; }
   __device__ __forceinline__ void read_slot(const float* p) {
+    const int at = fresh(threadIdx.x) * 4;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) r[t][s][n] = *reinterpret_cast<const f4*>(p + in_slot(t, s, n) + threadIdx.x * 4);
+        for (int n = 0; n < kTiles; ++n) r[t][s][n] = *reinterpret_cast<const f4*>(p + in_slot(t, s, n) + at);
   }
   __device__ __forceinline__ void write_slot(float* p) const {
+    const int at = fresh(threadIdx.x) * 4;
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
-        for (int n = 0; n < kTiles; ++n) *reinterpret_cast<f4*>(p + in_slot(t, s, n) + threadIdx.x * 4) = r[t][s][n];
+        for (int n = 0; n < kTiles; ++n) *reinterpret_cast<f4*>(p + in_slot(t, s, n) + at) = r[t][s][n];
   }
 
   // Rows lo .. hi - 1 of the arrays.
@@ -373,7 +391,7 @@ struct Walker {
     Word* const lp = lx + kC * kXs;
     uint32_t* const flags = reinterpret_cast<uint32_t*>(kMap ? lx : lp + kPWords);
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, li = lane & 15;
-    const int dir = a.back ? -1 : 1, n = hi - lo, row0 = a.back ? hi - 1 : lo;
+    const int n = hi - lo, row0 = a.back ? hi - 1 : lo;
     // fp32 widths that nobody rounded: no products of columns that are filled up, which
     // the fp32 MFMA's rate makes worth the branches (45 x 77: walks 88 -> 68 us)
     constexpr bool kSkip = !kWhole && sizeof(T) == 4 && kInner < 256;
@@ -399,14 +417,14 @@ struct Walker {
 
     Tile<T, kC, kInner, kWhole> tx, ty;
     Tile<T, kC, kCols, kWhole> tz;
-    if constexpr (!kMap) tx.start(a.x, a.x_stride, head / a.x_share, a.inner, 0, a.back);
-    ty.start(a.y, a.y_stride, head / a.y_share, a.inner, 0, a.back);
-    tz.start(a.z, a.z_stride, head / a.z_share, a.outer, col0, a.back);
+    if constexpr (!kMap) tx.start(a.x, a.x_stride, head / a.x_share, a.inner, 0, a.back, row0);
+    ty.start(a.y, a.y_stride, head / a.y_share, a.inner, 0, a.back, row0);
+    tz.start(a.z, a.z_stride, head / a.z_share, a.outer, col0, a.back, row0);
     const auto fetch = [&](int c) {
-      const int m = min(kC, n - c), row = row0 + dir * c;
-      if constexpr (!kMap) tx.load(row, m);
-      ty.load(row, m);
-      tz.load(row, m);
+      const int m = min(kC, n - c);
+      if constexpr (!kMap) tx.load(m);
+      ty.load(m);
+      tz.load(m);
     };
     // out's rows, the same way
     const uint32_t size = a.out_float ? 4 : sizeof(T), line = static_cast<uint32_t>(a.heads) * a.outer * size;
@@ -416,16 +434,20 @@ struct Walker {
       const int col = col0 + (k * 4 + wave) * 16 + 4 * g;
       out_off[k] = col < a.outer ? (a.back ? kC - 1 - li : li) * line + col * size : kNowhere;
     }
-    fetch(0);
-    for (int c = 0; c < n; c += kC) {
-      const int m = min(kC, n - c), flag = (c / kC) & 1;
-      __syncthreads();  // the tiles in front have been read
+    const auto place = [&](int flag) {
       if constexpr (!kMap) tx.store(lx);
       ty.store(ly);
       const uint32_t bad = tz.store(lz);
       if constexpr (!kMap)
         if (bad) flags[flag] = 1;
-      __syncthreads();
+    };
+    uint64_t out_at = reinterpret_cast<uint64_t>(a.out) + static_cast<int64_t>(a.back ? row0 - (kC - 1) : row0) * line +
+                      static_cast<int64_t>(head) * a.outer * size;
+    fetch(0);
+    place(0);
+    __syncthreads();
+    for (int c = 0; c < n; c += kC) {
+      const int m = min(kC, n - c), flag = (c / kC) & 1;
       if (c + kC < n) fetch(c + kC);
       if (in_for != m) weights(a, m);
       bool slow = false;
@@ -434,7 +456,7 @@ struct Walker {
         // P, tiles 0 .. below and on the diagonal in the order of their rows
 #pragma unroll
         for (int k = 0; k < (kRowTiles * (kRowTiles + 1) / 2 + 3) / 4; ++k) {
-          const int t = wave + 4 * k;
+          const int t = own_wave + 4 * k;
           const int ti = t >= 6 ? 3 : t >= 3 ? 2 : t >= 1 ? 1 : 0, tj = t - ti * (ti + 1) / 2;
           if (tj > ti || ti >= kRowTiles || 16 * ti >= m) break;
           f4 p = {0, 0, 0, 0};
@@ -442,8 +464,9 @@ struct Walker {
           for (int s = 0; s < kSteps; ++s)
             if (!step_out(s)) p = mfma(along<T>(ly, kXs, 16 * tj, s * K::kKw), along<T>(lx, kXs, 16 * ti, s * K::kKw), p);
           if (ti == tj) {
+            const int below_at = fresh(li - 4 * g);
 #pragma unroll
-            for (int i = 0; i < 4; ++i) p[i] = li >= 4 * g + i ? p[i] * at[i] : 0.0f;
+            for (int i = 0; i < 4; ++i) p[i] = below_at >= i ? p[i] * at[i] : 0.0f;
           } else {
             const float w = ti - tj == 1 ? far[1] : ti - tj == 2 ? far[kRowTiles > 2 ? 2 : 1] : far[kRowTiles - 1];
 #pragma unroll
@@ -602,47 +625,65 @@ struct Walker {
               }
             }
         }
-        unsigned char* const to = static_cast<unsigned char*>(a.out) +
-                                  static_cast<int64_t>(a.back ? row0 - c - (m - 1) : row0 + c) * line +
-                                  static_cast<int64_t>(head) * a.outer * size;
-        const auto buffer = buffer_of(to, (m - 1) * line + a.outer * size);
-        const uint32_t less = a.back ? (kC - m) * line : 0u;
+      }
+      __syncthreads();  // the tiles have been read
+      // (the next ones in front of this chunk's stores: a wait for loads is one for what
+      // was stored before them)
+      if (c + kC < n) place(flag ^ 1);
+      if constexpr (!kMap) {
+        const uint32_t few = static_cast<uint32_t>(kC - m) * line, less = a.back ? few : 0u;
+        const auto buffer = buffer_of(reinterpret_cast<const void*>(out_at + less), (kC - 1) * line + a.outer * size - few);
+        const int step = static_cast<int>(kC * line);
+        out_at += a.back ? -step : step;
+        const bool ragged = !kWhole && a.outer % 4;
+        const auto put = [&](auto wide) {
 #pragma unroll
-        for (int i = 0; i < kRowTiles; ++i)
+          for (int i = 0; i < kRowTiles; ++i)
 #pragma unroll
-          for (int k = 0; k < kTiles; ++k) {
-            const f4& v = o[i][k];
-            const uint32_t at = out_off[k] + (a.back ? -(16 * i * line) : 16 * i * line) - less;
-            const uint32_t pair[2] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
-            const bool wide = sizeof(T) == 4 || a.out_float;
-            const int left = a.outer - (col0 + (k * 4 + wave) * 16 + 4 * g);
-            const uint32_t there = left >= 4 ? at : kNowhere;
-            if (wide) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), buffer, there, 0, 0);
-            else __builtin_amdgcn_raw_buffer_store_b64(u2{pair[0], pair[1]}, buffer, there, 0, 0);
-            if (!kWhole && a.outer % 4) {
-              const bool some = left > 0 && left < 4;
+            for (int k = 0; k < kTiles; ++k) {
+              const f4& v = o[i][k];
+              const uint32_t at = out_off[k] + (a.back ? -(16 * i * line) : 16 * i * line) - less;
+              const uint32_t pair[2] = {bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+              const int left = a.outer - (col0 + (k * 4 + wave) * 16 + 4 * g);
+              const uint32_t there = ragged && left < 4 ? kNowhere : at;   // (out_off is, where none is left)
+              if constexpr (wide) __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, v), buffer, there, 0, 0);
+              else __builtin_amdgcn_raw_buffer_store_b64(u2{pair[0], pair[1]}, buffer, there, 0, 0);
+              if (ragged) {
+                const bool some = left > 0 && left < 4;
 #pragma unroll
-              for (int e = 0; e < 3; ++e) {
-                if (wide) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), buffer, some && e < left ? at + 4 * e : kNowhere, 0, 0);
-                else __builtin_amdgcn_raw_buffer_store_b16(static_cast<short>(pair[e / 2] >> (16 * (e & 1))), buffer, some && e < left ? at + 2 * e : kNowhere, 0, 0);
+                for (int e = 0; e < 3; ++e) {
+                  if constexpr (wide) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(v[e]), buffer, some && e < left ? at + 4 * e : kNowhere, 0, 0);
+                  else __builtin_amdgcn_raw_buffer_store_b16(static_cast<short>(pair[e / 2] >> (16 * (e & 1))), buffer, some && e < left ? at + 2 * e : kNowhere, 0, 0);
+                }
               }
             }
-          }
+        };
+        if constexpr (sizeof(T) == 4) {
+          put(std::true_type());
+        } else {
+          if (a.out_float) put(std::true_type());
+          else put(std::false_type());
+        }
       }
+      __syncthreads();
     }
   }
 };
 
 // Blocks that share a compute unit: what the state's registers leave room for.
-constexpr int blocks_of(int inner) { return inner == 256 ? 1 : 2; }
+constexpr int blocks_of(int inner, int tiles) { return inner == 256 ? 1 : inner * tiles == 64 ? 2 : 2; }
 
 template <class T, int kInner, int kTiles, bool kMap, bool kWhole>
-__global__ __launch_bounds__(kThreads, blocks_of(kInner)) void k_la_walk(const Walk a) {
+__global__ __launch_bounds__(kThreads, blocks_of(kInner, kTiles)) void k_la_walk(const Walks all) {
   typedef Walker<T, kInner, kTiles, kMap, kWhole> W;
+  const int turn = blockIdx.x / kXcds, group = __builtin_amdgcn_readfirstlane(turn / all.count);
+  const int block = group * kXcds + blockIdx.x % kXcds;
+  const Walk a = all.walk[turn - group * all.count];
   __shared__ __align__(16) unsigned char memory[W::kLds];
   typename W::Word* const lds = reinterpret_cast<typename W::Word*>(memory);
   const int units = a.heads * a.slices;
-  const int p = blockIdx.x / units, unit = blockIdx.x % units, head = unit / a.slices, slice = unit % a.slices;
+  const int p = block / units, unit = block % units, head = unit / a.slices, slice = unit % a.slices;
+  if (p >= all.parts) return;
   const int col0 = slice * W::kCols;
   W w;
   const float l = a.log_decay[head] * kL2e;
@@ -692,8 +733,9 @@ __global__ __launch_bounds__(kThreads, blocks_of(kInner)) void k_la_walk(const W
 // From what every piece adds to the state with which the next is entered, in the slot
 // of the piece that is left: for every sequence, one after another over its pieces.
 template <class T, int kInner, int kTiles>
-__global__ __launch_bounds__(kThreads) void k_la_join(const Walk a) {
+__global__ __launch_bounds__(kThreads) void k_la_join(const Walks all) {
   typedef Walker<T, kInner, kTiles, true, true> W;
+  const Walk& a = all.walk[blockIdx.y];
   constexpr int kPer = W::kState / 4, kAhead = 8;
   const int units = a.heads * a.slices, blocks = (units * kPer + kThreads - 1) / kThreads;
   const int s = blockIdx.x / blocks, id = static_cast<int>(blockIdx.x % blocks) * kThreads + static_cast<int>(threadIdx.x);
@@ -894,39 +936,51 @@ int kept(const soma_la_config& c, const float** begin, const float* end, unsigne
   return launch("k_la_copy", k_la_copy, grid, dim3(kThreads), 0, st, from, reinterpret_cast<float*>(at), n);
 }
 
-// fp32 gradients of every head, where heads share keys and values
-size_t sums_size(const soma_la_config& c) {
-  if (c.heads == c.kv_heads) return 0;
-  return up256(sizeof(float) * c.rows * c.heads * std::max(c.key_width, c.value_width));
+// fp32 gradients of every head, where heads share keys and values: of keys or values
+size_t sums_size(const soma_la_config& c, int width) {
+  return c.heads == c.kv_heads ? 0 : up256(sizeof(float) * c.rows * c.heads * width);
+}
+
+// Whether the walks for dq, dk and dv are of one shape.
+bool are_alike(const soma_la_config& c) {
+  const Shape a = shape_of(c.key_width, c.value_width), b = shape_of(c.value_width, c.key_width);
+  return a.inner == b.inner && a.tiles == b.tiles && a.slices == b.slices;
+}
+
+// Slots of the walks that run together, and behind them the copy and the sums.
+size_t all_slots(const soma_la_config& c, bool grad) {
+  const size_t one = slots_size(c, c.key_width, c.value_width);
+  if (!grad) return one;
+  return are_alike(c) ? 3 * one : std::max(one, 2 * slots_size(c, c.value_width, c.key_width));
 }
 
 size_t la_workspace(const soma_la_config& c, bool grad) {
-  size_t n = slots_size(c, c.key_width, c.value_width) + copy_size(c);
-  if (grad) n = std::max(n, slots_size(c, c.value_width, c.key_width)) + sums_size(c);
-  return n;
+  const size_t n = all_slots(c, grad) + copy_size(c);
+  return grad ? n + sums_size(c, c.key_width) + sums_size(c, c.value_width) : n;
 }
 
 template <class T, int kInner, int kTiles>
-int walk_as(const Walk& a, hipStream_t st) {
-  const int units = a.heads * a.slices, parts = a.piece ? a.pieces : a.sequences;
-  const dim3 grid(static_cast<unsigned>(units) * parts), block(kThreads);
+int walk_as(const Walks& all, hipStream_t st) {
+  const Walk& a = all.walk[0];
+  const int units = a.heads * a.slices;
+  const dim3 grid(((static_cast<unsigned>(units) * all.parts + kXcds - 1) / kXcds) * kXcds * all.count), block(kThreads);
   if (a.piece) {
     if (int rc = launch("k_la_walk (maps)", a.whole ? k_la_walk<T, kInner, kTiles, true, true> : k_la_walk<T, kInner, kTiles, true, false>,
-                        grid, block, 0, st, a))
+                        grid, block, 0, st, all))
       return rc;
     const unsigned blocks = (units * (kInner * 64 * kTiles / 4) + kThreads - 1) / kThreads;
-    if (int rc = launch("k_la_join", k_la_join<T, kInner, kTiles>, dim3(blocks * a.sequences), block, 0, st, a))
+    if (int rc = launch("k_la_join", k_la_join<T, kInner, kTiles>, dim3(blocks * a.sequences, all.count), block, 0, st, all))
       return rc;
   }
   return launch("k_la_walk", a.whole ? k_la_walk<T, kInner, kTiles, false, true> : k_la_walk<T, kInner, kTiles, false, false>, grid,
-                block, 0, st, a);
+                block, 0, st, all);
 }
 
 template <class T>
-int walk_of(const Walk& a, const Shape& s, hipStream_t st) {
-  if (s.inner == 64) return s.tiles == 1 ? walk_as<T, 64, 1>(a, st) : walk_as<T, 64, 2>(a, st);
-  if (s.inner == 128) return walk_as<T, 128, 1>(a, st);
-  return walk_as<T, 256, 1>(a, st);
+int walk_of(const Walks& all, const Shape& s, hipStream_t st) {
+  if (s.inner == 64) return s.tiles == 1 ? walk_as<T, 64, 1>(all, st) : walk_as<T, 64, 2>(all, st);
+  if (s.inner == 128) return walk_as<T, 128, 1>(all, st);
+  return walk_as<T, 256, 1>(all, st);
 }
 
 // An array of rows and what a walk needs to know of it.
@@ -936,33 +990,46 @@ struct Array {
   int share;
 };
 
-int walk(const soma_la_config& c, const Array& x, const Array& y, const Array& z, int inner, int outer, bool back,
-         const float* log_decay, const int32_t* offsets, const float* begin, float* end, bool transposed, void* out,
-         bool out_float, unsigned char* ws, hipStream_t st) {
-  const Shape s = shape_of(inner, outer);
+Walk walk_over(const soma_la_config& c, const Array& x, const Array& y, const Array& z, int inner, int outer, bool back,
+               const float* begin, float* end, bool transposed, void* out, bool out_float) {
   Walk a{};
   a.x = x.p, a.y = y.p, a.z = z.p;
   a.x_stride = x.stride, a.y_stride = y.stride, a.z_stride = z.stride;
   a.x_share = x.share, a.y_share = y.share, a.z_share = z.share;
   a.inner = inner, a.outer = outer;
-  a.whole = inner * type_size(c.type) % 16 == 0 && outer * type_size(c.type) % 16 == 0;
   a.out = out;
   a.out_float = out_float;
-  a.begin = begin, a.end = end, a.log_decay = log_decay;
+  a.begin = begin, a.end = end;
   a.row_stride = transposed ? 1 : outer;
   a.col_stride = transposed ? inner : 1;
-  a.offsets = offsets;
-  a.rows = c.rows, a.length = c.rows / c.sequences, a.sequences = c.sequences, a.heads = c.heads, a.slices = s.slices;
   a.back = back;
   a.p_scale = c.scale;
   a.in_scale = back ? c.scale : 1.0f;
   a.front_scale = back ? 1.0f : c.scale;
-  if (const int most = most_pieces(c, s)) {
-    a.piece = ((c.rows + most - 1) / most + 63) / 64 * 64;
-    a.pieces = (c.rows + a.piece - 1) / a.piece;
-    a.slots = reinterpret_cast<float*>(ws);
+  return a;
+}
+
+// Up to kMostWalks walks of one shape in one launch.
+int walk(const soma_la_config& c, std::initializer_list<Walk> walks, const float* log_decay, const int32_t* offsets,
+         unsigned char* ws, hipStream_t st) {
+  Walks all{};
+  const Shape s = shape_of(walks.begin()->inner, walks.begin()->outer);
+  const int most = most_pieces(c, s);
+  for (const Walk& w : walks) {
+    Walk& a = all.walk[all.count];
+    a = w;
+    a.whole = a.inner * type_size(c.type) % 16 == 0 && a.outer * type_size(c.type) % 16 == 0;
+    a.log_decay = log_decay, a.offsets = offsets;
+    a.rows = c.rows, a.length = c.rows / c.sequences, a.sequences = c.sequences, a.heads = c.heads, a.slices = s.slices;
+    if (most) {
+      a.piece = ((c.rows + most - 1) / most + 63) / 64 * 64;
+      a.pieces = (c.rows + a.piece - 1) / a.piece;
+      a.slots = reinterpret_cast<float*>(ws + all.count * slots_size(c, a.inner, a.outer));
+    }
+    ++all.count;
   }
-  return c.type == SOMA_FLOAT ? walk_of<float>(a, s, st) : walk_of<bf16>(a, s, st);
+  all.parts = most ? all.walk[0].pieces : c.sequences;
+  return c.type == SOMA_FLOAT ? walk_of<float>(all, s, st) : walk_of<bf16>(all, s, st);
 }
 
 // The arrays' bytes.
@@ -1024,10 +1091,10 @@ int soma_la_forward(const soma_la_config* cfg, const void* q, const void* k, con
   const int share = c.heads / c.kv_heads;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
   const hipStream_t st = stream_of(stream);
-  if (int rc = kept(c, &s0, sT, ws + slots_size(c, c.key_width, c.value_width), st)) return rc;
-  if (int rc = walk(c, {q, c.q_stride, 1}, {k, c.k_stride, share}, {v, c.v_stride, share}, c.key_width, c.value_width, false,
-                    log_decay, offsets, s0, sT, false, o, false, ws, st))
-    return rc;
+  if (int rc = kept(c, &s0, sT, ws + all_slots(c, false), st)) return rc;
+  const Walk to_o = walk_over(c, {q, c.q_stride, 1}, {k, c.k_stride, share}, {v, c.v_stride, share}, c.key_width, c.value_width,
+                              false, s0, sT, false, o, false);
+  if (int rc = walk(c, {to_o}, log_decay, offsets, ws, st)) return rc;
   return set_ok();
 }
 
@@ -1054,30 +1121,39 @@ int soma_la_backward(const soma_la_config* cfg, const void* q, const void* k, co
       ao{d_o, static_cast<int64_t>(c.heads) * c.value_width, 1};
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
   const hipStream_t st = stream_of(stream);
-  float* sums = nullptr;
-  if (share > 1)
-    sums = reinterpret_cast<float*>(ws + la_workspace(c, true) - sums_size(c));
-  const auto shared = [&](void* out, int width) -> int {
+  float *key_sums = nullptr, *value_sums = nullptr;
+  if (share > 1) {
+    unsigned char* const at = ws + all_slots(c, true) + copy_size(c);
+    key_sums = reinterpret_cast<float*>(at);
+    value_sums = reinterpret_cast<float*>(at + sums_size(c, c.key_width));
+  }
+  const auto shared = [&](const float* sums, void* out, int width) -> int {
     if (share == 1 || c.rows == 0) return SOMA_OK;
     const int64_t n = static_cast<int64_t>(c.rows) * c.kv_heads * width;
     const dim3 grid(static_cast<unsigned>(std::min<int64_t>((n + kThreads - 1) / kThreads, 8192)));
     if (c.type == SOMA_FLOAT)
-      return launch("k_la_share", k_la_share<float>, grid, dim3(kThreads), 0, st, static_cast<const float*>(sums),
-                    static_cast<float*>(out), n, width, share, offsets, c.sequences, c.rows, c.kv_heads * width);
-    return launch("k_la_share", k_la_share<bf16>, grid, dim3(kThreads), 0, st, static_cast<const float*>(sums),
-                  static_cast<bf16*>(out), n, width, share, offsets, c.sequences, c.rows, c.kv_heads * width);
+      return launch("k_la_share", k_la_share<float>, grid, dim3(kThreads), 0, st, sums, static_cast<float*>(out), n, width, share,
+                    offsets, c.sequences, c.rows, c.kv_heads * width);
+    return launch("k_la_share", k_la_share<bf16>, grid, dim3(kThreads), 0, st, sums, static_cast<bf16*>(out), n, width, share,
+                  offsets, c.sequences, c.rows, c.kv_heads * width);
   };
-  if (int rc = walk(c, ao, av, ak, c.value_width, c.key_width, false, log_decay, offsets, s0, nullptr, true, dq, false, ws, st))
-    return rc;
-  if (int rc = walk(c, av, ao, aq, c.value_width, c.key_width, true, log_decay, offsets, dsT, nullptr, true,
-                    share > 1 ? static_cast<void*>(sums) : dk, share > 1, ws, st))
-    return rc;
-  if (int rc = shared(dk, c.key_width)) return rc;
-  if (int rc = kept(c, &dsT, ds0, ws + slots_size(c, c.key_width, c.value_width), st)) return rc;
-  if (int rc = walk(c, ak, aq, ao, c.key_width, c.value_width, true, log_decay, offsets, dsT, ds0, false,
-                    share > 1 ? static_cast<void*>(sums) : dv, share > 1, ws, st))
-    return rc;
-  if (int rc = shared(dv, c.value_width)) return rc;
+  const Walk to_dq = walk_over(c, ao, av, ak, c.value_width, c.key_width, false, s0, nullptr, true, dq, false);
+  const Walk to_dk = walk_over(c, av, ao, aq, c.value_width, c.key_width, true, dsT, nullptr, true,
+                               share > 1 ? static_cast<void*>(key_sums) : dk, share > 1);
+  const auto to_dv = [&] {
+    return walk_over(c, ak, aq, ao, c.key_width, c.value_width, true, dsT, ds0, false,
+                     share > 1 ? static_cast<void*>(value_sums) : dv, share > 1);
+  };
+  // (dsT in ds0's place is read for dk before dv's walk writes it)
+  if (are_alike(c) && (!dsT || dsT != ds0)) {
+    if (int rc = walk(c, {to_dv(), to_dk, to_dq}, log_decay, offsets, ws, st)) return rc;
+  } else {
+    if (int rc = walk(c, {to_dk, to_dq}, log_decay, offsets, ws, st)) return rc;
+    if (int rc = kept(c, &dsT, ds0, ws + all_slots(c, true), st)) return rc;
+    if (int rc = walk(c, {to_dv()}, log_decay, offsets, ws, st)) return rc;
+  }
+  if (int rc = shared(key_sums, dk, c.key_width)) return rc;
+  if (int rc = shared(value_sums, dv, c.value_width)) return rc;
   return set_ok();
 }
 
