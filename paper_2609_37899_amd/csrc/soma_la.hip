@@ -906,16 +906,16 @@ Shape shape_of(int inner, int outer) {
 
 // Pieces: none where every sequence has its blocks and they are enough, or short.
 // Their number goes by the heads alone, so that a workspace serves fewer rows too.
-int most_pieces(const soma_la_config& c, const Shape& s) {
-  const int64_t units = static_cast<int64_t>(c.heads) * s.slices;
+int most_pieces(const soma_la_config& c, const Shape& s, int walks) {
+  const int64_t units = static_cast<int64_t>(c.heads) * s.slices * walks;
   const int few = c.type == SOMA_FLOAT ? 4 * Kind<float>::kC : 4 * Kind<bf16>::kC;
   if (units * c.sequences >= kEnough || c.rows <= static_cast<int64_t>(c.sequences) * few) return 0;
   return static_cast<int>(std::min<int64_t>(kMostPieces, (kEnough + units - 1) / units));
 }
 
-size_t slots_size(const soma_la_config& c, int inner, int outer) {
+size_t slots_size(const soma_la_config& c, int inner, int outer, int walks) {
   const Shape s = shape_of(inner, outer);
-  const int most = most_pieces(c, s);
+  const int most = most_pieces(c, s, walks);
   if (!most) return 0;
   return up256(sizeof(float) * most * c.heads * s.slices * s.inner * 64 * s.tiles);
 }
@@ -923,7 +923,7 @@ size_t slots_size(const soma_la_config& c, int inner, int outer) {
 // A copy of the states that a walk begins with, where it ends with the same array and
 // goes in pieces: one block may then read a state after another has written it.
 size_t copy_size(const soma_la_config& c) {
-  if (!most_pieces(c, shape_of(c.key_width, c.value_width))) return 0;
+  if (!most_pieces(c, shape_of(c.key_width, c.value_width), 1)) return 0;
   return up256(sizeof(float) * c.sequences * c.heads * c.key_width * c.value_width);
 }
 
@@ -949,9 +949,10 @@ bool are_alike(const soma_la_config& c) {
 
 // Slots of the walks that run together, and behind them the copy and the sums.
 size_t all_slots(const soma_la_config& c, bool grad) {
-  const size_t one = slots_size(c, c.key_width, c.value_width);
+  const size_t one = slots_size(c, c.key_width, c.value_width, 1);
   if (!grad) return one;
-  return are_alike(c) ? 3 * one : std::max(one, 2 * slots_size(c, c.value_width, c.key_width));
+  const size_t together = are_alike(c) ? 3 * slots_size(c, c.value_width, c.key_width, 3) : 0;
+  return std::max({one, 2 * slots_size(c, c.value_width, c.key_width, 2), together});
 }
 
 size_t la_workspace(const soma_la_config& c, bool grad) {
@@ -1014,7 +1015,7 @@ int walk(const soma_la_config& c, std::initializer_list<Walk> walks, const float
          unsigned char* ws, hipStream_t st) {
   Walks all{};
   const Shape s = shape_of(walks.begin()->inner, walks.begin()->outer);
-  const int most = most_pieces(c, s);
+  const int most = most_pieces(c, s, static_cast<int>(walks.size()));
   for (const Walk& w : walks) {
     Walk& a = all.walk[all.count];
     a = w;
@@ -1024,7 +1025,7 @@ int walk(const soma_la_config& c, std::initializer_list<Walk> walks, const float
     if (most) {
       a.piece = ((c.rows + most - 1) / most + 63) / 64 * 64;
       a.pieces = (c.rows + a.piece - 1) / a.piece;
-      a.slots = reinterpret_cast<float*>(ws + all.count * slots_size(c, a.inner, a.outer));
+      a.slots = reinterpret_cast<float*>(ws + all.count * slots_size(c, a.inner, a.outer, static_cast<int>(walks.size())));
     }
     ++all.count;
   }
