@@ -951,8 +951,8 @@ bool are_alike(const soma_la_config& c) {
 size_t all_slots(const soma_la_config& c, bool grad) {
   const size_t one = slots_size(c, c.key_width, c.value_width, 1);
   if (!grad) return one;
-  const size_t together = are_alike(c) ? 3 * slots_size(c, c.value_width, c.key_width, 3) : 0;
-  return std::max({one, 2 * slots_size(c, c.value_width, c.key_width, 2), together});
+  return are_alike(c) ? std::max(one, 3 * slots_size(c, c.value_width, c.key_width, 3))
+                      : std::max(one, 2 * slots_size(c, c.value_width, c.key_width, 2));
 }
 
 size_t la_workspace(const soma_la_config& c, bool grad) {
@@ -1010,12 +1010,12 @@ Walk walk_over(const soma_la_config& c, const Array& x, const Array& y, const Ar
   return a;
 }
 
-// Up to kMostWalks walks of one shape in one launch.
-int walk(const soma_la_config& c, std::initializer_list<Walk> walks, const float* log_decay, const int32_t* offsets,
+// Up to kMostWalks walks of one shape in one launch, in pieces as `together` would be.
+int walk(const soma_la_config& c, std::initializer_list<Walk> walks, int together, const float* log_decay, const int32_t* offsets,
          unsigned char* ws, hipStream_t st) {
   Walks all{};
   const Shape s = shape_of(walks.begin()->inner, walks.begin()->outer);
-  const int most = most_pieces(c, s, static_cast<int>(walks.size()));
+  const int most = most_pieces(c, s, together);
   for (const Walk& w : walks) {
     Walk& a = all.walk[all.count];
     a = w;
@@ -1025,7 +1025,7 @@ int walk(const soma_la_config& c, std::initializer_list<Walk> walks, const float
     if (most) {
       a.piece = ((c.rows + most - 1) / most + 63) / 64 * 64;
       a.pieces = (c.rows + a.piece - 1) / a.piece;
-      a.slots = reinterpret_cast<float*>(ws + all.count * slots_size(c, a.inner, a.outer, static_cast<int>(walks.size())));
+      a.slots = reinterpret_cast<float*>(ws + all.count * slots_size(c, a.inner, a.outer, together));
     }
     ++all.count;
   }
@@ -1095,7 +1095,7 @@ int soma_la_forward(const soma_la_config* cfg, const void* q, const void* k, con
   if (int rc = kept(c, &s0, sT, ws + all_slots(c, false), st)) return rc;
   const Walk to_o = walk_over(c, {q, c.q_stride, 1}, {k, c.k_stride, share}, {v, c.v_stride, share}, c.key_width, c.value_width,
                               false, s0, sT, false, o, false);
-  if (int rc = walk(c, {to_o}, log_decay, offsets, ws, st)) return rc;
+  if (int rc = walk(c, {to_o}, 1, log_decay, offsets, ws, st)) return rc;
   return set_ok();
 }
 
@@ -1145,13 +1145,15 @@ int soma_la_backward(const soma_la_config* cfg, const void* q, const void* k, co
     return walk_over(c, ak, aq, ao, c.key_width, c.value_width, true, dsT, ds0, false,
                      share > 1 ? static_cast<void*>(value_sums) : dv, share > 1);
   };
-  // (dsT in ds0's place is read for dk before dv's walk writes it)
-  if (are_alike(c) && (!dsT || dsT != ds0)) {
-    if (int rc = walk(c, {to_dv(), to_dk, to_dq}, log_decay, offsets, ws, st)) return rc;
+  // (dsT in ds0's place is read for dk before dv's walk writes it; the pieces stay the
+  // same, and with them the bits)
+  const bool alike = are_alike(c);
+  if (alike && (!dsT || dsT != ds0)) {
+    if (int rc = walk(c, {to_dv(), to_dk, to_dq}, 3, log_decay, offsets, ws, st)) return rc;
   } else {
-    if (int rc = walk(c, {to_dk, to_dq}, log_decay, offsets, ws, st)) return rc;
+    if (int rc = walk(c, {to_dk, to_dq}, alike ? 3 : 2, log_decay, offsets, ws, st)) return rc;
     if (int rc = kept(c, &dsT, ds0, ws + all_slots(c, true), st)) return rc;
-    if (int rc = walk(c, {to_dv()}, log_decay, offsets, ws, st)) return rc;
+    if (int rc = walk(c, {to_dv()}, alike ? 3 : 1, log_decay, offsets, ws, st)) return rc;
   }
   if (int rc = shared(key_sums, dk, c.key_width)) return rc;
   if (int rc = shared(value_sums, dv, c.value_width)) return rc;

@@ -186,6 +186,25 @@ def test_states_in_place_and_left_out(dtype, lengths):
         assert torch.equal(y[k], z[k]), k
 
 
+@pytest.mark.parametrize("lengths", [[0, 1, 130, 31], [3000], [700, 0, 900, 1, 1000]])
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("widths", [(3, 1, 40, 64), (2, 2, 100, 128), (4, 2, 130, 250)])
+def test_gradient_of_states_in_place(dtype, lengths, widths):
+    """ds0 over dsT where one launch forms all the gradients, and where two do: the same bits, and right ones."""
+    torch = require_gpu()
+    x, want = make(torch, dtype, widths, lengths)
+    plan = plan_of(torch, dtype, widths, x, len(lengths))
+    y = run(torch, plan, x)
+    torch.cuda.synchronize()
+    check(y, want, dtype)
+    z = {k: torch.full_like(v, 7.0) for k, v in y.items()}
+    z["ds0"] = x["dsT"].clone()
+    plan.backward(x["q"], x["k"], x["v"], x["log_decay"], x["do"], z["dq"], z["dk"], z["dv"], x["s0"], z["ds0"], z["ds0"], x["offsets"])
+    torch.cuda.synchronize()
+    for k in ("dq", "dk", "dv", "ds0"):
+        assert torch.equal(y[k], z[k]), k
+
+
 @pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
 @pytest.mark.parametrize("log_decay", [0.0, -1e-6, -1.0, -30.0, -1e4, float("-inf")])
 @pytest.mark.parametrize("lengths", [[150, 1, 33], [2100]])
