@@ -846,8 +846,9 @@ int soma_norm_forward(const soma_norm_config* cfg, const void* x_dev, const void
                       const soma_drop* drop, void* total_dev, void* y_dev, void* stream);
 
 /* The same with y in 8 bits: codes [rows][width], e4m3, and scales [rows] fp32,
- * y = code scale, scale = max |y_r| / 448 (a row of zeros: 0; a row that holds a NaN:
- * NaN), codes rounded to nearest even. */
+ * y = code scale, scale = max |y_r| / 448, at least 2^-126 (a row of zeros: 0; a row
+ * that holds a NaN: NaN; otherwise one that holds an infinity: infinity), codes rounded
+ * to nearest even. */
 int soma_norm_forward_codes(const soma_norm_config* cfg, const void* x_dev, const void* residual_dev,
                             const float* gain_dev, const soma_drop* drop, void* total_dev, void* codes_dev,
                             float* scales_dev, void* stream);

@@ -241,8 +241,10 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
   if constexpr (kCodes) {
     top = over_row<kLanes, true>(top, lds);
     const float nan = over_row<kLanes, true>(bad ? 1.0f : 0.0f, lds);
-    const float up = top > 0.0f ? 448.0f / top : 0.0f;
-    if (lane == 0) a.scales[row] = nan > 0.0f ? __uint_as_float(0x7FC00000u) : top * (1.0f / 448.0f);
+    // (a scale below the normal numbers has no reciprocal: such a row's is the least of them)
+    const bool tiny = top > 0.0f && top < 448.0f * 0x1p-126f;
+    const float up = tiny ? 0x1p126f : top > 0.0f ? 448.0f / top : 0.0f;
+    if (lane == 0) a.scales[row] = nan > 0.0f ? __uint_as_float(0x7FC00000u) : tiny ? 0x1p-126f : top * (1.0f / 448.0f);
     uint8_t* const y = static_cast<uint8_t*>(a.y) + static_cast<int64_t>(row) * a.width;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {

@@ -227,6 +227,29 @@ def test_norm_in_8_bits(types, rows, width):
     assert (np.abs(got).max(1) == 448).all()
 
 
+@pytest.mark.parametrize("small", [1e-36, 1e-38, 1e-40, 1e-44])
+def test_norm_in_8_bits_below_the_normal_numbers(small):
+    """Rows whose scale would be no normal number: 2^-126 (one with half its columns 0 is just above it), and codes as near as they come. y is off by a few u, and by a
+    step of 2^-149 where it is subnormal itself; its code by half a step, 2^-4 of it or 2^-10."""
+    torch = require_gpu()
+    x, w = make(torch, ("float32", "float32"), 5, 100, 0.0, residual=False)
+    x["x"][2], w["x"][2] = 0.0, 0.0
+    x["x"][3, ::2], w["x"][3, ::2] = 0.0, 0.0
+    gain = torch.full((100,), small, device="cuda")
+    plan = soma.RmsNorm(5, 100, torch.float32)
+    codes, scale = torch.empty(5, 100, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(5, device="cuda")
+    plan.forward(x["x"], gain, codes, None, None, scale)
+    torch.cuda.synchronize()
+    exact = w["x"] / np.sqrt((w["x"] ** 2).mean(1, keepdims=True) + np.float64(np.float32(1e-5))) * np.float64(np.float32(small))
+    got, scale = codes.double().cpu().numpy(), scale.double().cpu().numpy()
+    want = np.where(np.arange(5) == 2, 0.0, np.maximum(np.abs(exact).max(1) / 448, 2.0**-126))
+    assert (np.abs(scale - want) <= np.where(want > 2.0**-126, 60 * ref.U * want, 0.0)).all()
+    at = exact / np.maximum(want, 2.0**-126)[:, None]
+    assert (np.abs(got[:2] - at[:2]) <= 2.0**-4 * np.abs(at[:2]) + 2.0**-10 + 60 * ref.U * np.abs(at[:2]) + 2.0**-22).all()
+    assert (got[2] == 0).all() and (got[3, ::2] == 0).all()
+    assert (np.abs(got[3:] - at[3:]) <= 2.0**-4 * np.abs(at[3:]) + 2.0**-10 + 60 * ref.U * np.abs(at[3:]) + 2.0**-22).all()
+
+
 def test_norm_rows_of_zeros_and_not_finite():
     """A row's values reach no other row; zeros give zeros, also without eps in 8 bits' scale."""
     torch = require_gpu()
