@@ -738,7 +738,8 @@ int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_ou
  * finite (an infinity may become NaN), and nothing else: rows in front of it
  * and other sequences and heads never see it.
  * Constraints: rows in [0, 2^30], sequences in [1, 65535], heads in [1, 1024],
- * kv_heads a divisor of heads, both widths in [1, 256], strides up to 2^22. */
+ * kv_heads a divisor of heads, both widths in [1, 256], strides up to 2^22;
+ * sequences, heads and units of 64 columns of the wider of both: a product below 2^24. */
 typedef struct soma_la_config {
   int32_t rows;
   int32_t sequences;
@@ -800,7 +801,7 @@ typedef struct soma_drop {
  *   apart (residual NULL: none); y [rows][width], rows contiguous; it may be x or
  *   residual where their rows are so too.  drop NULL: p = 0.
  * In fp32, rounded once.  Constraints: rows in [0, 2^30], width in [1, 2^20], at most
- * 2^40 elements. */
+ * 2^34 elements. */
 typedef struct soma_dropout_config {
   int32_t rows;
   int32_t width;

@@ -42,6 +42,9 @@ int launch(const char* what, void (*kernel)(P...), dim3 grid, dim3 block, unsign
   return e == hipSuccess ? SOMA_OK : device_error(what, e);
 }
 
+// A launch has fewer than 2^32 threads.
+constexpr int64_t kMostThreads = int64_t{1} << 32;
+
 inline size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
 inline bool is_type(int32_t t) { return t == SOMA_FLOAT || t == SOMA_BFLOAT; }

@@ -896,6 +896,8 @@ int check_shape(const soma_la_config* cfg) {
   if (c.key_width < 1 || c.key_width > 256) return set_error(SOMA_ESHAPE, "key_width %d is out of range", c.key_width);
   if (c.value_width < 1 || c.value_width > 256) return set_error(SOMA_ESHAPE, "value_width %d is out of range", c.value_width);
   if (!std::isfinite(c.scale)) return set_error(SOMA_EINVAL, "scale must be finite");
+  if (static_cast<int64_t>(c.sequences) * c.heads * ((std::max(c.key_width, c.value_width) + 63) / 64) * kThreads >= kMostThreads)
+    return set_error(SOMA_ESHAPE, "more sequences and heads than a launch has blocks for");
   for (int64_t stride : {c.q_stride, c.k_stride, c.v_stride})
     if (stride > kMostStride) return set_error(SOMA_ESHAPE, "a row stride is out of range");
   if (c.q_stride < static_cast<int64_t>(c.heads) * c.key_width || c.k_stride < static_cast<int64_t>(c.kv_heads) * c.key_width ||
@@ -1030,6 +1032,11 @@ int walk(const soma_la_config& c, std::initializer_list<Walk> walks, int togethe
   Walks all{};
   const Shape s = shape_of(walks.begin()->inner, walks.begin()->outer);
   const int most = most_pieces(c, s, together);
+  if (walks.size() > 1 && !most && (static_cast<int64_t>(c.sequences) * c.heads * s.slices + kXcds) * walks.size() * kThreads >= kMostThreads) {
+    for (const Walk& w : walks)
+      if (int rc = walk(c, {w}, together, log_decay, offsets, ws, st)) return rc;
+    return SOMA_OK;
+  }
   for (const Walk& w : walks) {
     Walk& a = all.walk[all.count];
     a = w;

@@ -151,7 +151,7 @@ struct NormArgs {
   float* scales;              // forward into codes
   float* partial;             // backward: [blocks][width], or NULL
   int64_t x_stride, residual_stride;
-  int rows, width;
+  int first, rows, width;     // rows from `first` on (forward)
   int x_vec, residual_vec, total_vec, y_vec, dy_vec, dtotal_vec, dresidual_vec, dx_vec;
   float eps;
   Drop drop;
@@ -190,7 +190,7 @@ template <class T, class S, int kLanes, int kGroups, bool kCodes>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  const int lane = threadIdx.x % kLanes, row = blockIdx.x * kRows + threadIdx.x / kLanes;
+  const int lane = threadIdx.x % kLanes, row = a.first + static_cast<int>(blockIdx.x * kRows + threadIdx.x / kLanes);
   if (row >= a.rows) return;                // whole waves, or the block
   const Stream s(a.drop);
   float t[kGroups][8];
@@ -447,10 +447,13 @@ int backward_blocks(const soma_norm_config& c) {
 }
 
 template <class T, class S, int kLanes, int kGroups, bool kCodes>
-int forward_as(const NormArgs& a, hipStream_t st) {
-  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  return launch("k_norm_forward", k_norm_forward<T, S, kLanes, kGroups, kCodes>, dim3((a.rows + kRows - 1) / kRows),
-                dim3(kLanes < 256 ? 256 : kLanes), 0, st, a);
+int forward_as(NormArgs a, hipStream_t st) {
+  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1, kMost = static_cast<int>(kMostThreads / 2 / kLanes);
+  for (; a.first < a.rows; a.first += kMost)
+    if (int rc = launch("k_norm_forward", k_norm_forward<T, S, kLanes, kGroups, kCodes>,
+                        dim3((std::min(a.rows - a.first, kMost) + kRows - 1) / kRows), dim3(kLanes < 256 ? 256 : kLanes), 0, st, a))
+      return rc;
+  return SOMA_OK;
 }
 template <class T, class S, int kLanes, int kGroups>
 int backward_as(const NormArgs& a, int blocks, hipStream_t st) {
@@ -534,7 +537,7 @@ int soma_dropout(const soma_dropout_config* cfg, const void* x, const void* resi
   if (!is_type(c.type)) return set_error(SOMA_EINVAL, "type %d is none of enum soma_type", c.type);
   if (c.rows < 0 || c.rows > (1 << 30)) return set_error(SOMA_ESHAPE, "rows %d is out of range", c.rows);
   if (c.width < 1 || c.width > (1 << 20)) return set_error(SOMA_ESHAPE, "width %d is out of range", c.width);
-  if (static_cast<int64_t>(c.rows) * c.width > int64_t{1} << 40) return set_error(SOMA_ESHAPE, "more than 2^40 elements");
+  if (static_cast<int64_t>(c.rows) * c.width > int64_t{1} << 34) return set_error(SOMA_ESHAPE, "more than 2^34 elements");
   if (c.x_stride < c.width || c.residual_stride < c.width) return set_error(SOMA_ESHAPE, "a row stride is shorter than its row");
   if (c.x_stride > (int64_t{1} << 32) || c.residual_stride > (int64_t{1} << 32))
     return set_error(SOMA_ESHAPE, "a row stride is out of range");
@@ -558,8 +561,7 @@ int soma_dropout(const soma_dropout_config* cfg, const void* x, const void* resi
   a.x_vec = in_eights(x, a.x_stride, a.width, e);
   a.residual_vec = in_eights(residual, a.residual_stride, a.width, e);
   a.y_vec = is_aligned(y, 16);
-  const int64_t blocks = (a.rows * a.groups + 255) / 256;
-  if (blocks >= int64_t{1} << 31) return set_error(SOMA_ESHAPE, "more elements than a launch has lanes for");
+  const int64_t blocks = (a.rows * a.groups + 255) / 256;   // (of 2^34 elements at the most: fewer than 2^24)
   const auto kernel = c.type == SOMA_FLOAT ? (a.drop.cut ? k_dropout<float, true> : k_dropout<float, false>)
                                            : (a.drop.cut ? k_dropout<bf16, true> : k_dropout<bf16, false>);
   if (int rc = launch("k_dropout", kernel, dim3(static_cast<unsigned>(blocks)), dim3(256), 0, stream_of(stream), a)) return rc;

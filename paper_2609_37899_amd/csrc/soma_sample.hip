@@ -195,7 +195,8 @@ struct Row {
     return right < 64 ? m >> right : 0;
   }
 
-  __device__ __forceinline__ int bin_of(float l) const { return min(kBins - 1, static_cast<int>((top - l) * fine)); }
+  // (distances that are no number, of infinities and NaN, in the last)
+  __device__ __forceinline__ int bin_of(float l) const { return static_cast<int>(fminf((top - l) * fine, kBins - 1)); }
 
   template <class V>
   __device__ V over_block(V v) {

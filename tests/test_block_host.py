@@ -77,6 +77,20 @@ def test_linear_attention_shapes(lib, field, value, code):
     assert lib.soma_last_error()
 
 
+def test_more_blocks_than_a_launch_has(lib):
+    """2^24 blocks of 256 threads would be 2^32; dropout's elements are counted alike."""
+    out = ctypes.c_size_t()
+    for heads, width, code in ((256, 64, soma.SOMA_OK), (257, 64, soma.SOMA_ESHAPE), (128, 128, soma.SOMA_OK),
+                               (129, 65, soma.SOMA_ESHAPE), (64, 256, soma.SOMA_OK), (65, 193, soma.SOMA_ESHAPE)):
+        for kw in (dict(key_width=width, value_width=1), dict(key_width=1, value_width=width)):
+            c = la_cfg(rows=65535, sequences=65535, heads=heads, kv_heads=heads, q_stride=2**22, k_stride=2**22, v_stride=2**22, **kw)
+            assert lib.soma_la_workspace_size(c, 1, ctypes.byref(out)) == code, (heads, width)
+            if code:
+                assert forward(lib, c) == backward(lib, c) == step(lib, c) == code
+    many = dict(width=2**10, x_stride=2**10, residual_stride=2**10)
+    assert dropout(lib, dropout_cfg(rows=2**24 + 1, **many)) == soma.SOMA_ESHAPE
+
+
 def test_linear_attention_arguments(lib):
     out, c = ctypes.c_size_t(), la_cfg()
     assert lib.soma_la_workspace_size(None, 0, ctypes.byref(out)) == soma.SOMA_EINVAL

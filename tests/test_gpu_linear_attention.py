@@ -351,6 +351,24 @@ def test_captured_and_on_another_stream(dtype, lengths):
             assert torch.equal(out[k], z[k]), k
 
 
+def test_more_blocks_than_one_launch_has():
+    """So many sequences and heads that the gradients' walks take a launch each: o = scale q k v and its gradients, four
+    factors each, whose products are rounded thrice, and once more where P is formed (5 u with room for one)."""
+    torch = require_gpu()
+    n, H = 65535, 128
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, do = (torch.randn(n, H, device="cuda", generator=g) for _ in range(4))
+    l = torch.full((H,), -0.5, device="cuda")
+    o, dq, dk, dv = (torch.full_like(q, 7.0) for _ in range(4))
+    plan = soma.LinearAttention(n, n, H, 1, 1, torch.float32, scale=0.5)
+    plan.forward(q, k, v, l, o)
+    plan.backward(q, k, v, l, do, dq, dk, dv)
+    torch.cuda.synchronize()
+    for got, three in ((o, (q, k, v)), (dq, (do, v, k)), (dk, (v, do, q)), (dv, (k, q, do))):
+        want = 0.5 * three[0].double() * three[1].double() * three[2].double()
+        assert ((got.double() - want).abs() <= 5 * 2.0**-24 * want.abs() + 1e-37).all()
+
+
 def test_beyond_2_31_elements():
     """The last sequences of arrays of more than 2^31 elements, against a call of their own."""
     torch = require_gpu()

@@ -250,6 +250,20 @@ def test_norm_in_8_bits_below_the_normal_numbers(small):
     assert (np.abs(got[3:] - at[3:]) <= 2.0**-4 * np.abs(at[3:]) + 2.0**-10 + 60 * ref.U * np.abs(at[3:]) + 2.0**-22).all()
 
 
+def test_norm_of_more_rows_than_one_launch_takes():
+    """A wave a row: 2^25 rows a launch.  y = gain x / sqrt(x^2 + eps) in fp32: roundings of the square, its sum with eps
+    (half of theirs is left by the root), the root, its reciprocal and two products, 6 u, and one for the division."""
+    torch = require_gpu()
+    n = 2**25 + 7
+    x = torch.randn(n, 1, device="cuda")
+    y, t = torch.full_like(x, 7.0), torch.full_like(x, 7.0)
+    soma.RmsNorm(n, 1, torch.float32, eps=0.25).forward(x, torch.full((1,), 1.5, device="cuda"), y, None, t)
+    torch.cuda.synchronize()
+    assert torch.equal(t, x)
+    want = 1.5 * x.double() / (x.double() ** 2 + 0.25).sqrt()
+    assert ((y.double() - want).abs() <= 7 * 2.0**-24 * want.abs() + 1e-37).all()
+
+
 def test_norm_rows_of_zeros_and_not_finite():
     """A row's values reach no other row; zeros give zeros, also without eps in 8 bits' scale."""
     torch = require_gpu()
