@@ -55,10 +55,12 @@ struct Stream {
   }
 };
 
-// Eight elements at p + at, all of them inside and aligned, or those from lo to hi - 1.
+// Elements lo to hi - 1 of the eight at p + at.  Where groups are aligned (vec) all eight
+// are read at once, also at a row's two ends (what is around, not zeros then, belongs to
+// the rows before and behind), but for the last row (`last`).
 template <class T>
-__device__ __forceinline__ void load_eight(const T* p, int64_t at, bool vec, int lo, int hi, float (&x)[8]) {
-  if (vec && lo == 0 && hi == 8) {
+__device__ __forceinline__ void load_eight(const T* p, int64_t at, bool vec, bool last, int lo, int hi, float (&x)[8]) {
+  if (vec && (!last || (lo == 0 && hi == 8))) {
     if constexpr (sizeof(T) == 2) {
       const uint4 u = *reinterpret_cast<const uint4*>(p + at);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -76,6 +78,13 @@ __device__ __forceinline__ void load_eight(const T* p, int64_t at, bool vec, int
     for (int i = 0; i < 8; ++i) x[i] = i >= lo && i < hi ? load_value(p + at + i) : 0.0f;
   }
 }
+// Zeros around them (without a branch, which would part the loads of several groups:
+// 16,384 rows of 4,096 in codes 103 us for 96).
+__device__ __forceinline__ void clear_around(int lo, int hi, float (&x)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; ++i) x[i] = static_cast<unsigned>(i - lo) < static_cast<unsigned>(hi - lo) ? x[i] : 0.0f;
+}
+// Those elements, and nothing around them.
 template <class T>
 __device__ __forceinline__ void store_eight(T* p, int64_t at, bool vec, int lo, int hi, const float (&x)[8]) {
   if (vec && lo == 0 && hi == 8) {
@@ -112,9 +121,10 @@ __global__ __launch_bounds__(256) void k_dropout(const DropArgs a) {
   const int64_t group = (first >> 3) + (u - row * a.groups), col = group * 8 - first;
   const int lo = static_cast<int>(col < 0 ? -col : 0), hi = static_cast<int>(min(a.width - col, int64_t{8}));
   if (hi <= lo) return;
+  const bool last = row + 1 == a.rows;
   float x[8], r[8];
-  load_eight(static_cast<const T*>(a.x), row * a.x_stride + col, a.x_vec, lo, hi, x);
-  if (a.residual) load_eight(static_cast<const T*>(a.residual), row * a.residual_stride + col, a.residual_vec, lo, hi, r);
+  load_eight(static_cast<const T*>(a.x), row * a.x_stride + col, a.x_vec, last, lo, hi, x);
+  if (a.residual) load_eight(static_cast<const T*>(a.residual), row * a.residual_stride + col, a.residual_vec, last, lo, hi, r);
   if constexpr (kDrop) s.apply(group, x);
   if (a.residual) {
 #pragma unroll
@@ -158,7 +168,7 @@ struct NormArgs {
 };
 
 // Which elements of its row a lane's group k holds.
-template <int kLanes>
+template <int kLanes, bool kRagged>
 struct Group {
   int64_t block;
   int col, lo, hi;
@@ -167,52 +177,57 @@ struct Group {
     block = (first >> 3) + lane + kLanes * k;
     const int64_t c = block * 8 - first;
     col = static_cast<int>(min(c, static_cast<int64_t>(width)));
-    lo = col < 0 ? -col : 0;
-    hi = min(width - col, 8);               // <= lo: nothing
+    lo = kRagged && col < 0 ? -col : 0;
+    hi = kRagged ? min(width - col, 8) : col < width ? 8 : 0;     // <= lo: nothing
   }
 };
 
-// The gain of a group's columns, 0 outside.
-__device__ __forceinline__ void load_gain(const float* gain, int col, int lo, int hi, float (&g)[8]) {
-  if (lo == 0 && hi == 8 && (col & 3) == 0 && (reinterpret_cast<uintptr_t>(gain) & 15) == 0) {
-    const float4 a = load_four(gain + col), b = load_four(gain + col + 4);
-    g[0] = a.x, g[1] = a.y, g[2] = a.z, g[3] = a.w, g[4] = b.x, g[5] = b.y, g[6] = b.z, g[7] = b.w;
+// The gain of a group's columns, 0 outside.  (Loads of 16 bytes take a float's alignment.)
+__device__ __forceinline__ void load_gain(const float* gain, int width, int col, int lo, int hi, float (&g)[8]) {
+  typedef float Four __attribute__((ext_vector_type(4), aligned(4)));
+  if (lo == 0 && hi == 8) {
+    const Four a = *reinterpret_cast<const Four*>(gain + col), b = *reinterpret_cast<const Four*>(gain + col + 4);
+    g[0] = a[0], g[1] = a[1], g[2] = a[2], g[3] = a[3], g[4] = b[0], g[5] = b[1], g[6] = b[2], g[7] = b[3];
   } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[i] = i >= lo && i < hi ? gain[col + i] : 0.0f;
+    for (int i = 0; i < 8; ++i) g[i] = gain[min(max(col + i, 0), width - 1)];
+    clear_around(lo, hi, g);
   }
 }
 
-// T: x and y; S: residual and total; kLanes lanes a row, kGroups groups a lane.
+// T: x and y; S: residual and total; kLanes lanes a row, kGroups groups a lane; kRagged:
+// the width is no multiple of 8, and groups lie across the rows' ends.
 // 16,384 rows of 4,096 in bf16 with codes: 93 us, 470 MB at 5.05 TB/s; 65,536 of 512, bf16
 // with fp32 sums and dropout: 75 us, 403 MB at 5.4.
-template <class T, class S, int kLanes, int kGroups, bool kCodes>
+template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
   const int lane = threadIdx.x % kLanes, row = a.first + static_cast<int>(blockIdx.x * kRows + threadIdx.x / kLanes);
   if (row >= a.rows) return;                // whole waves, or the block
+  const bool last = row + 1 == a.rows;
   const Stream s(a.drop);
   float t[kGroups][8];
   float sum = 0.0f;
 #pragma unroll
   for (int k = 0; k < kGroups; ++k) {
-    const Group<kLanes> g(row, a.width, lane, k);
+    const Group<kLanes, kRagged> g(row, a.width, lane, k);
     if (g.hi <= g.lo) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[k][i] = 0.0f;
       continue;
     }
-    load_eight(static_cast<const T*>(a.x), row * a.x_stride + g.col, a.x_vec, g.lo, g.hi, t[k]);
+    load_eight(static_cast<const T*>(a.x), row * a.x_stride + g.col, a.x_vec, last, g.lo, g.hi, t[k]);
     if (a.residual) {
       float r[8];
-      load_eight(static_cast<const S*>(a.residual), row * a.residual_stride + g.col, a.residual_vec, g.lo, g.hi, r);
+      load_eight(static_cast<const S*>(a.residual), row * a.residual_stride + g.col, a.residual_vec, last, g.lo, g.hi, r);
       if (a.drop.cut) s.apply(g.block, t[k]);
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[k][i] = r[i] + t[k][i];
     } else if (a.drop.cut) {
       s.apply(g.block, t[k]);
     }
+    if constexpr (kRagged) clear_around(g.lo, g.hi, t[k]);
     if (a.total)
       store_eight(static_cast<S*>(a.total), static_cast<int64_t>(row) * a.width + g.col, a.total_vec, g.lo, g.hi, t[k]);
 #pragma unroll
@@ -223,10 +238,10 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
   bool bad = false;
 #pragma unroll
   for (int k = 0; k < kGroups; ++k) {
-    const Group<kLanes> g(row, a.width, lane, k);
+    const Group<kLanes, kRagged> g(row, a.width, lane, k);
     if (g.hi <= g.lo) continue;
     float gain[8];
-    load_gain(a.gain, g.col, g.lo, g.hi, gain);
+    load_gain(a.gain, a.width, g.col, g.lo, g.hi, gain);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       t[k][i] = t[k][i] * inv * gain[i];
@@ -248,7 +263,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
     uint8_t* const y = static_cast<uint8_t*>(a.y) + static_cast<int64_t>(row) * a.width;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const Group<kLanes> g(row, a.width, lane, k);
+      const Group<kLanes, kRagged> g(row, a.width, lane, k);
       if (g.hi <= g.lo) continue;
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[k][i] *= up;
@@ -268,16 +283,16 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
 }
 
 // With n = total / rms, h = dy gain:  dresidual = dtotal + (h - n mean(h n)) / rms,
-// dx = drop(dresidual), dgain = sum over rows of dy n.  Blocks walk over rows; a
-// lane's columns are the same in every row where the width is a multiple of 8 (kEven)
-// and their sums stay in registers, else in LDS.  65,536 rows of 512 (bf16, fp32 sums,
-// dropout): 112 us, 537 MB at 4.8 TB/s; 22,000 of 361 in fp32: 45 us, 159 MB at 3.5 (rows
-// begin anywhere in 16 bytes: loads one by one at their ends, sums in LDS).
-template <class T, class S, int kLanes, int kGroups, bool kEven>
+// dx = drop(dresidual), dgain = sum over rows of dy n.  Blocks walk over rows, a multiple
+// of 8 apart, so that whatever the width a lane's columns are the same in every row and
+// their sums stay in registers.  65,536 rows of 512 (bf16, fp32 sums, dropout): 112 us,
+// 537 MB at 4.8 TB/s; 22,000 of 361 in fp32: 42 us, 159 MB at 3.8 (rows
+// begin anywhere in 16 bytes: stores one by one at their ends).
+template <class T, class S, int kLanes, int kGroups, bool kRagged>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(const NormArgs a) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
   __shared__ float lds[16];
-  extern __shared__ float sums[];           // [kRows][width], eight columns nine apart
+  extern __shared__ float sums[];           // kRows > 1: [kRows][width], eight columns nine apart
   const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
   const int line = a.width + a.width / 8 + 1;
   float* const own = sums + mine * line;
@@ -287,22 +302,23 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
   for (int k = 0; k < kGroups; ++k)
 #pragma unroll
     for (int i = 0; i < 8; ++i) part[k][i] = 0.0f;
-  if constexpr (!kEven) {
-    for (int i = lane; i < line; i += kLanes) own[i] = 0.0f;
-    __syncthreads();
-  }
   for (int row = blockIdx.x * kRows + mine; row < a.rows; row += gridDim.x * kRows) {
     const int64_t at = static_cast<int64_t>(row) * a.width;
+    const bool last = row + 1 == a.rows;
     float t[kGroups][8], h[kGroups][8];
     float squares = 0.0f, dot = 0.0f;
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const Group<kLanes> g(row, a.width, lane, k);
+      const Group<kLanes, kRagged> g(row, a.width, lane, k);
       if (g.hi <= g.lo) continue;
-      load_eight(static_cast<const S*>(a.total), at + g.col, a.total_vec, g.lo, g.hi, t[k]);
-      load_eight(static_cast<const T*>(a.dy), at + g.col, a.dy_vec, g.lo, g.hi, h[k]);
+      load_eight(static_cast<const S*>(a.total), at + g.col, a.total_vec, last, g.lo, g.hi, t[k]);
+      load_eight(static_cast<const T*>(a.dy), at + g.col, a.dy_vec, last, g.lo, g.hi, h[k]);
       float gain[8];
-      load_gain(a.gain, g.col, g.lo, g.hi, gain);
+      load_gain(a.gain, a.width, g.col, g.lo, g.hi, gain);
+      if constexpr (kRagged) {
+        clear_around(g.lo, g.hi, t[k]);
+        clear_around(g.lo, g.hi, h[k]);
+      }
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         squares += t[k][i] * t[k][i];
@@ -315,12 +331,17 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
     const float mean = dot * inv / n;       // of h n
 #pragma unroll
     for (int k = 0; k < kGroups; ++k) {
-      const Group<kLanes> g(row, a.width, lane, k);
+      const Group<kLanes, kRagged> g(row, a.width, lane, k);
       if (g.hi <= g.lo) continue;
       float gain[8], d[8];
-      load_gain(a.gain, g.col, g.lo, g.hi, gain);
+      load_gain(a.gain, a.width, g.col, g.lo, g.hi, gain);
+      // (not kept in registers, of which 16 waves have 128 each)
+      if constexpr (kLanes == 1024) {
+        load_eight(static_cast<const T*>(a.dy), at + g.col, a.dy_vec, last, g.lo, g.hi, h[k]);
+        if constexpr (kRagged) clear_around(g.lo, g.hi, h[k]);
+      }
       if (a.dtotal) {
-        load_eight(static_cast<const S*>(a.dtotal), at + g.col, a.dtotal_vec, g.lo, g.hi, d);
+        load_eight(static_cast<const S*>(a.dtotal), at + g.col, a.dtotal_vec, last, g.lo, g.hi, d);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] = 0.0f;
@@ -328,8 +349,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const float x = t[k][i] * inv;
-        if constexpr (kEven) part[k][i] += h[k][i] * x;
-        else if (i >= g.lo && i < g.hi) own[g.col + i + (g.col + i) / 8] += h[k][i] * x;
+        part[k][i] += h[k][i] * x;
         d[i] += inv * (h[k][i] * gain[i] - x * mean);
       }
       if (a.dresidual) store_eight(static_cast<S*>(a.dresidual), at + g.col, a.dresidual_vec, g.lo, g.hi, d);
@@ -341,23 +361,19 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
   }
   if (!a.partial) return;
   float* const out = a.partial + static_cast<int64_t>(blockIdx.x) * a.width;
-  if constexpr (kEven && kRows == 1) {
 #pragma unroll
-    for (int k = 0; k < kGroups; ++k) {
-      const int col = (lane + kLanes * k) * 8;
-      if (col < a.width) store_eight(out, col, true, 0, 8, part[k]);
+  for (int k = 0; k < kGroups; ++k) {
+    const Group<kLanes, kRagged> g(blockIdx.x * kRows + mine, a.width, lane, k);
+    if (g.hi <= g.lo) continue;
+    if constexpr (kRows == 1) {
+      store_eight(out, g.col, a.width % 8 == 0, g.lo, g.hi, part[k]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i >= g.lo && i < g.hi) own[g.col + i + (g.col + i) / 8] = part[k][i];
     }
-  } else {
-    if constexpr (kEven) {
-#pragma unroll
-      for (int k = 0; k < kGroups; ++k) {
-        const int col = (lane + kLanes * k) * 8;
-        if (col < a.width) {
-#pragma unroll
-          for (int i = 0; i < 8; ++i) own[col + i + col / 8] = part[k][i];
-        }
-      }
-    }
+  }
+  if constexpr (kRows > 1) {
     __syncthreads();
     for (int c = threadIdx.x; c < a.width; c += kLanes * kRows) {
       float x = sums[c + c / 8];
@@ -439,28 +455,31 @@ int lanes_of(int width) {
   const int64_t g = groups_of(width);
   return g <= 256 ? 64 : g <= 1024 ? 256 : 1024;
 }
-// Blocks of the backward pass.  (512, 1,024 and 2,048: 22,000 rows of 361 in fp32 80.7,
+// Blocks of the backward pass: a block a row, or a multiple of eight.  (512, 1,024 and 2,048: 22,000 rows of 361 in fp32 80.7,
 // 81.7 and 88.6 us, both passes, 65,536 of 512 in bf16 194, 191 and 199.)
 int backward_blocks(const soma_norm_config& c) {
   const int lanes = lanes_of(c.width), rows = lanes < 256 ? 256 / lanes : 1;
   return std::max(1, std::min((c.rows + rows - 1) / rows, lanes < 1024 ? 1024 : 512));
 }
 
-template <class T, class S, int kLanes, int kGroups, bool kCodes>
-int forward_as(NormArgs a, hipStream_t st) {
+template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
+int forward_in(NormArgs a, hipStream_t st) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1, kMost = static_cast<int>(kMostThreads / 2 / kLanes);
   for (; a.first < a.rows; a.first += kMost)
-    if (int rc = launch("k_norm_forward", k_norm_forward<T, S, kLanes, kGroups, kCodes>,
+    if (int rc = launch("k_norm_forward", k_norm_forward<T, S, kLanes, kGroups, kCodes, kRagged>,
                         dim3((std::min(a.rows - a.first, kMost) + kRows - 1) / kRows), dim3(kLanes < 256 ? 256 : kLanes), 0, st, a))
       return rc;
   return SOMA_OK;
 }
+template <class T, class S, int kLanes, int kGroups, bool kCodes>
+int forward_as(const NormArgs& a, hipStream_t st) {
+  return a.width % 8 ? forward_in<T, S, kLanes, kGroups, kCodes, true>(a, st) : forward_in<T, S, kLanes, kGroups, kCodes, false>(a, st);
+}
 template <class T, class S, int kLanes, int kGroups>
 int backward_as(const NormArgs& a, int blocks, hipStream_t st) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  const bool even = a.width % 8 == 0;
-  const unsigned lds = even && kRows == 1 ? 0 : sizeof(float) * kRows * (a.width + a.width / 8 + 1);
-  const auto kernel = even ? k_norm_backward<T, S, kLanes, kGroups, true> : k_norm_backward<T, S, kLanes, kGroups, false>;
+  const unsigned lds = kRows == 1 ? 0 : sizeof(float) * kRows * (a.width + a.width / 8 + 1);
+  const auto kernel = a.width % 8 ? k_norm_backward<T, S, kLanes, kGroups, true> : k_norm_backward<T, S, kLanes, kGroups, false>;
   return launch("k_norm_backward", kernel, dim3(blocks), dim3(kLanes < 256 ? 256 : kLanes), lds, st, a);
 }
 

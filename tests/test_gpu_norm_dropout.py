@@ -250,6 +250,58 @@ def test_norm_in_8_bits_below_the_normal_numbers(small):
     assert (np.abs(got[3:] - at[3:]) <= 2.0**-4 * np.abs(at[3:]) + 2.0**-10 + 60 * ref.U * np.abs(at[3:]) + 2.0**-22).all()
 
 
+@pytest.mark.parametrize("rows,width", [(1100, 2051), (1030, 4099), (520, 8195)])
+def test_norm_gradient_over_rows_of_a_block(rows, width):
+    """More rows than blocks, at widths whose rows begin anywhere: the gain's gradient over all of them."""
+    torch = require_gpu()
+    x, w = make(torch, ("float32", "float32"), rows, width, 0.0)
+    plan = soma.RmsNorm(rows, width, torch.float32)
+    total, y, dr, dg = torch.empty_like(x["x"]), torch.empty_like(x["x"]), torch.empty_like(x["x"]), torch.empty_like(x["gain"])
+    plan.forward(x["x"], x["gain"], y, x["residual"], total)
+    plan.backward(total, x["gain"], x["dy"], x["dtotal"], dr, None, dg)
+    torch.cuda.synchronize()
+    eps = np.float64(np.float32(1e-5))
+    want = ref.norm(w["x"], w["residual"], w["gain"], eps, w["factor"])
+    near(y, want["y"], want["y_err"], "float32", "y")
+    back = ref.norm_backward(total.double().cpu().numpy(), w["gain"], w["dy"], w["dtotal"], eps, w["factor"])
+    near(dr, back["dresidual"], back["dresidual_err"], "float32", "dresidual")
+    near(dg, back["dgain"], back["dgain_err"], "float32", "dgain")
+
+
+@pytest.mark.parametrize("types", TYPES)
+@pytest.mark.parametrize("width", [5, 61, 509, 1001, 2051, 4099, 8195])
+def test_norm_rows_beside_rows_that_are_not_finite(types, width):
+    """Groups of eight that lie across two rows: what is not finite in one never reaches the other, nor do an array's
+    neighbours in memory."""
+    torch = require_gpu()
+    T, S = types
+    rows = 9
+    x, _ = make(torch, types, rows, width, 0.0)
+    plan = soma.RmsNorm(rows, width, getattr(torch, T), getattr(torch, S))
+
+    def run(bad):
+        a = {}
+        for n in ("x", "residual", "dy", "dtotal"):          # NaN in front of and behind each array
+            whole = torch.full((rows * width + 32,), float("nan"), dtype=x[n].dtype, device="cuda")
+            a[n] = whole[16:16 + rows * width].view(rows, width)
+            a[n].copy_(x[n])
+        if bad:
+            a["x"][1::2], a["dy"][1::2] = float("nan"), float("inf")
+        gain = torch.full((width + 16,), float("nan"), device="cuda")[8:8 + width]
+        gain.copy_(x["gain"])
+        y, codes = torch.empty_like(a["x"]), torch.empty(rows, width, dtype=torch.float8_e4m3fn, device="cuda")
+        t, s = torch.empty_like(a["residual"]), torch.empty(rows, device="cuda")
+        plan.forward(a["x"], gain, codes, a["residual"], t, s)
+        plan.forward(a["x"], gain, y, a["residual"], t)
+        dr, dx = torch.empty_like(t), torch.empty_like(y)
+        plan.backward(t, gain, a["dy"], a["dtotal"], dr, dx)
+        torch.cuda.synchronize()
+        return y, codes.float(), s, t, dr, dx
+
+    for a, b in zip(run(False), run(True)):
+        assert torch.isfinite(a).all() and torch.equal(a[::2], b[::2])
+
+
 def test_norm_of_more_rows_than_one_launch_takes():
     """A wave a row: 2^25 rows a launch.  y = gain x / sqrt(x^2 + eps) in fp32: roundings of the square, its sum with eps
     (half of theirs is left by the root), the root, its reciprocal and two products, 6 u, and one for the division."""
