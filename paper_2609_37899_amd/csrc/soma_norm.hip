@@ -6,7 +6,7 @@
 // A lane works on groups of eight elements, i = 8 b .. 8 b + 7 of the array as if its
 // rows lay side by side, which are one Philox block's (16 bits an element) and, where
 // rows do lie so, 16 or 32 aligned bytes whatever the width: only the groups at a row's
-// two ends go element by element.  The mask is formed again wherever it is needed.
+// two ends are stored element by element.  The mask is formed again wherever it is needed.
 //
 // Norm: a row is one wave's (up to 2,048 columns), or a block's of 256 or 1,024 lanes,
 // and stays in registers between its sum of squares and its output; each array is
@@ -154,6 +154,21 @@ __device__ __forceinline__ float over_row(float v, float* lds) {
   return v;
 }
 
+// Two sums at once.
+template <int kLanes>
+__device__ __forceinline__ void over_row(float& a, float& b, float* lds) {
+  a = wave_sum(a), b = wave_sum(b);
+  if constexpr (kLanes > 64) {
+    constexpr int kW = kLanes / 64;
+    __syncthreads();                        // lds has been read
+    if ((threadIdx.x & 63) == 0) lds[threadIdx.x >> 6] = a, lds[kW + (threadIdx.x >> 6)] = b;
+    __syncthreads();
+    a = lds[0], b = lds[kW];
+#pragma unroll
+    for (int w = 1; w < kW; ++w) a += lds[w], b += lds[kW + w];
+  }
+}
+
 struct NormArgs {
   const void *x, *residual, *dy, *dtotal;
   const float* gain;
@@ -197,8 +212,10 @@ __device__ __forceinline__ void load_gain(const float* gain, int width, int col,
 
 // T: x and y; S: residual and total; kLanes lanes a row, kGroups groups a lane; kRagged:
 // the width is no multiple of 8, and groups lie across the rows' ends.
-// 16,384 rows of 4,096 in bf16 with codes: 93 us, 470 MB at 5.05 TB/s; 65,536 of 512, bf16
-// with fp32 sums and dropout: 75 us, 403 MB at 5.4.
+// 16,384 rows of 4,096 in bf16 with codes: 91 us, 470 MB at 5.15 TB/s; 65,536 of 512, bf16
+// with fp32 sums and dropout: 71 us, 403 MB at 5.7; 22,000 of 361 in fp32: 25 us, 127 MB
+// at 5.1 (30 where rows' ends were read one element at a time; 4,099 columns in bf16, 8,192
+// rows: 107 us, now 54).
 template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
@@ -285,13 +302,12 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
 // With n = total / rms, h = dy gain:  dresidual = dtotal + (h - n mean(h n)) / rms,
 // dx = drop(dresidual), dgain = sum over rows of dy n.  Blocks walk over rows, a multiple
 // of 8 apart, so that whatever the width a lane's columns are the same in every row and
-// their sums stay in registers.  65,536 rows of 512 (bf16, fp32 sums, dropout): 112 us,
-// 537 MB at 4.8 TB/s; 22,000 of 361 in fp32: 42 us, 159 MB at 3.8 (rows
-// begin anywhere in 16 bytes: stores one by one at their ends).
+// their sums stay in registers.  65,536 rows of 512 (bf16, fp32 sums, dropout): 112 to
+// 118 us, 537 MB at 4.6 to 4.8 TB/s; 22,000 of 361 in fp32: 31 us, 159 MB at 5.1.
 template <class T, class S, int kLanes, int kGroups, bool kRagged>
 __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(const NormArgs a) {
   constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
-  __shared__ float lds[16];
+  __shared__ float lds[32];
   extern __shared__ float sums[];           // kRows > 1: [kRows][width], eight columns nine apart
   const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
   const int line = a.width + a.width / 8 + 1;
@@ -325,8 +341,7 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(c
         dot += h[k][i] * gain[i] * t[k][i];
       }
     }
-    squares = over_row<kLanes, false>(squares, lds);
-    dot = over_row<kLanes, false>(dot, lds);
+    over_row<kLanes>(squares, dot, lds);
     const float n = static_cast<float>(a.width), inv = 1.0f / sqrtf(squares / n + a.eps);
     const float mean = dot * inv / n;       // of h n
 #pragma unroll
@@ -455,8 +470,9 @@ int lanes_of(int width) {
   const int64_t g = groups_of(width);
   return g <= 256 ? 64 : g <= 1024 ? 256 : 1024;
 }
-// Blocks of the backward pass: a block a row, or a multiple of eight.  (512, 1,024 and 2,048: 22,000 rows of 361 in fp32 80.7,
-// 81.7 and 88.6 us, both passes, 65,536 of 512 in bf16 194, 191 and 199.)
+// Blocks of the backward pass: a block a row, or a multiple of eight.  (512, 1,024
+// and 2,048: 22,000 rows of 361 in fp32, both passes, 70, 63 and 70 us, 65,536 of 512 in
+// bf16 199, 193 and 199.)
 int backward_blocks(const soma_norm_config& c) {
   const int lanes = lanes_of(c.width), rows = lanes < 256 ? 256 / lanes : 1;
   return std::max(1, std::min((c.rows + rows - 1) / rows, lanes < 1024 ? 1024 : 512));
