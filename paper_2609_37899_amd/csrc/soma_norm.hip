@@ -8,8 +8,8 @@
 // rows do lie so, 16 or 32 aligned bytes whatever the width: only the groups at a row's
 // two ends are stored element by element.  The mask is formed again wherever it is needed.
 //
-// Norm: a row is one wave's (up to 2,048 columns), or a block's of 256 or 1,024 lanes,
-// and stays in registers between its sum of squares and its output; each array is
+// Norm: a row is one wave's (up to 2,048 columns; backward 1,024), or a block's of up to
+// 1,024 lanes, and stays in registers between its sum of squares and its output; each array is
 // read or written once.  Bound by memory, with dropout beside Philox's multiplications
 // (20 of 32 x 32 bits for eight elements).
 #include <hip/hip_runtime.h>
@@ -133,6 +133,10 @@ __global__ __launch_bounds__(256) void k_dropout(const DropArgs a) {
   store_eight(static_cast<T*>(a.y), first + col, a.y_vec, lo, hi, x);
 }
 
+// A block's threads, and its rows, where kLanes of them share one.
+constexpr int threads_of(int lanes) { return lanes == 64 ? 256 : lanes; }
+constexpr int rows_of(int lanes) { return lanes == 64 ? 4 : 1; }
+
 // Sum, or largest value, over the lanes that share a row, in every one of them.
 __device__ __forceinline__ float wave_sum(float v) {
 #pragma unroll
@@ -215,11 +219,11 @@ __device__ __forceinline__ void load_gain(const float* gain, int width, int col,
 // 16,384 rows of 4,096 in bf16 with codes: 91 us, 470 MB at 5.15 TB/s; 65,536 of 512, bf16
 // with fp32 sums and dropout: 71 us, 403 MB at 5.7; 22,000 of 361 in fp32: 25 us, 127 MB
 // at 5.1 (30 where rows' ends were read one element at a time; 4,099 columns in bf16, 8,192
-// rows: 107 us, now 54).
+// rows: 107 us, now 60).
 template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
-__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(const NormArgs a) {
+__global__ __launch_bounds__(threads_of(kLanes)) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
-  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
+  constexpr int kRows = rows_of(kLanes);
   const int lane = threadIdx.x % kLanes, row = a.first + static_cast<int>(blockIdx.x * kRows + threadIdx.x / kLanes);
   if (row >= a.rows) return;                // whole waves, or the block
   const bool last = row + 1 == a.rows;
@@ -305,8 +309,8 @@ __global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_forward(co
 // their sums stay in registers.  65,536 rows of 512 (bf16, fp32 sums, dropout): 112 to
 // 118 us, 537 MB at 4.6 to 4.8 TB/s; 22,000 of 361 in fp32: 31 us, 159 MB at 5.1.
 template <class T, class S, int kLanes, int kGroups, bool kRagged>
-__global__ __launch_bounds__(kLanes < 256 ? 256 : kLanes) void k_norm_backward(const NormArgs a) {
-  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
+__global__ __launch_bounds__(threads_of(kLanes)) void k_norm_backward(const NormArgs a) {
+  constexpr int kRows = rows_of(kLanes);
   __shared__ float lds[32];
   extern __shared__ float sums[];           // kRows > 1: [kRows][width], eight columns nine apart
   const int lane = threadIdx.x % kLanes, mine = threadIdx.x / kLanes;
@@ -468,22 +472,22 @@ int check_norm(const soma_norm_config* cfg) {
 
 int lanes_of(int width) {
   const int64_t g = groups_of(width);
-  return g <= 256 ? 64 : g <= 1024 ? 256 : 1024;
+  return g <= 128 ? 64 : g <= 256 ? 128 : g <= 512 ? 256 : g <= 1024 ? 512 : 1024;
 }
 // Blocks of the backward pass: a block a row, or a multiple of eight.  (512, 1,024
 // and 2,048: 22,000 rows of 361 in fp32, both passes, 70, 63 and 70 us, 65,536 of 512 in
 // bf16 199, 193 and 199.)
 int backward_blocks(const soma_norm_config& c) {
-  const int lanes = lanes_of(c.width), rows = lanes < 256 ? 256 / lanes : 1;
-  return std::max(1, std::min((c.rows + rows - 1) / rows, lanes < 1024 ? 1024 : 512));
+  const int lanes = lanes_of(c.width), rows = rows_of(lanes);
+  return std::max(1, std::min((c.rows + rows - 1) / rows, lanes == 64 ? 1024 : std::max(512, (1 << 18) / lanes)));
 }
 
 template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
 int forward_in(NormArgs a, hipStream_t st) {
-  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1, kMost = static_cast<int>(kMostThreads / 2 / kLanes);
+  constexpr int kRows = rows_of(kLanes), kMost = static_cast<int>(kMostThreads / 2 / kLanes);
   for (; a.first < a.rows; a.first += kMost)
     if (int rc = launch("k_norm_forward", k_norm_forward<T, S, kLanes, kGroups, kCodes, kRagged>,
-                        dim3((std::min(a.rows - a.first, kMost) + kRows - 1) / kRows), dim3(kLanes < 256 ? 256 : kLanes), 0, st, a))
+                        dim3((std::min(a.rows - a.first, kMost) + kRows - 1) / kRows), dim3(threads_of(kLanes)), 0, st, a))
       return rc;
   return SOMA_OK;
 }
@@ -493,23 +497,29 @@ int forward_as(const NormArgs& a, hipStream_t st) {
 }
 template <class T, class S, int kLanes, int kGroups>
 int backward_as(const NormArgs& a, int blocks, hipStream_t st) {
-  constexpr int kRows = kLanes < 256 ? 256 / kLanes : 1;
+  constexpr int kRows = rows_of(kLanes);
   const unsigned lds = kRows == 1 ? 0 : sizeof(float) * kRows * (a.width + a.width / 8 + 1);
   const auto kernel = a.width % 8 ? k_norm_backward<T, S, kLanes, kGroups, true> : k_norm_backward<T, S, kLanes, kGroups, false>;
-  return launch("k_norm_backward", kernel, dim3(blocks), dim3(kLanes < 256 ? 256 : kLanes), lds, st, a);
+  return launch("k_norm_backward", kernel, dim3(blocks), dim3(threads_of(kLanes)), lds, st, a);
 }
 
-// f(lanes, groups) with the instance for this width.
-template <class F>
+// f(lanes, groups) with the instance for this width.  Two groups a lane leave the
+// backward pass registers for twice the waves: 20,000 rows of 1,536 in bf16 84 us, four
+// groups in a wave 101; 8,192 of 5,120 117, four groups in 256 lanes 160.  (Forward 1,536:
+// 37 both ways, 1,100: 38 and 36; 5,120 in fp32: 139 and 153.)
+template <bool kForward, class F>
 int by_width(int width, F f) {
   const int64_t g = groups_of(width);
   using std::integral_constant;
 #define SOMA_NORM(l, n) f(integral_constant<int, l>{}, integral_constant<int, n>{})
   if (g <= 64) return SOMA_NORM(64, 1);
   if (g <= 128) return SOMA_NORM(64, 2);
-  if (g <= 256) return SOMA_NORM(64, 4);
+  if (g <= 256) {
+    if constexpr (kForward) return SOMA_NORM(64, 4);
+    else return SOMA_NORM(128, 2);
+  }
   if (g <= 512) return SOMA_NORM(256, 2);
-  if (g <= 1024) return SOMA_NORM(256, 4);
+  if (g <= 1024) return SOMA_NORM(512, 2);
   return SOMA_NORM(1024, 3);
 #undef SOMA_NORM
 }
@@ -549,7 +559,7 @@ int norm_forward(const soma_norm_config* cfg, const void* x, const void* residua
   a.y_vec = is_aligned(y, codes ? 8 : 16);
   const hipStream_t st = stream_of(stream);
   const int rc = by_type(c, [&](auto t, auto s) {
-    return by_width(c.width, [&](auto lanes, auto groups) {
+    return by_width<true>(c.width, [&](auto lanes, auto groups) {
       return codes ? forward_as<decltype(t), decltype(s), lanes(), groups(), true>(a, st)
                    : forward_as<decltype(t), decltype(s), lanes(), groups(), false>(a, st);
     });
@@ -648,7 +658,7 @@ int soma_norm_backward(const soma_norm_config* cfg, const void* total, const flo
   a.dresidual_vec = is_aligned(dresidual, 16), a.dx_vec = is_aligned(dx, 16);
   const hipStream_t st = stream_of(stream);
   if (int rc = by_type(c, [&](auto t, auto s) {
-        return by_width(c.width, [&](auto lanes, auto groups) {
+        return by_width<false>(c.width, [&](auto lanes, auto groups) {
           return backward_as<decltype(t), decltype(s), lanes(), groups()>(a, blocks, st);
         });
       }))

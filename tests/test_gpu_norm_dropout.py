@@ -250,7 +250,7 @@ def test_norm_in_8_bits_below_the_normal_numbers(small):
     assert (np.abs(got[3:] - at[3:]) <= 2.0**-4 * np.abs(at[3:]) + 2.0**-10 + 60 * ref.U * np.abs(at[3:]) + 2.0**-22).all()
 
 
-@pytest.mark.parametrize("rows,width", [(1100, 2051), (1030, 4099), (520, 8195)])
+@pytest.mark.parametrize("rows,width", [(2100, 1101), (1100, 2051), (1030, 4099), (520, 8195)])
 def test_norm_gradient_over_rows_of_a_block(rows, width):
     """More rows than blocks, at widths whose rows begin anywhere: the gain's gradient over all of them."""
     torch = require_gpu()
