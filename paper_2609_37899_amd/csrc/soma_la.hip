@@ -336,32 +336,49 @@ struct Walker {
   static __device__ __forceinline__ int inner_of(int t, int s, int lane) { return K::kKw * t + (lane >> 4) * K::kEl + 4 * s; }
   static __device__ __forceinline__ int outer_of(int wave, int n, int lane) { return (n * 4 + wave) * 16 + (lane & 15); }
 
+  // Where elements 0 .. 3 of r[t][s][n] lie in a state, and whether they are 16 bytes.
+  static __device__ __forceinline__ bool in_state(const Walk& a, int col0, int t, int s, int n, int l, uint32_t (&at)[4]) {
+    const int c = col0 + outer_of(l >> 6, n, l & 63), d = inner_of(t, s, l & 63);
+    const uint32_t rows = static_cast<uint32_t>(a.row_stride), cols = static_cast<uint32_t>(a.col_stride);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) at[i] = c < a.outer && d + i < a.inner ? 4 * ((d + i) * rows + c * cols) : kNowhere;
+    return rows == 1 && a.inner % 4 == 0;
+  }
+  // (through buffers: without a branch for each element; NULL is an empty one)
   __device__ __forceinline__ void read_state(const Walk& a, const float* p, int col0) {
-    const int l = fresh(threadIdx.x), lane = l & 63, wave = l >> 6;
+    const int l = fresh(threadIdx.x);
+    const auto buffer = buffer_of(p, p ? 4u * a.inner * a.outer : 0u);
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
-          const int c = col0 + outer_of(wave, n, lane), d = inner_of(t, s, lane);
+          uint32_t at[4];
+          if (in_state(a, col0, t, s, n, l, at)) {
+            r[t][s][n] = __builtin_bit_cast(f4, __builtin_amdgcn_raw_buffer_load_b128(buffer, at[0], 0, 0));
+          } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            r[t][s][n][i] = p && c < a.outer && d + i < a.inner ? p[(d + i) * a.row_stride + c * a.col_stride] : 0.0f;
+            for (int i = 0; i < 4; ++i) r[t][s][n][i] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(buffer, at[i], 0, 0));
+          }
         }
   }
   __device__ __forceinline__ void write_state(const Walk& a, float* p, int col0) const {
-    const int l = fresh(threadIdx.x), lane = l & 63, wave = l >> 6;
+    const int l = fresh(threadIdx.x);
+    const auto buffer = buffer_of(p, 4u * a.inner * a.outer);
 #pragma unroll
     for (int t = 0; t < kSteps; ++t)
 #pragma unroll
       for (int s = 0; s < kSub; ++s)
 #pragma unroll
         for (int n = 0; n < kTiles; ++n) {
-          const int c = col0 + outer_of(wave, n, lane), d = inner_of(t, s, lane);
+          uint32_t at[4];
+          if (in_state(a, col0, t, s, n, l, at)) {
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, r[t][s][n]), buffer, at[0], 0, 0);
+          } else {
 #pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (c < a.outer && d + i < a.inner) p[(d + i) * a.row_stride + c * a.col_stride] = r[t][s][n][i];
+            for (int i = 0; i < 4; ++i) __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(r[t][s][n][i]), buffer, at[i], 0, 0);
+          }
         }
   }
   // A slot holds the registers as they lie.
@@ -680,11 +697,12 @@ struct Walker {
 // without P 60.  Tried and left out: a third block a compute unit (no faster, and the
 // registers do not reach), rows that leave through LDS as whole lines (70.7 for 71).
 //
-// Blocks that share a compute unit: what the state's registers leave room for.
-constexpr int blocks_of(int inner) { return inner == 256 ? 1 : 2; }
+// Blocks that share a compute unit: what the state's registers leave room for (fp32, 158
+// sequences of 483 rows, 2 heads of 32 x 53, both passes: four blocks 184 us, three 230).
+constexpr int blocks_of(size_t element, int inner, int tiles) { return inner == 256 ? 1 : element == 4 && inner * tiles == 64 ? 4 : 2; }
 
 template <class T, int kInner, int kTiles, bool kMap, bool kWhole>
-__global__ __launch_bounds__(kThreads, blocks_of(kInner)) void k_la_walk(const Walks all) {
+__global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kInner, kTiles)) void k_la_walk(const Walks all) {
   typedef Walker<T, kInner, kTiles, kMap, kWhole> W;
   const int turn = blockIdx.x / kXcds, group = __builtin_amdgcn_readfirstlane(turn / all.count);
   const int block = group * kXcds + blockIdx.x % kXcds;
