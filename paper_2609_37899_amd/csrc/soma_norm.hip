@@ -18,6 +18,7 @@
 #include <cmath>
 
 #include "soma.h"
+#include "soma_eights.hpp"
 #include "soma_host.hpp"
 #include "soma_rng.hpp"
 #include "soma_types.hpp"
@@ -57,10 +58,11 @@ struct Stream {
 
 // Elements lo to hi - 1 of the eight at p + at.  Where groups are aligned (vec) all eight
 // are read at once, also at a row's two ends (what is around, not zeros then, belongs to
-// the rows before and behind), but for the last row (`last`).
+// the rows before and behind), but for the last row (`last`).  Rows so narrow that a group
+// reaches past the next one are never `vec`.
 template <class T>
 __device__ __forceinline__ void load_eight(const T* p, int64_t at, bool vec, bool last, int lo, int hi, float (&x)[8]) {
-  if (vec && (!last || (lo == 0 && hi == 8))) {
+  if (reads_whole(vec, last, lo, hi)) {
     if constexpr (sizeof(T) == 2) {
       const uint4 u = *reinterpret_cast<const uint4*>(p + at);
       const uint32_t w[4] = {u.x, u.y, u.z, u.w};
@@ -116,21 +118,20 @@ template <class T, bool kDrop>
 __global__ __launch_bounds__(256) void k_dropout(const DropArgs a) {
   const Stream s(a.drop);
   const int64_t u = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
-  const int64_t row = a.rows == 1 ? 0 : u / a.groups, first = row * a.width;
+  const int64_t row = a.rows == 1 ? 0 : u / a.groups;
   if (row >= a.rows) return;
-  const int64_t group = (first >> 3) + (u - row * a.groups), col = group * 8 - first;
-  const int lo = static_cast<int>(col < 0 ? -col : 0), hi = static_cast<int>(min(a.width - col, int64_t{8}));
-  if (hi <= lo) return;
+  const Eight g(row, a.width, u - row * a.groups);
+  if (g.hi <= g.lo) return;
   const bool last = row + 1 == a.rows;
   float x[8], r[8];
-  load_eight(static_cast<const T*>(a.x), row * a.x_stride + col, a.x_vec, last, lo, hi, x);
-  if (a.residual) load_eight(static_cast<const T*>(a.residual), row * a.residual_stride + col, a.residual_vec, last, lo, hi, r);
-  if constexpr (kDrop) s.apply(group, x);
+  load_eight(static_cast<const T*>(a.x), row * a.x_stride + g.col, a.x_vec, last, g.lo, g.hi, x);
+  if (a.residual) load_eight(static_cast<const T*>(a.residual), row * a.residual_stride + g.col, a.residual_vec, last, g.lo, g.hi, r);
+  if constexpr (kDrop) s.apply(g.block, x);
   if (a.residual) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) x[i] = r[i] + x[i];
   }
-  store_eight(static_cast<T*>(a.y), first + col, a.y_vec, lo, hi, x);
+  store_eight(static_cast<T*>(a.y), row * a.width + g.col, a.y_vec, g.lo, g.hi, x);
 }
 
 // A block's threads, and its rows, where kLanes of them share one.
@@ -184,21 +185,6 @@ struct NormArgs {
   int x_vec, residual_vec, total_vec, y_vec, dy_vec, dtotal_vec, dresidual_vec, dx_vec;
   float eps;
   Drop drop;
-};
-
-// Which elements of its row a lane's group k holds.
-template <int kLanes, bool kRagged>
-struct Group {
-  int64_t block;
-  int col, lo, hi;
-  __device__ __forceinline__ Group(int row, int width, int lane, int k) {
-    const int64_t first = static_cast<int64_t>(row) * width;
-    block = (first >> 3) + lane + kLanes * k;
-    const int64_t c = block * 8 - first;
-    col = static_cast<int>(min(c, static_cast<int64_t>(width)));
-    lo = kRagged && col < 0 ? -col : 0;
-    hi = kRagged ? min(width - col, 8) : col < width ? 8 : 0;     // <= lo: nothing
-  }
 };
 
 // The gain of a group's columns, 0 outside.  (Loads of 16 bytes take a float's alignment.)
@@ -447,13 +433,7 @@ int fill_drop(const soma_drop* d, Drop* out) {
   return SOMA_OK;
 }
 
-// Whether groups of eight are aligned in rows of this stride.
-bool in_eights(const void* p, int64_t stride, int64_t width, size_t e) {
-  return is_aligned(p, 16) && (stride - width) * static_cast<int64_t>(e) % 16 == 0;
-}
-
-// Groups that a row may touch.
-int64_t groups_of(int64_t width) { return width % 8 == 0 ? width / 8 : (width + 14) / 8; }
+bool in_eights(const void* p, int64_t stride, int64_t width, size_t e) { return soma::in_eights(is_aligned(p, 16), stride, width, e); }
 
 int check_norm(const soma_norm_config* cfg) {
   if (!cfg) return set_error(SOMA_EINVAL, "cfg is NULL");
@@ -654,7 +634,8 @@ int soma_norm_backward(const soma_norm_config* cfg, const void* total, const flo
   a.total = const_cast<void*>(total), a.gain = gain, a.dy = dy, a.dtotal = dtotal, a.dresidual = dresidual, a.dx = dx;
   a.partial = dgain ? static_cast<float*>(workspace) : nullptr;
   a.rows = c.rows, a.width = c.width, a.eps = c.eps;
-  a.total_vec = is_aligned(total, 16), a.dy_vec = is_aligned(dy, 16), a.dtotal_vec = is_aligned(dtotal, 16);
+  a.total_vec = in_eights(total, c.width, c.width, f), a.dy_vec = in_eights(dy, c.width, c.width, e);
+  a.dtotal_vec = in_eights(dtotal, c.width, c.width, f);
   a.dresidual_vec = is_aligned(dresidual, 16), a.dx_vec = is_aligned(dx, 16);
   const hipStream_t st = stream_of(stream);
   if (int rc = by_type(c, [&](auto t, auto s) {
