@@ -13,6 +13,25 @@ def pytest_configure(config):
     config.addinivalue_line("markers", "slow: takes more than a few seconds on the CPU")
 
 
+# Tests of the host's checks that also hand them arguments which pass, with addresses that
+# nobody allocated: without a device such a call ends there; with one its kernels would run
+# and access them.  The same calls on arrays of their own are in test_gpu_block_edges.py.
+PASS_MADE_UP_ADDRESSES = {
+    ("test_block_host.py", "test_linear_attention_of_no_rows_is_no_error"), ("test_block_host.py", "test_dropout_arguments"),
+    ("test_block_host.py", "test_norm_arguments"),
+}
+
+
+def pytest_collection_modifyitems(items):
+    found = [i for i in items if (i.path.name, getattr(i, "originalname", None)) in PASS_MADE_UP_ADDRESSES]
+    if not found:
+        return
+    import torch
+    if torch.cuda.device_count() > 0:
+        for i in found:
+            i.add_marker(pytest.mark.skip(reason="passes addresses that nobody allocated to calls that would run on the device"))
+
+
 @pytest.fixture(scope="session")
 def oracle_mod():
     import oracle
