@@ -22,6 +22,7 @@
 #pragma once
 
 #include "soma_kernels.hpp"
+#include "soma_wave.hpp"
 
 namespace soma {
 
@@ -396,8 +397,8 @@ __global__ __launch_bounds__(kThreads, narrow_head_blocks(KG)) void k_head_narro
           ces[n] = ce;
         }
       }
-      // One wave writes and reads ces: its LDS operations complete in order.
-      __builtin_amdgcn_wave_barrier();
+      // One wave writes and reads ces.
+      wave_lds_sync();
       if (lane == 0) {
         double tot = 0.0;
         for (int n = 0; n < 64; ++n) tot += static_cast<double>(ces[n]);

@@ -25,6 +25,7 @@
 #include "soma.h"
 #include "soma_host.hpp"
 #include "soma_types.hpp"
+#include "soma_wave.hpp"
 
 namespace soma {
 namespace {
@@ -154,16 +155,16 @@ struct Row {
         if (mine[k]) line[listed + __builtin_amdgcn_mbcnt_hi(here >> 32, __builtin_amdgcn_mbcnt_lo(static_cast<uint32_t>(here), 0))] = l[k];
         listed += __popcll(here);
         if (listed >= 64) {
-          __builtin_amdgcn_wave_barrier();
+          wave_lds_sync();
           f(line[lane], true);
           listed -= 64;
           const float rest = line[64 + lane];
-          __builtin_amdgcn_wave_barrier();
+          wave_lds_sync();
           line[lane] = rest;
         }
       });
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_lds_sync();
     f(lane < listed ? line[lane] : top, lane < listed);
   }
 

@@ -35,6 +35,7 @@
 #include "soma_kernels.hpp"
 #include "soma_body.hpp"
 #include "soma_mm.hpp"
+#include "soma_wave.hpp"
 
 namespace soma {
 
@@ -101,15 +102,6 @@ __device__ __forceinline__ float wave_max(float v) {
 #pragma unroll
   for (int o = 32; o >= 1; o >>= 1) v = fmaxf(v, __shfl_xor(v, o));
   return v;
-}
-
-// Orders a wave's LDS writes before its later LDS reads of other lanes'
-// words (a wave's LDS accesses execute in order; this keeps the compiler
-// from moving them).
-__device__ __forceinline__ void wave_lds_sync() {
-  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
-  __builtin_amdgcn_wave_barrier();
-  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
 }
 
 // Slot s of the pass: (expert, direction in the pass, sign).
