@@ -734,7 +734,9 @@ int soma_adamw_moments(soma_adamw* plan, float* const* m_out, float* const* v_ou
  * States, sums and decays are fp32.  bf16 operands enter the products as they are;
  * what is formed from them (q k^T, the states) as bf16 parts that hold 2^-15 of it,
  * in a state's own update all 24 bits; fp32 operands as they are.  A decay's power over n rows is
- * off by (|n log_decay| + 2) 2^-23 of itself.  A value that is not finite makes what it enters not
+ * off by at most (3 |n log_decay| + 8) 2^-23 of itself, however many rows they are; a state is
+ * rounded once for every 32 (fp32) or 64 rows (bf16) on its way, and in soma_la_step once a call,
+ * the call's decay with it.  A value that is not finite makes what it enters not
  * finite (an infinity may become NaN), and nothing else: rows in front of it
  * and other sequences and heads never see it.
  * Constraints: rows in [0, 2^30], sequences in [1, 65535], heads in [1, 1024],

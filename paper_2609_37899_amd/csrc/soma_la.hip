@@ -172,6 +172,15 @@ __device__ __forceinline__ int fresh(int x) {
   return x;
 }
 
+// A value that is the same in every lane, in a scalar register.
+__device__ __forceinline__ float first_lane(float x) { return __int_as_float(__builtin_amdgcn_readfirstlane(__float_as_int(x))); }
+
+// (a = 0: a^0 is 1)
+__device__ __forceinline__ float log2_decay(const Walk& a, int head) {
+  const float l = a.log_decay[head] * kL2e;
+  return l < -1e30f ? -1e30f : l;
+}
+
 // A fragment with zeros in the place of what is not finite.
 __device__ __forceinline__ b8 finite_part(const b8& f) {
   const uint4 u = __builtin_bit_cast(uint4, f);
@@ -266,6 +275,29 @@ struct Tile {
   }
 };
 
+// What a state is multiplied with, again and again, to be taken over n rows each time.  A
+// rounding of a^n to fp32 would be the same every time and add up (16,384 rows of
+// log a = -3e-6 in chunks of 32: 1.4e-5 of the state).  So the factors differ in their last
+// bit, and the first c of them sum up to c a^n, to 2^-24: their product is a^(c n) to
+// (3 |c n log a| + 1) 2^-23.  For a^n below a half a state is gone before roundings count.
+struct Factors {
+  float near, rest;           // a^n, and what it lacks in units of 2^-24
+  // (e^t - 1 by its series, whose tenth term is 2^-26 of it at the most)
+  __device__ __forceinline__ Factors(float l2, int n) {
+    const float y = l2 * static_cast<float>(n), t = y * 0.69314718f;
+    constexpr float over[] = {1.0f, 1.0f / 2, 1.0f / 6, 1.0f / 24, 1.0f / 120, 1.0f / 720, 1.0f / 5040, 1.0f / 40320, 1.0f / 362880};
+    float p = over[8];
+#pragma unroll
+    for (int k = 7; k >= 0; --k) p = fmaf(p, t, over[k]);
+    const float less = p * t, sum = 1.0f + less, left = ((1.0f - sum) + less) * 0x1p24f;
+    near = y > -1.0f ? sum : __builtin_amdgcn_exp2f(y);
+    rest = y > -1.0f ? left : 0.0f;
+  }
+  __device__ __forceinline__ float at(int c) const {
+    return near + (rintf(rest * static_cast<float>(c + 1)) - rintf(rest * static_cast<float>(c))) * 0x1p-24f;
+  }
+};
+
 // Fragment of an operand whose k lie side by side in a row: row l % 16, kEl values.
 template <class T>
 __device__ __forceinline__ typename Kind<T>::Frag along(const typename Kind<T>::Word* lds, int stride, int row, int k) {
@@ -306,8 +338,17 @@ struct Walker {
 
   f4 r[kSteps][kSub][kTiles];  // rows kKw t + (m / 4) kEl + m % 4 + 4 sub, m = 4 (l / 16) + element
   float l2;                    // log2 of the decay
+  Factors over_chunk;          // of a full one
   float in[kC / K::kKw][K::kEl];
   int in_for;
+
+  __device__ __forceinline__ explicit Walker(float log2_decay) : l2(log2_decay), over_chunk(l2, kC), in_for(-1) {
+    // (what has to stay over all chunks, where lanes have no registers left for it)
+    if constexpr (!kMap && !kWhole && (sizeof(T) == 2 ? kTiles == 2 : kInner * kTiles == 64)) {
+      over_chunk.near = first_lane(over_chunk.near);
+      over_chunk.rest = first_lane(over_chunk.rest);
+    }
+  }
 
   __device__ __forceinline__ float power(int n) const { return __builtin_amdgcn_exp2f(l2 * static_cast<float>(n)); }
 
@@ -544,7 +585,7 @@ struct Walker {
       }
 
       // the state, and P Z from the same fragments of Z
-      const float keep = power(m);
+      const float keep = m == kC ? over_chunk.at(c / kC) : power(m);
 #pragma unroll
       for (int t = 0; t < kSteps; ++t)
 #pragma unroll
@@ -713,10 +754,7 @@ __global__ __launch_bounds__(kThreads, blocks_of(sizeof(T), kInner, kTiles)) voi
   const int p = block / units, unit = block % units, head = unit / a.slices, slice = unit % a.slices;
   if (p >= all.parts) return;
   const int col0 = slice * W::kCols;
-  W w;
-  const float l = a.log_decay[head] * kL2e;
-  w.l2 = l < -1e30f ? -1e30f : l;           // a = 0: a^0 is 1
-  w.in_for = -1;
+  W w(log2_decay(a, head));
   const int64_t state = static_cast<int64_t>(a.inner) * a.outer;
   if constexpr (!kMap) {
     // tiles of P above the diagonal that a fragment reaches are zeros throughout
@@ -776,8 +814,11 @@ __global__ __launch_bounds__(kThreads) void k_la_join(const Walks all) {
   const int front = b / a.piece, back = (e - 1) / a.piece, count = back - front;
   if (count == 0) return;
   const int head = unit / a.slices, slice = unit % a.slices;
-  float l = a.log_decay[head] * kL2e;
-  l = l < -1e30f ? -1e30f : l;
+  const float l = log2_decay(a, head);
+  // (of the pieces that are left only the first may hold fewer rows of the sequence)
+  const Factors over_piece(l, a.piece);
+  const int first = (a.back ? e - back * a.piece : (front + 1) * a.piece - b);
+  const float over_first = __builtin_amdgcn_exp2f(l * static_cast<float>(first));
   f4 state = {0, 0, 0, 0};
   if (a.begin) {
     const int lane = at & 63, wave = (at >> 6) & 3, tile = at / kThreads;
@@ -800,9 +841,7 @@ __global__ __launch_bounds__(kThreads) void k_la_join(const Walks all) {
 #pragma unroll
     for (int k = 0; k < kAhead; ++k) {
       if (i0 + k >= count) break;
-      const int p = a.back ? back - (i0 + k) : front + i0 + k;
-      const int rows = min(e, (p + 1) * a.piece) - max(b, p * a.piece);
-      state = state * __builtin_amdgcn_exp2f(l * static_cast<float>(rows)) + add[k];
+      state = state * (i0 + k ? over_piece.at(i0 + k) : over_first) + add[k];
       *slot(i0 + k) = state;
     }
   }
