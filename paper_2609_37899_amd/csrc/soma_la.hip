@@ -1037,7 +1037,9 @@ template <class T, int kInner, int kTiles>
 int walk_as(const Walks& all, hipStream_t st) {
   const Walk& a = all.walk[0];
   const int units = a.heads * a.slices;
-  const dim3 grid(((static_cast<unsigned>(units) * all.parts + kXcds - 1) / kXcds) * kXcds * all.count), block(kThreads);
+  // (several walks share out whole rounds of the XCDs; one may have as many blocks as a launch)
+  const unsigned each = static_cast<unsigned>(units) * all.parts;
+  const dim3 grid(all.count == 1 ? each : (each + kXcds - 1) / kXcds * kXcds * all.count), block(kThreads);
   if (a.piece) {
     if (int rc = launch("k_la_walk (maps)", a.whole ? k_la_walk<T, kInner, kTiles, true, true> : k_la_walk<T, kInner, kTiles, true, false>,
                         grid, block, 0, st, all))

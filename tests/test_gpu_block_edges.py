@@ -63,3 +63,36 @@ def test_norm_in_place():
     plan.backward(total, x["gain"], x["dy"], d, d)
     torch.cuda.synchronize()
     assert torch.equal(r, total) and torch.equal(y, y2) and torch.equal(d, dr)
+
+
+@pytest.mark.parametrize("sequences,heads", [(20485, 819), (65535, 256)])
+def test_linear_attention_of_as_many_blocks_as_a_launch_has(sequences, heads):
+    """2^24 - 1 blocks of 256 threads, and 2^24 - 256: o = scale q (k v + a s0) and its gradients.  A term is at the most a
+    product of the matrix cores (which may cut: 2 u), one of a vector's lanes (1 u), a power of the decay (its exponent
+    of 0.72 rounded twice, 1.1 u, and 2 u of its own), and the sum of both terms (2 u): 9 u."""
+    torch = require_gpu()
+    assert sequences * heads in (2**24 - 1, 2**24 - 256)
+    g = torch.Generator(device="cuda").manual_seed(3)
+    q, k, v, do = (torch.randn(sequences, heads, device="cuda", generator=g) for _ in range(4))
+    s0, dsT = (torch.randn(sequences, heads, 1, 1, device="cuda", generator=g) for _ in range(2))
+    l = torch.full((heads,), -0.5, device="cuda")
+    a = l.double().exp()
+    o, dq, dk, dv = (torch.full_like(q, 7.0) for _ in range(4))
+    sT, ds0 = torch.full_like(s0, 7.0), torch.full_like(s0, 7.0)
+    plan = soma.LinearAttention(sequences, sequences, heads, 1, 1, torch.float32, scale=0.5)
+    plan.forward(q, k, v, l, o, s0, sT)
+    plan.backward(q, k, v, l, do, dq, dk, dv, s0, dsT, ds0)
+    torch.cuda.synchronize()
+
+    def near(got, one, two):
+        want, size = one + two, one.abs() + two.abs()
+        assert ((got.double() - want).abs() <= 9 * 2.0**-24 * size + 1e-37).all()
+
+    Q, K, V, D = (t.double() for t in (q, k, v, do))
+    S, G = s0.double().view_as(q), dsT.double().view_as(q)
+    near(o, 0.5 * Q * K * V, 0.5 * a * Q * S)
+    near(sT.view_as(q), K * V, a * S)
+    near(dq, 0.5 * D * V * K, 0.5 * a * D * S)
+    near(dk, 0.5 * V * D * Q, V * G)
+    near(dv, 0.5 * K * D * Q, K * G)
+    near(ds0.view_as(q), 0.5 * a * Q * D, a * G)
