@@ -994,14 +994,15 @@ size_t slots_size(const soma_la_config& c, int inner, int outer, int walks) {
 }
 
 // A copy of the states that a walk begins with, where it ends with the same array and
-// goes in pieces: one block may then read a state after another has written it.
+// goes in pieces: one block may then read a state after another has written it.  (A walk in
+// pieces as `together` would be is in pieces by itself: the size holds for both.)
 size_t copy_size(const soma_la_config& c) {
   if (!most_pieces(c, shape_of(c.key_width, c.value_width), 1)) return 0;
   return up256(sizeof(float) * c.sequences * c.heads * c.key_width * c.value_width);
 }
 
-int kept(const soma_la_config& c, const float** begin, const float* end, unsigned char* at, hipStream_t st) {
-  if (!*begin || *begin != end || !copy_size(c)) return SOMA_OK;
+int kept(const soma_la_config& c, int together, const float** begin, const float* end, unsigned char* at, hipStream_t st) {
+  if (!*begin || *begin != end || !most_pieces(c, shape_of(c.key_width, c.value_width), together)) return SOMA_OK;
   const int64_t n = static_cast<int64_t>(c.sequences) * c.heads * c.key_width * c.value_width;
   const dim3 grid(static_cast<unsigned>(std::min<int64_t>((n + kThreads - 1) / kThreads, 4096)));
   const float* from = *begin;
@@ -1172,7 +1173,7 @@ int soma_la_forward(const soma_la_config* cfg, const void* q, const void* k, con
   const int share = c.heads / c.kv_heads;
   unsigned char* const ws = static_cast<unsigned char*>(workspace);
   const hipStream_t st = stream_of(stream);
-  if (int rc = kept(c, &s0, sT, ws + all_slots(c, false), st)) return rc;
+  if (int rc = kept(c, 1, &s0, sT, ws + all_slots(c, false), st)) return rc;
   const Walk to_o = walk_over(c, {q, c.q_stride, 1}, {k, c.k_stride, share}, {v, c.v_stride, share}, c.key_width, c.value_width,
                               false, s0, sT, false, o, false);
   if (int rc = walk(c, {to_o}, 1, log_decay, offsets, ws, st)) return rc;
@@ -1232,7 +1233,7 @@ int soma_la_backward(const soma_la_config* cfg, const void* q, const void* k, co
     if (int rc = walk(c, {to_dv(), to_dk, to_dq}, 3, log_decay, offsets, ws, st)) return rc;
   } else {
     if (int rc = walk(c, {to_dk, to_dq}, alike ? 3 : 2, log_decay, offsets, ws, st)) return rc;
-    if (int rc = kept(c, &dsT, ds0, ws + all_slots(c, true), st)) return rc;
+    if (int rc = kept(c, alike ? 3 : 1, &dsT, ds0, ws + all_slots(c, true), st)) return rc;
     if (int rc = walk(c, {to_dv()}, alike ? 3 : 1, log_decay, offsets, ws, st)) return rc;
   }
   if (int rc = shared(key_sums, dk, c.key_width)) return rc;
