@@ -87,7 +87,7 @@ struct Row {
     u64 wave_count[kWaves];
     u64 border;
     uint32_t count[kBins];
-    uint32_t listed, found_bin, found_count;
+    uint32_t listed, found_bin;
     u64 found_weight;
   };
   Shared& s;
