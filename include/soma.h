@@ -697,7 +697,9 @@ void soma_adamw_destroy(soma_adamw* plan);
  *     upper 20 bits, v takes the larger root if (d + 1/2) 2^-20 is below
  *     (root^2 - smaller^2) / (larger^2 - smaller^2); with its lower 12, m the
  *     larger magnitude if (d + 1/2) 2^-12 is below (|m| - smaller) / (larger -
- *     smaller).  The same seed, t and inputs give the same bits. */
+ *     smaller).  The same seed, t and inputs give the same bits.  The words are those
+ *     of dropout's masks and of the probes under the same seed (soma_drop): a
+ *     program that draws those too takes another seed here. */
 enum soma_rounding {
   SOMA_ROUND_NEAREST = 0,
   SOMA_ROUND_RANDOM = 1
@@ -786,7 +788,11 @@ int soma_la_step(const soma_la_config* cfg, const void* q_dev, const void* k_dev
  * layer, lo32(t), hi32(b)), t = step + *step_dev.  With cut = p 65536, rounded, an
  * element whose bits are below cut is dropped, whatever its value: it counts as 0; what
  * is kept is multiplied with 65536 / (65536 - cut).  The mask is not stored: a gradient
- * forms it again from the same numbers.  `layer` tells masks of one step apart. */
+ * forms it again from the same numbers.  `layer` tells masks of one step apart; it does not
+ * tell them from other draws: under one seed the words are those that AdamW's random
+ * rounding takes for tensor `layer` in update t, and the probes for direction `layer` in step
+ * t.  What a program draws for different purposes needs a seed for each (0 in all of them,
+ * the classes' default, is one and the same). */
 typedef struct soma_drop {
   double p;                 /* in [0, 1), rounded to 2^-16; below 1 - 2^-17 */
   uint64_t seed;

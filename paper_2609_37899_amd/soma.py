@@ -697,7 +697,8 @@ class AdamW(_Plan):
     bfloat16 tensors (or None) that receive the new parameters too.
 
     rounding of moments in 8 bits: "random" for a training run, drawn from seed
-    and the update's number, or "nearest", the closest codes of a single step.  To
+    and the update's number, or "nearest", the closest codes of a single step.  (A
+    seed that dropout's masks do not have: they would be drawn from the same words.)  To
     nearest, v does not follow its average over many steps, since updates of less
     than half a code (3 to 6% of v) are lost."""
 
@@ -887,7 +888,8 @@ class LinearAttention(_Plan):
 
 class _Dropping(_Plan):
     """What the operators share that drop elements with probability ``drop`` (rounded to 2^-16): seed, step and layer of
-    a call name the mask, and a backward pass gives the same.  step may be an int64 tensor of one element on the device,
+    a call name the mask, and a backward pass gives the same.  A seed is for one purpose: AdamW's random rounding and the
+    probes draw the same words under the same seed (tensor or direction in the layer's place).  step may be an int64 tensor of one element on the device,
     which is read when the call runs, so that a captured call draws anew once its program has counted it up."""
 
     def _set_drop(self, drop):
