@@ -833,8 +833,9 @@ int soma_dropout(const soma_dropout_config* cfg, const void* x_dev, const void* 
  *           needs; NULL: not wanted.  It may be residual where that has contiguous
  *           rows.
  *   y       [rows][width] of `type`, rows contiguous.
- * sum_type is `type` or fp32.  drop NULL: p = 0.  Sums are fp32; y is formed from
- * total before that is rounded.
+ * sum_type is `type` or fp32.  drop NULL: p = 0.  Sums are fp32 (a row whose squares
+ * add up to more than fp32 holds gives zeros); y is formed from total before that is
+ * rounded.
  * Constraints: rows in [0, 2^30], width in [1, 2^14], eps finite and >= 0. */
 typedef struct soma_norm_config {
   int32_t rows;

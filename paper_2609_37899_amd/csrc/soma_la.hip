@@ -730,8 +730,8 @@ struct Walker {
   }
 };
 
-// 64 sequences of 1,024 rows, 8 heads of 64 x 64 in bf16: 70 to 75 us a walk, 3.6 to 3.8
-// TB/s where a copy's rate would take 52 (forward 74, the three gradients together 209).
+// 64 sequences of 1,024 rows, 8 heads of 64 x 64 in bf16: 70 to 76 us a walk, 3.5 to 3.8
+// TB/s where a copy's rate would take 52 (forward 76, the three gradients together 210).
 // Nothing is saturated: of a SIMD's cycles 38% issue vector instructions, most of them to
 // split fp32 into parts, 20% keep the matrix cores busy, and LDS works in 42%; the rest
 // are waits between a chunk's three barriers.  Without loads and stores it would take 55,

@@ -203,9 +203,10 @@ __device__ __forceinline__ void load_gain(const float* gain, int width, int col,
 // T: x and y; S: residual and total; kLanes lanes a row, kGroups groups a lane; kRagged:
 // the width is no multiple of 8, and groups lie across the rows' ends.
 // 16,384 rows of 4,096 in bf16 with codes: 91 us, 470 MB at 5.15 TB/s; 65,536 of 512, bf16
-// with fp32 sums and dropout: 71 us, 403 MB at 5.7; 22,000 of 361 in fp32: 25 us, 127 MB
-// at 5.1 (30 where rows' ends were read one element at a time; 4,099 columns in bf16, 8,192
-// rows: 107 us, now 60).
+// with fp32 sums and dropout: 71 us, 403 MB at 5.7.  Ragged widths fall behind where the
+// caches hold nothing of the inputs: 22,000 of 361 in fp32 34 to 36 us, 127 MB at 3.6 (25
+// where they do; of 360 30 and 22), 8,192 of 4,099 in bf16 66 us (52; of 4,096 54 and 42).
+// Rows' ends read one element at a time took 30 for those 25, and 107 for the 52.
 template <class T, class S, int kLanes, int kGroups, bool kCodes, bool kRagged>
 __global__ __launch_bounds__(threads_of(kLanes)) void k_norm_forward(const NormArgs a) {
   __shared__ float lds[16];
@@ -293,7 +294,8 @@ __global__ __launch_bounds__(threads_of(kLanes)) void k_norm_forward(const NormA
 // dx = drop(dresidual), dgain = sum over rows of dy n.  Blocks walk over rows, a multiple
 // of 8 apart, so that whatever the width a lane's columns are the same in every row and
 // their sums stay in registers.  65,536 rows of 512 (bf16, fp32 sums, dropout): 112 to
-// 118 us, 537 MB at 4.6 to 4.8 TB/s; 22,000 of 361 in fp32: 31 us, 159 MB at 5.1.
+// 119 us, 537 MB at 4.5 to 4.8 TB/s; 22,000 of 361 in fp32: 45 us, 159 MB at 3.5 (31 where
+// the caches hold a part of the inputs).
 template <class T, class S, int kLanes, int kGroups, bool kRagged>
 __global__ __launch_bounds__(threads_of(kLanes)) void k_norm_backward(const NormArgs a) {
   constexpr int kRows = rows_of(kLanes);
@@ -454,9 +456,10 @@ int lanes_of(int width) {
   const int64_t g = groups_of(width);
   return g <= 128 ? 64 : g <= 256 ? 128 : g <= 512 ? 256 : g <= 1024 ? 512 : 1024;
 }
-// Blocks of the backward pass: a block a row, or a multiple of eight.  (512, 1,024
-// and 2,048: 22,000 rows of 361 in fp32, both passes, 70, 63 and 70 us, 65,536 of 512 in
-// bf16 199, 193 and 199.)
+// Blocks of the backward pass: a block a row, or a multiple of eight, up to 1,024 of 64
+// lanes a row (512, 1,024 and 2,048: 22,000 rows of 361 in fp32, from the caches, both passes
+// 70, 63 and 70 us, 65,536 of 512 in bf16 199, 193 and 199), of more lanes as many lanes in
+// all: 2,048 of 128, 1,024 of 256, at least 512.
 int backward_blocks(const soma_norm_config& c) {
   const int lanes = lanes_of(c.width), rows = rows_of(lanes);
   return std::max(1, std::min((c.rows + rows - 1) / rows, lanes == 64 ? 1024 : std::max(512, (1 << 18) / lanes)));
